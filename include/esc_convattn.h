@@ -379,6 +379,109 @@ int esc_conv_fuse_backward(const void* cat, const void* grad_out, int B, int C, 
                            void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * ---- the block's window self-attention (Section 3.3) and its learned relative position bias ----
+ *
+ * The bias of a window of win_h x win_w pixels, between query i = (yi, xi) and key j = (yj, xj):
+ *
+ *   bias[h, i, j] = table[bucket[o], h],   o = (yi - yj + win_h - 1) (2 win_w - 1) + (xi - xj + win_w - 1)
+ *
+ *   table    [n_buckets, heads], the type of the call; -inf masks
+ *   bucket   [(2 win_h - 1)(2 win_w - 1)] int32 (device), the bucket of every offset; NULL: every offset has its own row of the
+ *            table (n_buckets has to be their number).  An entry outside [0, n_buckets) gives no bias and takes no gradient.
+ *   (2 win_h - 1)(2 win_w - 1) is at most 16384 (windows of 64 x 64, sequences of 8192 with win_h = 1).
+ *
+ * esc_relpos_bias_forward writes it as a matrix [heads, N, N] with N = win_h win_w (16-byte aligned), for an attention that takes
+ * one.  esc_relpos_bias_backward sums a gradient of that shape into grad_table [n_buckets, heads], fp32; a bucket that no
+ * offset has gets zero.  The order of the additions is fixed: the same input gives the same bits.
+ */
+int esc_relpos_bias_forward(const void* table, const int* bucket, int n_buckets, int heads, int win_h, int win_w, void* bias,
+                            int dtype, void* stream);
+size_t esc_relpos_bias_workspace_bytes(int heads, int win_h, int win_w);   /* 0 for invalid arguments */
+int esc_relpos_bias_backward(const void* grad_bias, const int* bucket, int n_buckets, int heads, int win_h, int win_w,
+                             float* grad_table, int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Self-attention over non-overlapping windows of a channels-last map; per image, head and window
+ *
+ *   out[i] = sum_j softmax_j(scale q[i] . k[j] + bias[i, j]) v[j]
+ *
+ * over the pixels i, j of the window.  Windows start at (0, 0); those at the right and lower border hold the pixels that the map
+ * has there (a map smaller than a window is one window), so the map needs no padding.  A sequence is a map with H = 1, win_h = 1.
+ *   q, k, v  [B,H,W,heads,head_dim], a pixel's heads*head_dim values dense, pixels `pixel_stride` values apart (rows and images
+ *            dense behind one another): tensors of their own, or slices of the output of one projection.  head_dim <= 64.
+ *            Fastest where the pointers are 16-byte aligned and head_dim and pixel_stride are multiples of 16 bytes.
+ *   table, bucket, n_buckets   the bias as above; table NULL: none.  An entry of -9984 or less (-10000 in bf16, a type's lowest value)
+ *            masks its offset as -inf does: such a key has no weight, also where all others of the row are masked
+ *   scale    in [1e-6, 1e6]
+ *   out      [B,H,W,heads,head_dim] dense, 16-byte aligned
+ *   lse      [B,heads,H,W] fp32, log of the sum of exp per row, which the backward pass takes; may be NULL.  A row whose keys
+ *            are all masked gives out = 0 and lse = -inf.
+ * Arithmetic: fp32; with bf16 tensors the products run on the tensor cores and p is rounded to bf16 as an operand of p v, not in
+ * the sum that divides it.  A masked key still has its q . k and its v multiplied by zero: NaN and infinities there spread.
+ */
+int esc_window_attention_forward(const void* q, const void* k, const void* v, int B, int heads, int head_dim, int H, int W,
+                                 long long pixel_stride, int win_h, int win_w, const void* table, const int* bucket,
+                                 int n_buckets, float scale, void* out, float* lse, int dtype, void* stream);
+
+/*
+ * Its backward pass.  out and lse are the forward call's.
+ *   grad_out              [B,H,W,heads,head_dim] dense, 16-byte aligned
+ *   grad_q, grad_k, grad_v   laid out like q, k, v, with the same pixel_stride (what lies between is left as it is)
+ *   grad_table            [n_buckets, heads] of the table's type, or NULL: with bf16 tensors the sums are made from p and out
+ *                         as rounded for the products, so bits beyond bf16 would say nothing
+ *   workspace             esc_window_attention_backward_workspace_bytes(...) bytes, 256-byte aligned, no preparation needed
+ * Every sum has a fixed order: the same input gives the same bits.
+ */
+size_t esc_window_attention_backward_workspace_bytes(int B, int heads, int head_dim, int H, int W, int win_h, int win_w);
+int esc_window_attention_backward(const void* q, const void* k, const void* v, int B, int heads, int head_dim, int H, int W,
+                                  long long pixel_stride, int win_h, int win_w, const void* table, const int* bucket,
+                                  int n_buckets, float scale, const void* out, const float* lse, const void* grad_out,
+                                  void* grad_q, void* grad_k, void* grad_v, void* grad_table, int dtype, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/*
+ * ---- AdamW over many tensors in one launch (the optimiser of the paper's training details) ----
+ *
+ *   g = grad_scale grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   p = (1 - lr wd) p - lr / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ *
+ * in fp32, whatever the types of the tensors.  States: ESC_STATES_F32 (m and v in fp32), or ESC_STATES_E4M3: m and sqrt(v) as e4m3
+ * values, each times an fp32 scale per 256 values of the tensor (largest magnitude / 448; the last scale of a tensor covers what
+ * is left).  Start with zeros in all of them.  Rounded to nearest: an entry moves when it changes by more than half a step (2^-4 of
+ * itself) against its 256 neighbours; a change that they all share is carried by the scale.  A root that is not zero is never
+ * stored as zero; magnitudes below 1e-30 are.
+ *
+ * The plan is a table of the tensors in device memory, made once and good for as long as they stay where they are:
+ *   sizes                 values of each tensor (zero is allowed), host
+ *   params, grads, exp_avgs, exp_avg_sqs   host arrays of device pointers; exp_avg_sqs holds v, or the roots
+ *   avg_scales, sq_scales host arrays of device pointers, ceil(size / 256) floats each; NULL with ESC_STATES_F32
+ *   copies                host array of device pointers (or NULL, as may be an entry): gets the new parameters rounded to bf16
+ *   plan                  esc_adamw_plan_bytes(...) bytes of device memory, 256-byte aligned
+ *   n_chunks              out: what esc_adamw_step has to be told
+ * Pointers aligned to four values are read four at a time, others one by one.  esc_adamw_plan_init waits for its copy to the device;
+ * it is refused (ESC_ERR_UNSUPPORTED) while `stream` is being captured.
+ */
+enum { ESC_STATES_F32 = 0, ESC_STATES_E4M3 = 1 };
+size_t esc_adamw_plan_bytes(int n_tensors, const long long* sizes);        /* 0 for invalid arguments */
+int esc_adamw_plan_init(int n_tensors, const long long* sizes, void* const* params, const void* const* grads, void* const* exp_avgs,
+                        void* const* exp_avg_sqs, float* const* avg_scales, float* const* sq_scales, void* const* copies,
+                        int param_dtype, int grad_dtype, int states, void* plan, size_t plan_bytes, long long* n_chunks,
+                        void* stream);
+
+/*
+ * One step (the first is 1).  The types are those of the plan.
+ *   scalars  device, 4 floats as esc_adamw_scalars gives them, or NULL.  They replace step, lr, weight_decay and grad_scale in
+ *            the kernel: a captured graph takes what they hold when it is replayed, where the arguments would stay what they were.
+ *   skip     device int or NULL: not zero, and the call changes nothing (gradients that overflowed)
+ * Two steps of one plan, or two plans that share tensors, must not overlap on the GPU.
+ */
+int esc_adamw_step(const void* plan, long long n_chunks, int param_dtype, int grad_dtype, int states, long long step, double lr,
+                   double beta1, double beta2, double eps, double weight_decay, double grad_scale, const float* scalars,
+                   const int* skip, void* stream);
+int esc_adamw_scalars(long long step, double lr, double beta1, double beta2, double weight_decay, double grad_scale,
+                      float* scalars_host);                                /* host: 4 floats */
+
+/*
  * Self-test of the error path that every device-side wait of this library shares: launches one thread that waits, with
  * the kernels' own bounded waits, for a count that nothing raises and then on a barrier that nothing signals.  Each wait gives up
  * after its poll limit (about one second); the second, if the first one's record was right, records ESC_DEV_TIMEOUT in the status word of `workspace` (any initialised forward or backward workspace, device)

@@ -71,6 +71,20 @@ def lib():
         L.esc_convattn_selftest_bounded_wait.argtypes = [vp, vp]
         L.esc_convattn_forward_host_submit.argtypes = [i, vp, i, i, i, i, i, i, vp, vp, vp, vp, i, i]
         L.esc_convattn_forward_host_wait.argtypes = [i]
+        ll, f, dbl = ctypes.c_longlong, ctypes.c_float, ctypes.c_double
+        L.esc_relpos_bias_forward.argtypes = [vp, vp, i, i, i, i, vp, i, vp]
+        L.esc_relpos_bias_workspace_bytes.argtypes = [i, i, i]
+        L.esc_relpos_bias_workspace_bytes.restype = sz
+        L.esc_relpos_bias_backward.argtypes = [vp, vp, i, i, i, i, vp, i, vp, sz, vp]
+        L.esc_window_attention_forward.argtypes = [vp, vp, vp, i, i, i, i, i, ll, i, i, vp, vp, i, f, vp, vp, i, vp]
+        L.esc_window_attention_backward_workspace_bytes.argtypes = [i, i, i, i, i, i, i]
+        L.esc_window_attention_backward_workspace_bytes.restype = sz
+        L.esc_window_attention_backward.argtypes = [vp, vp, vp, i, i, i, i, i, ll, i, i, vp, vp, i, f, vp, vp, vp, vp, vp, vp, vp, i, vp, sz, vp]
+        L.esc_adamw_plan_bytes.argtypes = [i, vp]
+        L.esc_adamw_plan_bytes.restype = sz
+        L.esc_adamw_plan_init.argtypes = [i, vp, vp, vp, vp, vp, vp, vp, vp, i, i, i, vp, sz, vp, vp]
+        L.esc_adamw_step.argtypes = [vp, ll, i, i, i, ll, dbl, dbl, dbl, dbl, dbl, dbl, vp, vp, vp]
+        L.esc_adamw_scalars.argtypes = [ll, dbl, dbl, dbl, dbl, dbl, vp]
         L.esc_convattn_set_tile_width.argtypes = [i]
         L.esc_convattn_set_stencil_engine.argtypes = [i]
         L.esc_convattn_set_fused_stage1.argtypes = [i]
@@ -80,6 +94,8 @@ def lib():
         L.esc_last_error.restype = ctypes.c_char_p
         for name in ("esc_convattn_forward", "esc_convattn_forward_ex", "esc_convattn_forward_fused", "esc_convattn_workspace_init",
                      "esc_convattn_dynkernel", "esc_convattn_dynkernel_static", "esc_convattn_forward_mlp", "esc_convattn_dynkernel_mlp", "esc_convattn_forward_pw", "esc_convattn_stencil_pw", "esc_convattn_forward_dense", "esc_convattn_stencil_dense", "esc_convattn_forward_variant", "esc_convattn_backward", "esc_convattn_backward_mlp", "esc_convattn_backward_pw", "esc_convattn_backward_dense", "esc_convattn_backward_variant", "esc_conv_fuse_backward", "esc_convattn_stencil", "esc_convattn_forward_host", "esc_convattn_forward_host_submit", "esc_convattn_forward_host_wait",
+                     "esc_relpos_bias_forward", "esc_relpos_bias_backward", "esc_window_attention_forward", "esc_window_attention_backward",
+                     "esc_adamw_plan_init", "esc_adamw_step", "esc_adamw_scalars",
                      "esc_convattn_device_status", "esc_convattn_last_path", "esc_convattn_last_tile_width", "esc_convattn_set_tile_width", "esc_convattn_set_stencil_engine", "esc_convattn_set_fused_stage1", "esc_convattn_set_dense_engine", "esc_convattn_last_launches",
                      "esc_version"):
             getattr(L, name).restype = i
@@ -470,3 +486,227 @@ def esc_convattn_forward_host_wait(slot) -> None:
 
 def esc_convattn_device_status(workspace, stream=None) -> int:
     return lib().esc_convattn_device_status(_ptr(workspace), _stream(stream))
+
+
+# ---- window self-attention, its relative position bias, AdamW ---------------------------------------------------------------
+
+
+def _on_device(*tensors):
+    """The tensors' one device, made current for the call that follows: kernels run where the data are."""
+    import torch
+
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1 or next(iter(devices)).type != "cuda":
+        raise ValueError(f"the tensors of a call have to be on one CUDA device, not on {sorted(map(str, devices))}")
+    return torch.cuda.device(devices.pop())
+
+
+def _dense(name, t, shape, dtype):
+    if t is None:
+        return
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} has to be a contiguous {tuple(shape)} tensor of {dtype}, not {tuple(t.shape)} of {t.dtype}")
+
+
+def _bucket_arg(bucket, win_h, win_w):
+    if bucket is None:
+        return
+    import torch
+
+    if bucket.numel() != (2 * win_h - 1) * (2 * win_w - 1) or bucket.dtype != torch.int32 or not bucket.is_contiguous():
+        raise ValueError(f"bucket has to be a contiguous int32 tensor with an entry for each of the {(2 * win_h - 1) * (2 * win_w - 1)} offsets")
+
+
+def esc_relpos_bias_forward(table, bucket, win_h, win_w, bias, stream=None):
+    """bias [heads, N, N] (N = win_h win_w) from table [n_buckets, heads]; bucket: int32 bucket of every offset, or None."""
+    n, heads = (int(x) for x in table.shape)
+    _dense("table", table, (n, heads), table.dtype)
+    _dense("bias", bias, (heads, win_h * win_w, win_h * win_w), table.dtype)
+    _bucket_arg(bucket, win_h, win_w)
+    with _on_device(table, bucket, bias):
+        _check(lib().esc_relpos_bias_forward(_ptr(table), _ptr(bucket), n, heads, win_h, win_w, _ptr(bias), _dtype_code(table), _stream(stream)),
+               "esc_relpos_bias_forward")
+    return bias
+
+
+def esc_relpos_bias_workspace_bytes(heads, win_h, win_w) -> int:
+    return int(lib().esc_relpos_bias_workspace_bytes(heads, win_h, win_w))
+
+
+def new_relpos_bias_workspace(heads, win_h, win_w, device="cuda"):
+    import torch
+
+    n = esc_relpos_bias_workspace_bytes(heads, win_h, win_w)
+    if n == 0:
+        raise ValueError("invalid window")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def esc_relpos_bias_backward(grad_bias, bucket, win_h, win_w, grad_table, workspace=None, stream=None):
+    """grad_table [n_buckets, heads] fp32 from grad_bias [heads, N, N]."""
+    import torch
+
+    n, heads = (int(x) for x in grad_table.shape)
+    _dense("grad_table", grad_table, (n, heads), torch.float32)
+    _dense("grad_bias", grad_bias, (heads, win_h * win_w, win_h * win_w), grad_bias.dtype)
+    _bucket_arg(bucket, win_h, win_w)
+    with _on_device(grad_bias, bucket, grad_table, workspace):
+        if workspace is None:
+            workspace = new_relpos_bias_workspace(heads, win_h, win_w)
+        _check(lib().esc_relpos_bias_backward(_ptr(grad_bias), _ptr(bucket), n, heads, win_h, win_w, _ptr(grad_table), _dtype_code(grad_bias),
+                                              _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+               "esc_relpos_bias_backward")
+    return grad_table
+
+
+def _pixels(heads, **maps):
+    """(B, H, W, head_dim, pixel stride) of maps [B, H, W, heads * head_dim] that are laid out alike."""
+    first = None
+    for name, t in maps.items():
+        if t.dim() != 4 or t.shape[3] % heads != 0:
+            raise ValueError(f"{name} has to be [B, H, W, heads * head_dim]")
+        B, H, W, C = (int(x) for x in t.shape)
+        # the pixels' distance: from the innermost axis that has more than one entry
+        step = t.stride(2) if W > 1 else t.stride(1) if H > 1 else t.stride(0) if B > 1 else C
+        got = (B, H, W, C // heads, int(step)), t.dtype
+        ok = (C == 1 or t.stride(3) == 1) and (W == 1 or t.stride(2) == step) and (H == 1 or t.stride(1) == step * W) and (B == 1 or t.stride(0) == step * W * H)
+        if not ok or got != (first or got):
+            raise ValueError(f"{name}: pixels have to be dense in their channels, evenly spaced, and alike in all of {', '.join(maps)}")
+        first = got
+    return first[0]
+
+
+def esc_window_attention_forward(q, k, v, heads, win_h, win_w, table, bucket, scale, out, lse=None, stream=None):
+    """out [B, H, W, heads * head_dim] (and lse [B, heads, H, W] fp32) of the self-attention over windows.
+
+    q, k, v: [B, H, W, heads * head_dim], of their own or slices along the last axis of one packed tensor; table
+    [n_buckets, heads] with the bucket of every offset (None: one row per offset), or None for no bias."""
+    import torch
+
+    B, H, W, d, step = _pixels(heads, q=q, k=k, v=v)
+    _dense("out", out, (B, H, W, heads * d), q.dtype)
+    _dense("lse", lse, (B, heads, H, W), torch.float32)
+    n = 0 if table is None else int(table.shape[0])
+    _dense("table", table, (n, heads), q.dtype)
+    _bucket_arg(bucket, win_h, win_w)
+    with _on_device(q, k, v, table, bucket, out, lse):
+        _check(lib().esc_window_attention_forward(_ptr(q), _ptr(k), _ptr(v), B, heads, d, H, W, step, win_h, win_w, _ptr(table), _ptr(bucket), n, scale,
+                                                  _ptr(out), _ptr(lse), _dtype_code(q), _stream(stream)),
+               "esc_window_attention_forward")
+    return out
+
+
+def esc_window_attention_backward_workspace_bytes(B, heads, head_dim, H, W, win_h, win_w) -> int:
+    return int(lib().esc_window_attention_backward_workspace_bytes(B, heads, head_dim, H, W, win_h, win_w))
+
+
+def new_window_attention_workspace(B, heads, head_dim, H, W, win_h, win_w, device="cuda"):
+    """Scratch of esc_window_attention_backward."""
+    import torch
+
+    n = esc_window_attention_backward_workspace_bytes(B, heads, head_dim, H, W, win_h, win_w)
+    if n == 0:
+        raise ValueError("invalid problem size")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def esc_window_attention_backward(q, k, v, heads, win_h, win_w, table, bucket, scale, out, lse, grad_out, grad_q, grad_k, grad_v, grad_table=None,
+                                  workspace=None, stream=None):
+    """Gradients of esc_window_attention_forward; grad_q, grad_k, grad_v are laid out like q, k, v."""
+    import torch
+
+    B, H, W, d, step = _pixels(heads, q=q, k=k, v=v, grad_q=grad_q, grad_k=grad_k, grad_v=grad_v)
+    _dense("out", out, (B, H, W, heads * d), q.dtype)
+    _dense("grad_out", grad_out, (B, H, W, heads * d), q.dtype)
+    _dense("lse", lse, (B, heads, H, W), torch.float32)
+    n = 0 if table is None else int(table.shape[0])
+    _dense("table", table, (n, heads), q.dtype)
+    _dense("grad_table", grad_table, (n, heads), q.dtype)
+    _bucket_arg(bucket, win_h, win_w)
+    with _on_device(q, k, v, table, bucket, out, lse, grad_out, grad_q, grad_k, grad_v, grad_table, workspace):
+        if workspace is None:
+            workspace = new_window_attention_workspace(B, heads, d, H, W, win_h, win_w)
+        _check(lib().esc_window_attention_backward(_ptr(q), _ptr(k), _ptr(v), B, heads, d, H, W, step, win_h, win_w, _ptr(table), _ptr(bucket), n, scale,
+                                                   _ptr(out), _ptr(lse), _ptr(grad_out), _ptr(grad_q), _ptr(grad_k), _ptr(grad_v), _ptr(grad_table),
+                                                   _dtype_code(q), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+               "esc_window_attention_backward")
+    return grad_q, grad_k, grad_v, grad_table
+
+
+ESC_STATES_F32, ESC_STATES_E4M3 = 0, 1
+ADAMW_QUANT = 256   # values of a tensor that share a scale with ESC_STATES_E4M3
+
+
+def esc_adamw_plan_bytes(sizes) -> int:
+    return int(lib().esc_adamw_plan_bytes(len(sizes), (ctypes.c_longlong * len(sizes))(*sizes)))
+
+
+class AdamwPlan:
+    """A list of tensors in device memory, as esc_adamw_step takes it.  It keeps the tensors."""
+
+    def __init__(self, table, n_chunks, param_dtype, grad_dtype, states, tensors):
+        self.table, self.n_chunks, self.param_dtype, self.grad_dtype, self.states, self.tensors = table, n_chunks, param_dtype, grad_dtype, states, tensors
+
+
+def esc_adamw_plan_init(params, grads, exp_avgs, exp_avg_sqs, avg_scales=None, sq_scales=None, copies=None, stream=None):
+    """The plan of a list of tensors: parameters and gradients of fp32 or bf16, states of fp32, or of float8_e4m3fn with fp32 scales
+    of ceil(size / 256) entries (exp_avg_sqs then holds the square roots); copies (bf16) and single entries of it may be None."""
+    import torch
+
+    n = len(params)
+    if n == 0 or not (n == len(grads) == len(exp_avgs) == len(exp_avg_sqs)) or any(x is not None and len(x) != n for x in (avg_scales, sq_scales, copies)):
+        raise ValueError("the lists have to be as long as one another, and not empty")
+    p, g, s = params[0].dtype, grads[0].dtype, exp_avgs[0].dtype
+    eight = s == torch.float8_e4m3fn
+    if not eight and s != torch.float32:
+        raise TypeError(f"unsupported dtype {s} of the states")
+    if eight != (avg_scales is not None) or eight != (sq_scales is not None):
+        raise ValueError("states in 8 bits have scales, others have none")
+    sizes = [t.numel() for t in params]
+
+    def pointers(name, tensors, dtype, counts):
+        if tensors is None:
+            return None
+        for t, count in zip(tensors, counts):
+            if t is not None and (t.numel() != count or t.dtype != dtype or not t.is_contiguous()):
+                raise ValueError(f"{name}: contiguous tensors of {dtype}, as many values as the parameters (scales: one for 256)")
+        return (ctypes.c_void_p * n)(*[t.data_ptr() if t is not None and t.numel() else None for t in tensors])
+
+    scales = [-(-k // ADAMW_QUANT) for k in sizes]
+    lists = [("params", params, p, sizes), ("grads", grads, g, sizes), ("exp_avgs", exp_avgs, s, sizes), ("exp_avg_sqs", exp_avg_sqs, s, sizes),
+             ("avg_scales", avg_scales, torch.float32, scales), ("sq_scales", sq_scales, torch.float32, scales), ("copies", copies, torch.bfloat16, sizes)]
+    every = [t for _, ts, _, _ in lists if ts is not None for t in ts if t is not None]
+    arrays = [pointers(*x) for x in lists]
+    states = ESC_STATES_E4M3 if eight else ESC_STATES_F32
+    chunks = ctypes.c_longlong()
+    with _on_device(*every):
+        bytes_ = esc_adamw_plan_bytes(sizes)
+        if bytes_ == 0:
+            raise ValueError("invalid sizes")
+        table = torch.empty(bytes_, dtype=torch.uint8, device="cuda")
+        _check(lib().esc_adamw_plan_init(n, (ctypes.c_longlong * n)(*sizes), *arrays, _dtype_code(params[0]), _dtype_code(grads[0]), states, _ptr(table), bytes_,
+                                         ctypes.byref(chunks), _stream(stream)), "esc_adamw_plan_init")
+    return AdamwPlan(table, chunks.value, _dtype_code(params[0]), _dtype_code(grads[0]), states, every)
+
+
+new_adamw_plan = esc_adamw_plan_init
+
+
+def esc_adamw_scalars(step, lr, beta1, beta2, weight_decay, grad_scale=1.0):
+    """The four numbers that a `scalars` tensor of esc_adamw_step holds."""
+    out = (ctypes.c_float * 4)()
+    _check(lib().esc_adamw_scalars(int(step), lr, beta1, beta2, weight_decay, grad_scale, out), "esc_adamw_scalars")
+    return list(out)
+
+
+def esc_adamw_step(plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, grad_scale=1.0, scalars=None, skip=None, stream=None):
+    """One AdamW step over the plan's tensors.  scalars (4 fp32 on the device, from esc_adamw_scalars) replaces step, lr, weight_decay and
+    grad_scale, for captured graphs; skip: an int32 on the device, not zero: the call changes nothing."""
+    import torch
+
+    _dense("scalars", scalars, (4,), torch.float32)
+    if skip is not None and (skip.numel() != 1 or skip.dtype != torch.int32):
+        raise ValueError("skip has to be one int32")
+    with _on_device(plan.table, scalars, skip):
+        _check(lib().esc_adamw_step(_ptr(plan.table), plan.n_chunks, plan.param_dtype, plan.grad_dtype, plan.states, int(step), lr, beta1, beta2, eps,
+                                    weight_decay, grad_scale, _ptr(scalars), _ptr(skip), _stream(stream)), "esc_adamw_step")

@@ -2,19 +2,21 @@
 from __future__ import annotations
 
 import os
+import re
 import shutil
 import subprocess
+from concurrent.futures import ThreadPoolExecutor
 from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 LIB_DIR = PKG / "lib"
+OBJ_DIR = LIB_DIR / "obj"
 LIB = LIB_DIR / "libesc_convattn.so"
 INCLUDE = PKG.parent / "include"
 
 NVCC_FLAGS = [
-    "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-shared", "-Xcompiler", "-fPIC", "--use_fast_math=false",
+    "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC",
 ]
 
 
@@ -29,25 +31,50 @@ def sources():
     return sorted(CSRC.glob("*.cu"))
 
 
+def _includes(path: Path, seen: set) -> set:
+    """`path` and the files of this package that it includes, directly or not."""
+    if path in seen or not path.exists():
+        return seen
+    seen.add(path)
+    for name in re.findall(r'^\s*#include "([^"]+)"', path.read_text(), flags=re.M):
+        _includes((path.parent / name).resolve(), seen)
+    return seen
+
+
+def _newest(src: Path) -> float:
+    return max(p.stat().st_mtime for p in _includes(src.resolve(), set()))
+
+
 def needs_build() -> bool:
     if not LIB.exists():
         return True
     t = LIB.stat().st_mtime
-    deps = list(CSRC.glob("*.cu")) + list(CSRC.glob("*.cuh")) + list(INCLUDE.glob("*.h"))
+    deps = list(CSRC.glob("*.cu")) + list(CSRC.glob("*.cuh")) + list(CSRC.glob("*.h")) + list(INCLUDE.glob("*.h"))
     return any(d.stat().st_mtime > t for d in deps)
 
 
 def build(force: bool = False, verbose: bool = False) -> Path:
-    """Compile every .cu under csrc/ into lib/libesc_convattn.so."""
+    """Compile every .cu under csrc/ (side by side) and link lib/libesc_convattn.so.
+
+    Without `force` an object file newer than its source and everything that one includes is taken as it is."""
     if not force and not needs_build():
         return LIB
     LIB_DIR.mkdir(exist_ok=True)
+    OBJ_DIR.mkdir(exist_ok=True)
+    flags = [*NVCC_FLAGS, *(["-Xptxas=-v"] if verbose else []), "-I", str(INCLUDE)]
+
+    def compiled(src: Path) -> Path:
+        obj = OBJ_DIR / (src.stem + ".o")
+        if force or not obj.exists() or obj.stat().st_mtime <= _newest(src):
+            tmp = obj.with_suffix(".tmp%d.o" % os.getpid())
+            subprocess.check_call([_nvcc(), *flags, "-c", "-o", str(tmp), str(src)])
+            os.replace(tmp, obj)
+        return obj
+
+    with ThreadPoolExecutor() as pool:
+        objects = list(pool.map(compiled, sources()))
     tmp = LIB.with_suffix(".so.tmp%d" % os.getpid())
-    flags = [f for f in NVCC_FLAGS if not f.startswith("--use_fast_math")]
-    cmd = [_nvcc(), *flags, "-I", str(INCLUDE), "-o", str(tmp), *map(str, sources())]
-    if verbose:
-        cmd.insert(1, "-Xptxas=-v")
-    subprocess.check_call(cmd)
+    subprocess.check_call([_nvcc(), *NVCC_FLAGS, "-shared", "-o", str(tmp), *map(str, objects)])
     os.replace(tmp, LIB)
     return LIB
 

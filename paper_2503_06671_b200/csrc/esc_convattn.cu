@@ -14,6 +14,7 @@
 #include <string>
 #include <utility>
 
+#include "abi.h"
 #include "common.cuh"
 #include "gap_dynkernel.cuh"
 #include "stencil_generic.cuh"
@@ -57,6 +58,14 @@ int cuda_fail(cudaError_t e, const char* what) {
         cudaError_t e__ = (call);                             \
         if (e__ != cudaSuccess) return cuda_fail(e__, #call); \
     } while (0)
+
+}  // namespace
+namespace esc { namespace abi {
+int cuda_fail(cudaError_t e, const char* what) { return ::cuda_fail(e, what); }
+void launches_reset() { g_last_launches = 0; }
+void launched() { ++g_last_launches; }
+}}  // namespace esc::abi
+namespace {
 
 size_t elem_size(int dtype) { return dtype == ESC_BF16 ? 2 : 4; }
 
