@@ -150,6 +150,19 @@ template <int D> int forward_f32(const Call& c, void* out, float* lse, cudaStrea
     return launched();
 }
 
+template <int D, bool TWICE> int forward_bf16_t(const Call& c, void* out, float* lse, cudaStream_t st) {
+    using namespace wa::tc;
+    const int most = c.tokens() > 0 ? (c.tokens() + kQueries - 1) / kQueries : 1, tiles = (most + kMaxWarps - 1) / kMaxWarps, warps = (most + tiles - 1) / tiles;
+    const size_t smem = Smem<D>::bytes(Bias(c.wh, c.ww), TWICE);
+    ESC_TRY(allow_smem(forward<D, TWICE>, smem));
+    forward<D, TWICE><<<(unsigned)(c.windows() * c.heads * tiles), warps * 32, smem, st>>>(maps_of<bf16>(c), tiles, static_cast<bf16*>(out), lse);
+    return launched();
+}
+// Two copies of the table where they leave room for two blocks on an SM.
+template <int D> int forward_bf16(const Call& c, void* out, float* lse, cudaStream_t st) {
+    return wa::tc::Smem<D>::bytes(wa::tc::Bias(c.wh, c.ww), true) <= 112 * 1024 ? forward_bf16_t<D, true>(c, out, lse, st) : forward_bf16_t<D, false>(c, out, lse, st);
+}
+
 // Groups of a grid whose blocks add up sums for the table's gradient: about as many blocks as the SMs hold at two each.
 int table_groups(const Call& c) {
     const long long most = std::max(1LL, 2LL * abi::sm_count() / c.heads);
@@ -259,7 +272,8 @@ int esc_window_attention_forward(const void* q, const void* k, const void* v, in
         if (abi::overlap(out, c.dense_bytes(), p, c.strided_bytes()) || (lse && abi::overlap(lse, (size_t)c.pixels() * heads * 4, p, c.strided_bytes()))) return ESC_ERR_ALIAS;
     if (lse && abi::overlap(lse, (size_t)c.pixels() * heads * 4, out, c.dense_bytes())) return ESC_ERR_ALIAS;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == ESC_BF16) return ESC_ERR_UNSUPPORTED;
+    if (dtype == ESC_BF16)
+        return head_dim <= 16 ? forward_bf16<16>(c, out, lse, st) : head_dim <= 32 ? forward_bf16<32>(c, out, lse, st) : forward_bf16<64>(c, out, lse, st);
     return head_dim <= 16 ? forward_f32<16>(c, out, lse, st) : head_dim <= 32 ? forward_f32<32>(c, out, lse, st) : forward_f32<64>(c, out, lse, st);
 }
 

@@ -1,0 +1,46 @@
+// Warp-level bf16 tensor-core products: mma.sync.m16n8k16 (bf16 x bf16, fp32 sums) and the loads that feed it.  With g = lane / 4 and
+// t = lane % 4 a lane holds
+//   A [16 x 16]  a0: row g, columns 2t, 2t+1;  a1: row g + 8;  a2, a3: the same, columns + 8
+//   B [16 x 8]   b0: rows 2t, 2t+1, column g;  b1: rows + 8
+//   C [16 x 8]   c0, c1: row g, columns 2t, 2t+1;  c2, c3: row g + 8
+#pragma once
+#include "common.cuh"
+
+namespace esc { namespace wmma16 {
+
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1, float c2, float c3) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void ldsm(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool real) {   // 16 bytes, zeros where there is nothing to read
+    const int n = real ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// A staged tile: rows of D bf16 values in 16-byte pieces, the pieces of a row exchanged so that eight neighbouring rows' pieces of one
+// column, which an ldmatrix reads at a time, lie in different banks.
+template <int D> struct Tile {
+    static constexpr int kPieces = D / 8, kRowBytes = D * 2, kPeriod = 8 / kPieces;   // rows that 128 bytes hold
+    static __device__ __forceinline__ uint32_t at(int row, int piece) { return row * kRowBytes + ((piece ^ ((row / kPeriod) & (kPieces - 1))) << 4); }
+};
+
+}}  // namespace esc::wmma16

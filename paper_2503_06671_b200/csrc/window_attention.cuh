@@ -14,6 +14,7 @@
 #pragma once
 #include "common.cuh"
 #include "relpos_bias.cuh"
+#include "warp_mma.cuh"
 
 namespace esc { namespace winatt {
 
@@ -223,4 +224,248 @@ forward(Maps<float> m, int tiles, float* __restrict__ out, float* __restrict__ l
 }
 
 }  // namespace f32
+
+// ---- bf16: tensor cores ---------------------------------------------------------------------------------------------------
+// A warp has 32 queries (two tiles of 16) as A operands in registers; the block's keys and values pass by in staged tiles of 64.  s and
+// p never leave the registers: the accumulators of q k^T are, rounded to bf16, the A operand of p v.
+namespace tc {
+using bf16 = __nv_bfloat16;
+constexpr int kKeys = 64, kMaxWarps = 8, kQueries = 32;
+
+// The table in shared memory backwards, so that neighbouring keys read upwards, with rows of 2 ww entries: entry (key j, query i) is at
+// B(j) - A(i) + const, and in a window of even width the pair of keys that a lane holds starts at a place whose parity is
+// the query's.  A second copy one entry further along makes the odd ones even: both read pairs.
+struct Bias {
+    int pitch, size;                               // entries of a row, of a copy
+    __host__ __device__ Bias(int wh, int ww) : pitch(2 * ww), size((2 * wh - 1) * 2 * ww + 32) {}
+};
+__host__ __device__ constexpr int bias_gap() { return 16; }   // between the copies, so that their pairs lie in different banks
+
+// 16-byte pieces of `rows` rows of D channels, from the window's token `first` on.
+template <int D, int ROWS> struct Rows {
+    using T = wmma16::Tile<D>;
+    static __device__ __forceinline__ void stage(const bf16* __restrict__ src, long long stride, int W, const Window& w, int head_off, int d, bool wide, int first, uint32_t dst) {
+        const int n = w.tokens();
+        for (int e = threadIdx.x; e < ROWS * T::kPieces; e += blockDim.x) {
+            const int r = e / T::kPieces, c = e % T::kPieces, token = first + r;
+            const int y = token / w.w;
+            const long long pixel = w.pixel + (long long)y * W + (token - y * w.w);
+            const bool real = token < n && c * 8 < d;
+            const bf16* p = src + (real ? pixel * stride + head_off + c * 8 : 0);
+            const uint32_t at = dst + T::at(r, c);
+            if (wide) {
+                wmma16::cp16(at, p, real);
+            } else {
+                uint32_t v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t lo = real && c * 8 + 2 * i < d ? (uint32_t)__bfloat16_as_ushort(p[2 * i]) : 0u;
+                    const uint32_t hi = real && c * 8 + 2 * i + 1 < d ? (uint32_t)__bfloat16_as_ushort(p[2 * i + 1]) : 0u;
+                    v[i] = lo | hi << 16;
+                }
+                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+            }
+        }
+    }
+};
+
+// Whether rows of d channels can be read in pieces of 16 bytes.
+__device__ __forceinline__ bool pieces(const void* p, long long stride, int d) {
+    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride % 8 == 0 && d % 8 == 0;
+}
+
+template <int D> struct Smem {
+    static constexpr int kTile = kKeys * D * 2;
+    static __host__ __device__ size_t bytes(const Bias& b, bool twice) { return 4 * kTile + 2 * kKeys * 4 + (size_t)b.size * 4 * (twice ? 2 : 1) + (twice ? bias_gap() * 4 : 0); }
+};
+
+template <int D, bool TWICE>
+__global__ void __launch_bounds__(kMaxWarps * 32, D <= 32 ? 2 : 1)
+forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse) {
+    using namespace wmma16;
+    constexpr int KC = D / 16, NT = kKeys / 8, ON = D / 8;          // steps along the channels, tiles of 8 keys, of 8 channels of out
+    extern __shared__ __align__(128) unsigned char raw[];
+    int* bs = reinterpret_cast<int*>(raw + 4 * Smem<D>::kTile);     // B of the staged keys, two tiles
+    float* table = reinterpret_cast<float*>(bs + 2 * kKeys);
+    const uint32_t tile0 = smem_addr(raw);
+    int id = blockIdx.x;
+    const int tile = id % tiles; id /= tiles;
+    const int head = id % m.heads;
+    const Window w = window_at(m, id / m.heads);
+    const int n = w.tokens(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int block_first = tile * (blockDim.x >> 5) * kQueries, first = block_first + warp * kQueries;
+    if (block_first >= n) return;
+    const Bias bias(m.wh, m.ww);
+    const int head_off = head * m.d;
+    const bool wide_k = pieces(m.k, m.stride, m.d), wide_v = pieces(m.v, m.stride, m.d);
+
+    auto stage = [&](int key, int buf) {
+        Rows<D, kKeys>::stage(m.k, m.stride, m.W, w, head_off, m.d, wide_k, key, tile0 + buf * 2 * Smem<D>::kTile);
+        Rows<D, kKeys>::stage(m.v, m.stride, m.W, w, head_off, m.d, wide_v, key, tile0 + (buf * 2 + 1) * Smem<D>::kTile);
+        for (int r = threadIdx.x; r < kKeys; r += blockDim.x) {
+            const int j = key + r < n ? key + r : 0, y = j / w.w;    // keys behind the last read the first one's bias, an even place like theirs
+            bs[buf * kKeys + r] = y * bias.pitch + j - y * w.w;
+        }
+        cp_commit();
+    };
+    stage(0, 0);
+    // the table, backwards: entry (dy, dx) at (wh - 1 - dy) pitch + ww - 1 - dx
+    {
+        const int cols = 2 * m.ww - 1, rows = 2 * m.wh - 1;
+        for (int o = threadIdx.x; o < rows * cols; o += blockDim.x) {
+            const int r = o / cols, c = o - r * cols;
+            const float x = relpos::table_at(m.table, m.bucket, m.n_buckets, m.heads, head, o);
+            const float v = x <= kMasked ? -INFINITY : x * m.inv_scale;
+            const int at = (rows - 1 - r) * bias.pitch + cols - 1 - c;
+            table[at] = v;
+            if (TWICE) table[bias.size + bias_gap() + at + 1] = v;
+        }
+    }
+    const bool pairs = TWICE && (w.w & 1) == 0;
+
+    // queries: operands, and where their rows of the bias start
+    uint32_t q[2][KC][4];
+    int at[4];                                                      // rows g, g + 8 of both tiles
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int i = min(first + 8 * r + g, n - 1);
+        const int y = i / w.w, x = i - y * w.w;
+        at[r] = (m.wh - 1 - y) * bias.pitch + m.ww - 1 - x;          // + B(j): the place of (i, j)
+        const bf16* p = m.q + (w.pixel + (long long)y * m.W + x) * m.stride + head_off;
+        const bool even = ((reinterpret_cast<uintptr_t>(p) & 3) == 0);
+#pragma unroll
+        for (int k = 0; k < KC; ++k)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int c = 16 * k + 8 * h + 2 * t;
+                uint32_t v = 0;
+                if (even && c + 1 < m.d) v = *reinterpret_cast<const uint32_t*>(p + c);
+                else {
+                    if (c < m.d) v = __bfloat16_as_ushort(p[c]);
+                    if (c + 1 < m.d) v |= (uint32_t)__bfloat16_as_ushort(p[c + 1]) << 16;
+                }
+                q[r >> 1][k][(r & 1) + 2 * h] = v;
+            }
+        if (TWICE && pairs && (at[r] & 1)) at[r] += bias.size + bias_gap() + 1;
+    }
+    const float c = m.scale * kLog2e;
+    float o[2][ON][4], top[4], sum[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) { top[r] = -INFINITY; sum[r] = 0.0f; }
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int x = 0; x < ON; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[a][x][e] = 0.0f;
+
+    for (int key = 0, buf = 0; key < n; key += kKeys, buf ^= 1) {
+        cp_wait<0>();
+        __syncthreads();                                            // this tile is there, the other one is free
+        if (key + kKeys < n) stage(key + kKeys, buf ^ 1);
+        const uint32_t ks = tile0 + buf * 2 * Smem<D>::kTile, vs = ks + Smem<D>::kTile;
+        float s[2][NT][4];
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            const int* b = bs + buf * kKeys + 8 * x + 2 * t;
+            if (pairs) {
+                const int b0 = b[0];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float2 v = *reinterpret_cast<const float2*>(table + at[r] + b0);
+                    s[r >> 1][x][2 * (r & 1)] = v.x; s[r >> 1][x][2 * (r & 1) + 1] = v.y;
+                }
+            } else {
+                const int b0 = b[0], b1 = b[1];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    s[r >> 1][x][2 * (r & 1)] = table[at[r] + b0]; s[r >> 1][x][2 * (r & 1) + 1] = table[at[r] + b1];
+                }
+            }
+        }
+        // keys of a pair of tiles as B operands: rows 8 (lane / 16) + lane % 8, piece lane / 8 % 2 of the 16 channels
+#pragma unroll
+        for (int x = 0; x < NT; x += 2)
+#pragma unroll
+            for (int k = 0; k < KC; ++k) {
+                uint32_t b[4];
+                ldsm(b, ks + Tile<D>::at(8 * x + (lane >> 4) * 8 + (lane & 7), 2 * k + ((lane >> 3) & 1)));
+#pragma unroll
+                for (int a = 0; a < 2; ++a) { mma(s[a][x], q[a][k], b[0], b[1]); mma(s[a][x + 1], q[a][k], b[2], b[3]); }
+            }
+        if (key + kKeys > n) {
+#pragma unroll
+            for (int x = 0; x < NT; ++x)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (key + 8 * x + 2 * t + e >= n) s[0][x][e] = s[0][x][e + 2] = s[1][x][e] = s[1][x][e + 2] = -INFINITY;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int a = r >> 1, e = 2 * (r & 1);
+            float x = fmaxf(s[a][0][e], s[a][0][e + 1]);
+#pragma unroll
+            for (int y = 1; y < NT; ++y) x = fmaxf(x, fmaxf(s[a][y][e], s[a][y][e + 1]));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+            x = fmaxf(x, top[r]);
+            const float base = x == -INFINITY ? 0.0f : x * c, old = ex2(fmaf(top[r], c, -base));
+            top[r] = x;
+            float part = 0.0f;
+#pragma unroll
+            for (int y = 0; y < NT; ++y) {
+                s[a][y][e] = ex2(fmaf(s[a][y][e], c, -base));
+                s[a][y][e + 1] = ex2(fmaf(s[a][y][e + 1], c, -base));
+                part += s[a][y][e] + s[a][y][e + 1];
+            }
+            sum[r] = fmaf(sum[r], old, part);
+#pragma unroll
+            for (int y = 0; y < ON; ++y) { o[a][y][e] *= old; o[a][y][e + 1] *= old; }
+        }
+        // p v: 16 keys at a time; values transposed on the way in: rows 8 (lane / 8 % 2) + lane % 8, piece lane / 16 of 16 channels
+#pragma unroll
+        for (int x = 0; x < NT; x += 2) {
+            uint32_t p[2][4];
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+                p[a][0] = pack(s[a][x][0], s[a][x][1]); p[a][1] = pack(s[a][x][2], s[a][x][3]);
+                p[a][2] = pack(s[a][x + 1][0], s[a][x + 1][1]); p[a][3] = pack(s[a][x + 1][2], s[a][x + 1][3]);
+            }
+#pragma unroll
+            for (int k = 0; k < KC; ++k) {
+                uint32_t b[4];
+                ldsm_t(b, vs + Tile<D>::at(8 * x + ((lane >> 3) & 1) * 8 + (lane & 7), 2 * k + (lane >> 4)));
+#pragma unroll
+                for (int a = 0; a < 2; ++a) { mma(o[a][2 * k], p[a], b[0], b[1]); mma(o[a][2 * k + 1], p[a], b[2], b[3]); }
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        float x = sum[r];
+        x += __shfl_xor_sync(0xffffffffu, x, 1);
+        x += __shfl_xor_sync(0xffffffffu, x, 2);
+        const int i = first + 8 * r + g, a = r >> 1, e = 2 * (r & 1);
+        if (i >= n) continue;
+        const long long pixel = pixel_of(m, w, i);
+        const float inv = x == 0.0f ? 0.0f : 1.0f / x;
+        bf16* to = out + (pixel * m.heads + head) * m.d;
+        const bool even = (m.d & 1) == 0;
+#pragma unroll
+        for (int y = 0; y < ON; ++y) {
+            const int ch = 8 * y + 2 * t;
+            const float u = o[a][y][e] * inv, v = o[a][y][e + 1] * inv;
+            if (even && ch < m.d) *reinterpret_cast<uint32_t*>(to + ch) = pack(u, v);
+            else {
+                if (ch < m.d) to[ch] = __float2bfloat16_rn(u);
+                if (ch + 1 < m.d) to[ch + 1] = __float2bfloat16_rn(v);
+            }
+        }
+        if (lse && t == 0) {
+            const long long hw = (long long)m.H * m.W;
+            lse[((long long)w.b * m.heads + head) * hw + pixel - w.b * hw] = x == 0.0f ? -INFINITY : fmaf(top[r], m.scale, logf(x));
+        }
+    }
+}
+}  // namespace tc
 }}  // namespace esc::winatt
