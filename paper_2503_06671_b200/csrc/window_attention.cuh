@@ -60,6 +60,45 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// Two fp32 values in one register pair, and arithmetic on both at a time.
+using Two = unsigned long long;
+__device__ __forceinline__ Two two(float x, float y) {
+    Two d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(x), "f"(y));
+    return d;
+}
+__device__ __forceinline__ void apart(Two v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ Two add2(Two a, Two b) {
+    Two d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+    Two d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float2 lds2(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr));
+    return v;
+}
+__device__ __forceinline__ float lds1(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+    return v;
+}
+
 // The head's table into shared memory, divided by the scale.
 template <typename T> __device__ __forceinline__ void stage_table(const Maps<T>& m, int head, float* dst) {
     const int offsets = (2 * m.wh - 1) * (2 * m.ww - 1);
@@ -230,7 +269,8 @@ forward(Maps<float> m, int tiles, float* __restrict__ out, float* __restrict__ l
 // p never leave the registers: the accumulators of q k^T are, rounded to bf16, the A operand of p v.
 namespace tc {
 using bf16 = __nv_bfloat16;
-constexpr int kKeys = 64, kMaxWarps = 8, kQueries = 32;
+constexpr int kKeys = 128, kStep = 32, kMaxWarps = 8, kQueries = 32;   // keys of a staged tile, of a step; queries of a warp
+constexpr float kSlack = 8.0f;                     // a row's base follows its maximum where that is 2^8 above
 
 // The table in shared memory backwards, so that neighbouring keys read upwards, with rows of 2 ww entries: entry (key j, query i) is at
 // B(j) - A(i) + const, and in a window of even width the pair of keys that a lane holds starts at a place whose parity is
@@ -241,17 +281,37 @@ struct Bias {
 };
 __host__ __device__ constexpr int bias_gap() { return 16; }   // between the copies, so that their pairs lie in different banks
 
-// 16-byte pieces of `rows` rows of D channels, from the window's token `first` on.
+// Where the tokens of a staged tile are.  One warp walks them, kPer of a lane's own 32 apart, and leaves for each its distance in pixels
+// from the window's first and 4 B, its distance in the table (tokens behind the last get the first one's, which is as even as theirs would be).
+template <int ROWS> struct Walk {
+    static constexpr int kPer = ROWS / 32;
+    int y[kPer], x[kPer], step_y, step_x;
+    __device__ __forceinline__ void start(const Window& w, int lane) {
+        step_y = ROWS / w.w; step_x = ROWS - step_y * w.w;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) { const int r = lane + 32 * i; y[i] = r / w.w; x[i] = r - y[i] * w.w; }
+    }
+    __device__ __forceinline__ void next(const Window& w, int W, int pitch, int lane, long long* pixel, int* b) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const bool in = y[i] < w.h;
+            pixel[lane + 32 * i] = in ? (long long)y[i] * W + x[i] : -1;
+            b[lane + 32 * i] = in ? 4 * (y[i] * pitch + x[i]) : 0;
+            y[i] += step_y; x[i] += step_x;
+            if (x[i] >= w.w) { x[i] -= w.w; ++y[i]; }
+        }
+    }
+};
+
+// ROWS rows of D channels into a staged tile; `pixel` from Walk.
 template <int D, int ROWS> struct Rows {
     using T = wmma16::Tile<D>;
-    static __device__ __forceinline__ void stage(const bf16* __restrict__ src, long long stride, int W, const Window& w, int head_off, int d, bool wide, int first, uint32_t dst) {
-        const int n = w.tokens();
+    static __device__ __forceinline__ void stage(const bf16* __restrict__ first, long long stride, int d, bool wide, const long long* pixel, uint32_t dst) {
         for (int e = threadIdx.x; e < ROWS * T::kPieces; e += blockDim.x) {
-            const int r = e / T::kPieces, c = e % T::kPieces, token = first + r;
-            const int y = token / w.w;
-            const long long pixel = w.pixel + (long long)y * W + (token - y * w.w);
-            const bool real = token < n && c * 8 < d;
-            const bf16* p = src + (real ? pixel * stride + head_off + c * 8 : 0);
+            const int r = e / T::kPieces, c = e % T::kPieces;
+            const long long px = pixel[r];
+            const bool real = px >= 0 && c * 8 < d;
+            const bf16* p = first + (real ? px * stride + c * 8 : 0);
             const uint32_t at = dst + T::at(r, c);
             if (wide) {
                 wmma16::cp16(at, p, real);
@@ -276,17 +336,20 @@ __device__ __forceinline__ bool pieces(const void* p, long long stride, int d) {
 
 template <int D> struct Smem {
     static constexpr int kTile = kKeys * D * 2;
-    static __host__ __device__ size_t bytes(const Bias& b, bool twice) { return 4 * kTile + 2 * kKeys * 4 + (size_t)b.size * 4 * (twice ? 2 : 1) + (twice ? bias_gap() * 4 : 0); }
+    static constexpr int kWalk = 3 * kKeys * (8 + 4);   // pixels and B of three tiles
+    static __host__ __device__ size_t bytes(const Bias& b, bool twice) { return 4 * kTile + kWalk + (size_t)b.size * 4 * (twice ? 2 : 1) + (twice ? bias_gap() * 4 : 0); }
 };
 
 template <int D, bool TWICE>
 __global__ void __launch_bounds__(kMaxWarps * 32, D <= 32 ? 2 : 1)
 forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse) {
     using namespace wmma16;
-    constexpr int KC = D / 16, NT = kKeys / 8, ON = D / 8;          // steps along the channels, tiles of 8 keys, of 8 channels of out
+    constexpr int KC = D / 16, NT = kStep / 8, ON = D / 8;          // steps along the channels, tiles of 8 keys, of 8 channels of out
+    constexpr int kTile = Smem<D>::kTile;
     extern __shared__ __align__(128) unsigned char raw[];
-    int* bs = reinterpret_cast<int*>(raw + 4 * Smem<D>::kTile);     // B of the staged keys, two tiles
-    float* table = reinterpret_cast<float*>(bs + 2 * kKeys);
+    long long* pixels = reinterpret_cast<long long*>(raw + 4 * kTile);
+    int* bs = reinterpret_cast<int*>(pixels + 3 * kKeys);
+    float* table = reinterpret_cast<float*>(bs + 3 * kKeys);
     const uint32_t tile0 = smem_addr(raw);
     int id = blockIdx.x;
     const int tile = id % tiles; id /= tiles;
@@ -297,15 +360,17 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
     if (block_first >= n) return;
     const Bias bias(m.wh, m.ww);
     const int head_off = head * m.d;
+    const bf16 *k0 = m.k + w.pixel * m.stride + head_off, *v0 = m.v + w.pixel * m.stride + head_off;
     const bool wide_k = pieces(m.k, m.stride, m.d), wide_v = pieces(m.v, m.stride, m.d);
-
-    auto stage = [&](int key, int buf) {
-        Rows<D, kKeys>::stage(m.k, m.stride, m.W, w, head_off, m.d, wide_k, key, tile0 + buf * 2 * Smem<D>::kTile);
-        Rows<D, kKeys>::stage(m.v, m.stride, m.W, w, head_off, m.d, wide_v, key, tile0 + (buf * 2 + 1) * Smem<D>::kTile);
-        for (int r = threadIdx.x; r < kKeys; r += blockDim.x) {
-            const int j = key + r < n ? key + r : 0, y = j / w.w;    // keys behind the last read the first one's bias, an even place like theirs
-            bs[buf * kKeys + r] = y * bias.pitch + j - y * w.w;
-        }
+    Walk<kKeys> walk;
+    if (warp == 0) {
+        walk.start(w, lane);
+        walk.next(w, m.W, bias.pitch, lane, pixels, bs);
+    }
+    __syncthreads();
+    auto stage = [&](int buf, int place) {
+        Rows<D, kKeys>::stage(k0, m.stride, m.d, wide_k, pixels + place * kKeys, tile0 + buf * 2 * kTile);
+        Rows<D, kKeys>::stage(v0, m.stride, m.d, wide_v, pixels + place * kKeys, tile0 + (buf * 2 + 1) * kTile);
         cp_commit();
     };
     stage(0, 0);
@@ -321,16 +386,17 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
             if (TWICE) table[bias.size + bias_gap() + at + 1] = v;
         }
     }
+    if (warp == 0 && kKeys < n) walk.next(w, m.W, bias.pitch, lane, pixels + kKeys, bs + kKeys);
     const bool pairs = TWICE && (w.w & 1) == 0;
 
     // queries: operands, and where their rows of the bias start
     uint32_t q[2][KC][4];
-    int at[4];                                                      // rows g, g + 8 of both tiles
+    uint32_t at[4];                                                 // rows g, g + 8 of both tiles; + 4 B(j): where (i, j) is
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const int i = min(first + 8 * r + g, n - 1);
         const int y = i / w.w, x = i - y * w.w;
-        at[r] = (m.wh - 1 - y) * bias.pitch + m.ww - 1 - x;          // + B(j): the place of (i, j)
+        at[r] = (m.wh - 1 - y) * bias.pitch + m.ww - 1 - x;
         const bf16* p = m.q + (w.pixel + (long long)y * m.W + x) * m.stride + head_off;
         const bool even = ((reinterpret_cast<uintptr_t>(p) & 3) == 0);
 #pragma unroll
@@ -347,11 +413,17 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
                 q[r >> 1][k][(r & 1) + 2 * h] = v;
             }
         if (TWICE && pairs && (at[r] & 1)) at[r] += bias.size + bias_gap() + 1;
+        at[r] = smem_addr(table) + 4 * at[r];
     }
     const float c = m.scale * kLog2e;
-    float o[2][ON][4], top[4], sum[4];
+    const Two by = two(c, c);
+    // A row's powers are 2^(c s - base).  The base is the row's first maximum and moves only when one is kSlack above it (p is then at
+    // most 2^8, which costs nothing in a floating format), so that most steps only look whether any row of the warp has to move.
+    const float slack = kSlack / c;
+    float o[2][ON][4], top[4], limit[4];
+    Two off[4], sum[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) { top[r] = -INFINITY; sum[r] = 0.0f; }
+    for (int r = 0; r < 4; ++r) { top[r] = limit[r] = -INFINITY; sum[r] = off[r] = two(0.0f, 0.0f); }
 #pragma unroll
     for (int a = 0; a < 2; ++a)
 #pragma unroll
@@ -359,90 +431,114 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[a][x][e] = 0.0f;
 
-    for (int key = 0, buf = 0; key < n; key += kKeys, buf ^= 1) {
+    for (int tile_key = 0, buf = 0, place = 0; tile_key < n; tile_key += kKeys, buf ^= 1) {
+        const int next = place == 2 ? 0 : place + 1, free = 3 - place - next;
         cp_wait<0>();
-        __syncthreads();                                            // this tile is there, the other one is free
-        if (key + kKeys < n) stage(key + kKeys, buf ^ 1);
-        const uint32_t ks = tile0 + buf * 2 * Smem<D>::kTile, vs = ks + Smem<D>::kTile;
-        float s[2][NT][4];
+        __syncthreads();                                            // this tile and the next one's places are there; the other tile and the last one's places are free
+        if (tile_key + kKeys < n) stage(buf ^ 1, next);
+        if (warp == 0 && tile_key + 2 * kKeys < n) walk.next(w, m.W, bias.pitch, lane, pixels + free * kKeys, bs + free * kKeys);
+        const int steps = min(kKeys, n - tile_key + kStep - 1) / kStep;
+#pragma unroll 1
+        for (int step = 0; step < steps; ++step) {
+            const int key = tile_key + step * kStep;
+            const uint32_t ks = tile0 + buf * 2 * kTile + step * (kStep * D * 2), vs = ks + kTile;
+            const int* b = bs + place * kKeys + step * kStep + 2 * t;
+            float s[2][NT][4];
 #pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            const int* b = bs + buf * kKeys + 8 * x + 2 * t;
-            if (pairs) {
-                const int b0 = b[0];
+            for (int x = 0; x < NT; ++x) {
+                if (pairs) {
+                    const int b0 = b[8 * x];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float2 v = lds2(at[r] + b0);
+                        s[r >> 1][x][2 * (r & 1)] = v.x; s[r >> 1][x][2 * (r & 1) + 1] = v.y;
+                    }
+                } else {
+                    const int b0 = b[8 * x], b1 = b[8 * x + 1];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        s[r >> 1][x][2 * (r & 1)] = lds1(at[r] + b0); s[r >> 1][x][2 * (r & 1) + 1] = lds1(at[r] + b1);
+                    }
+                }
+            }
+            // keys of a pair of tiles as B operands: rows 8 (lane / 16) + lane % 8, piece lane / 8 % 2 of the 16 channels
+#pragma unroll
+            for (int x = 0; x < NT; x += 2)
+#pragma unroll
+                for (int k = 0; k < KC; ++k) {
+                    uint32_t f[4];
+                    ldsm(f, ks + Tile<D>::at(8 * x + (lane >> 4) * 8 + (lane & 7), 2 * k + ((lane >> 3) & 1)));
+#pragma unroll
+                    for (int a = 0; a < 2; ++a) { mma(s[a][x], q[a][k], f[0], f[1]); mma(s[a][x + 1], q[a][k], f[2], f[3]); }
+                }
+            if (key + kStep > n) {
+#pragma unroll
+                for (int x = 0; x < NT; ++x)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        if (key + 8 * x + 2 * t + e >= n) s[0][x][e] = s[0][x][e + 2] = s[1][x][e] = s[1][x][e + 2] = -INFINITY;
+            }
+            float high[4];
+            bool over = false;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int a = r >> 1, e = 2 * (r & 1);
+                high[r] = fmaxf(s[a][0][e], s[a][0][e + 1]);
+#pragma unroll
+                for (int y = 1; y < NT; ++y) high[r] = max3(high[r], s[a][y][e], s[a][y][e + 1]);
+                over |= high[r] > limit[r];
+            }
+            if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float2 v = *reinterpret_cast<const float2*>(table + at[r] + b0);
-                    s[r >> 1][x][2 * (r & 1)] = v.x; s[r >> 1][x][2 * (r & 1) + 1] = v.y;
+                    const int a = r >> 1, e = 2 * (r & 1);
+                    float x = fmaxf(high[r], top[r]);
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+                    const float base = x == -INFINITY ? 0.0f : x * c, old = ex2(fmaf(top[r], c, -base));   // 2^-inf = 0 the first time
+                    top[r] = x;
+                    limit[r] = x + slack;
+                    off[r] = two(-base, -base);
+                    sum[r] = mul2(sum[r], two(old, old));
+#pragma unroll
+                    for (int y = 0; y < ON; ++y) { o[a][y][e] *= old; o[a][y][e + 1] *= old; }
                 }
-            } else {
-                const int b0 = b[0], b1 = b[1];
+            }
+#pragma unroll
+            for (int y = 0; y < NT; ++y)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    s[r >> 1][x][2 * (r & 1)] = table[at[r] + b0]; s[r >> 1][x][2 * (r & 1) + 1] = table[at[r] + b1];
+                    const int a = r >> 1, e = 2 * (r & 1);
+                    float u, v;
+                    apart(fma2(two(s[a][y][e], s[a][y][e + 1]), by, off[r]), u, v);
+                    s[a][y][e] = ex2(u); s[a][y][e + 1] = ex2(v);
+                    sum[r] = add2(sum[r], two(s[a][y][e], s[a][y][e + 1]));
+                }
+            // p v: 16 keys at a time; values transposed on the way in: rows 8 (lane / 8 % 2) + lane % 8, piece lane / 16 of 16 channels
+#pragma unroll
+            for (int x = 0; x < NT; x += 2) {
+                uint32_t p[2][4];
+#pragma unroll
+                for (int a = 0; a < 2; ++a) {
+                    p[a][0] = pack(s[a][x][0], s[a][x][1]); p[a][1] = pack(s[a][x][2], s[a][x][3]);
+                    p[a][2] = pack(s[a][x + 1][0], s[a][x + 1][1]); p[a][3] = pack(s[a][x + 1][2], s[a][x + 1][3]);
+                }
+#pragma unroll
+                for (int k = 0; k < KC; ++k) {
+                    uint32_t f[4];
+                    ldsm_t(f, vs + Tile<D>::at(8 * x + ((lane >> 3) & 1) * 8 + (lane & 7), 2 * k + (lane >> 4)));
+#pragma unroll
+                    for (int a = 0; a < 2; ++a) { mma(o[a][2 * k], p[a], f[0], f[1]); mma(o[a][2 * k + 1], p[a], f[2], f[3]); }
                 }
             }
         }
-        // keys of a pair of tiles as B operands: rows 8 (lane / 16) + lane % 8, piece lane / 8 % 2 of the 16 channels
-#pragma unroll
-        for (int x = 0; x < NT; x += 2)
-#pragma unroll
-            for (int k = 0; k < KC; ++k) {
-                uint32_t b[4];
-                ldsm(b, ks + Tile<D>::at(8 * x + (lane >> 4) * 8 + (lane & 7), 2 * k + ((lane >> 3) & 1)));
-#pragma unroll
-                for (int a = 0; a < 2; ++a) { mma(s[a][x], q[a][k], b[0], b[1]); mma(s[a][x + 1], q[a][k], b[2], b[3]); }
-            }
-        if (key + kKeys > n) {
-#pragma unroll
-            for (int x = 0; x < NT; ++x)
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    if (key + 8 * x + 2 * t + e >= n) s[0][x][e] = s[0][x][e + 2] = s[1][x][e] = s[1][x][e + 2] = -INFINITY;
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int a = r >> 1, e = 2 * (r & 1);
-            float x = fmaxf(s[a][0][e], s[a][0][e + 1]);
-#pragma unroll
-            for (int y = 1; y < NT; ++y) x = fmaxf(x, fmaxf(s[a][y][e], s[a][y][e + 1]));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-            x = fmaxf(x, top[r]);
-            const float base = x == -INFINITY ? 0.0f : x * c, old = ex2(fmaf(top[r], c, -base));
-            top[r] = x;
-            float part = 0.0f;
-#pragma unroll
-            for (int y = 0; y < NT; ++y) {
-                s[a][y][e] = ex2(fmaf(s[a][y][e], c, -base));
-                s[a][y][e + 1] = ex2(fmaf(s[a][y][e + 1], c, -base));
-                part += s[a][y][e] + s[a][y][e + 1];
-            }
-            sum[r] = fmaf(sum[r], old, part);
-#pragma unroll
-            for (int y = 0; y < ON; ++y) { o[a][y][e] *= old; o[a][y][e + 1] *= old; }
-        }
-        // p v: 16 keys at a time; values transposed on the way in: rows 8 (lane / 8 % 2) + lane % 8, piece lane / 16 of 16 channels
-#pragma unroll
-        for (int x = 0; x < NT; x += 2) {
-            uint32_t p[2][4];
-#pragma unroll
-            for (int a = 0; a < 2; ++a) {
-                p[a][0] = pack(s[a][x][0], s[a][x][1]); p[a][1] = pack(s[a][x][2], s[a][x][3]);
-                p[a][2] = pack(s[a][x + 1][0], s[a][x + 1][1]); p[a][3] = pack(s[a][x + 1][2], s[a][x + 1][3]);
-            }
-#pragma unroll
-            for (int k = 0; k < KC; ++k) {
-                uint32_t b[4];
-                ldsm_t(b, vs + Tile<D>::at(8 * x + ((lane >> 3) & 1) * 8 + (lane & 7), 2 * k + (lane >> 4)));
-#pragma unroll
-                for (int a = 0; a < 2; ++a) { mma(o[a][2 * k], p[a], b[0], b[1]); mma(o[a][2 * k + 1], p[a], b[2], b[3]); }
-            }
-        }
+        place = next;
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        float x = sum[r];
+        float x, y_;
+        apart(sum[r], x, y_);
+        x += y_;
         x += __shfl_xor_sync(0xffffffffu, x, 1);
         x += __shfl_xor_sync(0xffffffffu, x, 2);
         const int i = first + 8 * r + g, a = r >> 1, e = 2 * (r & 1);
