@@ -169,6 +169,14 @@ int table_groups(const Call& c) {
     return (int)std::min(most, c.windows() * ((c.tokens() + 31) / 32));
 }
 
+// And of the tensor-core kernel, whose blocks have one tile of keys each: about two rounds of two blocks per SM.
+int key_tiles(const Call& c) { return (c.tokens() + wa::bwd::tc::kPairK - 1) / wa::bwd::tc::kPairK; }
+int pair_groups(const Call& c) {
+    const long long most = std::max(1LL, 4LL * abi::sm_count() / ((long long)c.heads * key_tiles(c)));
+    return (int)std::min(most, c.windows());
+}
+int table_slices(const Call& c) { return c.dtype == ESC_BF16 ? pair_groups(c) * key_tiles(c) : table_groups(c); }
+
 struct BackwardWs { float *dots, *part, *dense; size_t bytes; };
 BackwardWs carve(void* ws, const Call& c) {
     BackwardWs w;
@@ -177,7 +185,7 @@ BackwardWs carve(void* ws, const Call& c) {
     auto take = [&](size_t floats) { float* p = reinterpret_cast<float*>(base + off); off += abi::round_up(floats * sizeof(float), 256); return p; };
     const size_t offsets = (size_t)rp::offsets_of(c.wh, c.ww) * c.heads;
     w.dots = take((size_t)c.pixels() * c.heads);
-    w.part = take(offsets * table_groups(c));
+    w.part = take(offsets * std::max(table_groups(c), pair_groups(c) * key_tiles(c)));
     w.dense = take(offsets);
     w.bytes = off;
     return w;
@@ -200,6 +208,28 @@ template <int D> int backward_f32(const Call& c, wa::bwd::Grads<float> g, cudaSt
     if (!g.part) g.groups = (int)std::min<long long>(c.windows() * u.tiles, 0x7fffffff / c.heads);
     ESC_TRY(allow_smem(grad_q<D>, smem));
     grad_q<D><<<(unsigned)(g.groups * c.heads), u.threads, smem, st>>>(m, g, u.tiles);
+    return launched();
+}
+
+template <int D, bool KEYS, bool TWICE> int grad_rows_bf16(const Call& c, const wa::bwd::Grads<bf16>& g, cudaStream_t st) {
+    using namespace wa::bwd::tc;
+    constexpr int rows = 16 * row_tiles(D);
+    const int most = (c.tokens() + rows - 1) / rows, tiles = (most + kMaxWarps - 1) / kMaxWarps, warps = (most + tiles - 1) / tiles;
+    const size_t smem = RowSmem<D>::bytes(Bias(c.wh, c.ww), TWICE);
+    ESC_TRY(allow_smem(grad_rows<D, KEYS, TWICE>, smem));
+    grad_rows<D, KEYS, TWICE><<<(unsigned)(c.windows() * c.heads * tiles), warps * 32, smem, st>>>(maps_of<bf16>(c), g, tiles);
+    return launched();
+}
+template <int D> int backward_bf16(const Call& c, wa::bwd::Grads<bf16> g, cudaStream_t st) {
+    using namespace wa::bwd::tc;
+    const bool twice = RowSmem<D>::bytes(Bias(c.wh, c.ww), true) <= (D <= 16 ? 112 : 224) * 1024;
+    ESC_TRY(twice ? (grad_rows_bf16<D, true, true>(c, g, st)) : (grad_rows_bf16<D, true, false>(c, g, st)));
+    ESC_TRY(twice ? (grad_rows_bf16<D, false, true>(c, g, st)) : (grad_rows_bf16<D, false, false>(c, g, st)));
+    if (!g.part) return ESC_OK;
+    g.groups = pair_groups(c);
+    const size_t smem = PairSmem<D>::bytes((int)rp::offsets_of(c.wh, c.ww));
+    ESC_TRY(allow_smem(grad_table<D>, smem));
+    grad_table<D><<<(unsigned)(g.groups * key_tiles(c) * c.heads), 256, smem, st>>>(maps_of<bf16>(c), g, key_tiles(c));
     return launched();
 }
 
@@ -305,13 +335,22 @@ int esc_window_attention_backward(const void* q, const void* k, const void* v, i
     const BackwardWs w = carve(workspace, c);
     if (!workspace || !abi::aligned(workspace, 256) || workspace_bytes < w.bytes) return ESC_ERR_WORKSPACE;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == ESC_BF16) return ESC_ERR_UNSUPPORTED;
+    const int slices = table_slices(c);
+    float* part = grad_table ? w.part : nullptr;
+    if (dtype == ESC_BF16) {
+        ESC_TRY(launch_row_dots<bf16>(c, grad_out, out, w.dots, st));
+        const wa::bwd::Grads<bf16> g{static_cast<const bf16*>(grad_out), lse, w.dots, static_cast<bf16*>(grad_q), static_cast<bf16*>(grad_k), static_cast<bf16*>(grad_v),
+                                     part, (int)c.windows(), 0};
+        ESC_TRY(head_dim <= 16 ? backward_bf16<16>(c, g, st) : head_dim <= 32 ? backward_bf16<32>(c, g, st) : backward_bf16<64>(c, g, st));
+        if (!part) return ESC_OK;
+        return launch_table_sums<bf16>(part, w.dense, slices, false, heads, win_h, win_w, bucket, n_buckets, static_cast<bf16*>(grad_table), st);
+    }
     ESC_TRY(launch_row_dots<float>(c, grad_out, out, w.dots, st));
-    const wa::bwd::Grads<float> g{static_cast<const float*>(grad_out), lse, w.dots, static_cast<float*>(grad_q), static_cast<float*>(grad_k),
-                                  static_cast<float*>(grad_v), grad_table ? w.part : nullptr, (int)c.windows(), table_groups(c)};
+    const wa::bwd::Grads<float> g{static_cast<const float*>(grad_out), lse, w.dots, static_cast<float*>(grad_q), static_cast<float*>(grad_k), static_cast<float*>(grad_v),
+                                  part, (int)c.windows(), table_groups(c)};
     ESC_TRY(head_dim <= 16 ? backward_f32<16>(c, g, st) : head_dim <= 32 ? backward_f32<32>(c, g, st) : backward_f32<64>(c, g, st));
-    if (!grad_table) return ESC_OK;
-    return launch_table_sums<float>(w.part, w.dense, table_groups(c), false, heads, win_h, win_w, bucket, n_buckets, static_cast<float*>(grad_table), st);
+    if (!part) return ESC_OK;
+    return launch_table_sums<float>(part, w.dense, slices, false, heads, win_h, win_w, bucket, n_buckets, static_cast<float*>(grad_table), st);
 }
 
 }  // extern "C"

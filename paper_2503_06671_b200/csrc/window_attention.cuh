@@ -303,14 +303,14 @@ template <int ROWS> struct Walk {
     }
 };
 
-// ROWS rows of D channels into a staged tile; `pixel` from Walk.
+// ROWS rows of D channels into a staged tile, from the pixels (in [0, end), others give zeros) behind `first`.
 template <int D, int ROWS> struct Rows {
     using T = wmma16::Tile<D>;
-    static __device__ __forceinline__ void stage(const bf16* __restrict__ first, long long stride, int d, bool wide, const long long* pixel, uint32_t dst) {
+    static __device__ __forceinline__ void stage(const bf16* __restrict__ first, long long stride, int d, bool wide, const long long* pixel, uint32_t dst, long long end = 0x7fffffffffffffffLL) {
         for (int e = threadIdx.x; e < ROWS * T::kPieces; e += blockDim.x) {
             const int r = e / T::kPieces, c = e % T::kPieces;
             const long long px = pixel[r];
-            const bool real = px >= 0 && c * 8 < d;
+            const bool real = px >= 0 && px < end && c * 8 < d;
             const bf16* p = first + (real ? px * stride + c * 8 : 0);
             const uint32_t at = dst + T::at(r, c);
             if (wide) {
@@ -339,6 +339,50 @@ template <int D> struct Smem {
     static constexpr int kWalk = 3 * kKeys * (8 + 4);   // pixels and B of three tiles
     static __host__ __device__ size_t bytes(const Bias& b, bool twice) { return 4 * kTile + kWalk + (size_t)b.size * 4 * (twice ? 2 : 1) + (twice ? bias_gap() * 4 : 0); }
 };
+
+// The head's table for rows of queries (backwards: entry (dy, dx) at (wh - 1 - dy) pitch + ww - 1 - dx) or for rows of keys (as it is).
+template <bool TWICE, bool BACKWARDS> __device__ __forceinline__ void stage_bias(const Maps<bf16>& m, int head, const Bias& bias, float* table) {
+    const int cols = 2 * m.ww - 1, rows = 2 * m.wh - 1;
+    for (int o = threadIdx.x; o < rows * cols; o += blockDim.x) {
+        const int r = o / cols, c = o - r * cols;
+        const float x = relpos::table_at(m.table, m.bucket, m.n_buckets, m.heads, head, o);
+        const float v = x <= kMasked ? -INFINITY : x * m.inv_scale;
+        const int at = BACKWARDS ? (rows - 1 - r) * bias.pitch + cols - 1 - c : r * bias.pitch + c;
+        table[at] = v;
+        if (TWICE) table[bias.size + bias_gap() + at + 1] = v;
+    }
+}
+// Address in the staged table of the row (query or key) at (y, x), to which 4 (pitch y' + x') of the other one is added.
+template <bool TWICE> __device__ __forceinline__ uint32_t bias_row(const Maps<bf16>& m, const Bias& bias, bool pairs, int y, int x, uint32_t table) {
+    int at = (m.wh - 1 - y) * bias.pitch + m.ww - 1 - x;
+    if (TWICE && pairs && (at & 1)) at += bias.size + bias_gap() + 1;
+    return table + 4 * at;
+}
+// A row's channels as the A operand's registers of row g (half 0) or g + 8 (half 1).
+template <int KC> __device__ __forceinline__ void load_operand(const bf16* __restrict__ p, int d, int t, int half, uint32_t (&q)[KC][4]) {
+    const bool even = (reinterpret_cast<uintptr_t>(p) & 3) == 0;
+#pragma unroll
+    for (int k = 0; k < KC; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int c = 16 * k + 8 * h + 2 * t;
+            uint32_t v = 0;
+            if (even && c + 1 < d) v = *reinterpret_cast<const uint32_t*>(p + c);
+            else {
+                if (c < d) v = __bfloat16_as_ushort(p[c]);
+                if (c + 1 < d) v |= (uint32_t)__bfloat16_as_ushort(p[c + 1]) << 16;
+            }
+            q[k][half + 2 * h] = v;
+        }
+}
+// Two neighbouring channels of a result.
+__device__ __forceinline__ void store_pair(bf16* to, int ch, int d, float u, float v) {
+    if (ch + 1 < d && (reinterpret_cast<uintptr_t>(to) & 3) == 0) *reinterpret_cast<uint32_t*>(to + ch) = wmma16::pack(u, v);
+    else {
+        if (ch < d) to[ch] = __float2bfloat16_rn(u);
+        if (ch + 1 < d) to[ch + 1] = __float2bfloat16_rn(v);
+    }
+}
 
 template <int D, bool TWICE>
 __global__ void __launch_bounds__(kMaxWarps * 32, D <= 32 ? 2 : 1)
@@ -374,46 +418,18 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
         cp_commit();
     };
     stage(0, 0);
-    // the table, backwards: entry (dy, dx) at (wh - 1 - dy) pitch + ww - 1 - dx
-    {
-        const int cols = 2 * m.ww - 1, rows = 2 * m.wh - 1;
-        for (int o = threadIdx.x; o < rows * cols; o += blockDim.x) {
-            const int r = o / cols, c = o - r * cols;
-            const float x = relpos::table_at(m.table, m.bucket, m.n_buckets, m.heads, head, o);
-            const float v = x <= kMasked ? -INFINITY : x * m.inv_scale;
-            const int at = (rows - 1 - r) * bias.pitch + cols - 1 - c;
-            table[at] = v;
-            if (TWICE) table[bias.size + bias_gap() + at + 1] = v;
-        }
-    }
+    stage_bias<TWICE, true>(m, head, bias, table);
     if (warp == 0 && kKeys < n) walk.next(w, m.W, bias.pitch, lane, pixels + kKeys, bs + kKeys);
     const bool pairs = TWICE && (w.w & 1) == 0;
 
     // queries: operands, and where their rows of the bias start
-    uint32_t q[2][KC][4];
-    uint32_t at[4];                                                 // rows g, g + 8 of both tiles; + 4 B(j): where (i, j) is
+    uint32_t q[2][KC][4], at[4];                                    // at + 4 B(j): where (i, j) is
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const int i = min(first + 8 * r + g, n - 1);
         const int y = i / w.w, x = i - y * w.w;
-        at[r] = (m.wh - 1 - y) * bias.pitch + m.ww - 1 - x;
-        const bf16* p = m.q + (w.pixel + (long long)y * m.W + x) * m.stride + head_off;
-        const bool even = ((reinterpret_cast<uintptr_t>(p) & 3) == 0);
-#pragma unroll
-        for (int k = 0; k < KC; ++k)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int c = 16 * k + 8 * h + 2 * t;
-                uint32_t v = 0;
-                if (even && c + 1 < m.d) v = *reinterpret_cast<const uint32_t*>(p + c);
-                else {
-                    if (c < m.d) v = __bfloat16_as_ushort(p[c]);
-                    if (c + 1 < m.d) v |= (uint32_t)__bfloat16_as_ushort(p[c + 1]) << 16;
-                }
-                q[r >> 1][k][(r & 1) + 2 * h] = v;
-            }
-        if (TWICE && pairs && (at[r] & 1)) at[r] += bias.size + bias_gap() + 1;
-        at[r] = smem_addr(table) + 4 * at[r];
+        at[r] = bias_row<TWICE>(m, bias, pairs, y, x, smem_addr(table));
+        load_operand<KC>(m.q + (w.pixel + (long long)y * m.W + x) * m.stride + head_off, m.d, t, r & 1, q[r >> 1]);
     }
     const float c = m.scale * kLog2e;
     const Two by = two(c, c);
@@ -546,17 +562,8 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
         const long long pixel = pixel_of(m, w, i);
         const float inv = x == 0.0f ? 0.0f : 1.0f / x;
         bf16* to = out + (pixel * m.heads + head) * m.d;
-        const bool even = (m.d & 1) == 0;
 #pragma unroll
-        for (int y = 0; y < ON; ++y) {
-            const int ch = 8 * y + 2 * t;
-            const float u = o[a][y][e] * inv, v = o[a][y][e + 1] * inv;
-            if (even && ch < m.d) *reinterpret_cast<uint32_t*>(to + ch) = pack(u, v);
-            else {
-                if (ch < m.d) to[ch] = __float2bfloat16_rn(u);
-                if (ch + 1 < m.d) to[ch + 1] = __float2bfloat16_rn(v);
-            }
-        }
+        for (int y = 0; y < ON; ++y) store_pair(to, 8 * y + 2 * t, m.d, o[a][y][e] * inv, o[a][y][e + 1] * inv);
         if (lse && t == 0) {
             const long long hw = (long long)m.H * m.W;
             lse[((long long)w.b * m.heads + head) * hw + pixel - w.b * hw] = x == 0.0f ? -INFINITY : fmaf(top[r], m.scale, logf(x));

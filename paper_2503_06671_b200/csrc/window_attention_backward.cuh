@@ -212,4 +212,363 @@ grad_q(Maps<float> m, Grads<float> g, int tiles) {
 }
 
 }  // namespace f32
+
+// ---- bf16: tensor cores ---------------------------------------------------------------------------------------------------
+// Three kernels that each make p and dp anew from products of registers and staged tiles, so that every sum has one owner: the first
+// with rows of keys (g_k, g_v), the second with rows of queries (g_q), the third with a tile of query-key pairs that all windows pass
+// by (the table's gradient: the pairs' sums over the windows stay in registers, and go to their offsets once).
+namespace tc {
+using namespace winatt::tc;
+constexpr int kCols = 128;                                          // staged columns: queries for rows of keys, keys for rows of queries
+__host__ __device__ constexpr int row_tiles(int D) { return D <= 32 ? 2 : 1; }   // tiles of 16 rows of a warp
+
+template <int D> struct RowSmem {
+    static constexpr int kTile = kCols * D * 2, kWalk = 3 * kCols * (8 + 4), kRows = 2 * kCols * 2 * 4;   // base and D of two tiles' columns
+    static __host__ __device__ size_t bytes(const Bias& b, bool twice) { return 4 * kTile + kWalk + kRows + (size_t)b.size * 4 * (twice ? 2 : 1) + (twice ? bias_gap() * 4 : 0); }
+};
+
+// KEYS: rows are keys (operands k and v), columns queries (q and go): g_k += ds^T q, g_v += p^T go.
+// Else: rows are queries (q and go), columns keys (k and v): g_q += ds k.
+template <int D, bool KEYS, bool TWICE>
+__global__ void __launch_bounds__(kMaxWarps * 32, D <= 16 ? 2 : 1)
+grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
+    using namespace wmma16;
+    constexpr int KC = D / 16, ON = D / 8, MT = row_tiles(D), R = 2 * MT;   // R: rows that a lane has a part of
+    constexpr int kTile = RowSmem<D>::kTile;
+    extern __shared__ __align__(128) unsigned char raw[];
+    long long* pixels = reinterpret_cast<long long*>(raw + 4 * kTile);
+    int* bs = reinterpret_cast<int*>(pixels + 3 * kCols);
+    float* bases = reinterpret_cast<float*>(bs + 3 * kCols);        // [two tiles][-base, -D][kCols]
+    float* table = bases + 4 * kCols;
+    const uint32_t tile0 = smem_addr(raw);
+    int id = blockIdx.x;
+    const int tile = id % tiles; id /= tiles;
+    const int head = id % m.heads;
+    const Window w = window_at(m, id / m.heads);
+    const int n = w.tokens(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int block_first = tile * (blockDim.x >> 5) * (16 * MT), first = block_first + warp * 16 * MT;
+    if (block_first >= n) return;
+    const Bias bias(m.wh, m.ww);
+    const long long dense = (long long)m.heads * m.d, off = (long long)head * m.d, row0 = row_of(m, w, head, w.pixel);
+    const bf16 *c1 = (KEYS ? m.q : m.k) + w.pixel * m.stride + off, *c2 = KEYS ? gr.go + w.pixel * dense + off : m.v + w.pixel * m.stride + off;
+    const long long stride2 = KEYS ? dense : m.stride;
+    const bool wide1 = pieces(KEYS ? m.q : m.k, m.stride, m.d), wide2 = pieces(KEYS ? gr.go : m.v, stride2, m.d);
+    Walk<kCols> walk;
+    if (warp == 0) {
+        walk.start(w, lane);
+        walk.next(w, m.W, bias.pitch, lane, pixels, bs);
+    }
+    __syncthreads();
+    auto stage = [&](int buf, int place) {
+        const long long* px = pixels + place * kCols;
+        Rows<D, kCols>::stage(c1, m.stride, m.d, wide1, px, tile0 + buf * 2 * kTile);
+        Rows<D, kCols>::stage(c2, stride2, m.d, wide2, px, tile0 + (buf * 2 + 1) * kTile);
+        cp_commit();
+        if (KEYS)
+            for (int r = threadIdx.x; r < kCols; r += blockDim.x) {
+                const bool in = px[r] >= 0;
+                bases[(2 * buf) * kCols + r] = in ? -base_of(gr.lse[row0 + px[r]]) : -INFINITY;   // a column that is none: p = 0
+                bases[(2 * buf + 1) * kCols + r] = in ? -gr.dots[row0 + px[r]] : 0.0f;
+            }
+    };
+    stage(0, 0);
+    stage_bias<TWICE, !KEYS>(m, head, bias, table);
+    if (warp == 0 && kCols < n) walk.next(w, m.W, bias.pitch, lane, pixels + kCols, bs + kCols);
+    const bool pairs = TWICE && (w.w & 1) == 0;
+
+    uint32_t a1[MT][KC][4], a2[MT][KC][4], at[R];
+    float dot[R];
+    Two base[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const bool in = first + 8 * r + g < n;
+        const int i = min(first + 8 * r + g, n - 1), y = i / w.w, x = i - y * w.w;
+        const long long px = (long long)y * m.W + x;
+        at[r] = bias_row<TWICE>(m, bias, pairs, y, x, smem_addr(table));
+        load_operand<KC>((KEYS ? m.k : m.q) + (w.pixel + px) * m.stride + off, m.d, t, r & 1, a1[r >> 1]);
+        load_operand<KC>(KEYS ? m.v + (w.pixel + px) * m.stride + off : gr.go + (w.pixel + px) * dense + off, m.d, t, r & 1, a2[r >> 1]);
+        const float b = KEYS || !in ? -INFINITY : -base_of(gr.lse[row0 + px]);
+        base[r] = two(b, b);
+        dot[r] = KEYS ? 0.0f : -gr.dots[row0 + px];
+    }
+    const float c = m.scale * kLog2e;
+    const Two by = two(c, c);
+    float acc1[MT][ON][4], acc2[KEYS ? MT : 1][ON][4];
+#pragma unroll
+    for (int x = 0; x < ON; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int a = 0; a < MT; ++a) { acc1[a][x][e] = 0.0f; if (KEYS) acc2[a][x][e] = 0.0f; }
+
+    for (int tile_col = 0, buf = 0, place = 0; tile_col < n; tile_col += kCols, buf ^= 1) {
+        const int next = place == 2 ? 0 : place + 1, free = 3 - place - next;
+        cp_wait<0>();
+        __syncthreads();
+        if (tile_col + kCols < n) stage(buf ^ 1, next);
+        if (warp == 0 && tile_col + 2 * kCols < n) walk.next(w, m.W, bias.pitch, lane, pixels + free * kCols, bs + free * kCols);
+        const int steps = min(kCols, n - tile_col + 15) / 16;
+        const uint32_t t1 = tile0 + buf * 2 * kTile, t2 = t1 + kTile;
+#pragma unroll 1
+        for (int step = 0; step < steps; ++step) {
+            const int* b = bs + place * kCols + step * 16 + 2 * t;
+            float s[MT][2][4], dp[MT][2][4];
+            float2 col_base[2], col_dot[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int b0 = b[8 * x], b1 = pairs ? 0 : b[8 * x + 1];
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float2 v = pairs ? lds2(at[r] + b0) : make_float2(lds1(at[r] + b0), lds1(at[r] + b1));
+                    s[r >> 1][x][2 * (r & 1)] = v.x; s[r >> 1][x][2 * (r & 1) + 1] = v.y;
+                }
+                if (KEYS) {
+                    const float* row = bases + 2 * buf * kCols + step * 16 + 8 * x + 2 * t;
+                    col_base[x] = *reinterpret_cast<const float2*>(row);
+                    col_dot[x] = *reinterpret_cast<const float2*>(row + kCols);
+                }
+            }
+            const int row = step * 16 + (lane >> 4) * 8 + (lane & 7), piece = (lane >> 3) & 1;
+#pragma unroll
+            for (int k = 0; k < KC; ++k) {
+                uint32_t f[4], h[4];
+                ldsm(f, t1 + Tile<D>::at(row, 2 * k + piece));
+                ldsm(h, t2 + Tile<D>::at(row, 2 * k + piece));
+#pragma unroll
+                for (int a = 0; a < MT; ++a) {
+                    mma(s[a][0], a1[a][k], f[0], f[1]); mma(s[a][1], a1[a][k], f[2], f[3]);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (k > 0) mma(dp[a][x], a2[a][k], h[2 * x], h[2 * x + 1]);
+                        else if (KEYS) mma(dp[a][x], a2[a][k], h[2 * x], h[2 * x + 1], col_dot[x].x, col_dot[x].y, col_dot[x].x, col_dot[x].y);
+                        else mma(dp[a][x], a2[a][k], h[2 * x], h[2 * x + 1], dot[2 * a], dot[2 * a], dot[2 * a + 1], dot[2 * a + 1]);
+                    }
+                }
+            }
+            const bool cut = !KEYS && tile_col + step * 16 + 16 > n;
+#pragma unroll
+            for (int a = 0; a < MT; ++a) {
+                uint32_t pp[4], pd[4];
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const Two bb = KEYS ? two(col_base[x].x, col_base[x].y) : base[2 * a + e];
+                        float u, v;
+                        apart(fma2(two(s[a][x][2 * e], s[a][x][2 * e + 1]), by, bb), u, v);
+                        u = ex2(u); v = ex2(v);
+                        if (cut) {
+                            const int j = tile_col + step * 16 + 8 * x + 2 * t;
+                            if (j >= n) u = 0.0f;
+                            if (j + 1 >= n) v = 0.0f;
+                        }
+                        if (KEYS) pp[2 * x + e] = pack(u, v);
+                        apart(mul2(two(u, v), two(dp[a][x][2 * e], dp[a][x][2 * e + 1])), u, v);
+                        pd[2 * x + e] = pack(u, v);
+                    }
+                const int trow = step * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), tpiece = lane >> 4;
+#pragma unroll
+                for (int k = 0; k < KC; ++k) {
+                    uint32_t f[4];
+                    ldsm_t(f, t1 + Tile<D>::at(trow, 2 * k + tpiece));
+                    mma(acc1[a][2 * k], pd, f[0], f[1]); mma(acc1[a][2 * k + 1], pd, f[2], f[3]);
+                    if (KEYS) {
+                        ldsm_t(f, t2 + Tile<D>::at(trow, 2 * k + tpiece));
+                        mma(acc2[a][2 * k], pp, f[0], f[1]); mma(acc2[a][2 * k + 1], pp, f[2], f[3]);
+                    }
+                }
+            }
+        }
+        place = next;
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int i = first + 8 * r + g, a = r >> 1, e = 2 * (r & 1);
+        if (i >= n) continue;
+        const long long to = pixel_of(m, w, i) * m.stride + off;
+#pragma unroll
+        for (int x = 0; x < ON; ++x) {
+            store_pair((KEYS ? gr.g_k : gr.g_q) + to, 8 * x + 2 * t, m.d, acc1[a][x][e] * m.scale, acc1[a][x][e + 1] * m.scale);
+            if (KEYS) store_pair(gr.g_v + to, 8 * x + 2 * t, m.d, acc2[a][x][e], acc2[a][x][e + 1]);
+        }
+    }
+}
+
+// The table's gradient.  A block has one head, 64 keys and a group of windows; for 128 queries at a time it walks its windows with the sums
+// of ds of its 128 x 64 pairs in registers (a warp 32 x 32, and their bias there too, so that nothing of the table is read in the
+// loop).  Windows of one width share the tokens' places; those of the last column, where it is narrower, come second.
+// Then every thread adds up the pairs of some offsets.
+constexpr int kPairQ = 128, kPairK = 64;
+template <int D> struct PairSmem {
+    static constexpr int kQ = kPairQ * D * 2, kK = kPairK * D * 2, kBuf = 2 * kQ + 2 * kK;
+    static constexpr int kSums = kPairQ * (kPairK + 1) * 4;         // the pairs' sums, over the staged tiles
+    static constexpr int kData = 2 * kBuf > kSums ? 2 * kBuf : kSums;
+    static __host__ __device__ size_t bytes(int offsets) { return kData + (2 * 2 * kPairQ + offsets) * sizeof(float) + (kPairQ + kPairK) * 8; }
+};
+template <int D>
+__global__ void __launch_bounds__(256, D <= 16 ? 2 : 1)
+grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles) {
+    using namespace wmma16;
+    constexpr int KC = D / 16;
+    using S = PairSmem<D>;
+    extern __shared__ __align__(128) unsigned char raw[];
+    float* bases = reinterpret_cast<float*>(raw + S::kData);        // [two windows][-base, -D][kPairQ]
+    long long* px = reinterpret_cast<long long*>(bases + 4 * kPairQ);   // of the queries, of the keys
+    float* sums = reinterpret_cast<float*>(px + kPairQ + kPairK);
+    const uint32_t data = smem_addr(raw);
+    const int head = blockIdx.x % m.heads, id = blockIdx.x / m.heads, group = id / key_tiles, key0 = id % key_tiles * kPairK;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, wq = (warp >> 1) * 32, wk = (warp & 1) * 32;
+    const int pitch = 2 * m.ww - 1, offsets = (2 * m.wh - 1) * pitch;
+    const long long dense = (long long)m.heads * m.d, off = (long long)head * m.d, hw = (long long)m.H * m.W;
+    const bool wide_q = pieces(m.q, m.stride, m.d), wide_k = pieces(m.k, m.stride, m.d), wide_v = pieces(m.v, m.stride, m.d), wide_g = pieces(gr.go, dense, m.d);
+    const float c = m.scale * kLog2e;
+    const Two by = two(c, c);
+    for (int o = threadIdx.x; o < offsets; o += 256) sums[o] = 0.0f;
+    const int full = m.W / m.ww, rest = m.W - full * m.ww;          // windows of whole width in a row; the last one's width
+    const int tall = min(m.wh, m.H);                                // rows of the tallest window
+    for (int narrow = 0; narrow < 2; ++narrow) {
+        const int per_row = narrow ? (rest > 0) : full, width = narrow ? rest : m.ww;
+        const int count = m.B * m.ny * per_row, tokens = tall * width;
+        if (count == 0 || key0 >= tokens) continue;
+        auto window = [&](int i) {                                  // the group's i-th
+            const int at = group + i * gr.groups, row = at / per_row;
+            return window_at(m, row * m.nx + (narrow ? full : at - row * per_row));
+        };
+        const int mine = group < count ? (count - group + gr.groups - 1) / gr.groups : 0;
+        if (mine == 0) continue;
+        for (int q0 = 0; q0 < tokens; q0 += kPairQ) {
+            __syncthreads();                                        // the last queries' sums and places are done with
+            for (int r = threadIdx.x; r < kPairQ + kPairK; r += 256) {
+                const int i = r < kPairQ ? q0 + r : key0 + r - kPairQ, y = i / width;
+                px[r] = i < tokens ? (long long)y * m.W + i - y * width : -1;
+            }
+            float bias[2][4][4], sum[2][4][4];
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int i = q0 + wq + 16 * a + 8 * (e >> 1) + g, j = key0 + wk + 8 * x + 2 * t + (e & 1);
+                        float v = -INFINITY;                        // pairs that are none: p = 0
+                        if (i < tokens && j < tokens) {
+                            v = relpos::table_at(m.table, m.bucket, m.n_buckets, m.heads, head, (i / width - j / width + m.wh - 1) * pitch + i % width - j % width + m.ww - 1);
+                            v = v <= kMasked ? -INFINITY : v * m.inv_scale;
+                        }
+                        bias[a][x][e] = v;
+                        sum[a][x][e] = 0.0f;
+                    }
+            __syncthreads();
+            auto stage = [&](int i, int buf) {
+                const Window w = window(i);
+                const uint32_t dst = data + buf * S::kBuf;
+                const long long end = (long long)(w.h - 1) * m.W + width;   // rows of a shorter window end early
+                Rows<D, kPairQ>::stage(m.q + w.pixel * m.stride + off, m.stride, m.d, wide_q, px, dst, end);
+                Rows<D, kPairQ>::stage(gr.go + w.pixel * dense + off, dense, m.d, wide_g, px, dst + S::kQ, end);
+                Rows<D, kPairK>::stage(m.k + w.pixel * m.stride + off, m.stride, m.d, wide_k, px + kPairQ, dst + 2 * S::kQ, end);
+                Rows<D, kPairK>::stage(m.v + w.pixel * m.stride + off, m.stride, m.d, wide_v, px + kPairQ, dst + 2 * S::kQ + S::kK, end);
+                cp_commit();
+                const long long row0 = ((long long)w.b * m.heads + head) * hw + w.pixel - w.b * hw;
+                for (int r = threadIdx.x; r < kPairQ; r += 256) {
+                    const bool in = px[r] >= 0 && px[r] < end;
+                    bases[2 * buf * kPairQ + r] = in ? -base_of(gr.lse[row0 + px[r]]) : -INFINITY;
+                    bases[(2 * buf + 1) * kPairQ + r] = in ? -gr.dots[row0 + px[r]] : 0.0f;
+                }
+            };
+            stage(0, 0);
+            for (int i = 0, buf = 0; i < mine; ++i, buf ^= 1) {
+                cp_wait<0>();
+                __syncthreads();
+                if (i + 1 < mine) stage(i + 1, buf ^ 1);
+                const Window w = window(i);
+                const int n = w.tokens();                           // keys from here on are not this window's
+                const uint32_t dst = data + buf * S::kBuf;
+                uint32_t q[2][KC][4], go[2][KC][4];
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int k = 0; k < KC; ++k) {
+                        const int row = wq + 16 * a + (lane & 15), piece = 2 * k + (lane >> 4);
+                        ldsm(q[a][k], dst + Tile<D>::at(row, piece));
+                        ldsm(go[a][k], dst + S::kQ + Tile<D>::at(row, piece));
+                    }
+                float dot[4];
+                Two base[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float b = bases[2 * buf * kPairQ + wq + 8 * r + g];
+                    base[r] = two(b, b);
+                    dot[r] = bases[(2 * buf + 1) * kPairQ + wq + 8 * r + g];
+                }
+#pragma unroll
+                for (int x = 0; x < 4; x += 2) {
+                    float s[2][2][4], dp[2][2][4];
+                    const int row = wk + 8 * x + (lane >> 4) * 8 + (lane & 7), piece = (lane >> 3) & 1;
+#pragma unroll
+                    for (int k = 0; k < KC; ++k) {
+                        uint32_t f[4], h[4];
+                        ldsm(f, dst + 2 * S::kQ + Tile<D>::at(row, 2 * k + piece));
+                        ldsm(h, dst + 2 * S::kQ + S::kK + Tile<D>::at(row, 2 * k + piece));
+#pragma unroll
+                        for (int a = 0; a < 2; ++a)
+#pragma unroll
+                            for (int y = 0; y < 2; ++y) {
+                                if (k > 0) { mma(s[a][y], q[a][k], f[2 * y], f[2 * y + 1]); mma(dp[a][y], go[a][k], h[2 * y], h[2 * y + 1]); }
+                                else {
+                                    const float* b = bias[a][x + y];
+                                    mma(s[a][y], q[a][k], f[2 * y], f[2 * y + 1], b[0], b[1], b[2], b[3]);
+                                    mma(dp[a][y], go[a][k], h[2 * y], h[2 * y + 1], dot[2 * a], dot[2 * a], dot[2 * a + 1], dot[2 * a + 1]);
+                                }
+                            }
+                    }
+                    const bool cut = key0 + wk + 8 * x + 16 > n;
+#pragma unroll
+                    for (int a = 0; a < 2; ++a)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                float u, v;
+                                apart(fma2(two(s[a][y][2 * e], s[a][y][2 * e + 1]), by, base[2 * a + e]), u, v);
+                                u = ex2(u); v = ex2(v);
+                                if (cut) {
+                                    const int j = key0 + wk + 8 * (x + y) + 2 * t;
+                                    if (j >= n) u = 0.0f;
+                                    if (j + 1 >= n) v = 0.0f;
+                                }
+                                float* to = &sum[a][x + y][2 * e];
+                                apart(fma2(two(u, v), two(dp[a][y][2 * e], dp[a][y][2 * e + 1]), two(to[0], to[1])), to[0], to[1]);
+                            }
+                }
+            }
+            // the pairs' sums to their offsets: every thread takes some offsets and walks the keys
+            __syncthreads();
+            float* pair = reinterpret_cast<float*>(raw);
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) pair[(wq + 16 * a + 8 * (e >> 1) + g) * (kPairK + 1) + wk + 8 * x + 2 * t + (e & 1)] = sum[a][x][e];
+            __syncthreads();
+            const int q_end = min(q0 + kPairQ, tokens), k_end = min(key0 + kPairK, tokens);
+            const int dy_lo = q0 / width - (k_end - 1) / width, dy_hi = (q_end - 1) / width - key0 / width, cols = 2 * width - 1;
+            for (int o = threadIdx.x; o < (dy_hi - dy_lo + 1) * cols; o += 256) {
+                const int dy = dy_lo + o / cols, dx = o % cols - (width - 1);
+                float v = 0.0f;
+                int yj = key0 / width, xj = key0 - yj * width;
+                for (int j = key0; j < k_end; ++j) {
+                    const int xi = xj + dx, i = (yj + dy) * width + xi;
+                    if ((unsigned)xi < (unsigned)width && i >= q0 && i < q_end) v += pair[(i - q0) * (kPairK + 1) + j - key0];
+                    if (++xj == width) { xj = 0; ++yj; }
+                }
+                sums[(dy + m.wh - 1) * pitch + dx + m.ww - 1] += v;
+            }
+        }
+    }
+    __syncthreads();
+    float* part = gr.part + ((size_t)id * m.heads + head) * offsets;
+    for (int o = threadIdx.x; o < offsets; o += 256) part[o] = sums[o];
+}
+}  // namespace tc
 }}}  // namespace esc::winatt::bwd
