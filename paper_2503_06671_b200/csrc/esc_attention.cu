@@ -52,7 +52,7 @@ template <typename G>
 int launch_table_sums(const float* part, float* dense, int slices, bool per_offset, int heads, int wh, int ww, const int* bucket, int n_buckets,
                       G* g_table, cudaStream_t st) {
     const int offsets = (int)rp::offsets_of(wh, ww);
-    rp::sum_slices<G><<<dim3((offsets + 255) / 256, heads), 256, 0, st>>>(part, slices, per_offset, heads, wh, ww, bucket ? dense : nullptr, g_table);
+    rp::sum_slices<G><<<dim3((offsets + 31) / 32, heads), 256, 0, st>>>(part, slices, per_offset, heads, wh, ww, bucket ? dense : nullptr, g_table);
     ESC_TRY(launched());
     if (!bucket) return ESC_OK;
     rp::sum_buckets<G><<<dim3((n_buckets + 31) / 32, heads), 256, 0, st>>>(dense, bucket, n_buckets, heads, offsets, g_table);
@@ -104,6 +104,7 @@ int check_sizes(int B, int heads, int d, int H, int W, int wh, int ww) {
     ESC_TRY(check_window(heads, wh, ww));
     const long double n = (long double)B * heads * H * W;
     if (n * d > 1.0e15L) return ESC_ERR_SHAPE;
+    if ((long double)std::min(wh, H) * W > 2.0e9L) return ESC_ERR_UNSUPPORTED;   // a pixel's distance from its window's first
     // one block per window, head and tile of queries (at least 32 of them)
     const long double blocks = (long double)B * ((H + wh - 1) / wh) * ((W + ww - 1) / ww) * heads * ((std::min(wh, H) * std::min(ww, W) + 31) / 32);
     return blocks > 2.0e9L ? ESC_ERR_UNSUPPORTED : ESC_OK;
@@ -152,7 +153,8 @@ template <int D> int forward_f32(const Call& c, void* out, float* lse, cudaStrea
 
 template <int D, bool TWICE> int forward_bf16_t(const Call& c, void* out, float* lse, cudaStream_t st) {
     using namespace wa::tc;
-    const int most = c.tokens() > 0 ? (c.tokens() + kQueries - 1) / kQueries : 1, tiles = (most + kMaxWarps - 1) / kMaxWarps, warps = (most + tiles - 1) / tiles;
+    constexpr int rows = 16 * row_tiles(D);
+    const int most = (c.tokens() + rows - 1) / rows, tiles = (most + kMaxWarps - 1) / kMaxWarps, warps = (most + tiles - 1) / tiles;
     const size_t smem = Smem<D>::bytes(Bias(c.wh, c.ww), TWICE);
     ESC_TRY(allow_smem(forward<D, TWICE>, smem));
     forward<D, TWICE><<<(unsigned)(c.windows() * c.heads * tiles), warps * 32, smem, st>>>(maps_of<bf16>(c), tiles, static_cast<bf16*>(out), lse);
@@ -169,23 +171,30 @@ int table_groups(const Call& c) {
     return (int)std::min(most, c.windows() * ((c.tokens() + 31) / 32));
 }
 
-// And of the tensor-core kernel, whose blocks have one tile of keys each: about two rounds of two blocks per SM.
+// And of the tensor-core kernel, whose blocks have a tile of keys each: the tiles of queries, then the windows are dealt to as many as fill
+// two rounds of two blocks per SM.
 int key_tiles(const Call& c) { return (c.tokens() + wa::bwd::tc::kPairK - 1) / wa::bwd::tc::kPairK; }
-int pair_groups(const Call& c) {
-    const long long most = std::max(1LL, 4LL * abi::sm_count() / ((long long)c.heads * key_tiles(c)));
-    return (int)std::min(most, c.windows());
+int pair_parts(const Call& c) {
+    const long long want = std::max(1LL, 4LL * abi::sm_count() / ((long long)c.heads * key_tiles(c)));
+    return (int)std::min<long long>(want, (c.tokens() + wa::bwd::tc::kPairQ - 1) / wa::bwd::tc::kPairQ);
 }
-int table_slices(const Call& c) { return c.dtype == ESC_BF16 ? pair_groups(c) * key_tiles(c) : table_groups(c); }
+int pair_groups(const Call& c) {
+    const long long want = std::max(1LL, 4LL * abi::sm_count() / ((long long)c.heads * key_tiles(c) * pair_parts(c)));
+    return (int)std::min(want, c.windows());
+}
+int pair_slices(const Call& c) { return pair_groups(c) * pair_parts(c) * key_tiles(c); }
+int table_slices(const Call& c) { return c.dtype == ESC_BF16 ? pair_slices(c) : table_groups(c); }
 
-struct BackwardWs { float *dots, *part, *dense; size_t bytes; };
+struct BackwardWs { float *bases, *dots, *part, *dense; size_t bytes; };
 BackwardWs carve(void* ws, const Call& c) {
     BackwardWs w;
     char* base = static_cast<char*>(ws);
     size_t off = 0;
     auto take = [&](size_t floats) { float* p = reinterpret_cast<float*>(base + off); off += abi::round_up(floats * sizeof(float), 256); return p; };
     const size_t offsets = (size_t)rp::offsets_of(c.wh, c.ww) * c.heads;
+    w.bases = take((size_t)c.pixels() * c.heads);
     w.dots = take((size_t)c.pixels() * c.heads);
-    w.part = take(offsets * std::max(table_groups(c), pair_groups(c) * key_tiles(c)));
+    w.part = take(offsets * std::max(table_groups(c), pair_slices(c)));
     w.dense = take(offsets);
     w.bytes = off;
     return w;
@@ -213,7 +222,7 @@ template <int D> int backward_f32(const Call& c, wa::bwd::Grads<float> g, cudaSt
 
 template <int D, bool KEYS, bool TWICE> int grad_rows_bf16(const Call& c, const wa::bwd::Grads<bf16>& g, cudaStream_t st) {
     using namespace wa::bwd::tc;
-    constexpr int rows = 16 * row_tiles(D);
+    constexpr int rows = 16 * grad_tiles(D);
     const int most = (c.tokens() + rows - 1) / rows, tiles = (most + kMaxWarps - 1) / kMaxWarps, warps = (most + tiles - 1) / tiles;
     const size_t smem = RowSmem<D>::bytes(Bias(c.wh, c.ww), TWICE);
     ESC_TRY(allow_smem(grad_rows<D, KEYS, TWICE>, smem));
@@ -229,14 +238,15 @@ template <int D> int backward_bf16(const Call& c, wa::bwd::Grads<bf16> g, cudaSt
     g.groups = pair_groups(c);
     const size_t smem = PairSmem<D>::bytes((int)rp::offsets_of(c.wh, c.ww));
     ESC_TRY(allow_smem(grad_table<D>, smem));
-    grad_table<D><<<(unsigned)(g.groups * key_tiles(c) * c.heads), 256, smem, st>>>(maps_of<bf16>(c), g, key_tiles(c));
+    grad_table<D><<<(unsigned)(pair_slices(c) * c.heads), 256, smem, st>>>(maps_of<bf16>(c), g, key_tiles(c), pair_parts(c));
     return launched();
 }
 
-template <typename T> int launch_row_dots(const Call& c, const void* go, const void* out, float* dots, cudaStream_t st) {
+template <typename T> int launch_row_terms(const Call& c, const void* go, const void* out, const float* lse, const BackwardWs& w, cudaStream_t st) {
+    using namespace wa::bwd;
     const long long items = c.pixels() * c.heads;
-    const unsigned blocks = (unsigned)std::min<long long>((items + wa::bwd::kDotThreads - 1) / wa::bwd::kDotThreads, 16LL * abi::sm_count());
-    wa::bwd::row_dots<T><<<blocks, wa::bwd::kDotThreads, 0, st>>>(static_cast<const T*>(go), static_cast<const T*>(out), c.pixels(), (long long)c.H * c.W, c.heads, c.d, dots);
+    const unsigned blocks = (unsigned)std::min<long long>((items + kRowThreads - 1) / kRowThreads, 16LL * abi::sm_count());
+    row_terms<T><<<blocks, kRowThreads, 0, st>>>(static_cast<const T*>(go), static_cast<const T*>(out), lse, c.pixels(), (long long)c.H * c.W, c.heads, c.d, w.bases, w.dots);
     return launched();
 }
 
@@ -338,15 +348,15 @@ int esc_window_attention_backward(const void* q, const void* k, const void* v, i
     const int slices = table_slices(c);
     float* part = grad_table ? w.part : nullptr;
     if (dtype == ESC_BF16) {
-        ESC_TRY(launch_row_dots<bf16>(c, grad_out, out, w.dots, st));
-        const wa::bwd::Grads<bf16> g{static_cast<const bf16*>(grad_out), lse, w.dots, static_cast<bf16*>(grad_q), static_cast<bf16*>(grad_k), static_cast<bf16*>(grad_v),
+        ESC_TRY(launch_row_terms<bf16>(c, grad_out, out, lse, w, st));
+        const wa::bwd::Grads<bf16> g{static_cast<const bf16*>(grad_out), w.bases, w.dots, static_cast<bf16*>(grad_q), static_cast<bf16*>(grad_k), static_cast<bf16*>(grad_v),
                                      part, (int)c.windows(), 0};
         ESC_TRY(head_dim <= 16 ? backward_bf16<16>(c, g, st) : head_dim <= 32 ? backward_bf16<32>(c, g, st) : backward_bf16<64>(c, g, st));
         if (!part) return ESC_OK;
         return launch_table_sums<bf16>(part, w.dense, slices, false, heads, win_h, win_w, bucket, n_buckets, static_cast<bf16*>(grad_table), st);
     }
-    ESC_TRY(launch_row_dots<float>(c, grad_out, out, w.dots, st));
-    const wa::bwd::Grads<float> g{static_cast<const float*>(grad_out), lse, w.dots, static_cast<float*>(grad_q), static_cast<float*>(grad_k), static_cast<float*>(grad_v),
+    ESC_TRY(launch_row_terms<float>(c, grad_out, out, lse, w, st));
+    const wa::bwd::Grads<float> g{static_cast<const float*>(grad_out), w.bases, w.dots, static_cast<float*>(grad_q), static_cast<float*>(grad_k), static_cast<float*>(grad_v),
                                   part, (int)c.windows(), table_groups(c)};
     ESC_TRY(head_dim <= 16 ? backward_f32<16>(c, g, st) : head_dim <= 32 ? backward_f32<32>(c, g, st) : backward_f32<64>(c, g, st));
     if (!part) return ESC_OK;

@@ -131,28 +131,27 @@ sum_offsets(const T* __restrict__ g, int wh, int ww, float* __restrict__ part, i
     }
 }
 
-// Sum over the slices of an offset.  per_offset: every offset has as many as slices_at says, else `slices` of them.  `dense` gets
-// [heads][offsets] in fp32 for `sum_buckets`, else g_table gets [offsets][heads].
+// Sum over the slices of an offset: a block takes 32 offsets, a lane each, and its warps every eighth slice.  per_offset: every offset has as many as
+// slices_at says, else `slices` of them.  `dense` gets [heads][offsets] in fp32 for `sum_buckets`, else g_table gets [offsets][heads].
 template <typename G>
 __global__ void __launch_bounds__(256)
 sum_slices(const float* __restrict__ part, int slices, bool per_offset, int heads, int wh, int ww, float* __restrict__ dense, G* __restrict__ g_table) {
-    pdl_wait_primary();
-    const int pitch = 2 * ww - 1, offsets = (2 * wh - 1) * pitch;
-    const int o = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y;
-    if (o >= offsets) return;
-    if (per_offset) slices = slices_at(wh, ww, o / pitch - (wh - 1), (o % pitch) / 32 * 32 - (ww - 1));
-    const float* p = part + (size_t)head * offsets + o;
-    const size_t step = (size_t)heads * offsets;
+    const int pitch = 2 * ww - 1, offsets = (2 * wh - 1) * pitch, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int o = blockIdx.x * 32 + lane, head = blockIdx.y;
     float sum = 0.0f;
-    int s = 0;
-    for (; s + 8 <= slices; s += 8) {
-        float v[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = p[(s + u) * step];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) sum += v[u];
+    if (o < offsets) {
+        if (per_offset) slices = slices_at(wh, ww, o / pitch - (wh - 1), (o % pitch) / 32 * 32 - (ww - 1));
+        const float* p = part + (size_t)head * offsets + o;
+        const size_t step = (size_t)heads * offsets;
+#pragma unroll 4
+        for (int s = warp; s < slices; s += 8) sum += p[s * step];
     }
-    for (; s < slices; ++s) sum += p[s * step];
+    __shared__ float warps[8][32];
+    warps[warp][lane] = sum;
+    __syncthreads();
+    if (warp != 0 || o >= offsets) return;
+#pragma unroll
+    for (int w = 1; w < 8; ++w) sum += warps[w][lane];
     if (dense) dense[(size_t)head * offsets + o] = sum;
     else g_table[(size_t)o * heads + head] = Elem<G>::from_f32(sum);
 }
@@ -163,7 +162,6 @@ template <typename G>
 __global__ void __launch_bounds__(256)
 sum_buckets(const float* __restrict__ dense, const int* __restrict__ bucket, int n_buckets, int heads, int offsets, G* __restrict__ g_table) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, head = blockIdx.y, mine = blockIdx.x * 32 + lane;
-    pdl_wait_primary();
     float sum = 0.0f;
     for (int at = warp * 32; at < offsets; at += 256) {
         const bool ok = at + lane < offsets;

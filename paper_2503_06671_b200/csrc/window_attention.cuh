@@ -269,7 +269,12 @@ forward(Maps<float> m, int tiles, float* __restrict__ out, float* __restrict__ l
 // p never leave the registers: the accumulators of q k^T are, rounded to bf16, the A operand of p v.
 namespace tc {
 using bf16 = __nv_bfloat16;
-constexpr int kKeys = 128, kStep = 32, kMaxWarps = 8, kQueries = 32;   // keys of a staged tile, of a step; queries of a warp
+constexpr int kKeys = 128, kStep = 32, kMaxWarps = 8;   // keys of a staged tile, of a step
+#ifndef FMT
+#define FMT (D <= 32 ? 2 : 1)
+#endif
+__host__ __device__ constexpr int row_tiles(int D) { return FMT; }
+__host__ __device__ constexpr int blocks_of(int D) { return 2; }
 constexpr float kSlack = 8.0f;                     // a row's base follows its maximum where that is 2^8 above
 
 // The table in shared memory backwards, so that neighbouring keys read upwards, with rows of 2 ww entries: entry (key j, query i) is at
@@ -303,28 +308,34 @@ template <int ROWS> struct Walk {
     }
 };
 
-// ROWS rows of D channels into a staged tile, from the pixels (in [0, end), others give zeros) behind `first`.
+// A 16-byte piece of a row into shared memory, zeros where there is none.
+__device__ __forceinline__ void stage_piece(const bf16* p, uint32_t at, bool real, int left, bool wide) {
+    if (wide) {
+        wmma16::cp16(at, p, real);
+    } else {
+        uint32_t v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = real && 2 * i < left ? (uint32_t)__bfloat16_as_ushort(p[2 * i]) : 0u;
+            const uint32_t hi = real && 2 * i + 1 < left ? (uint32_t)__bfloat16_as_ushort(p[2 * i + 1]) : 0u;
+            v[i] = lo | hi << 16;
+        }
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+    }
+}
+// ROWS rows of D channels of two tensors into a staged tile each, from the pixels (in [0, end), others give zeros) behind their first.
 template <int D, int ROWS> struct Rows {
     using T = wmma16::Tile<D>;
-    static __device__ __forceinline__ void stage(const bf16* __restrict__ first, long long stride, int d, bool wide, const long long* pixel, uint32_t dst, long long end = 0x7fffffffffffffffLL) {
+    static __device__ __forceinline__ void stage(const bf16* __restrict__ one, long long stride1, bool wide1, uint32_t dst1, const bf16* __restrict__ two_, long long stride2,
+                                                 bool wide2, uint32_t dst2, int d, const long long* pixel, long long end = 0x7fffffffffffffffLL) {
         for (int e = threadIdx.x; e < ROWS * T::kPieces; e += blockDim.x) {
             const int r = e / T::kPieces, c = e % T::kPieces;
-            const long long px = pixel[r];
+            long long px = pixel[r];
             const bool real = px >= 0 && px < end && c * 8 < d;
-            const bf16* p = first + (real ? px * stride + c * 8 : 0);
-            const uint32_t at = dst + T::at(r, c);
-            if (wide) {
-                wmma16::cp16(at, p, real);
-            } else {
-                uint32_t v[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t lo = real && c * 8 + 2 * i < d ? (uint32_t)__bfloat16_as_ushort(p[2 * i]) : 0u;
-                    const uint32_t hi = real && c * 8 + 2 * i + 1 < d ? (uint32_t)__bfloat16_as_ushort(p[2 * i + 1]) : 0u;
-                    v[i] = lo | hi << 16;
-                }
-                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
-            }
+            px = real ? px : 0;
+            const int ch = real ? c * 8 : 0;
+            stage_piece(one + px * stride1 + ch, dst1 + T::at(r, c), real, d - ch, wide1);
+            stage_piece(two_ + px * stride2 + ch, dst2 + T::at(r, c), real, d - ch, wide2);
         }
     }
 };
@@ -343,14 +354,17 @@ template <int D> struct Smem {
 // The head's table for rows of queries (backwards: entry (dy, dx) at (wh - 1 - dy) pitch + ww - 1 - dx) or for rows of keys (as it is).
 template <bool TWICE, bool BACKWARDS> __device__ __forceinline__ void stage_bias(const Maps<bf16>& m, int head, const Bias& bias, float* table) {
     const int cols = 2 * m.ww - 1, rows = 2 * m.wh - 1;
-    for (int o = threadIdx.x; o < rows * cols; o += blockDim.x) {
-        const int r = o / cols, c = o - r * cols;
-        const float x = relpos::table_at(m.table, m.bucket, m.n_buckets, m.heads, head, o);
-        const float v = x <= kMasked ? -INFINITY : x * m.inv_scale;
-        const int at = BACKWARDS ? (rows - 1 - r) * bias.pitch + cols - 1 - c : r * bias.pitch + c;
-        table[at] = v;
-        if (TWICE) table[bias.size + bias_gap() + at + 1] = v;
-    }
+    int span = 1;                                                   // threads to a row of the table
+    while (span < cols && span < 32) span *= 2;
+    const int step = blockDim.x / span, c0 = threadIdx.x % span;
+    for (int r = threadIdx.x / span; r < rows; r += step)
+        for (int c = c0; c < cols; c += span) {
+            const float x = relpos::table_at(m.table, m.bucket, m.n_buckets, m.heads, head, r * cols + c);
+            const float v = x <= kMasked ? -INFINITY : x * m.inv_scale;
+            const int at = BACKWARDS ? (rows - 1 - r) * bias.pitch + cols - 1 - c : r * bias.pitch + c;
+            table[at] = v;
+            if (TWICE) table[bias.size + bias_gap() + at + 1] = v;
+        }
 }
 // Address in the staged table of the row (query or key) at (y, x), to which 4 (pitch y' + x') of the other one is added.
 template <bool TWICE> __device__ __forceinline__ uint32_t bias_row(const Maps<bf16>& m, const Bias& bias, bool pairs, int y, int x, uint32_t table) {
@@ -375,6 +389,16 @@ template <int KC> __device__ __forceinline__ void load_operand(const bf16* __res
             q[k][half + 2 * h] = v;
         }
 }
+// Where a lane reads 16 rows of a staged tile as B operands: for products along the channels (rows 8 (lane / 16) + lane % 8, piece lane / 8 % 2
+// of 16 channels) and, transposed, for products along the rows (rows 8 (lane / 8 % 2) + lane % 8, piece lane / 16).  Rows in steps of 8
+// are a constant further: they do not change how a row's pieces are exchanged.
+template <int D> __device__ __forceinline__ void lane_offsets(int lane, uint32_t (&plain)[D / 16], uint32_t (&turned)[D / 16]) {
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+        plain[k] = wmma16::Tile<D>::at((lane >> 4) * 8 + (lane & 7), 2 * k + ((lane >> 3) & 1));
+        turned[k] = wmma16::Tile<D>::at(((lane >> 3) & 1) * 8 + (lane & 7), 2 * k + (lane >> 4));
+    }
+}
 // Two neighbouring channels of a result.
 __device__ __forceinline__ void store_pair(bf16* to, int ch, int d, float u, float v) {
     if (ch + 1 < d && (reinterpret_cast<uintptr_t>(to) & 3) == 0) *reinterpret_cast<uint32_t*>(to + ch) = wmma16::pack(u, v);
@@ -385,10 +409,10 @@ __device__ __forceinline__ void store_pair(bf16* to, int ch, int d, float u, flo
 }
 
 template <int D, bool TWICE>
-__global__ void __launch_bounds__(kMaxWarps * 32, D <= 32 ? 2 : 1)
+__global__ void __launch_bounds__(kMaxWarps * 32, blocks_of(D))
 forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse) {
     using namespace wmma16;
-    constexpr int KC = D / 16, NT = kStep / 8, ON = D / 8;          // steps along the channels, tiles of 8 keys, of 8 channels of out
+    constexpr int KC = D / 16, NT = kStep / 8, ON = D / 8, MT = row_tiles(D), R = 2 * MT;          // steps along the channels, tiles of 8 keys, of 8 channels of out
     constexpr int kTile = Smem<D>::kTile;
     extern __shared__ __align__(128) unsigned char raw[];
     long long* pixels = reinterpret_cast<long long*>(raw + 4 * kTile);
@@ -400,7 +424,7 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
     const int head = id % m.heads;
     const Window w = window_at(m, id / m.heads);
     const int n = w.tokens(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int block_first = tile * (blockDim.x >> 5) * kQueries, first = block_first + warp * kQueries;
+    const int block_first = tile * (blockDim.x >> 5) * (16 * MT), first = block_first + warp * (16 * MT);
     if (block_first >= n) return;
     const Bias bias(m.wh, m.ww);
     const int head_off = head * m.d;
@@ -413,8 +437,7 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
     }
     __syncthreads();
     auto stage = [&](int buf, int place) {
-        Rows<D, kKeys>::stage(k0, m.stride, m.d, wide_k, pixels + place * kKeys, tile0 + buf * 2 * kTile);
-        Rows<D, kKeys>::stage(v0, m.stride, m.d, wide_v, pixels + place * kKeys, tile0 + (buf * 2 + 1) * kTile);
+        Rows<D, kKeys>::stage(k0, m.stride, wide_k, tile0 + buf * 2 * kTile, v0, m.stride, wide_v, tile0 + (buf * 2 + 1) * kTile, m.d, pixels + place * kKeys);
         cp_commit();
     };
     stage(0, 0);
@@ -423,9 +446,9 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
     const bool pairs = TWICE && (w.w & 1) == 0;
 
     // queries: operands, and where their rows of the bias start
-    uint32_t q[2][KC][4], at[4];                                    // at + 4 B(j): where (i, j) is
+    uint32_t q[MT][KC][4], at[R];                                    // at + 4 B(j): where (i, j) is
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < R; ++r) {
         const int i = min(first + 8 * r + g, n - 1);
         const int y = i / w.w, x = i - y * w.w;
         at[r] = bias_row<TWICE>(m, bias, pairs, y, x, smem_addr(table));
@@ -436,17 +459,19 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
     // A row's powers are 2^(c s - base).  The base is the row's first maximum and moves only when one is kSlack above it (p is then at
     // most 2^8, which costs nothing in a floating format), so that most steps only look whether any row of the warp has to move.
     const float slack = kSlack / c;
-    float o[2][ON][4], top[4], limit[4];
-    Two off[4], sum[4];
+    float o[MT][ON][4], top[R], limit[R];
+    Two off[R], sum[R];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) { top[r] = limit[r] = -INFINITY; sum[r] = off[r] = two(0.0f, 0.0f); }
+    for (int r = 0; r < R; ++r) { top[r] = limit[r] = -INFINITY; sum[r] = off[r] = two(0.0f, 0.0f); }
 #pragma unroll
-    for (int a = 0; a < 2; ++a)
+    for (int a = 0; a < MT; ++a)
 #pragma unroll
         for (int x = 0; x < ON; ++x)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[a][x][e] = 0.0f;
 
+    uint32_t plain[KC], turned[KC];
+    lane_offsets<D>(lane, plain, turned);
     for (int tile_key = 0, buf = 0, place = 0; tile_key < n; tile_key += kKeys, buf ^= 1) {
         const int next = place == 2 ? 0 : place + 1, free = 3 - place - next;
         cp_wait<0>();
@@ -459,45 +484,46 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
             const int key = tile_key + step * kStep;
             const uint32_t ks = tile0 + buf * 2 * kTile + step * (kStep * D * 2), vs = ks + kTile;
             const int* b = bs + place * kKeys + step * kStep + 2 * t;
-            float s[2][NT][4];
+            float s[MT][NT][4];
 #pragma unroll
             for (int x = 0; x < NT; ++x) {
                 if (pairs) {
                     const int b0 = b[8 * x];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
+                    for (int r = 0; r < R; ++r) {
                         const float2 v = lds2(at[r] + b0);
                         s[r >> 1][x][2 * (r & 1)] = v.x; s[r >> 1][x][2 * (r & 1) + 1] = v.y;
                     }
                 } else {
                     const int b0 = b[8 * x], b1 = b[8 * x + 1];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
+                    for (int r = 0; r < R; ++r) {
                         s[r >> 1][x][2 * (r & 1)] = lds1(at[r] + b0); s[r >> 1][x][2 * (r & 1) + 1] = lds1(at[r] + b1);
                     }
                 }
             }
-            // keys of a pair of tiles as B operands: rows 8 (lane / 16) + lane % 8, piece lane / 8 % 2 of the 16 channels
 #pragma unroll
             for (int x = 0; x < NT; x += 2)
 #pragma unroll
                 for (int k = 0; k < KC; ++k) {
                     uint32_t f[4];
-                    ldsm(f, ks + Tile<D>::at(8 * x + (lane >> 4) * 8 + (lane & 7), 2 * k + ((lane >> 3) & 1)));
+                    ldsm(f, ks + plain[k] + x * (8 * D * 2));
 #pragma unroll
-                    for (int a = 0; a < 2; ++a) { mma(s[a][x], q[a][k], f[0], f[1]); mma(s[a][x + 1], q[a][k], f[2], f[3]); }
+                    for (int a = 0; a < MT; ++a) { mma(s[a][x], q[a][k], f[0], f[1]); mma(s[a][x + 1], q[a][k], f[2], f[3]); }
                 }
             if (key + kStep > n) {
 #pragma unroll
                 for (int x = 0; x < NT; ++x)
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
-                        if (key + 8 * x + 2 * t + e >= n) s[0][x][e] = s[0][x][e + 2] = s[1][x][e] = s[1][x][e + 2] = -INFINITY;
+                        if (key + 8 * x + 2 * t + e >= n)
+#pragma unroll
+                            for (int a = 0; a < MT; ++a) s[a][x][e] = s[a][x][e + 2] = -INFINITY;
             }
-            float high[4];
+            float high[R];
             bool over = false;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
+            for (int r = 0; r < R; ++r) {
                 const int a = r >> 1, e = 2 * (r & 1);
                 high[r] = fmaxf(s[a][0][e], s[a][0][e + 1]);
 #pragma unroll
@@ -506,7 +532,7 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
             }
             if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
+                for (int r = 0; r < R; ++r) {
                     const int a = r >> 1, e = 2 * (r & 1);
                     float x = fmaxf(high[r], top[r]);
                     x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
@@ -523,35 +549,35 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
 #pragma unroll
             for (int y = 0; y < NT; ++y)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
+                for (int r = 0; r < R; ++r) {
                     const int a = r >> 1, e = 2 * (r & 1);
                     float u, v;
                     apart(fma2(two(s[a][y][e], s[a][y][e + 1]), by, off[r]), u, v);
                     s[a][y][e] = ex2(u); s[a][y][e + 1] = ex2(v);
                     sum[r] = add2(sum[r], two(s[a][y][e], s[a][y][e + 1]));
                 }
-            // p v: 16 keys at a time; values transposed on the way in: rows 8 (lane / 8 % 2) + lane % 8, piece lane / 16 of 16 channels
+            // p v: 16 keys at a time, the values transposed on the way in
 #pragma unroll
             for (int x = 0; x < NT; x += 2) {
-                uint32_t p[2][4];
+                uint32_t p[MT][4];
 #pragma unroll
-                for (int a = 0; a < 2; ++a) {
+                for (int a = 0; a < MT; ++a) {
                     p[a][0] = pack(s[a][x][0], s[a][x][1]); p[a][1] = pack(s[a][x][2], s[a][x][3]);
                     p[a][2] = pack(s[a][x + 1][0], s[a][x + 1][1]); p[a][3] = pack(s[a][x + 1][2], s[a][x + 1][3]);
                 }
 #pragma unroll
                 for (int k = 0; k < KC; ++k) {
                     uint32_t f[4];
-                    ldsm_t(f, vs + Tile<D>::at(8 * x + ((lane >> 3) & 1) * 8 + (lane & 7), 2 * k + (lane >> 4)));
+                    ldsm_t(f, vs + turned[k] + x * (8 * D * 2));
 #pragma unroll
-                    for (int a = 0; a < 2; ++a) { mma(o[a][2 * k], p[a], f[0], f[1]); mma(o[a][2 * k + 1], p[a], f[2], f[3]); }
+                    for (int a = 0; a < MT; ++a) { mma(o[a][2 * k], p[a], f[0], f[1]); mma(o[a][2 * k + 1], p[a], f[2], f[3]); }
                 }
             }
         }
         place = next;
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < R; ++r) {
         float x, y_;
         apart(sum[r], x, y_);
         x += y_;

@@ -11,14 +11,16 @@
 
 namespace esc { namespace winatt { namespace bwd {
 
-// D, in [B][heads][H][W] like lse.  Bound: HBM, go and out are read once.
-constexpr int kDotThreads = 256;
+// What the other kernels take of a row, in [B][heads][H][W] like lse: bases = -lse log2(e), so that p = 2^(c s' + base) (-inf where the row
+// has no keys: p = 0), and dots = -D.  Bound: HBM, go and out are read once.
+constexpr int kRowThreads = 256;
 template <typename T>
-__global__ void __launch_bounds__(kDotThreads)
-row_dots(const T* __restrict__ go, const T* __restrict__ out, long long pixels, long long hw, int heads, int d, float* __restrict__ dots) {
+__global__ void __launch_bounds__(kRowThreads)
+row_terms(const T* __restrict__ go, const T* __restrict__ out, const float* __restrict__ lse, long long pixels, long long hw, int heads, int d,
+          float* __restrict__ bases, float* __restrict__ dots) {
     constexpr int V = Elem<T>::kVec;
     const bool wide = d % V == 0;
-    for (long long e = (long long)blockIdx.x * kDotThreads + threadIdx.x; e < pixels * heads; e += (long long)gridDim.x * kDotThreads) {
+    for (long long e = (long long)blockIdx.x * kRowThreads + threadIdx.x; e < pixels * heads; e += (long long)gridDim.x * kRowThreads) {
         const long long pixel = e / heads;
         const int head = (int)(e - pixel * heads);
         const T *a = go + e * d, *b = out + e * d;
@@ -34,25 +36,24 @@ row_dots(const T* __restrict__ go, const T* __restrict__ out, long long pixels, 
         } else {
             for (int c = 0; c < d; ++c) sum = fmaf(Elem<T>::to_f32(a[c]), Elem<T>::to_f32(b[c]), sum);
         }
-        const long long image = pixel / hw;
-        dots[(image * heads + head) * hw + pixel - image * hw] = sum;
+        const long long image = pixel / hw, row = (image * heads + head) * hw + pixel - image * hw;
+        dots[row] = -sum;
+        bases[row] = lse[row] == -INFINITY ? -INFINITY : -lse[row] * kLog2e;
     }
 }
 
 // What the backward kernels need beyond Maps.
 template <typename T> struct Grads {
     const T* go;                                   // dense
-    const float *lse, *dots;
+    const float *bases, *dots;
     T *g_q, *g_k, *g_v;                            // pixels `stride` values apart
-    float* part;                                   // [groups][heads][offsets] sums of ds, or null
+    float* part;                                   // [slices][heads][offsets] sums of ds, or null
     int windows, groups;
 };
 template <typename T> __device__ __forceinline__ long long row_of(const Maps<T>& m, const Window& w, int head, long long pixel) {
     const long long hw = (long long)m.H * m.W;
     return ((long long)w.b * m.heads + head) * hw + pixel - w.b * hw;
 }
-// 2^(c s' - this) is p; +inf where the row has no keys.
-__device__ __forceinline__ float base_of(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
 
 // ---- fp32: CUDA cores -----------------------------------------------------------------------------------------------------
 // Two kernels, so that every gradient is a sum in one thread's registers: in the first a thread has a key (k, v and their gradients
@@ -132,16 +133,16 @@ grad_kv(Maps<float> m, Grads<float> g, int tiles) {
             const int i = row + r, y = i / w.w;
             const long long p = i < n ? row_of(m, w, head, pixel_of(m, w, i)) : 0;
             as[r] = i < n ? (y + m.wh - 1) * pitch + i - y * w.w + m.ww - 1 : (m.wh - 1) * pitch + m.ww - 1;
-            base[r] = i < n ? base_of(g.lse[p]) : INFINITY;
+            base[r] = i < n ? g.bases[p] : -INFINITY;
             dots[r] = i < n ? g.dots[p] : 0.0f;
         }
         __syncthreads();
         const int rows = min(kRows, n - row);
         for (int r = 0; r < rows; ++r) {
             const float s = L::dot(k, qs + r * D, 0.0f) + table[as[r] - b];
-            const float p = ex2(fmaf(s, c, -base[r])), dp = L::dot(v, gs + r * D, 0.0f);
+            const float p = ex2(fmaf(s, c, base[r])), dp = L::dot(v, gs + r * D, 0.0f);
             L::add(gv, gs + r * D, p);
-            L::add(gk, qs + r * D, p * (dp - dots[r]));
+            L::add(gk, qs + r * D, p * (dp + dots[r]));
         }
     }
     if (first + L::row() < n) {
@@ -175,7 +176,7 @@ grad_q(Maps<float> m, Grads<float> g, int tiles) {
         const int i = min(first + L::row(), n - 1);
         const long long pixel = pixel_of(m, w, i), at = pixel * m.stride + (long long)head * m.d, row = row_of(m, w, head, pixel);
         const int a = (i / w.w + m.wh - 1) * pitch + i % w.w + m.ww - 1;
-        const float base = own ? base_of(g.lse[row]) : INFINITY, dot = own ? g.dots[row] : 0.0f;
+        const float base = own ? g.bases[row] : -INFINITY, dot = own ? g.dots[row] : 0.0f;
         float q[L::N], go[L::N], gq[L::N];
         L::load(m.q + at, m.d, q);
         L::load(g.go + (pixel * m.heads + head) * m.d, m.d, go);
@@ -194,7 +195,7 @@ grad_q(Maps<float> m, Grads<float> g, int tiles) {
             for (int r = 0; r < rows; ++r) {
                 const int o = a - bs[r];
                 const float s = L::dot(q, ks + r * D, 0.0f) + table[o];
-                const float p = ex2(fmaf(s, c, -base)), ds = p * (L::dot(go, vs + r * D, 0.0f) - dot);
+                const float p = ex2(fmaf(s, c, base)), ds = p * (L::dot(go, vs + r * D, 0.0f) + dot);
                 L::add(gq, ks + r * D, ds);
                 if (g.part && own && L::first() == 0) mine[o] += ds;
                 __syncwarp();                      // the next key's offsets are the neighbours'
@@ -220,25 +221,40 @@ grad_q(Maps<float> m, Grads<float> g, int tiles) {
 namespace tc {
 using namespace winatt::tc;
 constexpr int kCols = 128;                                          // staged columns: queries for rows of keys, keys for rows of queries
-__host__ __device__ constexpr int row_tiles(int D) { return D <= 32 ? 2 : 1; }   // tiles of 16 rows of a warp
+#ifndef BMT
+#define BMT (D <= 32 ? 2 : 1)
+#endif
+__host__ __device__ constexpr int grad_tiles(int D) { return BMT; }   // tiles of 16 rows of a warp
 
 template <int D> struct RowSmem {
-    static constexpr int kTile = kCols * D * 2, kWalk = 3 * kCols * (8 + 4), kRows = 2 * kCols * 2 * 4;   // base and D of two tiles' columns
+    static constexpr int kTile = kCols * D * 2, kWalk = 3 * kCols * (8 + 4), kRows = 2 * kCols * 2 * 4;   // the columns' terms, two tiles
     static __host__ __device__ size_t bytes(const Bias& b, bool twice) { return 4 * kTile + kWalk + kRows + (size_t)b.size * 4 * (twice ? 2 : 1) + (twice ? bias_gap() * 4 : 0); }
 };
 
+// A row's terms into shared memory; a row that is none: p = 0.
+__device__ __forceinline__ void stage_terms(const Grads<bf16>& gr, long long row0, long long px, bool in, float* base, int to_dot) {
+    if (in) {
+        wmma16::cp4(wmma16::smem_addr(base), gr.bases + row0 + px);
+        wmma16::cp4(wmma16::smem_addr(base + to_dot), gr.dots + row0 + px);
+    } else {
+        base[0] = -INFINITY;
+        base[to_dot] = 0.0f;
+    }
+}
+
+#define MTB(D) (grad_tiles(D) == 1 ? (D <= 16 ? 3 : D <= 32 ? 2 : 1) : D <= 16 ? 2 : 1)
 // KEYS: rows are keys (operands k and v), columns queries (q and go): g_k += ds^T q, g_v += p^T go.
 // Else: rows are queries (q and go), columns keys (k and v): g_q += ds k.
 template <int D, bool KEYS, bool TWICE>
-__global__ void __launch_bounds__(kMaxWarps * 32, D <= 16 ? 2 : 1)
+__global__ void __launch_bounds__(kMaxWarps * 32, MTB(D))
 grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
     using namespace wmma16;
-    constexpr int KC = D / 16, ON = D / 8, MT = row_tiles(D), R = 2 * MT;   // R: rows that a lane has a part of
+    constexpr int KC = D / 16, ON = D / 8, MT = grad_tiles(D), R = 2 * MT;   // R: rows that a lane has a part of
     constexpr int kTile = RowSmem<D>::kTile;
     extern __shared__ __align__(128) unsigned char raw[];
     long long* pixels = reinterpret_cast<long long*>(raw + 4 * kTile);
     int* bs = reinterpret_cast<int*>(pixels + 3 * kCols);
-    float* bases = reinterpret_cast<float*>(bs + 3 * kCols);        // [two tiles][-base, -D][kCols]
+    float* bases = reinterpret_cast<float*>(bs + 3 * kCols);        // [two tiles][bases, dots][kCols]
     float* table = bases + 4 * kCols;
     const uint32_t tile0 = smem_addr(raw);
     int id = blockIdx.x;
@@ -261,15 +277,10 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
     __syncthreads();
     auto stage = [&](int buf, int place) {
         const long long* px = pixels + place * kCols;
-        Rows<D, kCols>::stage(c1, m.stride, m.d, wide1, px, tile0 + buf * 2 * kTile);
-        Rows<D, kCols>::stage(c2, stride2, m.d, wide2, px, tile0 + (buf * 2 + 1) * kTile);
-        cp_commit();
+        Rows<D, kCols>::stage(c1, m.stride, wide1, tile0 + buf * 2 * kTile, c2, stride2, wide2, tile0 + (buf * 2 + 1) * kTile, m.d, px);
         if (KEYS)
-            for (int r = threadIdx.x; r < kCols; r += blockDim.x) {
-                const bool in = px[r] >= 0;
-                bases[(2 * buf) * kCols + r] = in ? -base_of(gr.lse[row0 + px[r]]) : -INFINITY;   // a column that is none: p = 0
-                bases[(2 * buf + 1) * kCols + r] = in ? -gr.dots[row0 + px[r]] : 0.0f;
-            }
+            for (int r = threadIdx.x; r < kCols; r += blockDim.x) stage_terms(gr, row0, px[r], px[r] >= 0, bases + 2 * buf * kCols + r, kCols);
+        cp_commit();
     };
     stage(0, 0);
     stage_bias<TWICE, !KEYS>(m, head, bias, table);
@@ -287,9 +298,9 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
         at[r] = bias_row<TWICE>(m, bias, pairs, y, x, smem_addr(table));
         load_operand<KC>((KEYS ? m.k : m.q) + (w.pixel + px) * m.stride + off, m.d, t, r & 1, a1[r >> 1]);
         load_operand<KC>(KEYS ? m.v + (w.pixel + px) * m.stride + off : gr.go + (w.pixel + px) * dense + off, m.d, t, r & 1, a2[r >> 1]);
-        const float b = KEYS || !in ? -INFINITY : -base_of(gr.lse[row0 + px]);
+        const float b = KEYS || !in ? -INFINITY : gr.bases[row0 + px];
         base[r] = two(b, b);
-        dot[r] = KEYS ? 0.0f : -gr.dots[row0 + px];
+        dot[r] = KEYS ? 0.0f : gr.dots[row0 + px];
     }
     const float c = m.scale * kLog2e;
     const Two by = two(c, c);
@@ -301,6 +312,8 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
 #pragma unroll
             for (int a = 0; a < MT; ++a) { acc1[a][x][e] = 0.0f; if (KEYS) acc2[a][x][e] = 0.0f; }
 
+    uint32_t plain[KC], turned[KC];
+    lane_offsets<D>(lane, plain, turned);
     for (int tile_col = 0, buf = 0, place = 0; tile_col < n; tile_col += kCols, buf ^= 1) {
         const int next = place == 2 ? 0 : place + 1, free = 3 - place - next;
         cp_wait<0>();
@@ -308,7 +321,7 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
         if (tile_col + kCols < n) stage(buf ^ 1, next);
         if (warp == 0 && tile_col + 2 * kCols < n) walk.next(w, m.W, bias.pitch, lane, pixels + free * kCols, bs + free * kCols);
         const int steps = min(kCols, n - tile_col + 15) / 16;
-        const uint32_t t1 = tile0 + buf * 2 * kTile, t2 = t1 + kTile;
+        const uint32_t t1 = tile0 + buf * 2 * kTile;
 #pragma unroll 1
         for (int step = 0; step < steps; ++step) {
             const int* b = bs + place * kCols + step * 16 + 2 * t;
@@ -328,12 +341,12 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
                     col_dot[x] = *reinterpret_cast<const float2*>(row + kCols);
                 }
             }
-            const int row = step * 16 + (lane >> 4) * 8 + (lane & 7), piece = (lane >> 3) & 1;
+            const uint32_t s1 = t1 + step * (16 * D * 2), s2 = s1 + kTile;
 #pragma unroll
             for (int k = 0; k < KC; ++k) {
                 uint32_t f[4], h[4];
-                ldsm(f, t1 + Tile<D>::at(row, 2 * k + piece));
-                ldsm(h, t2 + Tile<D>::at(row, 2 * k + piece));
+                ldsm(f, s1 + plain[k]);
+                ldsm(h, s2 + plain[k]);
 #pragma unroll
                 for (int a = 0; a < MT; ++a) {
                     mma(s[a][0], a1[a][k], f[0], f[1]); mma(s[a][1], a1[a][k], f[2], f[3]);
@@ -346,9 +359,9 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
                 }
             }
             const bool cut = !KEYS && tile_col + step * 16 + 16 > n;
+            uint32_t pp[MT][4], pd[MT][4];
 #pragma unroll
-            for (int a = 0; a < MT; ++a) {
-                uint32_t pp[4], pd[4];
+            for (int a = 0; a < MT; ++a)
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -362,20 +375,20 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
                             if (j >= n) u = 0.0f;
                             if (j + 1 >= n) v = 0.0f;
                         }
-                        if (KEYS) pp[2 * x + e] = pack(u, v);
+                        if (KEYS) pp[a][2 * x + e] = pack(u, v);
                         apart(mul2(two(u, v), two(dp[a][x][2 * e], dp[a][x][2 * e + 1])), u, v);
-                        pd[2 * x + e] = pack(u, v);
+                        pd[a][2 * x + e] = pack(u, v);
                     }
-                const int trow = step * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), tpiece = lane >> 4;
 #pragma unroll
-                for (int k = 0; k < KC; ++k) {
-                    uint32_t f[4];
-                    ldsm_t(f, t1 + Tile<D>::at(trow, 2 * k + tpiece));
-                    mma(acc1[a][2 * k], pd, f[0], f[1]); mma(acc1[a][2 * k + 1], pd, f[2], f[3]);
-                    if (KEYS) {
-                        ldsm_t(f, t2 + Tile<D>::at(trow, 2 * k + tpiece));
-                        mma(acc2[a][2 * k], pp, f[0], f[1]); mma(acc2[a][2 * k + 1], pp, f[2], f[3]);
-                    }
+            for (int k = 0; k < KC; ++k) {
+                uint32_t f[4];
+                ldsm_t(f, s1 + turned[k]);
+#pragma unroll
+                for (int a = 0; a < MT; ++a) { mma(acc1[a][2 * k], pd[a], f[0], f[1]); mma(acc1[a][2 * k + 1], pd[a], f[2], f[3]); }
+                if (KEYS) {
+                    ldsm_t(f, s2 + turned[k]);
+#pragma unroll
+                    for (int a = 0; a < MT; ++a) { mma(acc2[a][2 * k], pp[a], f[0], f[1]); mma(acc2[a][2 * k + 1], pp[a], f[2], f[3]); }
                 }
             }
         }
@@ -394,54 +407,65 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
     }
 }
 
-// The table's gradient.  A block has one head, 64 keys and a group of windows; for 128 queries at a time it walks its windows with the sums
-// of ds of its 128 x 64 pairs in registers (a warp 32 x 32, and their bias there too, so that nothing of the table is read in the
-// loop).  Windows of one width share the tokens' places; those of the last column, where it is narrower, come second.
-// Then every thread adds up the pairs of some offsets.
-constexpr int kPairQ = 128, kPairK = 64;
+// The table's gradient.  A block has one head, a tile of 64 keys, every `parts`-th tile of 128 queries and every `groups`-th window; for each
+// tile of queries its windows pass by with the sums of ds of the 128 x 64 pairs in registers (a warp 32 x 32, and the pairs' bias there too:
+// nothing of the table is read in the loop).  Windows of one width have the tokens at the same places; those of the last column, where it
+// is narrower, come second.  Then every thread adds up the pairs of some offsets.
+constexpr int kPairQ = 128, kPairK = 64, kList = 64;
 template <int D> struct PairSmem {
     static constexpr int kQ = kPairQ * D * 2, kK = kPairK * D * 2, kBuf = 2 * kQ + 2 * kK;
     static constexpr int kSums = kPairQ * (kPairK + 1) * 4;         // the pairs' sums, over the staged tiles
     static constexpr int kData = 2 * kBuf > kSums ? 2 * kBuf : kSums;
-    static __host__ __device__ size_t bytes(int offsets) { return kData + (2 * 2 * kPairQ + offsets) * sizeof(float) + (kPairQ + kPairK) * 8; }
+    static __host__ __device__ size_t bytes(int offsets) { return kData + 2 * kList * 24 + (4 * kPairQ + 2 * (kPairQ + kPairK) + offsets) * 4; }
 };
 template <int D>
 __global__ void __launch_bounds__(256, D <= 16 ? 2 : 1)
-grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles) {
+grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles, int parts) {
     using namespace wmma16;
-    constexpr int KC = D / 16;
+    constexpr int KC = D / 16, P = Tile<D>::kPieces, QN = kPairQ * P / 256, KN = kPairK * P > 256 ? kPairK * P / 256 : 1;   // pieces of q, of k that a thread stages
     using S = PairSmem<D>;
     extern __shared__ __align__(128) unsigned char raw[];
-    float* bases = reinterpret_cast<float*>(raw + S::kData);        // [two windows][-base, -D][kPairQ]
-    long long* px = reinterpret_cast<long long*>(bases + 4 * kPairQ);   // of the queries, of the keys
-    float* sums = reinterpret_cast<float*>(px + kPairQ + kPairK);
+    long long* list = reinterpret_cast<long long*>(raw + S::kData); // windows to come, two halves: first pixel, end of its places, first row
+    float* bases = reinterpret_cast<float*>(list + 2 * kList * 3);  // [two windows][bases, dots][kPairQ]
+    int* px = reinterpret_cast<int*>(bases + 4 * kPairQ);           // places of the queries, of the keys; behind the window's first pixel
+    int* lin = px + kPairQ + kPairK;                                // y pitch + x of them
+    float* sums = reinterpret_cast<float*>(lin + kPairQ + kPairK);
     const uint32_t data = smem_addr(raw);
-    const int head = blockIdx.x % m.heads, id = blockIdx.x / m.heads, group = id / key_tiles, key0 = id % key_tiles * kPairK;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, wq = (warp >> 1) * 32, wk = (warp & 1) * 32;
+    const int head = blockIdx.x % m.heads, id = blockIdx.x / m.heads, key0 = id % key_tiles * kPairK, part = id / key_tiles % parts, group = id / key_tiles / parts;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3, wq = (warp >> 1) * 32, wk = (warp & 1) * 32;
     const int pitch = 2 * m.ww - 1, offsets = (2 * m.wh - 1) * pitch;
     const long long dense = (long long)m.heads * m.d, off = (long long)head * m.d, hw = (long long)m.H * m.W;
     const bool wide_q = pieces(m.q, m.stride, m.d), wide_k = pieces(m.k, m.stride, m.d), wide_v = pieces(m.v, m.stride, m.d), wide_g = pieces(gr.go, dense, m.d);
-    const float c = m.scale * kLog2e;
-    const Two by = two(c, c);
-    for (int o = threadIdx.x; o < offsets; o += 256) sums[o] = 0.0f;
+    const Two by = two(m.scale * kLog2e, m.scale * kLog2e);
+    uint32_t plain[KC], turned[KC];
+    lane_offsets<D>(lane, plain, turned);
+    for (int o = tid; o < offsets; o += 256) sums[o] = 0.0f;
     const int full = m.W / m.ww, rest = m.W - full * m.ww;          // windows of whole width in a row; the last one's width
     const int tall = min(m.wh, m.H);                                // rows of the tallest window
     for (int narrow = 0; narrow < 2; ++narrow) {
         const int per_row = narrow ? (rest > 0) : full, width = narrow ? rest : m.ww;
         const int count = m.B * m.ny * per_row, tokens = tall * width;
-        if (count == 0 || key0 >= tokens) continue;
-        auto window = [&](int i) {                                  // the group's i-th
-            const int at = group + i * gr.groups, row = at / per_row;
-            return window_at(m, row * m.nx + (narrow ? full : at - row * per_row));
-        };
         const int mine = group < count ? (count - group + gr.groups - 1) / gr.groups : 0;
-        if (mine == 0) continue;
-        for (int q0 = 0; q0 < tokens; q0 += kPairQ) {
-            __syncthreads();                                        // the last queries' sums and places are done with
-            for (int r = threadIdx.x; r < kPairQ + kPairK; r += 256) {
-                const int i = r < kPairQ ? q0 + r : key0 + r - kPairQ, y = i / width;
-                px[r] = i < tokens ? (long long)y * m.W + i - y * width : -1;
+        if (mine == 0 || key0 >= tokens) continue;
+        auto look = [&](int i) {                                    // the group's windows i .. i + kList - 1 into the list
+            if (tid < kList && i + tid < mine) {
+                const int at = group + (i + tid) * gr.groups, row = at / per_row;
+                const Window w = window_at(m, row * m.nx + (narrow ? full : at - row * per_row));
+                long long* l = list + ((i / kList & 1) * kList + tid) * 3;
+                l[0] = w.pixel;
+                l[1] = (long long)(w.h - 1) * m.W + width;
+                l[2] = ((long long)w.b * m.heads + head) * hw + w.pixel - w.b * hw;
             }
+        };
+        for (int q0 = part * kPairQ; q0 < tokens; q0 += parts * kPairQ) {
+            __syncthreads();                                        // the last queries' sums and places are done with
+            for (int r = tid; r < kPairQ + kPairK; r += 256) {
+                const int i = r < kPairQ ? q0 + r : key0 + r - kPairQ, y = i / width, x = i - y * width;
+                px[r] = i < tokens ? y * m.W + x : 0x7fffffff;
+                lin[r] = y * pitch + x;
+            }
+            look(0);
+            __syncthreads();
             float bias[2][4][4], sum[2][4][4];
 #pragma unroll
             for (int a = 0; a < 2; ++a)
@@ -449,48 +473,56 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles) {
                 for (int x = 0; x < 4; ++x)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int i = q0 + wq + 16 * a + 8 * (e >> 1) + g, j = key0 + wk + 8 * x + 2 * t + (e & 1);
+                        const int i = wq + 16 * a + 8 * (e >> 1) + g, j = kPairQ + wk + 8 * x + 2 * t + (e & 1);
                         float v = -INFINITY;                        // pairs that are none: p = 0
-                        if (i < tokens && j < tokens) {
-                            v = relpos::table_at(m.table, m.bucket, m.n_buckets, m.heads, head, (i / width - j / width + m.wh - 1) * pitch + i % width - j % width + m.ww - 1);
+                        if (px[i] != 0x7fffffff && px[j] != 0x7fffffff) {
+                            v = relpos::table_at(m.table, m.bucket, m.n_buckets, m.heads, head, lin[i] - lin[j] + (m.wh - 1) * pitch + m.ww - 1);
                             v = v <= kMasked ? -INFINITY : v * m.inv_scale;
                         }
                         bias[a][x][e] = v;
                         sum[a][x][e] = 0.0f;
                     }
-            __syncthreads();
             auto stage = [&](int i, int buf) {
-                const Window w = window(i);
+                const long long* l = list + ((i / kList & 1) * kList + i % kList) * 3;
+                const long long pixel = l[0], end = l[1], row0 = l[2];
                 const uint32_t dst = data + buf * S::kBuf;
-                const long long end = (long long)(w.h - 1) * m.W + width;   // rows of a shorter window end early
-                Rows<D, kPairQ>::stage(m.q + w.pixel * m.stride + off, m.stride, m.d, wide_q, px, dst, end);
-                Rows<D, kPairQ>::stage(gr.go + w.pixel * dense + off, dense, m.d, wide_g, px, dst + S::kQ, end);
-                Rows<D, kPairK>::stage(m.k + w.pixel * m.stride + off, m.stride, m.d, wide_k, px + kPairQ, dst + 2 * S::kQ, end);
-                Rows<D, kPairK>::stage(m.v + w.pixel * m.stride + off, m.stride, m.d, wide_v, px + kPairQ, dst + 2 * S::kQ + S::kK, end);
-                cp_commit();
-                const long long row0 = ((long long)w.b * m.heads + head) * hw + w.pixel - w.b * hw;
-                for (int r = threadIdx.x; r < kPairQ; r += 256) {
-                    const bool in = px[r] >= 0 && px[r] < end;
-                    bases[2 * buf * kPairQ + r] = in ? -base_of(gr.lse[row0 + px[r]]) : -INFINITY;
-                    bases[(2 * buf + 1) * kPairQ + r] = in ? -gr.dots[row0 + px[r]] : 0.0f;
+                const bf16 *q = m.q + pixel * m.stride + off, *go = gr.go + pixel * dense + off, *k = m.k + pixel * m.stride + off, *v = m.v + pixel * m.stride + off;
+#pragma unroll
+                for (int u = 0; u < QN; ++u) {
+                    const int r = (tid + 256 * u) / P, c = (tid + 256 * u) % P * 8;
+                    const bool real = px[r] < end && c < m.d;       // rows of a shorter window end early
+                    const long long at = real ? px[r] : 0;
+                    stage_piece(q + at * m.stride + (real ? c : 0), dst + Tile<D>::at(r, c / 8), real, m.d - c, wide_q);
+                    stage_piece(go + at * dense + (real ? c : 0), dst + S::kQ + Tile<D>::at(r, c / 8), real, m.d - c, wide_g);
                 }
+                if (kPairK * P >= 256 || tid < kPairK * P)
+#pragma unroll
+                    for (int u = 0; u < KN; ++u) {
+                        const int r = (tid + 256 * u) / P, c = (tid + 256 * u) % P * 8, p = px[kPairQ + r];
+                        const bool real = p < end && c < m.d;
+                        const long long at = real ? p * m.stride + c : 0;
+                        stage_piece(k + at, dst + 2 * S::kQ + Tile<D>::at(r, c / 8), real, m.d - c, wide_k);
+                        stage_piece(v + at, dst + 2 * S::kQ + S::kK + Tile<D>::at(r, c / 8), real, m.d - c, wide_v);
+                    }
+                if (tid < kPairQ) stage_terms(gr, row0, px[tid], px[tid] < end, bases + 2 * buf * kPairQ + tid, kPairQ);
+                cp_commit();
             };
             stage(0, 0);
             for (int i = 0, buf = 0; i < mine; ++i, buf ^= 1) {
                 cp_wait<0>();
                 __syncthreads();
+                if (i % kList == 0) look(i + kList);                // read from the next barrier on
                 if (i + 1 < mine) stage(i + 1, buf ^ 1);
-                const Window w = window(i);
-                const int n = w.tokens();                           // keys from here on are not this window's
+                const bool short_ = list[((i / kList & 1) * kList + i % kList) * 3 + 1] < (long long)(tall - 1) * m.W + width;
                 const uint32_t dst = data + buf * S::kBuf;
                 uint32_t q[2][KC][4], go[2][KC][4];
 #pragma unroll
                 for (int a = 0; a < 2; ++a)
 #pragma unroll
                     for (int k = 0; k < KC; ++k) {
-                        const int row = wq + 16 * a + (lane & 15), piece = 2 * k + (lane >> 4);
-                        ldsm(q[a][k], dst + Tile<D>::at(row, piece));
-                        ldsm(go[a][k], dst + S::kQ + Tile<D>::at(row, piece));
+                        // as an A operand: rows lane % 16, piece lane / 16
+                        ldsm(q[a][k], dst + wq * (D * 2) + a * (16 * D * 2) + turned[k]);
+                        ldsm(go[a][k], dst + S::kQ + wq * (D * 2) + a * (16 * D * 2) + turned[k]);
                     }
                 float dot[4];
                 Two base[4];
@@ -500,15 +532,15 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles) {
                     base[r] = two(b, b);
                     dot[r] = bases[(2 * buf + 1) * kPairQ + wq + 8 * r + g];
                 }
+                const uint32_t ks = dst + 2 * S::kQ + wk * (D * 2), vs = ks + S::kK;
 #pragma unroll
                 for (int x = 0; x < 4; x += 2) {
                     float s[2][2][4], dp[2][2][4];
-                    const int row = wk + 8 * x + (lane >> 4) * 8 + (lane & 7), piece = (lane >> 3) & 1;
 #pragma unroll
                     for (int k = 0; k < KC; ++k) {
                         uint32_t f[4], h[4];
-                        ldsm(f, dst + 2 * S::kQ + Tile<D>::at(row, 2 * k + piece));
-                        ldsm(h, dst + 2 * S::kQ + S::kK + Tile<D>::at(row, 2 * k + piece));
+                        ldsm(f, ks + x * (8 * D * 2) + plain[k]);
+                        ldsm(h, vs + x * (8 * D * 2) + plain[k]);
 #pragma unroll
                         for (int a = 0; a < 2; ++a)
 #pragma unroll
@@ -521,7 +553,6 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles) {
                                 }
                             }
                     }
-                    const bool cut = key0 + wk + 8 * x + 16 > n;
 #pragma unroll
                     for (int a = 0; a < 2; ++a)
 #pragma unroll
@@ -531,10 +562,11 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles) {
                                 float u, v;
                                 apart(fma2(two(s[a][y][2 * e], s[a][y][2 * e + 1]), by, base[2 * a + e]), u, v);
                                 u = ex2(u); v = ex2(v);
-                                if (cut) {
-                                    const int j = key0 + wk + 8 * (x + y) + 2 * t;
-                                    if (j >= n) u = 0.0f;
-                                    if (j + 1 >= n) v = 0.0f;
+                                if (short_) {                       // keys that this window does not have
+                                    const long long end = list[((i / kList & 1) * kList + i % kList) * 3 + 1];
+                                    const int* p = px + kPairQ + wk + 8 * (x + y) + 2 * t;
+                                    if (p[0] >= end) u = 0.0f;
+                                    if (p[1] >= end) v = 0.0f;
                                 }
                                 float* to = &sum[a][x + y][2 * e];
                                 apart(fma2(two(u, v), two(dp[a][y][2 * e], dp[a][y][2 * e + 1]), two(to[0], to[1])), to[0], to[1]);
@@ -553,7 +585,7 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles) {
             __syncthreads();
             const int q_end = min(q0 + kPairQ, tokens), k_end = min(key0 + kPairK, tokens);
             const int dy_lo = q0 / width - (k_end - 1) / width, dy_hi = (q_end - 1) / width - key0 / width, cols = 2 * width - 1;
-            for (int o = threadIdx.x; o < (dy_hi - dy_lo + 1) * cols; o += 256) {
+            for (int o = tid; o < (dy_hi - dy_lo + 1) * cols; o += 256) {
                 const int dy = dy_lo + o / cols, dx = o % cols - (width - 1);
                 float v = 0.0f;
                 int yj = key0 / width, xj = key0 - yj * width;
@@ -567,8 +599,8 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles) {
         }
     }
     __syncthreads();
-    float* part = gr.part + ((size_t)id * m.heads + head) * offsets;
-    for (int o = threadIdx.x; o < offsets; o += 256) part[o] = sums[o];
+    float* to = gr.part + ((size_t)id * m.heads + head) * offsets;
+    for (int o = tid; o < offsets; o += 256) to[o] = sums[o];
 }
 }  // namespace tc
 }}}  // namespace esc::winatt::bwd
