@@ -7,7 +7,6 @@
 #include "relpos_bias.cuh"
 #include "window_attention.cuh"
 #include "window_attention_backward.cuh"
-#include "window_attention_umma.cuh"
 
 namespace {
 
@@ -161,17 +160,8 @@ template <int D, bool TWICE> int forward_bf16_t(const Call& c, void* out, float*
     forward<D, TWICE><<<(unsigned)(c.windows() * c.heads * tiles), warps * 32, smem, st>>>(maps_of<bf16>(c), tiles, static_cast<bf16*>(out), lse);
     return launched();
 }
-template <int D, bool TWICE> int forward_umma_t(const Call& c, void* out, float* lse, cudaStream_t st) {
-    using namespace wa::umma;
-    const int tiles = (c.tokens() + kGroups * kRows - 1) / (kGroups * kRows);
-    const size_t smem = Smem<D>::bytes(Bias(c.wh, c.ww), TWICE);
-    ESC_TRY(allow_smem(forward<D, TWICE>, smem));
-    forward<D, TWICE><<<(unsigned)(c.windows() * c.heads * tiles), kThreads, smem, st>>>(maps_of<bf16>(c), tiles, static_cast<bf16*>(out), lse);
-    return launched();
-}
 // Two copies of the table where they leave room for two blocks on an SM.
 template <int D> int forward_bf16(const Call& c, void* out, float* lse, cudaStream_t st) {
-    if (c.tokens() >= 128) return wa::umma::Smem<D>::bytes(wa::tc::Bias(c.wh, c.ww), true) <= 113 * 1024 ? forward_umma_t<D, true>(c, out, lse, st) : forward_umma_t<D, false>(c, out, lse, st);
     return wa::tc::Smem<D>::bytes(wa::tc::Bias(c.wh, c.ww), true) <= 112 * 1024 ? forward_bf16_t<D, true>(c, out, lse, st) : forward_bf16_t<D, false>(c, out, lse, st);
 }
 

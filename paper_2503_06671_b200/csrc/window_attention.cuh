@@ -302,12 +302,6 @@ template <int ROWS> struct Walk {
             const bool in = y[i] < w.h;
             pixel[lane + 32 * i] = in ? (long long)y[i] * W + x[i] : -1;
             b[lane + 32 * i] = in ? 4 * (y[i] * pitch + x[i]) : 0;
-        }
-        step(w);
-    }
-    __device__ __forceinline__ void step(const Window& w) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
             y[i] += step_y; x[i] += step_x;
             if (x[i] >= w.w) { x[i] -= w.w; ++y[i]; }
         }
