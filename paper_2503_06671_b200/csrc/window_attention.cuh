@@ -269,12 +269,10 @@ forward(Maps<float> m, int tiles, float* __restrict__ out, float* __restrict__ l
 // p never leave the registers: the accumulators of q k^T are, rounded to bf16, the A operand of p v.
 namespace tc {
 using bf16 = __nv_bfloat16;
-constexpr int kKeys = 128, kStep = 32, kMaxWarps = 8;   // keys of a staged tile, of a step
-#ifndef FMT
-#define FMT (D <= 32 ? 2 : 1)
-#endif
-__host__ __device__ constexpr int row_tiles(int D) { return FMT; }
-__host__ __device__ constexpr int blocks_of(int D) { return 2; }
+constexpr int kKeys = 128, kMaxWarps = 8;          // keys of a staged tile
+__host__ __device__ constexpr int row_tiles(int D) { return D <= 32 ? 2 : 1; }   // tiles of 16 queries of a warp
+__host__ __device__ constexpr int blocks_of(int D) { return D <= 16 ? 3 : 2; }      // on an SM
+__host__ __device__ constexpr int step_of(int D) { return D <= 16 ? 16 : 32; }      // keys of a step
 constexpr float kSlack = 8.0f;                     // a row's base follows its maximum where that is 2^8 above
 
 // The table in shared memory backwards, so that neighbouring keys read upwards, with rows of 2 ww entries: entry (key j, query i) is at
@@ -412,7 +410,7 @@ template <int D, bool TWICE>
 __global__ void __launch_bounds__(kMaxWarps * 32, blocks_of(D))
 forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse) {
     using namespace wmma16;
-    constexpr int KC = D / 16, NT = kStep / 8, ON = D / 8, MT = row_tiles(D), R = 2 * MT;          // steps along the channels, tiles of 8 keys, of 8 channels of out
+    constexpr int KC = D / 16, kStep = step_of(D), NT = kStep / 8, ON = D / 8, MT = row_tiles(D), R = 2 * MT;          // steps along the channels, tiles of 8 keys, of 8 channels of out
     constexpr int kTile = Smem<D>::kTile;
     extern __shared__ __align__(128) unsigned char raw[];
     long long* pixels = reinterpret_cast<long long*>(raw + 4 * kTile);
@@ -455,14 +453,12 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
         load_operand<KC>(m.q + (w.pixel + (long long)y * m.W + x) * m.stride + head_off, m.d, t, r & 1, q[r >> 1]);
     }
     const float c = m.scale * kLog2e;
-    const Two by = two(c, c);
     // A row's powers are 2^(c s - base).  The base is the row's first maximum and moves only when one is kSlack above it (p is then at
     // most 2^8, which costs nothing in a floating format), so that most steps only look whether any row of the warp has to move.
     const float slack = kSlack / c;
-    float o[MT][ON][4], top[R], limit[R];
-    Two off[R], sum[R];
+    float o[MT][ON][4], limit[R], off[R], sum[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) { top[r] = limit[r] = -INFINITY; sum[r] = off[r] = two(0.0f, 0.0f); }
+    for (int r = 0; r < R; ++r) { limit[r] = -INFINITY; sum[r] = off[r] = 0.0f; }
 #pragma unroll
     for (int a = 0; a < MT; ++a)
 #pragma unroll
@@ -472,115 +468,114 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
 
     uint32_t plain[KC], turned[KC];
     lane_offsets<D>(lane, plain, turned);
+    // Some keys of a staged tile; `paired`: two neighbours' bias is read at a time, `ends`: the window may end within them.
+    auto keys_at = [&](int step, bool paired, bool ends, int buf, int place, int left) {
+        const uint32_t ks = tile0 + buf * 2 * kTile + step * (kStep * D * 2), vs = ks + kTile;
+        const int* b = bs + place * kKeys + step * kStep + 2 * t;
+        float s[MT][NT][4];
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            const int b0 = b[8 * x], b1 = paired ? 0 : b[8 * x + 1];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float2 v = paired ? lds2(at[r] + b0) : make_float2(lds1(at[r] + b0), lds1(at[r] + b1));
+                s[r >> 1][x][2 * (r & 1)] = v.x; s[r >> 1][x][2 * (r & 1) + 1] = v.y;
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < NT; x += 2)
+#pragma unroll
+            for (int k = 0; k < KC; ++k) {
+                uint32_t f[4];
+                ldsm(f, ks + plain[k] + x * (8 * D * 2));
+#pragma unroll
+                for (int a = 0; a < MT; ++a) { mma(s[a][x], q[a][k], f[0], f[1]); mma(s[a][x + 1], q[a][k], f[2], f[3]); }
+            }
+        if (ends && left < (step + 1) * kStep) {
+#pragma unroll
+            for (int x = 0; x < NT; ++x)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (step * kStep + 8 * x + 2 * t + e >= left)
+#pragma unroll
+                        for (int a = 0; a < MT; ++a) s[a][x][e] = s[a][x][e + 2] = -INFINITY;
+        }
+        float high[R];
+        bool over = false;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int a = r >> 1, e = 2 * (r & 1);
+            high[r] = fmaxf(s[a][0][e], s[a][0][e + 1]);
+#pragma unroll
+            for (int y = 1; y < NT; ++y) high[r] = max3(high[r], s[a][y][e], s[a][y][e + 1]);
+            over |= high[r] > limit[r];
+        }
+        if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float top = limit[r] - slack;                 // -inf the first time, and 2^-inf = 0
+                float x = fmaxf(high[r], top);
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+                limit[r] = x + slack;
+                const float to = x == -INFINITY ? 0.0f : -x * c, old = top == -INFINITY ? 0.0f : ex2(to - off[r]);
+                off[r] = to;
+                sum[r] *= old;
+#pragma unroll
+                for (int y = 0; y < ON; ++y) { o[r >> 1][y][2 * (r & 1)] *= old; o[r >> 1][y][2 * (r & 1) + 1] *= old; }
+            }
+        }
+#pragma unroll
+        for (int y = 0; y < NT; ++y)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int a = r >> 1, e = 2 * (r & 1);
+                s[a][y][e] = ex2(fmaf(s[a][y][e], c, off[r]));
+                s[a][y][e + 1] = ex2(fmaf(s[a][y][e + 1], c, off[r]));
+                sum[r] += s[a][y][e] + s[a][y][e + 1];
+            }
+        // p v: 16 keys at a time, the values transposed on the way in
+#pragma unroll
+        for (int x = 0; x < NT; x += 2) {
+            uint32_t p[MT][4];
+#pragma unroll
+            for (int a = 0; a < MT; ++a) {
+                p[a][0] = pack(s[a][x][0], s[a][x][1]); p[a][1] = pack(s[a][x][2], s[a][x][3]);
+                p[a][2] = pack(s[a][x + 1][0], s[a][x + 1][1]); p[a][3] = pack(s[a][x + 1][2], s[a][x + 1][3]);
+            }
+#pragma unroll
+            for (int k = 0; k < KC; ++k) {
+                uint32_t f[4];
+                ldsm_t(f, vs + turned[k] + x * (8 * D * 2));
+#pragma unroll
+                for (int a = 0; a < MT; ++a) { mma(o[a][2 * k], p[a], f[0], f[1]); mma(o[a][2 * k + 1], p[a], f[2], f[3]); }
+            }
+        }
+    };
     for (int tile_key = 0, buf = 0, place = 0; tile_key < n; tile_key += kKeys, buf ^= 1) {
         const int next = place == 2 ? 0 : place + 1, free = 3 - place - next;
         cp_wait<0>();
         __syncthreads();                                            // this tile and the next one's places are there; the other tile and the last one's places are free
         if (tile_key + kKeys < n) stage(buf ^ 1, next);
         if (warp == 0 && tile_key + 2 * kKeys < n) walk.next(w, m.W, bias.pitch, lane, pixels + free * kKeys, bs + free * kKeys);
-        const int steps = min(kKeys, n - tile_key + kStep - 1) / kStep;
+        const int left = n - tile_key;
+        if (TWICE && pairs) {
+            if (left >= kKeys) {
+#pragma unroll 2
+                for (int step = 0; step < kKeys / kStep; ++step) keys_at(step, true, false, buf, place, left);
+            } else {
 #pragma unroll 1
-        for (int step = 0; step < steps; ++step) {
-            const int key = tile_key + step * kStep;
-            const uint32_t ks = tile0 + buf * 2 * kTile + step * (kStep * D * 2), vs = ks + kTile;
-            const int* b = bs + place * kKeys + step * kStep + 2 * t;
-            float s[MT][NT][4];
-#pragma unroll
-            for (int x = 0; x < NT; ++x) {
-                if (pairs) {
-                    const int b0 = b[8 * x];
-#pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        const float2 v = lds2(at[r] + b0);
-                        s[r >> 1][x][2 * (r & 1)] = v.x; s[r >> 1][x][2 * (r & 1) + 1] = v.y;
-                    }
-                } else {
-                    const int b0 = b[8 * x], b1 = b[8 * x + 1];
-#pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        s[r >> 1][x][2 * (r & 1)] = lds1(at[r] + b0); s[r >> 1][x][2 * (r & 1) + 1] = lds1(at[r] + b1);
-                    }
-                }
+                for (int step = 0; step * kStep < left; ++step) keys_at(step, true, true, buf, place, left);
             }
-#pragma unroll
-            for (int x = 0; x < NT; x += 2)
-#pragma unroll
-                for (int k = 0; k < KC; ++k) {
-                    uint32_t f[4];
-                    ldsm(f, ks + plain[k] + x * (8 * D * 2));
-#pragma unroll
-                    for (int a = 0; a < MT; ++a) { mma(s[a][x], q[a][k], f[0], f[1]); mma(s[a][x + 1], q[a][k], f[2], f[3]); }
-                }
-            if (key + kStep > n) {
-#pragma unroll
-                for (int x = 0; x < NT; ++x)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        if (key + 8 * x + 2 * t + e >= n)
-#pragma unroll
-                            for (int a = 0; a < MT; ++a) s[a][x][e] = s[a][x][e + 2] = -INFINITY;
-            }
-            float high[R];
-            bool over = false;
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const int a = r >> 1, e = 2 * (r & 1);
-                high[r] = fmaxf(s[a][0][e], s[a][0][e + 1]);
-#pragma unroll
-                for (int y = 1; y < NT; ++y) high[r] = max3(high[r], s[a][y][e], s[a][y][e + 1]);
-                over |= high[r] > limit[r];
-            }
-            if (__any_sync(0xffffffffu, over)) {
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const int a = r >> 1, e = 2 * (r & 1);
-                    float x = fmaxf(high[r], top[r]);
-                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-                    const float base = x == -INFINITY ? 0.0f : x * c, old = ex2(fmaf(top[r], c, -base));   // 2^-inf = 0 the first time
-                    top[r] = x;
-                    limit[r] = x + slack;
-                    off[r] = two(-base, -base);
-                    sum[r] = mul2(sum[r], two(old, old));
-#pragma unroll
-                    for (int y = 0; y < ON; ++y) { o[a][y][e] *= old; o[a][y][e + 1] *= old; }
-                }
-            }
-#pragma unroll
-            for (int y = 0; y < NT; ++y)
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const int a = r >> 1, e = 2 * (r & 1);
-                    float u, v;
-                    apart(fma2(two(s[a][y][e], s[a][y][e + 1]), by, off[r]), u, v);
-                    s[a][y][e] = ex2(u); s[a][y][e + 1] = ex2(v);
-                    sum[r] = add2(sum[r], two(s[a][y][e], s[a][y][e + 1]));
-                }
-            // p v: 16 keys at a time, the values transposed on the way in
-#pragma unroll
-            for (int x = 0; x < NT; x += 2) {
-                uint32_t p[MT][4];
-#pragma unroll
-                for (int a = 0; a < MT; ++a) {
-                    p[a][0] = pack(s[a][x][0], s[a][x][1]); p[a][1] = pack(s[a][x][2], s[a][x][3]);
-                    p[a][2] = pack(s[a][x + 1][0], s[a][x + 1][1]); p[a][3] = pack(s[a][x + 1][2], s[a][x + 1][3]);
-                }
-#pragma unroll
-                for (int k = 0; k < KC; ++k) {
-                    uint32_t f[4];
-                    ldsm_t(f, vs + turned[k] + x * (8 * D * 2));
-#pragma unroll
-                    for (int a = 0; a < MT; ++a) { mma(o[a][2 * k], p[a], f[0], f[1]); mma(o[a][2 * k + 1], p[a], f[2], f[3]); }
-                }
-            }
+        } else {
+#pragma unroll 1
+            for (int step = 0; step < (min(kKeys, left) + kStep - 1) / kStep; ++step) keys_at(step, false, true, buf, place, left);
         }
         place = next;
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        float x, y_;
-        apart(sum[r], x, y_);
-        x += y_;
+        float x = sum[r];
         x += __shfl_xor_sync(0xffffffffu, x, 1);
         x += __shfl_xor_sync(0xffffffffu, x, 2);
         const int i = first + 8 * r + g, a = r >> 1, e = 2 * (r & 1);
@@ -592,7 +587,7 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
         for (int y = 0; y < ON; ++y) store_pair(to, 8 * y + 2 * t, m.d, o[a][y][e] * inv, o[a][y][e + 1] * inv);
         if (lse && t == 0) {
             const long long hw = (long long)m.H * m.W;
-            lse[((long long)w.b * m.heads + head) * hw + pixel - w.b * hw] = x == 0.0f ? -INFINITY : fmaf(top[r], m.scale, logf(x));
+            lse[((long long)w.b * m.heads + head) * hw + pixel - w.b * hw] = x == 0.0f ? -INFINITY : fmaf(off[r], -kLn2, logf(x));
         }
     }
 }

@@ -221,10 +221,14 @@ grad_q(Maps<float> m, Grads<float> g, int tiles) {
 namespace tc {
 using namespace winatt::tc;
 constexpr int kCols = 128;                                          // staged columns: queries for rows of keys, keys for rows of queries
-#ifndef BMT
-#define BMT (D <= 32 ? 2 : 1)
+#ifndef GT
+#define GT (D <= 32 ? 2 : 1)
 #endif
-__host__ __device__ constexpr int grad_tiles(int D) { return BMT; }   // tiles of 16 rows of a warp
+__host__ __device__ constexpr int grad_tiles(int D) { return GT; }   // tiles of 16 rows of a warp
+#ifndef GBL
+#define GBL (D <= 16 ? 2 : 1)
+#endif
+__host__ __device__ constexpr int grad_blocks(int D) { return GBL; }                // on an SM
 
 template <int D> struct RowSmem {
     static constexpr int kTile = kCols * D * 2, kWalk = 3 * kCols * (8 + 4), kRows = 2 * kCols * 2 * 4;   // the columns' terms, two tiles
@@ -242,11 +246,10 @@ __device__ __forceinline__ void stage_terms(const Grads<bf16>& gr, long long row
     }
 }
 
-#define MTB(D) (grad_tiles(D) == 1 ? (D <= 16 ? 3 : D <= 32 ? 2 : 1) : D <= 16 ? 2 : 1)
 // KEYS: rows are keys (operands k and v), columns queries (q and go): g_k += ds^T q, g_v += p^T go.
 // Else: rows are queries (q and go), columns keys (k and v): g_q += ds k.
 template <int D, bool KEYS, bool TWICE>
-__global__ void __launch_bounds__(kMaxWarps * 32, MTB(D))
+__global__ void __launch_bounds__(kMaxWarps * 32, grad_blocks(D))
 grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
     using namespace wmma16;
     constexpr int KC = D / 16, ON = D / 8, MT = grad_tiles(D), R = 2 * MT;   // R: rows that a lane has a part of
@@ -288,8 +291,7 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
     const bool pairs = TWICE && (w.w & 1) == 0;
 
     uint32_t a1[MT][KC][4], a2[MT][KC][4], at[R];
-    float dot[R];
-    Two base[R];
+    float dot[R], base[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const bool in = first + 8 * r + g < n;
@@ -298,12 +300,10 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
         at[r] = bias_row<TWICE>(m, bias, pairs, y, x, smem_addr(table));
         load_operand<KC>((KEYS ? m.k : m.q) + (w.pixel + px) * m.stride + off, m.d, t, r & 1, a1[r >> 1]);
         load_operand<KC>(KEYS ? m.v + (w.pixel + px) * m.stride + off : gr.go + (w.pixel + px) * dense + off, m.d, t, r & 1, a2[r >> 1]);
-        const float b = KEYS || !in ? -INFINITY : gr.bases[row0 + px];
-        base[r] = two(b, b);
+        base[r] = KEYS || !in ? -INFINITY : gr.bases[row0 + px];
         dot[r] = KEYS ? 0.0f : gr.dots[row0 + px];
     }
     const float c = m.scale * kLog2e;
-    const Two by = two(c, c);
     float acc1[MT][ON][4], acc2[KEYS ? MT : 1][ON][4];
 #pragma unroll
     for (int x = 0; x < ON; ++x)
@@ -314,83 +314,89 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
 
     uint32_t plain[KC], turned[KC];
     lane_offsets<D>(lane, plain, turned);
+    // 16 staged columns; `paired`: two neighbours' bias is read at a time, `ends`: the window may end within them.
+    auto cols_at = [&](int step, bool paired, bool ends, int buf, int place, int left) {
+        const uint32_t s1 = tile0 + buf * 2 * kTile + step * (16 * D * 2), s2 = s1 + kTile;
+        const int* b = bs + place * kCols + step * 16 + 2 * t;
+        float s[MT][2][4], dp[MT][2][4];
+        float2 col_base[2], col_dot[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int b0 = b[8 * x], b1 = paired ? 0 : b[8 * x + 1];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float2 v = paired ? lds2(at[r] + b0) : make_float2(lds1(at[r] + b0), lds1(at[r] + b1));
+                s[r >> 1][x][2 * (r & 1)] = v.x; s[r >> 1][x][2 * (r & 1) + 1] = v.y;
+            }
+            if (KEYS) {
+                const float* row = bases + 2 * buf * kCols + step * 16 + 8 * x + 2 * t;
+                col_base[x] = *reinterpret_cast<const float2*>(row);
+                col_dot[x] = *reinterpret_cast<const float2*>(row + kCols);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+            uint32_t f[4], h[4];
+            ldsm(f, s1 + plain[k]);
+            ldsm(h, s2 + plain[k]);
+#pragma unroll
+            for (int a = 0; a < MT; ++a) {
+                mma(s[a][0], a1[a][k], f[0], f[1]); mma(s[a][1], a1[a][k], f[2], f[3]);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (k > 0) mma(dp[a][x], a2[a][k], h[2 * x], h[2 * x + 1]);
+                    else if (KEYS) mma(dp[a][x], a2[a][k], h[2 * x], h[2 * x + 1], col_dot[x].x, col_dot[x].y, col_dot[x].x, col_dot[x].y);
+                    else mma(dp[a][x], a2[a][k], h[2 * x], h[2 * x + 1], dot[2 * a], dot[2 * a], dot[2 * a + 1], dot[2 * a + 1]);
+                }
+            }
+        }
+        uint32_t pp[MT][4], pd[MT][4];
+#pragma unroll
+        for (int a = 0; a < MT; ++a)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float u = ex2(fmaf(s[a][x][2 * e], c, KEYS ? col_base[x].x : base[2 * a + e])), v = ex2(fmaf(s[a][x][2 * e + 1], c, KEYS ? col_base[x].y : base[2 * a + e]));
+                    if (!KEYS && ends) {
+                        const int j = step * 16 + 8 * x + 2 * t;
+                        if (j >= left) u = 0.0f;
+                        if (j + 1 >= left) v = 0.0f;
+                    }
+                    if (KEYS) pp[a][2 * x + e] = pack(u, v);
+                    pd[a][2 * x + e] = pack(u * dp[a][x][2 * e], v * dp[a][x][2 * e + 1]);
+                }
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+            uint32_t f[4];
+            ldsm_t(f, s1 + turned[k]);
+#pragma unroll
+            for (int a = 0; a < MT; ++a) { mma(acc1[a][2 * k], pd[a], f[0], f[1]); mma(acc1[a][2 * k + 1], pd[a], f[2], f[3]); }
+            if (KEYS) {
+                ldsm_t(f, s2 + turned[k]);
+#pragma unroll
+                for (int a = 0; a < MT; ++a) { mma(acc2[a][2 * k], pp[a], f[0], f[1]); mma(acc2[a][2 * k + 1], pp[a], f[2], f[3]); }
+            }
+        }
+    };
     for (int tile_col = 0, buf = 0, place = 0; tile_col < n; tile_col += kCols, buf ^= 1) {
         const int next = place == 2 ? 0 : place + 1, free = 3 - place - next;
         cp_wait<0>();
         __syncthreads();
         if (tile_col + kCols < n) stage(buf ^ 1, next);
         if (warp == 0 && tile_col + 2 * kCols < n) walk.next(w, m.W, bias.pitch, lane, pixels + free * kCols, bs + free * kCols);
-        const int steps = min(kCols, n - tile_col + 15) / 16;
-        const uint32_t t1 = tile0 + buf * 2 * kTile;
+        const int left = n - tile_col;
+        if (TWICE && pairs) {
+            if (left >= kCols) {
+#pragma unroll 2
+                for (int step = 0; step < kCols / 16; ++step) cols_at(step, true, false, buf, place, left);
+            } else {
 #pragma unroll 1
-        for (int step = 0; step < steps; ++step) {
-            const int* b = bs + place * kCols + step * 16 + 2 * t;
-            float s[MT][2][4], dp[MT][2][4];
-            float2 col_base[2], col_dot[2];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int b0 = b[8 * x], b1 = pairs ? 0 : b[8 * x + 1];
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const float2 v = pairs ? lds2(at[r] + b0) : make_float2(lds1(at[r] + b0), lds1(at[r] + b1));
-                    s[r >> 1][x][2 * (r & 1)] = v.x; s[r >> 1][x][2 * (r & 1) + 1] = v.y;
-                }
-                if (KEYS) {
-                    const float* row = bases + 2 * buf * kCols + step * 16 + 8 * x + 2 * t;
-                    col_base[x] = *reinterpret_cast<const float2*>(row);
-                    col_dot[x] = *reinterpret_cast<const float2*>(row + kCols);
-                }
+                for (int step = 0; step * 16 < left; ++step) cols_at(step, true, true, buf, place, left);
             }
-            const uint32_t s1 = t1 + step * (16 * D * 2), s2 = s1 + kTile;
-#pragma unroll
-            for (int k = 0; k < KC; ++k) {
-                uint32_t f[4], h[4];
-                ldsm(f, s1 + plain[k]);
-                ldsm(h, s2 + plain[k]);
-#pragma unroll
-                for (int a = 0; a < MT; ++a) {
-                    mma(s[a][0], a1[a][k], f[0], f[1]); mma(s[a][1], a1[a][k], f[2], f[3]);
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        if (k > 0) mma(dp[a][x], a2[a][k], h[2 * x], h[2 * x + 1]);
-                        else if (KEYS) mma(dp[a][x], a2[a][k], h[2 * x], h[2 * x + 1], col_dot[x].x, col_dot[x].y, col_dot[x].x, col_dot[x].y);
-                        else mma(dp[a][x], a2[a][k], h[2 * x], h[2 * x + 1], dot[2 * a], dot[2 * a], dot[2 * a + 1], dot[2 * a + 1]);
-                    }
-                }
-            }
-            const bool cut = !KEYS && tile_col + step * 16 + 16 > n;
-            uint32_t pp[MT][4], pd[MT][4];
-#pragma unroll
-            for (int a = 0; a < MT; ++a)
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const Two bb = KEYS ? two(col_base[x].x, col_base[x].y) : base[2 * a + e];
-                        float u, v;
-                        apart(fma2(two(s[a][x][2 * e], s[a][x][2 * e + 1]), by, bb), u, v);
-                        u = ex2(u); v = ex2(v);
-                        if (cut) {
-                            const int j = tile_col + step * 16 + 8 * x + 2 * t;
-                            if (j >= n) u = 0.0f;
-                            if (j + 1 >= n) v = 0.0f;
-                        }
-                        if (KEYS) pp[a][2 * x + e] = pack(u, v);
-                        apart(mul2(two(u, v), two(dp[a][x][2 * e], dp[a][x][2 * e + 1])), u, v);
-                        pd[a][2 * x + e] = pack(u, v);
-                    }
-#pragma unroll
-            for (int k = 0; k < KC; ++k) {
-                uint32_t f[4];
-                ldsm_t(f, s1 + turned[k]);
-#pragma unroll
-                for (int a = 0; a < MT; ++a) { mma(acc1[a][2 * k], pd[a], f[0], f[1]); mma(acc1[a][2 * k + 1], pd[a], f[2], f[3]); }
-                if (KEYS) {
-                    ldsm_t(f, s2 + turned[k]);
-#pragma unroll
-                    for (int a = 0; a < MT; ++a) { mma(acc2[a][2 * k], pp[a], f[0], f[1]); mma(acc2[a][2 * k + 1], pp[a], f[2], f[3]); }
-                }
-            }
+        } else {
+#pragma unroll 1
+            for (int step = 0; step < (min(kCols, left) + 15) / 16; ++step) cols_at(step, false, true, buf, place, left);
         }
         place = next;
     }
@@ -408,15 +414,16 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
 }
 
 // The table's gradient.  A block has one head, a tile of 64 keys, every `parts`-th tile of 128 queries and every `groups`-th window; for each
-// tile of queries its windows pass by with the sums of ds of the 128 x 64 pairs in registers (a warp 32 x 32, and the pairs' bias there too:
-// nothing of the table is read in the loop).  Windows of one width have the tokens at the same places; those of the last column, where it
-// is narrower, come second.  Then every thread adds up the pairs of some offsets.
+// tile of queries its windows pass by with the sums of ds of the 128 x 64 pairs in registers (a warp 32 x 32), their bias laid
+// out as the products' C operands once.  Windows of one shape have the tokens at the same places; those that the border cuts come
+// behind the whole ones.  Then every thread adds up the pairs of some offsets.
 constexpr int kPairQ = 128, kPairK = 64, kList = 64;
 template <int D> struct PairSmem {
     static constexpr int kQ = kPairQ * D * 2, kK = kPairK * D * 2, kBuf = 2 * kQ + 2 * kK;
     static constexpr int kSums = kPairQ * (kPairK + 1) * 4;         // the pairs' sums, over the staged tiles
     static constexpr int kData = 2 * kBuf > kSums ? 2 * kBuf : kSums;
-    static __host__ __device__ size_t bytes(int offsets) { return kData + 2 * kList * 24 + (4 * kPairQ + 2 * (kPairQ + kPairK) + offsets) * 4; }
+    static constexpr int kBias = 256 * 8 * 16;                      // the pairs' bias, eight C operands a thread
+    static __host__ __device__ size_t bytes(int offsets) { return kData + kBias + 2 * kList * 16 + (4 * kPairQ + 2 * (kPairQ + kPairK) + offsets) * 4; }
 };
 template <int D>
 __global__ void __launch_bounds__(256, D <= 16 ? 2 : 1)
@@ -425,8 +432,9 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles, int parts) {
     constexpr int KC = D / 16, P = Tile<D>::kPieces, QN = kPairQ * P / 256, KN = kPairK * P > 256 ? kPairK * P / 256 : 1;   // pieces of q, of k that a thread stages
     using S = PairSmem<D>;
     extern __shared__ __align__(128) unsigned char raw[];
-    long long* list = reinterpret_cast<long long*>(raw + S::kData); // windows to come, two halves: first pixel, end of its places, first row
-    float* bases = reinterpret_cast<float*>(list + 2 * kList * 3);  // [two windows][bases, dots][kPairQ]
+    float4* bias = reinterpret_cast<float4*>(raw + S::kData) + threadIdx.x;   // of this thread, 256 apart
+    long long* list = reinterpret_cast<long long*>(raw + S::kData + S::kBias); // windows to come, two halves: first pixel, first row
+    float* bases = reinterpret_cast<float*>(list + 2 * kList * 2);  // [two windows][bases, dots][kPairQ]
     int* px = reinterpret_cast<int*>(bases + 4 * kPairQ);           // places of the queries, of the keys; behind the window's first pixel
     int* lin = px + kPairQ + kPairK;                                // y pitch + x of them
     float* sums = reinterpret_cast<float*>(lin + kPairQ + kPairK);
@@ -436,61 +444,62 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles, int parts) {
     const int pitch = 2 * m.ww - 1, offsets = (2 * m.wh - 1) * pitch;
     const long long dense = (long long)m.heads * m.d, off = (long long)head * m.d, hw = (long long)m.H * m.W;
     const bool wide_q = pieces(m.q, m.stride, m.d), wide_k = pieces(m.k, m.stride, m.d), wide_v = pieces(m.v, m.stride, m.d), wide_g = pieces(gr.go, dense, m.d);
-    const Two by = two(m.scale * kLog2e, m.scale * kLog2e);
+    const float c = m.scale * kLog2e;
     uint32_t plain[KC], turned[KC];
     lane_offsets<D>(lane, plain, turned);
     for (int o = tid; o < offsets; o += 256) sums[o] = 0.0f;
-    const int full = m.W / m.ww, rest = m.W - full * m.ww;          // windows of whole width in a row; the last one's width
-    const int tall = min(m.wh, m.H);                                // rows of the tallest window
-    for (int narrow = 0; narrow < 2; ++narrow) {
-        const int per_row = narrow ? (rest > 0) : full, width = narrow ? rest : m.ww;
-        const int count = m.B * m.ny * per_row, tokens = tall * width;
+    const int full_x = m.W / m.ww, rest_x = m.W - full_x * m.ww, full_y = m.H / m.wh, rest_y = m.H - full_y * m.wh;   // whole windows, and what is left
+    for (int kind = 0; kind < 4; ++kind) {
+        const int per_row = kind & 1 ? (rest_x > 0) : full_x, width = kind & 1 ? rest_x : m.ww, per_col = kind & 2 ? (rest_y > 0) : full_y, height = kind & 2 ? rest_y : m.wh;
+        const int count = m.B * per_col * per_row, tokens = height * width;
         const int mine = group < count ? (count - group + gr.groups - 1) / gr.groups : 0;
         if (mine == 0 || key0 >= tokens) continue;
         auto look = [&](int i) {                                    // the group's windows i .. i + kList - 1 into the list
             if (tid < kList && i + tid < mine) {
-                const int at = group + (i + tid) * gr.groups, row = at / per_row;
-                const Window w = window_at(m, row * m.nx + (narrow ? full : at - row * per_row));
-                long long* l = list + ((i / kList & 1) * kList + tid) * 3;
-                l[0] = w.pixel;
-                l[1] = (long long)(w.h - 1) * m.W + width;
-                l[2] = ((long long)w.b * m.heads + head) * hw + w.pixel - w.b * hw;
+                const int at = group + (i + tid) * gr.groups, line = at / per_row, b = line / per_col;
+                const int wy = kind & 2 ? full_y : line - b * per_col, wx = kind & 1 ? full_x : at - line * per_row;
+                const long long pixel = (long long)b * hw + (long long)wy * m.wh * m.W + wx * m.ww;
+                long long* l = list + ((i / kList & 1) * kList + tid) * 2;
+                l[0] = pixel;
+                l[1] = ((long long)b * m.heads + head) * hw + pixel - b * hw;
             }
         };
         for (int q0 = part * kPairQ; q0 < tokens; q0 += parts * kPairQ) {
             __syncthreads();                                        // the last queries' sums and places are done with
             for (int r = tid; r < kPairQ + kPairK; r += 256) {
                 const int i = r < kPairQ ? q0 + r : key0 + r - kPairQ, y = i / width, x = i - y * width;
-                px[r] = i < tokens ? y * m.W + x : 0x7fffffff;
+                px[r] = i < tokens ? y * m.W + x : -1;
                 lin[r] = y * pitch + x;
             }
             look(0);
             __syncthreads();
-            float bias[2][4][4], sum[2][4][4];
+            float sum[2][4][4];
 #pragma unroll
             for (int a = 0; a < 2; ++a)
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
+                for (int x = 0; x < 4; ++x) {
+                    float v[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int i = wq + 16 * a + 8 * (e >> 1) + g, j = kPairQ + wk + 8 * x + 2 * t + (e & 1);
-                        float v = -INFINITY;                        // pairs that are none: p = 0
-                        if (px[i] != 0x7fffffff && px[j] != 0x7fffffff) {
-                            v = relpos::table_at(m.table, m.bucket, m.n_buckets, m.heads, head, lin[i] - lin[j] + (m.wh - 1) * pitch + m.ww - 1);
-                            v = v <= kMasked ? -INFINITY : v * m.inv_scale;
+                        v[e] = -INFINITY;                           // pairs that are none: p = 0
+                        if (px[i] >= 0 && px[j] >= 0) {
+                            v[e] = relpos::table_at(m.table, m.bucket, m.n_buckets, m.heads, head, lin[i] - lin[j] + (m.wh - 1) * pitch + m.ww - 1);
+                            v[e] = v[e] <= kMasked ? -INFINITY : v[e] * m.inv_scale;
                         }
-                        bias[a][x][e] = v;
                         sum[a][x][e] = 0.0f;
                     }
+                    bias[(4 * a + x) * 256] = make_float4(v[0], v[1], v[2], v[3]);
+                }
             auto stage = [&](int i, int buf) {
-                const long long* l = list + ((i / kList & 1) * kList + i % kList) * 3;
-                const long long pixel = l[0], end = l[1], row0 = l[2];
+                const long long* l = list + ((i / kList & 1) * kList + i % kList) * 2;
+                const long long pixel = l[0], row0 = l[1];
                 const uint32_t dst = data + buf * S::kBuf;
                 const bf16 *q = m.q + pixel * m.stride + off, *go = gr.go + pixel * dense + off, *k = m.k + pixel * m.stride + off, *v = m.v + pixel * m.stride + off;
 #pragma unroll
                 for (int u = 0; u < QN; ++u) {
                     const int r = (tid + 256 * u) / P, c = (tid + 256 * u) % P * 8;
-                    const bool real = px[r] < end && c < m.d;       // rows of a shorter window end early
+                    const bool real = px[r] >= 0 && c < m.d;
                     const long long at = real ? px[r] : 0;
                     stage_piece(q + at * m.stride + (real ? c : 0), dst + Tile<D>::at(r, c / 8), real, m.d - c, wide_q);
                     stage_piece(go + at * dense + (real ? c : 0), dst + S::kQ + Tile<D>::at(r, c / 8), real, m.d - c, wide_g);
@@ -499,12 +508,12 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles, int parts) {
 #pragma unroll
                     for (int u = 0; u < KN; ++u) {
                         const int r = (tid + 256 * u) / P, c = (tid + 256 * u) % P * 8, p = px[kPairQ + r];
-                        const bool real = p < end && c < m.d;
+                        const bool real = p >= 0 && c < m.d;
                         const long long at = real ? p * m.stride + c : 0;
                         stage_piece(k + at, dst + 2 * S::kQ + Tile<D>::at(r, c / 8), real, m.d - c, wide_k);
                         stage_piece(v + at, dst + 2 * S::kQ + S::kK + Tile<D>::at(r, c / 8), real, m.d - c, wide_v);
                     }
-                if (tid < kPairQ) stage_terms(gr, row0, px[tid], px[tid] < end, bases + 2 * buf * kPairQ + tid, kPairQ);
+                if (tid < kPairQ) stage_terms(gr, row0, px[tid], px[tid] >= 0, bases + 2 * buf * kPairQ + tid, kPairQ);
                 cp_commit();
             };
             stage(0, 0);
@@ -513,7 +522,6 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles, int parts) {
                 __syncthreads();
                 if (i % kList == 0) look(i + kList);                // read from the next barrier on
                 if (i + 1 < mine) stage(i + 1, buf ^ 1);
-                const bool short_ = list[((i / kList & 1) * kList + i % kList) * 3 + 1] < (long long)(tall - 1) * m.W + width;
                 const uint32_t dst = data + buf * S::kBuf;
                 uint32_t q[2][KC][4], go[2][KC][4];
 #pragma unroll
@@ -524,18 +532,23 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles, int parts) {
                         ldsm(q[a][k], dst + wq * (D * 2) + a * (16 * D * 2) + turned[k]);
                         ldsm(go[a][k], dst + S::kQ + wq * (D * 2) + a * (16 * D * 2) + turned[k]);
                     }
-                float dot[4];
-                Two base[4];
+                float dot[4], base[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float b = bases[2 * buf * kPairQ + wq + 8 * r + g];
-                    base[r] = two(b, b);
+                    base[r] = bases[2 * buf * kPairQ + wq + 8 * r + g];
                     dot[r] = bases[(2 * buf + 1) * kPairQ + wq + 8 * r + g];
                 }
                 const uint32_t ks = dst + 2 * S::kQ + wk * (D * 2), vs = ks + S::kK;
 #pragma unroll
                 for (int x = 0; x < 4; x += 2) {
                     float s[2][2][4], dp[2][2][4];
+#pragma unroll
+                    for (int a = 0; a < 2; ++a)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const float4 v = bias[(4 * a + x + y) * 256];
+                            s[a][y][0] = v.x; s[a][y][1] = v.y; s[a][y][2] = v.z; s[a][y][3] = v.w;
+                        }
 #pragma unroll
                     for (int k = 0; k < KC; ++k) {
                         uint32_t f[4], h[4];
@@ -545,12 +558,9 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles, int parts) {
                         for (int a = 0; a < 2; ++a)
 #pragma unroll
                             for (int y = 0; y < 2; ++y) {
-                                if (k > 0) { mma(s[a][y], q[a][k], f[2 * y], f[2 * y + 1]); mma(dp[a][y], go[a][k], h[2 * y], h[2 * y + 1]); }
-                                else {
-                                    const float* b = bias[a][x + y];
-                                    mma(s[a][y], q[a][k], f[2 * y], f[2 * y + 1], b[0], b[1], b[2], b[3]);
-                                    mma(dp[a][y], go[a][k], h[2 * y], h[2 * y + 1], dot[2 * a], dot[2 * a], dot[2 * a + 1], dot[2 * a + 1]);
-                                }
+                                mma(s[a][y], q[a][k], f[2 * y], f[2 * y + 1]);
+                                if (k > 0) mma(dp[a][y], go[a][k], h[2 * y], h[2 * y + 1]);
+                                else mma(dp[a][y], go[a][k], h[2 * y], h[2 * y + 1], dot[2 * a], dot[2 * a], dot[2 * a + 1], dot[2 * a + 1]);
                             }
                     }
 #pragma unroll
@@ -559,17 +569,9 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles, int parts) {
                         for (int y = 0; y < 2; ++y)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                float u, v;
-                                apart(fma2(two(s[a][y][2 * e], s[a][y][2 * e + 1]), by, base[2 * a + e]), u, v);
-                                u = ex2(u); v = ex2(v);
-                                if (short_) {                       // keys that this window does not have
-                                    const long long end = list[((i / kList & 1) * kList + i % kList) * 3 + 1];
-                                    const int* p = px + kPairQ + wk + 8 * (x + y) + 2 * t;
-                                    if (p[0] >= end) u = 0.0f;
-                                    if (p[1] >= end) v = 0.0f;
-                                }
                                 float* to = &sum[a][x + y][2 * e];
-                                apart(fma2(two(u, v), two(dp[a][y][2 * e], dp[a][y][2 * e + 1]), two(to[0], to[1])), to[0], to[1]);
+                                to[0] = fmaf(ex2(fmaf(s[a][y][2 * e], c, base[2 * a + e])), dp[a][y][2 * e], to[0]);
+                                to[1] = fmaf(ex2(fmaf(s[a][y][2 * e + 1], c, base[2 * a + e])), dp[a][y][2 * e + 1], to[1]);
                             }
                 }
             }
