@@ -17,6 +17,8 @@ using bf16 = __nv_bfloat16;
 
 bool known(int dtype) { return dtype == ESC_F32 || dtype == ESC_BF16; }
 
+constexpr size_t kMostSmem = 227 * 1024;           // of a block
+
 // Shared memory beyond 48 KB, once more for every call: the attribute belongs to the current device, and setting it again
 // is cheaper than remembering which devices have it.
 template <typename K> int allow_smem(K kernel, size_t bytes) {
@@ -61,8 +63,8 @@ int launch_table_sums(const float* part, float* dense, int slices, bool per_offs
 
 template <typename T>
 int bias_forward_t(const void* table, const int* bucket, int n_buckets, int heads, int wh, int ww, void* bias, cudaStream_t st) {
-    const int groups = (ww + rp::kRows - 1) / rp::kRows, rows = std::min(rp::kRows, ww);
-    const size_t smem = (size_t)(rp::skew(wh * (ww + rows - 1)) + 1) * sizeof(float);
+    const int groups = (ww + rp::kRows - 1) / rp::kRows;
+    const size_t smem = (size_t)rp::strip_floats(wh, ww, esc::Elem<T>::kVec) * sizeof(float);
     ESC_TRY(allow_smem(rp::fill<T>, smem));
     rp::fill<T><<<(unsigned)(heads * wh * groups), rp::kFillThreads, smem, st>>>(static_cast<const T*>(table), bucket, n_buckets, heads, wh, ww, static_cast<T*>(bias));
     return launched();
@@ -236,9 +238,11 @@ template <int D> int backward_bf16(const Call& c, wa::bwd::Grads<bf16> g, cudaSt
     ESC_TRY(twice ? (grad_rows_bf16<D, false, true>(c, g, st)) : (grad_rows_bf16<D, false, false>(c, g, st)));
     if (!g.part) return ESC_OK;
     g.groups = pair_groups(c);
-    const size_t smem = PairSmem<D>::bytes((int)rp::offsets_of(c.wh, c.ww));
+    const int offsets = (int)rp::offsets_of(c.wh, c.ww);
+    const bool staged = PairSmem<D>::bytes(offsets, true) <= kMostSmem;
+    const size_t smem = PairSmem<D>::bytes(offsets, staged);
     ESC_TRY(allow_smem(grad_table<D>, smem));
-    grad_table<D><<<(unsigned)(pair_slices(c) * c.heads), 256, smem, st>>>(maps_of<bf16>(c), g, key_tiles(c), pair_parts(c));
+    grad_table<D><<<(unsigned)(pair_slices(c) * c.heads), 256, smem, st>>>(maps_of<bf16>(c), g, key_tiles(c), pair_parts(c), staged);
     return launched();
 }
 

@@ -65,29 +65,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// Two fp32 values in one register pair, and arithmetic on both at a time.
-using Two = unsigned long long;
-__device__ __forceinline__ Two two(float x, float y) {
-    Two d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(x), "f"(y));
-    return d;
-}
-__device__ __forceinline__ void apart(Two v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
-    Two d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ Two add2(Two a, Two b) {
-    Two d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ Two mul2(Two a, Two b) {
-    Two d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 __device__ __forceinline__ float2 lds2(uint32_t addr) {
     float2 v;
     asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr));
@@ -99,13 +76,15 @@ __device__ __forceinline__ float lds1(uint32_t addr) {
     return v;
 }
 
-// The head's table into shared memory, divided by the scale.
+// An offset's bias, divided by the scale.
+template <typename T> __device__ __forceinline__ float bias_of(const Maps<T>& m, int head, int o) {
+    const float v = relpos::table_at(m.table, m.bucket, m.n_buckets, m.heads, head, o);
+    return v <= kMasked ? -INFINITY : v * m.inv_scale;
+}
+// The head's into shared memory.
 template <typename T> __device__ __forceinline__ void stage_table(const Maps<T>& m, int head, float* dst) {
     const int offsets = (2 * m.wh - 1) * (2 * m.ww - 1);
-    for (int o = threadIdx.x; o < offsets; o += blockDim.x) {
-        const float t = relpos::table_at(m.table, m.bucket, m.n_buckets, m.heads, head, o);
-        dst[o] = t <= kMasked ? -INFINITY : t * m.inv_scale;
-    }
+    for (int o = threadIdx.x; o < offsets; o += blockDim.x) dst[o] = bias_of(m, head, o);
 }
 
 // ---- fp32: CUDA cores -----------------------------------------------------------------------------------------------------
@@ -357,8 +336,7 @@ template <bool TWICE, bool BACKWARDS> __device__ __forceinline__ void stage_bias
     const int step = blockDim.x / span, c0 = threadIdx.x % span;
     for (int r = threadIdx.x / span; r < rows; r += step)
         for (int c = c0; c < cols; c += span) {
-            const float x = relpos::table_at(m.table, m.bucket, m.n_buckets, m.heads, head, r * cols + c);
-            const float v = x <= kMasked ? -INFINITY : x * m.inv_scale;
+            const float v = bias_of(m, head, r * cols + c);
             const int at = BACKWARDS ? (rows - 1 - r) * bias.pitch + cols - 1 - c : r * bias.pitch + c;
             table[at] = v;
             if (TWICE) table[bias.size + bias_gap() + at + 1] = v;

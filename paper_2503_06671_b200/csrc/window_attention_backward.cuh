@@ -221,14 +221,8 @@ grad_q(Maps<float> m, Grads<float> g, int tiles) {
 namespace tc {
 using namespace winatt::tc;
 constexpr int kCols = 128;                                          // staged columns: queries for rows of keys, keys for rows of queries
-#ifndef GT
-#define GT (D <= 32 ? 2 : 1)
-#endif
-__host__ __device__ constexpr int grad_tiles(int D) { return GT; }   // tiles of 16 rows of a warp
-#ifndef GBL
-#define GBL (D <= 16 ? 2 : 1)
-#endif
-__host__ __device__ constexpr int grad_blocks(int D) { return GBL; }                // on an SM
+__host__ __device__ constexpr int grad_tiles(int D) { return D <= 32 ? 2 : 1; }    // tiles of 16 rows of a warp
+__host__ __device__ constexpr int grad_blocks(int D) { return D <= 16 ? 2 : 1; }   // on an SM
 
 template <int D> struct RowSmem {
     static constexpr int kTile = kCols * D * 2, kWalk = 3 * kCols * (8 + 4), kRows = 2 * kCols * 2 * 4;   // the columns' terms, two tiles
@@ -423,11 +417,12 @@ template <int D> struct PairSmem {
     static constexpr int kSums = kPairQ * (kPairK + 1) * 4;         // the pairs' sums, over the staged tiles
     static constexpr int kData = 2 * kBuf > kSums ? 2 * kBuf : kSums;
     static constexpr int kBias = 256 * 8 * 16;                      // the pairs' bias, eight C operands a thread
-    static __host__ __device__ size_t bytes(int offsets) { return kData + kBias + 2 * kList * 16 + (4 * kPairQ + 2 * (kPairQ + kPairK) + offsets) * 4; }
+    static __host__ __device__ size_t bytes(int offsets, bool staged) { return kData + kBias + 2 * kList * 16 + (4 * kPairQ + 2 * (kPairQ + kPairK) + (staged ? 2 : 1) * offsets) * 4; }
 };
 template <int D>
-__global__ void __launch_bounds__(256, D <= 16 ? 2 : 1)
-grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles, int parts) {
+__global__ void __launch_bounds__(256, D <= 32 ? 2 : 1)
+grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles, int parts, bool staged) {   // staged: there is room for the head's table
+
     using namespace wmma16;
     constexpr int KC = D / 16, P = Tile<D>::kPieces, QN = kPairQ * P / 256, KN = kPairK * P > 256 ? kPairK * P / 256 : 1;   // pieces of q, of k that a thread stages
     using S = PairSmem<D>;
@@ -447,7 +442,11 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles, int parts) {
     const float c = m.scale * kLog2e;
     uint32_t plain[KC], turned[KC];
     lane_offsets<D>(lane, plain, turned);
-    for (int o = tid; o < offsets; o += 256) sums[o] = 0.0f;
+    float* table = sums + offsets;
+    for (int o = tid; o < offsets; o += 256) {
+        if (staged) table[o] = bias_of(m, head, o);
+        sums[o] = 0.0f;
+    }
     const int full_x = m.W / m.ww, rest_x = m.W - full_x * m.ww, full_y = m.H / m.wh, rest_y = m.H - full_y * m.wh;   // whole windows, and what is left
     for (int kind = 0; kind < 4; ++kind) {
         const int per_row = kind & 1 ? (rest_x > 0) : full_x, width = kind & 1 ? rest_x : m.ww, per_col = kind & 2 ? (rest_y > 0) : full_y, height = kind & 2 ? rest_y : m.wh;
@@ -482,11 +481,8 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles, int parts) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int i = wq + 16 * a + 8 * (e >> 1) + g, j = kPairQ + wk + 8 * x + 2 * t + (e & 1);
-                        v[e] = -INFINITY;                           // pairs that are none: p = 0
-                        if (px[i] >= 0 && px[j] >= 0) {
-                            v[e] = relpos::table_at(m.table, m.bucket, m.n_buckets, m.heads, head, lin[i] - lin[j] + (m.wh - 1) * pitch + m.ww - 1);
-                            v[e] = v[e] <= kMasked ? -INFINITY : v[e] * m.inv_scale;
-                        }
+                        const int o = lin[i] - lin[j] + (m.wh - 1) * pitch + m.ww - 1;
+                        v[e] = px[i] < 0 || px[j] < 0 ? -INFINITY : staged ? table[o] : bias_of(m, head, o);   // pairs that are none: p = 0
                         sum[a][x][e] = 0.0f;
                     }
                     bias[(4 * a + x) * 256] = make_float4(v[0], v[1], v[2], v[3]);
@@ -523,56 +519,40 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles, int parts) {
                 if (i % kList == 0) look(i + kList);                // read from the next barrier on
                 if (i + 1 < mine) stage(i + 1, buf ^ 1);
                 const uint32_t dst = data + buf * S::kBuf;
-                uint32_t q[2][KC][4], go[2][KC][4];
-#pragma unroll
-                for (int a = 0; a < 2; ++a)
-#pragma unroll
-                    for (int k = 0; k < KC; ++k) {
-                        // as an A operand: rows lane % 16, piece lane / 16
-                        ldsm(q[a][k], dst + wq * (D * 2) + a * (16 * D * 2) + turned[k]);
-                        ldsm(go[a][k], dst + S::kQ + wq * (D * 2) + a * (16 * D * 2) + turned[k]);
-                    }
-                float dot[4], base[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    base[r] = bases[2 * buf * kPairQ + wq + 8 * r + g];
-                    dot[r] = bases[(2 * buf + 1) * kPairQ + wq + 8 * r + g];
-                }
                 const uint32_t ks = dst + 2 * S::kQ + wk * (D * 2), vs = ks + S::kK;
 #pragma unroll
-                for (int x = 0; x < 4; x += 2) {
-                    float s[2][2][4], dp[2][2][4];
+                for (int a = 0; a < 2; ++a) {                       // 16 queries at a time
+                    uint32_t q[KC][4], go[KC][4];
+                    const uint32_t rows = dst + (wq + 16 * a) * (D * 2);
 #pragma unroll
-                    for (int a = 0; a < 2; ++a)
+                    for (int k = 0; k < KC; ++k) { ldsm(q[k], rows + turned[k]); ldsm(go[k], rows + S::kQ + turned[k]); }   // as A operands: rows lane % 16, piece lane / 16
+                    const float* terms = bases + 2 * buf * kPairQ + wq + 16 * a + g;
+                    const float base[2] = {terms[0], terms[8]}, dot[2] = {terms[kPairQ], terms[kPairQ + 8]};
+#pragma unroll
+                    for (int x = 0; x < 4; x += 2) {
+                        float s[2][4], dp[2][4];
 #pragma unroll
                         for (int y = 0; y < 2; ++y) {
                             const float4 v = bias[(4 * a + x + y) * 256];
-                            s[a][y][0] = v.x; s[a][y][1] = v.y; s[a][y][2] = v.z; s[a][y][3] = v.w;
+                            s[y][0] = v.x; s[y][1] = v.y; s[y][2] = v.z; s[y][3] = v.w;
                         }
 #pragma unroll
-                    for (int k = 0; k < KC; ++k) {
-                        uint32_t f[4], h[4];
-                        ldsm(f, ks + x * (8 * D * 2) + plain[k]);
-                        ldsm(h, vs + x * (8 * D * 2) + plain[k]);
-#pragma unroll
-                        for (int a = 0; a < 2; ++a)
+                        for (int k = 0; k < KC; ++k) {
+                            uint32_t f[4], h[4];
+                            ldsm(f, ks + x * (8 * D * 2) + plain[k]);
+                            ldsm(h, vs + x * (8 * D * 2) + plain[k]);
 #pragma unroll
                             for (int y = 0; y < 2; ++y) {
-                                mma(s[a][y], q[a][k], f[2 * y], f[2 * y + 1]);
-                                if (k > 0) mma(dp[a][y], go[a][k], h[2 * y], h[2 * y + 1]);
-                                else mma(dp[a][y], go[a][k], h[2 * y], h[2 * y + 1], dot[2 * a], dot[2 * a], dot[2 * a + 1], dot[2 * a + 1]);
+                                mma(s[y], q[k], f[2 * y], f[2 * y + 1]);
+                                if (k > 0) mma(dp[y], go[k], h[2 * y], h[2 * y + 1]);
+                                else mma(dp[y], go[k], h[2 * y], h[2 * y + 1], dot[0], dot[0], dot[1], dot[1]);
                             }
-                    }
-#pragma unroll
-                    for (int a = 0; a < 2; ++a)
+                        }
 #pragma unroll
                         for (int y = 0; y < 2; ++y)
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                float* to = &sum[a][x + y][2 * e];
-                                to[0] = fmaf(ex2(fmaf(s[a][y][2 * e], c, base[2 * a + e])), dp[a][y][2 * e], to[0]);
-                                to[1] = fmaf(ex2(fmaf(s[a][y][2 * e + 1], c, base[2 * a + e])), dp[a][y][2 * e + 1], to[1]);
-                            }
+                            for (int e = 0; e < 4; ++e) sum[a][x + y][e] = fmaf(ex2(fmaf(s[y][e], c, base[e >> 1])), dp[y][e], sum[a][x + y][e]);
+                    }
                 }
             }
             // the pairs' sums to their offsets: every thread takes some offsets and walks the keys
@@ -590,11 +570,11 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles, int parts) {
             for (int o = tid; o < (dy_hi - dy_lo + 1) * cols; o += 256) {
                 const int dy = dy_lo + o / cols, dx = o % cols - (width - 1);
                 float v = 0.0f;
-                int yj = key0 / width, xj = key0 - yj * width;
-                for (int j = key0; j < k_end; ++j) {
-                    const int xi = xj + dx, i = (yj + dy) * width + xi;
-                    if ((unsigned)xi < (unsigned)width && i >= q0 && i < q_end) v += pair[(i - q0) * (kPairK + 1) + j - key0];
-                    if (++xj == width) { xj = 0; ++yj; }
+                for (int yj = key0 / width, j0 = key0; j0 < k_end; ++yj, j0 = yj * width) {   // a row of keys; the queries next to it are a row too
+                    const int shift = dy * width + dx;              // i - j
+                    const int lo = max(max(j0, yj * width - dx), q0 - shift), hi = min(min(min(k_end, (yj + 1) * width), (yj + 1) * width - dx), q_end - shift);
+                    const float* from = pair + (lo + shift - q0) * (kPairK + 1) + lo - key0;
+                    for (int j = lo; j < hi; ++j, from += kPairK + 2) v += *from;
                 }
                 sums[(dy + m.wh - 1) * pitch + dx + m.ww - 1] += v;
             }
