@@ -87,22 +87,23 @@ template <> __device__ __forceinline__ float one_in<__nv_fp8_e4m3>(const __nv_fp
 template <typename T> __device__ __forceinline__ void one_out(T* p, float f) { *p = Elem<T>::from_f32(f); }
 template <> __device__ __forceinline__ void one_out<__nv_fp8_e4m3>(__nv_fp8_e4m3* p, float f) { *p = __nv_fp8_e4m3(f); }   // to nearest, saturating
 
-// A lane's values of its warp's run: four at 4 lane and four at 128 + 4 lane, so that every access of a warp is one piece.
-template <typename T> __device__ __forceinline__ void in(const T* base, int n, bool wide, int lane, float* f) {
+// A lane's values of its warp's run: four at 4 lane and four at 128 + 4 lane, so that every access of a warp is one piece.  WHOLE: the run has
+// all its values and its pointers suit accesses of four; nothing is looked at per value then.
+template <bool WHOLE, typename T> __device__ __forceinline__ void in(const T* base, int n, int lane, float* f) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int at = 128 * h + 4 * lane;
-        if (wide && at + 4 <= n) Four<T>::load(base + at, f + 4 * h);
+        if (WHOLE) Four<T>::load(base + at, f + 4 * h);
         else
 #pragma unroll
             for (int i = 0; i < 4; ++i) f[4 * h + i] = at + i < n ? one_in<T>(base + at + i) : 0.0f;
     }
 }
-template <typename T> __device__ __forceinline__ void out(T* base, int n, bool wide, int lane, const float* f) {
+template <bool WHOLE, typename T> __device__ __forceinline__ void out(T* base, int n, int lane, const float* f) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int at = 128 * h + 4 * lane;
-        if (wide && at + 4 <= n) Four<T>::store(base + at, f + 4 * h);
+        if (WHOLE) Four<T>::store(base + at, f + 4 * h);
         else
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -110,46 +111,42 @@ template <typename T> __device__ __forceinline__ void out(T* base, int n, bool w
     }
 }
 
-// The scale of a warp's values x, which become the values to store.  Infinities do not count for the scale (they are stored as the
-// largest value), NaN stays NaN.
-__device__ __forceinline__ float scale_values(float* x, bool root) {
+// The largest magnitude of a warp's values.  Infinities do not count (they are stored as the largest value), nor does NaN, which stays.
+__device__ __forceinline__ float largest(const float* x, bool finite_only) {
     float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]) <= 3.0e38f ? fabsf(x[i]) : 0.0f);
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, !finite_only || fabsf(x[i]) <= 3.0e38f ? fabsf(x[i]) : 0.0f);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    return top;
+}
+// The scale of a warp's values x, which become the values to store.
+template <bool ROOT> __device__ __forceinline__ float scale_values(float* x) {
+    float top = largest(x, false);
+    if (top > 3.0e38f) top = largest(x, true);
     const bool some = top >= kTiny;
-    const float inverse = some ? __fmul_rn(kE4m3Max, __frcp_rn(top)) : 0.0f;
+    const float inverse = some ? __fmul_rn(kE4m3Max, __frcp_rn(top)) : 0.0f, least = some ? kE4m3Least : 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float y = __fmul_rn(x[i], inverse);
-        x[i] = root && some && x[i] > 0.0f && y < kE4m3Least ? kE4m3Least : y;
+        x[i] = ROOT && x[i] > 0.0f && y < least ? least : y;
     }
     return some ? __fmul_rn(top, 1.0f / kE4m3Max) : 0.0f;
 }
 
-// P, G: types of the parameters and the gradients; S: float or __nv_fp8_e4m3 for the states.
-// scalars (device, may be null) replaces keep, size, root and grad_scale, so that a captured graph can be replayed with other
-// steps and rates; skip (device, may be null): nothing is done where it is not zero.
-template <typename P, typename G, typename S>
-__global__ void __launch_bounds__(kThreads)
-step(const Chunk* __restrict__ chunks, Hyper h, const float* __restrict__ scalars, const int* __restrict__ skip) {
+// One run of a warp.
+template <bool WHOLE, typename P, typename G, typename S>
+__device__ __forceinline__ void step_run(const Chunk& c, const Hyper& h, int warp, int lane, int n) {
     constexpr bool kEight = sizeof(S) == 1;
-    if (skip && *skip != 0) return;
-    const Chunk c = chunks[blockIdx.x];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = warp * kQuant, n = min(c.n - first, kQuant);
-    if (n <= 0) return;
-    const bool wide = c.wide != 0;
+    const int first = warp * kQuant;
     P* cp = static_cast<P*>(c.p) + first;
     S *cm = static_cast<S*>(c.m) + first, *cv = static_cast<S*>(c.v) + first;
-    float p[8], g[8], m[8], v[8];
-    in<G>(static_cast<const G*>(c.g) + first, n, wide, lane, g);
-    in<S>(cm, n, wide, lane, m);
-    in<S>(cv, n, wide, lane, v);
-    in<P>(cp, n, wide, lane, p);
-    if (scalars) { h.keep = scalars[0]; h.size = scalars[1]; h.root = scalars[2]; h.grad_scale = scalars[3]; }
-    float ms = 0.0f, vs = 0.0f;
+    float p[8], g[8], m[8], v[8], ms = 0.0f, vs = 0.0f;
+    in<WHOLE, G>(static_cast<const G*>(c.g) + first, n, lane, g);
+    in<WHOLE, S>(cm, n, lane, m);
+    in<WHOLE, S>(cv, n, lane, v);
     if (kEight) { ms = c.m_scale[warp]; vs = c.v_scale[warp]; }
+    in<WHOLE, P>(cp, n, lane, p);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float gi = __fmul_rn(g[i], h.grad_scale);
@@ -161,18 +158,34 @@ step(const Chunk* __restrict__ chunks, Hyper h, const float* __restrict__ scalar
         m[i] = __fadd_rn(__fmul_rn(m[i], h.beta1), __fmul_rn(gi, h.one1));
         v[i] = __fadd_rn(__fmul_rn(v[i], h.beta2), __fmul_rn(__fmul_rn(gi, gi), h.one2));
         const float r = __fsqrt_rn(v[i]);
-        p[i] = __fsub_rn(__fmul_rn(p[i], h.keep), __fmul_rn(__fdiv_rn(m[i], __fadd_rn(__fmul_rn(r, h.root), h.eps)), h.size));
+        // the quotient to 2 ulp (an exact one is half of the update's instructions); nothing that is stored in 8 bits comes from it
+        p[i] = __fsub_rn(__fmul_rn(p[i], h.keep), __fmul_rn(__fdividef(m[i], __fadd_rn(__fmul_rn(r, h.root), h.eps)), h.size));
         if (kEight) v[i] = r;
     }
-    out<P>(cp, n, wide, lane, p);
-    if (c.copy) out<__nv_bfloat16>(c.copy + first, n, wide, lane, p);
+    out<WHOLE, P>(cp, n, lane, p);
+    if (c.copy) out<WHOLE, __nv_bfloat16>(c.copy + first, n, lane, p);
     if (kEight) {
-        ms = scale_values(m, false);
-        vs = scale_values(v, true);
+        ms = scale_values<false>(m);
+        vs = scale_values<true>(v);
         if (lane == 0) { c.m_scale[warp] = ms; c.v_scale[warp] = vs; }
     }
-    out<S>(cm, n, wide, lane, m);
-    out<S>(cv, n, wide, lane, v);
+    out<WHOLE, S>(cm, n, lane, m);
+    out<WHOLE, S>(cv, n, lane, v);
+}
+
+// P, G: types of the parameters and the gradients; S: float or __nv_fp8_e4m3 for the states.
+// scalars (device, may be null) replaces keep, size, root and grad_scale, so that a captured graph can be replayed with other
+// steps and rates; skip (device, may be null): nothing is done where it is not zero.
+template <typename P, typename G, typename S>
+__global__ void __launch_bounds__(kThreads)
+step(const Chunk* __restrict__ chunks, Hyper h, const float* __restrict__ scalars, const int* __restrict__ skip) {
+    if (skip && *skip != 0) return;
+    const Chunk c = chunks[blockIdx.x];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = min(c.n - warp * kQuant, kQuant);
+    if (n <= 0) return;
+    if (scalars) { h.keep = scalars[0]; h.size = scalars[1]; h.root = scalars[2]; h.grad_scale = scalars[3]; }
+    if (c.wide && n == kQuant) step_run<true, P, G, S>(c, h, warp, lane, n);
+    else step_run<false, P, G, S>(c, h, warp, lane, n);
 }
 
 }}  // namespace esc::adamw

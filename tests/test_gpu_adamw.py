@@ -2,9 +2,9 @@
 numpy (a code is a choice between two neighbours that one rounding can turn).
 
 Bounds, in roundings of u = 2^-24: m 4 (the gradient's scale, the factor's own, product, sum), v 6 (the scale twice, the square, the
-factor's own, product, sum).  p: 3 of |p| (1 - lr wd itself, the product, the difference); the update m's own and 12 of itself (3 from v
-under the root, the root, its factor and their product, eps and the sum, the quotient, the rate and its product, the difference); in
-bf16 half a step, 2^-8 |p|, more."""
+factor's own, product, sum).  p: 3 of |p| (1 - lr wd itself, the product, the difference); the update m's own and 15 of itself (3 from v
+under the root, the root, its factor and their product, eps and the sum, the quotient 4: it is within 2 ulp, the rate and its product,
+the difference); in bf16 half a step, 2^-8 |p|, more."""
 import math
 
 import numpy as np
@@ -64,7 +64,7 @@ def formula(p, g, m, v, t, grad_scale, lr, beta1, beta2, eps, weight_decay):
     up = lr / (1 - beta1 ** t) * m2 / (v2.sqrt() / math.sqrt(1 - beta2 ** t) + eps)
     e_m = 4 * U * (beta1 * m.abs() + (1 - beta1) * g.abs()) + 1e-40
     e_v = 6 * U * v2 + 1e-40
-    e_p = 3 * U * p.abs() + 12 * U * up.abs() + up.abs() * torch.where(m2 != 0, e_m / m2.abs().clamp(min=1e-300), 0.0) + 1e-40
+    e_p = 3 * U * p.abs() + 15 * U * up.abs() + up.abs() * torch.where(m2 != 0, e_m / m2.abs().clamp(min=1e-300), 0.0) + 1e-40
     return p * (1 - lr * weight_decay) - up, m2, v2, e_p, e_m, e_v
 
 
