@@ -6,6 +6,7 @@ an NCHW call takes a contiguous [B,C,H,W] tensor, an NHWC call a contiguous [B,H
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from pathlib import Path
 
@@ -491,14 +492,17 @@ def esc_convattn_device_status(workspace, stream=None) -> int:
 # ---- window self-attention, its relative position bias, AdamW ---------------------------------------------------------------
 
 
-def _on_device(*tensors):
+_HERE = contextlib.nullcontext()
+
+
+def _on_device(first, *others):
     """The tensors' one device, made current for the call that follows: kernels run where the data are."""
     import torch
 
-    devices = {t.device for t in tensors if t is not None}
-    if len(devices) != 1 or next(iter(devices)).type != "cuda":
-        raise ValueError(f"the tensors of a call have to be on one CUDA device, not on {sorted(map(str, devices))}")
-    return torch.cuda.device(devices.pop())
+    device = first.device
+    if device.type != "cuda" or any(t is not None and t.device != device for t in others):
+        raise ValueError("the tensors of a call have to be on one CUDA device")
+    return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
 
 def _dense(name, t, shape, dtype):

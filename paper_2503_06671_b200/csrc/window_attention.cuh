@@ -20,6 +20,9 @@ namespace esc { namespace winatt {
 
 constexpr int kMaxHeadDim = 64;
 constexpr float kMasked = -9984.0f;          // -10000 as bf16 rounds it
+// A row's powers are 2^(c s - base).  The base is the row's first maximum and moves only when one is kSlack above it (p is then at
+// most 2^8, which costs nothing in a floating format), so that most steps only look whether it has to.
+constexpr float kSlack = 8.0f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // What every kernel of the attention needs to know.  q, k, v and their gradients have pixels `stride` values apart; out and its
@@ -65,6 +68,24 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
+// Two fp32 values in one register pair, and arithmetic on both at a time.
+using Two = unsigned long long;
+__device__ __forceinline__ Two two(float x, float y) {
+    Two d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(x), "f"(y));
+    return d;
+}
+__device__ __forceinline__ void apart(Two v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+    Two d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 __device__ __forceinline__ float2 lds2(uint32_t addr) {
     float2 v;
     asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr));
@@ -90,7 +111,8 @@ template <typename T> __device__ __forceinline__ void stage_table(const Maps<T>&
 // ---- fp32: CUDA cores -----------------------------------------------------------------------------------------------------
 // A thread has Q queries (their channels, accumulators, running maxima and sums in registers); the block's keys and values are
 // staged kKeys at a time as rows of D channels, which all threads read at the same address.  D: d rounded up, the rest is zero.
-// Bound: the FP32 pipe, 2 D multiply-adds per pair of query and key next to about 10 other instructions.
+// Bound: the FP32 pipe, 2 D multiply-adds per pair of query and key (two at a time: they issue in half the slots, at the same rate)
+// next to about 10 other instructions.
 namespace f32 {
 constexpr int kThreads = 128, kKeys = 32, kStep = 8;
 
@@ -139,17 +161,20 @@ forward(Maps<float> m, int tiles, float* __restrict__ out, float* __restrict__ l
     if (first >= n) return;
     stage_table(m, head, table);
     const float c = m.scale * kLog2e;
-    float q[Q][D], acc[Q][D], top[Q], sum[Q];
+    const float slack = kSlack / c;
+    Two q[Q][D / 2], acc[Q][D / 2];                // pairs of channels
+    float limit[Q], off[Q], sum[Q];                // p = 2^(c s + off); the row's base moves where a score is above the limit
     int at[Q];                                     // A(i): offset of key j is A(i) - B(j)
 #pragma unroll
     for (int a = 0; a < Q; ++a) {
         const int i = min(first + a * (int)blockDim.x + (int)threadIdx.x, n - 1);   // spare threads repeat the last query
-        load_row<D>(m.q + pixel_of(m, w, i) * m.stride + (long long)head * m.d, m.d, q[a]);
+        float row[D];
+        load_row<D>(m.q + pixel_of(m, w, i) * m.stride + (long long)head * m.d, m.d, row);
         const int y = i / w.w;
         at[a] = (y + m.wh - 1) * pitch + i - y * w.w + m.ww - 1;
-        top[a] = -INFINITY; sum[a] = 0.0f;
+        limit[a] = -INFINITY; sum[a] = off[a] = 0.0f;
 #pragma unroll
-        for (int x = 0; x < D; ++x) acc[a][x] = 0.0f;
+        for (int x = 0; x < D / 2; ++x) { q[a][x] = two(row[2 * x], row[2 * x + 1]); acc[a][x] = two(0.0f, 0.0f); }
     }
     for (int key = 0; key < n; key += kKeys) {
         __syncthreads();
@@ -166,53 +191,55 @@ forward(Maps<float> m, int tiles, float* __restrict__ out, float* __restrict__ l
 #pragma unroll
             for (int u = 0; u < kStep; ++u) {
                 const int b = bs[r + u];
-                const float4* kr = reinterpret_cast<const float4*>(ks + (r + u) * D);
+                const ulonglong2* kr = reinterpret_cast<const ulonglong2*>(ks + (r + u) * D);
+                Two d[Q];
 #pragma unroll
-                for (int a = 0; a < Q; ++a) s[a][u] = table[at[a] - b];
+                for (int a = 0; a < Q; ++a) d[a] = two(table[at[a] - b], 0.0f);
 #pragma unroll
                 for (int x = 0; x < D / 4; ++x) {
-                    const float4 k4 = kr[x];
+                    const ulonglong2 k4 = kr[x];
 #pragma unroll
-                    for (int a = 0; a < Q; ++a) {
-                        s[a][u] = fmaf(q[a][4 * x], k4.x, s[a][u]);
-                        s[a][u] = fmaf(q[a][4 * x + 1], k4.y, s[a][u]);
-                        s[a][u] = fmaf(q[a][4 * x + 2], k4.z, s[a][u]);
-                        s[a][u] = fmaf(q[a][4 * x + 3], k4.w, s[a][u]);
-                    }
+                    for (int a = 0; a < Q; ++a) { d[a] = fma2(q[a][2 * x], k4.x, d[a]); d[a] = fma2(q[a][2 * x + 1], k4.y, d[a]); }
                 }
-                if (r + u >= keys)
 #pragma unroll
-                    for (int a = 0; a < Q; ++a) s[a][u] = -INFINITY;
+                for (int a = 0; a < Q; ++a) {
+                    float x, y;
+                    apart(d[a], x, y);
+                    s[a][u] = r + u < keys ? x + y : -INFINITY;
+                }
             }
 #pragma unroll
             for (int a = 0; a < Q; ++a) {
-                float t = top[a];
+                float high = s[a][0];
 #pragma unroll
-                for (int u = 0; u < kStep; ++u) t = fmaxf(t, s[a][u]);
-                const float base = t == -INFINITY ? 0.0f : t * c, old = ex2(fmaf(top[a], c, -base));   // first step: 2^-inf = 0
-                top[a] = t;
-                sum[a] *= old;
+                for (int u = 1; u < kStep; ++u) high = fmaxf(high, s[a][u]);
+                if (high > limit[a]) {
+                    const float top = limit[a] - slack, to = -high * c, old = top == -INFINITY ? 0.0f : ex2(to - off[a]);
+                    limit[a] = high + slack;
+                    off[a] = to;
+                    sum[a] *= old;
 #pragma unroll
-                for (int x = 0; x < D; ++x) acc[a][x] *= old;
+                    for (int x = 0; x < D / 2; ++x) acc[a][x] = mul2(acc[a][x], two(old, old));
+                }
+                float part = 0.0f;
 #pragma unroll
                 for (int u = 0; u < kStep; ++u) {
-                    s[a][u] = ex2(fmaf(s[a][u], c, -base));
-                    sum[a] += s[a][u];
+                    s[a][u] = ex2(fmaf(s[a][u], c, off[a]));
+                    part += s[a][u];
                 }
+                sum[a] += part;
             }
 #pragma unroll
             for (int u = 0; u < kStep; ++u) {
-                const float4* vr = reinterpret_cast<const float4*>(vs + (r + u) * D);
+                const ulonglong2* vr = reinterpret_cast<const ulonglong2*>(vs + (r + u) * D);
+                Two p[Q];
+#pragma unroll
+                for (int a = 0; a < Q; ++a) p[a] = two(s[a][u], s[a][u]);
 #pragma unroll
                 for (int x = 0; x < D / 4; ++x) {
-                    const float4 v4 = vr[x];
+                    const ulonglong2 v4 = vr[x];
 #pragma unroll
-                    for (int a = 0; a < Q; ++a) {
-                        acc[a][4 * x] = fmaf(s[a][u], v4.x, acc[a][4 * x]);
-                        acc[a][4 * x + 1] = fmaf(s[a][u], v4.y, acc[a][4 * x + 1]);
-                        acc[a][4 * x + 2] = fmaf(s[a][u], v4.z, acc[a][4 * x + 2]);
-                        acc[a][4 * x + 3] = fmaf(s[a][u], v4.w, acc[a][4 * x + 3]);
-                    }
+                    for (int a = 0; a < Q; ++a) { acc[a][2 * x] = fma2(p[a], v4.x, acc[a][2 * x]); acc[a][2 * x + 1] = fma2(p[a], v4.y, acc[a][2 * x + 1]); }
                 }
             }
         }
@@ -225,18 +252,24 @@ forward(Maps<float> m, int tiles, float* __restrict__ out, float* __restrict__ l
         const float inv = sum[a] == 0.0f ? 0.0f : 1.0f / sum[a];
         float* o = out + (pixel * m.heads + head) * m.d;
         const bool wide = m.d % 4 == 0;
-        if (wide) {
 #pragma unroll
-            for (int x = 0; x < D; x += 4)
-                if (x < m.d) *reinterpret_cast<float4*>(o + x) = make_float4(acc[a][x] * inv, acc[a][x + 1] * inv, acc[a][x + 2] * inv, acc[a][x + 3] * inv);
-        } else {
-#pragma unroll
-            for (int x = 0; x < D; ++x)
-                if (x < m.d) o[x] = acc[a][x] * inv;
+        for (int x = 0; x < D; x += 4) {
+            float4 v;
+            apart(acc[a][x / 2], v.x, v.y);
+            apart(acc[a][x / 2 + 1], v.z, v.w);
+            v.x *= inv; v.y *= inv; v.z *= inv; v.w *= inv;
+            if (wide) {
+                if (x < m.d) *reinterpret_cast<float4*>(o + x) = v;
+            } else {
+                if (x < m.d) o[x] = v.x;
+                if (x + 1 < m.d) o[x + 1] = v.y;
+                if (x + 2 < m.d) o[x + 2] = v.z;
+                if (x + 3 < m.d) o[x + 3] = v.w;
+            }
         }
         if (lse) {
             const long long hw = (long long)m.H * m.W;
-            lse[((long long)w.b * m.heads + head) * hw + pixel - w.b * hw] = sum[a] == 0.0f ? -INFINITY : fmaf(top[a], m.scale, logf(sum[a]));
+            lse[((long long)w.b * m.heads + head) * hw + pixel - w.b * hw] = sum[a] == 0.0f ? -INFINITY : fmaf(off[a], -kLn2, logf(sum[a]));
         }
     }
 }
@@ -252,7 +285,6 @@ constexpr int kKeys = 128, kMaxWarps = 8;          // keys of a staged tile
 __host__ __device__ constexpr int row_tiles(int D) { return D <= 32 ? 2 : 1; }   // tiles of 16 queries of a warp
 __host__ __device__ constexpr int blocks_of(int D) { return D <= 16 ? 3 : 2; }      // on an SM
 __host__ __device__ constexpr int step_of(int D) { return D <= 16 ? 16 : 32; }      // keys of a step
-constexpr float kSlack = 8.0f;                     // a row's base follows its maximum where that is 2^8 above
 
 // The table in shared memory backwards, so that neighbouring keys read upwards, with rows of 2 ww entries: entry (key j, query i) is at
 // B(j) - A(i) + const, and in a window of even width the pair of keys that a lane holds starts at a place whose parity is
@@ -431,8 +463,6 @@ forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse
         load_operand<KC>(m.q + (w.pixel + (long long)y * m.W + x) * m.stride + head_off, m.d, t, r & 1, q[r >> 1]);
     }
     const float c = m.scale * kLog2e;
-    // A row's powers are 2^(c s - base).  The base is the row's first maximum and moves only when one is kSlack above it (p is then at
-    // most 2^8, which costs nothing in a floating format), so that most steps only look whether any row of the warp has to move.
     const float slack = kSlack / c;
     float o[MT][ON][4], limit[R], off[R], sum[R];
 #pragma unroll

@@ -70,33 +70,48 @@ template <int D> struct Lane {                     // a thread's share of a row
     static __device__ __forceinline__ int row() { return threadIdx.x / S; }
     static __device__ __forceinline__ int first() { return threadIdx.x % S * N; }
     static __device__ __forceinline__ int rows() { return blockDim.x / S; }
-    static __device__ __forceinline__ void load(const float* __restrict__ src, int d, float* f) {
+    // Pairs of channels, two multiply-adds at a time.
+    static __device__ __forceinline__ void load(const float* __restrict__ src, int d, Two* f) {
 #pragma unroll
-        for (int c = 0; c < N; ++c) f[c] = first() + c < d ? src[first() + c] : 0.0f;
+        for (int c = 0; c < N; c += 2) f[c / 2] = two(first() + c < d ? src[first() + c] : 0.0f, first() + c + 1 < d ? src[first() + c + 1] : 0.0f);
     }
-    static __device__ __forceinline__ void store(float* __restrict__ dst, int d, const float* f, float by) {
+    static __device__ __forceinline__ void clear(Two* f) {
 #pragma unroll
-        for (int c = 0; c < N; ++c)
-            if (first() + c < d) dst[first() + c] = f[c] * by;
+        for (int c = 0; c < N / 2; ++c) f[c] = two(0.0f, 0.0f);
     }
-    static __device__ __forceinline__ float dot(const float* f, const float* row, float sum) {
-        const float4* r = reinterpret_cast<const float4*>(row + first());
+    static __device__ __forceinline__ void store(float* __restrict__ dst, int d, const Two* f, float by) {
+#pragma unroll
+        for (int c = 0; c < N; c += 2) {
+            float x, y;
+            apart(f[c / 2], x, y);
+            if (first() + c < d) dst[first() + c] = x * by;
+            if (first() + c + 1 < d) dst[first() + c + 1] = y * by;
+        }
+    }
+    static __device__ __forceinline__ float dot(const Two* f, const float* row) {
+        const ulonglong2* r = reinterpret_cast<const ulonglong2*>(row + first());
+        Two s0 = two(0.0f, 0.0f), s1 = s0;
 #pragma unroll
         for (int c = 0; c < N / 4; ++c) {
-            const float4 v = r[c];
-            sum = fmaf(f[4 * c], v.x, sum); sum = fmaf(f[4 * c + 1], v.y, sum);
-            sum = fmaf(f[4 * c + 2], v.z, sum); sum = fmaf(f[4 * c + 3], v.w, sum);
+            const ulonglong2 v = r[c];
+            s0 = fma2(f[2 * c], v.x, s0);
+            s1 = fma2(f[2 * c + 1], v.y, s1);
         }
+        float a, b, x, y;
+        apart(s0, a, b);
+        apart(s1, x, y);
+        float sum = (a + b) + (x + y);
         if (S == 2) sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         return sum;
     }
-    static __device__ __forceinline__ void add(float* f, const float* row, float by) {
-        const float4* r = reinterpret_cast<const float4*>(row + first());
+    static __device__ __forceinline__ void add(Two* f, const float* row, float by) {
+        const ulonglong2* r = reinterpret_cast<const ulonglong2*>(row + first());
+        const Two b = two(by, by);
 #pragma unroll
         for (int c = 0; c < N / 4; ++c) {
-            const float4 v = r[c];
-            f[4 * c] = fmaf(by, v.x, f[4 * c]); f[4 * c + 1] = fmaf(by, v.y, f[4 * c + 1]);
-            f[4 * c + 2] = fmaf(by, v.z, f[4 * c + 2]); f[4 * c + 3] = fmaf(by, v.w, f[4 * c + 3]);
+            const ulonglong2 v = r[c];
+            f[2 * c] = fma2(b, v.x, f[2 * c]);
+            f[2 * c + 1] = fma2(b, v.y, f[2 * c + 1]);
         }
     }
 };
@@ -120,11 +135,11 @@ grad_kv(Maps<float> m, Grads<float> g, int tiles) {
     const int j = min(first + L::row(), n - 1);
     const long long pixel = pixel_of(m, w, j), at = pixel * m.stride + (long long)head * m.d;
     const int b = j / w.w * pitch + j % w.w;
-    float k[L::N], v[L::N], gk[L::N], gv[L::N];
+    Two k[L::N / 2], v[L::N / 2], gk[L::N / 2], gv[L::N / 2];
     L::load(m.k + at, m.d, k);
     L::load(m.v + at, m.d, v);
-#pragma unroll
-    for (int x = 0; x < L::N; ++x) gk[x] = gv[x] = 0.0f;
+    L::clear(gk);
+    L::clear(gv);
     for (int row = 0; row < n; row += kRows) {
         __syncthreads();
         stage_rows<D>(m, m.q, m.stride, w, head, row, qs);
@@ -139,8 +154,8 @@ grad_kv(Maps<float> m, Grads<float> g, int tiles) {
         __syncthreads();
         const int rows = min(kRows, n - row);
         for (int r = 0; r < rows; ++r) {
-            const float s = L::dot(k, qs + r * D, 0.0f) + table[as[r] - b];
-            const float p = ex2(fmaf(s, c, base[r])), dp = L::dot(v, gs + r * D, 0.0f);
+            const float s = L::dot(k, qs + r * D) + table[as[r] - b];
+            const float p = ex2(fmaf(s, c, base[r])), dp = L::dot(v, gs + r * D);
             L::add(gv, gs + r * D, p);
             L::add(gk, qs + r * D, p * (dp + dots[r]));
         }
@@ -177,11 +192,10 @@ grad_q(Maps<float> m, Grads<float> g, int tiles) {
         const long long pixel = pixel_of(m, w, i), at = pixel * m.stride + (long long)head * m.d, row = row_of(m, w, head, pixel);
         const int a = (i / w.w + m.wh - 1) * pitch + i % w.w + m.ww - 1;
         const float base = own ? g.bases[row] : -INFINITY, dot = own ? g.dots[row] : 0.0f;
-        float q[L::N], go[L::N], gq[L::N];
+        Two q[L::N / 2], go[L::N / 2], gq[L::N / 2];
         L::load(m.q + at, m.d, q);
         L::load(g.go + (pixel * m.heads + head) * m.d, m.d, go);
-#pragma unroll
-        for (int x = 0; x < L::N; ++x) gq[x] = 0.0f;
+        L::clear(gq);
         for (int key = 0; key < n; key += kRows) {
             __syncthreads();
             stage_rows<D>(m, m.k, m.stride, w, head, key, ks);
@@ -194,8 +208,8 @@ grad_q(Maps<float> m, Grads<float> g, int tiles) {
             const int rows = min(kRows, n - key);
             for (int r = 0; r < rows; ++r) {
                 const int o = a - bs[r];
-                const float s = L::dot(q, ks + r * D, 0.0f) + table[o];
-                const float p = ex2(fmaf(s, c, base)), ds = p * (L::dot(go, vs + r * D, 0.0f) + dot);
+                const float s = L::dot(q, ks + r * D) + table[o];
+                const float p = ex2(fmaf(s, c, base)), ds = p * (L::dot(go, vs + r * D) + dot);
                 L::add(gq, ks + r * D, ds);
                 if (g.part && own && L::first() == 0) mine[o] += ds;
                 __syncwarp();                      // the next key's offsets are the neighbours'
