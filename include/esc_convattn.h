@@ -388,7 +388,7 @@ int esc_conv_fuse_backward(const void* cat, const void* grad_out, int B, int C, 
  *   table    [n_buckets, heads], the type of the call; -inf masks
  *   bucket   [(2 win_h - 1)(2 win_w - 1)] int32 (device), the bucket of every offset; NULL: every offset has its own row of the
  *            table (n_buckets has to be their number).  An entry outside [0, n_buckets) gives no bias and takes no gradient.
- *   (2 win_h - 1)(2 win_w - 1) is at most 16384 (windows of 64 x 64, sequences of 8192 with win_h = 1).
+ *   (2 win_h - 1)(2 win_w - 1) is at most 16384 (windows of 64 x 64, sequences of 8192 with win_h = 1), else ESC_ERR_UNSUPPORTED.
  *
  * esc_relpos_bias_forward writes it as a matrix [heads, N, N] with N = win_h win_w (16-byte aligned), for an attention that takes
  * one.  esc_relpos_bias_backward sums a gradient of that shape into grad_table [n_buckets, heads], fp32; a bucket that no
@@ -473,7 +473,7 @@ int esc_adamw_plan_init(int n_tensors, const long long* sizes, void* const* para
  *   scalars  device, 4 floats as esc_adamw_scalars gives them, or NULL.  They replace step, lr, weight_decay and grad_scale in
  *            the kernel: a captured graph takes what they hold when it is replayed, where the arguments would stay what they were.
  *   skip     device int or NULL: not zero, and the call changes nothing (gradients that overflowed)
- * Two steps of one plan, or two plans that share tensors, must not overlap on the GPU.
+ * Two steps of one plan, or two plans that share tensors, must not overlap on the GPU; no tensor may be in a list twice.
  */
 int esc_adamw_step(const void* plan, long long n_chunks, int param_dtype, int grad_dtype, int states, long long step, double lr,
                    double beta1, double beta2, double eps, double weight_decay, double grad_scale, const float* scalars,
@@ -554,7 +554,7 @@ int esc_convattn_last_tile_width(void);
  * Returns ESC_ERR_UNSUPPORTED for any other value.  For tests and tuning. */
 int esc_convattn_set_tile_width(int tile_width);
 
-/* Number of kernels the last forward / stage call on this thread launched. */
+/* Number of kernels the last forward / stage / backward / attention / bias / AdamW call on this thread launched. */
 int esc_convattn_last_launches(void);
 
 const char* esc_status_string(int status);

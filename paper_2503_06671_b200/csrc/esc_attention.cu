@@ -144,13 +144,19 @@ Tiling tile_rows(int tokens, int most_threads, int per_thread, int lanes) {
     return {(tokens + per_tile - 1) / per_tile, threads};
 }
 
-template <int D> int forward_f32(const Call& c, void* out, float* lse, cudaStream_t st) {
+template <int D, int Q> int forward_f32_q(const Call& c, void* out, float* lse, cudaStream_t st) {
     using namespace wa::f32;
-    const Tiling t = tile_rows(c.tokens(), kThreads, queries_of(D), 1);
+    const Tiling t = tile_rows(c.tokens(), kThreads, Q, 1);
     const size_t smem = (size_t)(2 * kKeys * D + kKeys + rp::offsets_of(c.wh, c.ww)) * sizeof(float);
-    ESC_TRY(allow_smem(forward<D>, smem));
-    forward<D><<<(unsigned)(c.windows() * c.heads * t.tiles), t.threads, smem, st>>>(maps_of<float>(c), t.tiles, static_cast<float*>(out), lse);
+    ESC_TRY(allow_smem(forward<D, Q>, smem));
+    forward<D, Q><<<(unsigned)(c.windows() * c.heads * t.tiles), t.threads, smem, st>>>(maps_of<float>(c), t.tiles, static_cast<float*>(out), lse);
     return launched();
+}
+// Two queries a thread halve the reads of keys and values; not where that leaves the SMs fewer than 16 warps each, or a thread too many channels.
+// 427x240, windows of 24, 4 heads of 16: 593 us with two, 637 with one; 4 x 64x64, 3 heads: 150 with two, 112 with one.
+template <int D> int forward_f32(const Call& c, void* out, float* lse, cudaStream_t st) {
+    const bool many = c.windows() * c.heads * c.tokens() >= 2LL * 16 * 32 * abi::sm_count();
+    return D <= 16 && many ? forward_f32_q<D, D <= 16 ? 2 : 1>(c, out, lse, st) : forward_f32_q<D, 1>(c, out, lse, st);
 }
 
 template <int D, bool TWICE> int forward_bf16_t(const Call& c, void* out, float* lse, cudaStream_t st) {
@@ -167,11 +173,22 @@ template <int D> int forward_bf16(const Call& c, void* out, float* lse, cudaStre
     return wa::tc::Smem<D>::bytes(wa::tc::Bias(c.wh, c.ww), true) <= 112 * 1024 ? forward_bf16_t<D, true>(c, out, lse, st) : forward_bf16_t<D, false>(c, out, lse, st);
 }
 
-// Groups of a grid whose blocks add up sums for the table's gradient: about as many blocks as the SMs hold at two each.
-int table_groups(const Call& c) {
-    const long long most = std::max(1LL, 2LL * abi::sm_count() / c.heads);
-    return (int)std::min(most, c.windows() * ((c.tokens() + 31) / 32));
+// The fp32 kernel that adds up sums for the table's gradient: one copy of the offsets per warp beside the table and the staged rows of D
+// channels.  Its groups: as many blocks as the SMs hold, at most four each.
+struct SumsPlan { Tiling t; size_t smem; int groups; };
+SumsPlan sums_plan(const Call& c, int D, bool sums) {
+    using namespace wa::bwd::f32;
+    const size_t offsets = (size_t)rp::offsets_of(c.wh, c.ww) * sizeof(float), rest = (2 * kRows * D + kRows) * sizeof(float);
+    const int warps = sums ? (int)std::min<size_t>(kThreads / 32, (kMostSmem - rest) / offsets - 1) : kThreads / 32;
+    SumsPlan p;
+    p.t = tile_rows(c.tokens(), warps * 32, 1, lanes_of(D));
+    p.smem = rest + offsets * (sums ? 1 + p.t.threads / 32 : 1);
+    const long long units = c.windows() * p.t.tiles, per_sm = std::max<long long>(1, std::min<long long>(4, kMostSmem / (p.smem + 1024)));
+    p.groups = (int)std::min<long long>(units, sums ? std::max(1LL, per_sm * abi::sm_count() / c.heads) : 0x7fffffff / c.heads);
+    return p;
 }
+int padded(int d) { return d <= 16 ? 16 : d <= 32 ? 32 : 64; }
+int table_groups(const Call& c) { return sums_plan(c, padded(c.d), true).groups; }
 
 // And of the tensor-core kernel, whose blocks have a tile of keys each: the tiles of queries, then the windows are dealt to as many as fill
 // two rounds of two blocks per SM.
@@ -207,18 +224,14 @@ template <int D> int backward_f32(const Call& c, wa::bwd::Grads<float> g, cudaSt
     const wa::Maps<float> m = maps_of<float>(c);
     const size_t offsets = (size_t)rp::offsets_of(c.wh, c.ww);
     const Tiling t = tile_rows(c.tokens(), kThreads, 1, lanes_of(D));
-    size_t smem = (2 * kRows * D + 3 * kRows + offsets) * sizeof(float);
+    const size_t smem = (2 * kRows * D + 3 * kRows + offsets) * sizeof(float);
     ESC_TRY(allow_smem(grad_kv<D>, smem));
     grad_kv<D><<<(unsigned)(c.windows() * c.heads * t.tiles), t.threads, smem, st>>>(m, g, t.tiles);
     ESC_TRY(launched());
-    // one copy of the offsets per warp beside the table
-    const size_t rest = (2 * kRows * D + kRows) * sizeof(float), room = 220 * 1024 - rest;
-    const int warps = g.part ? (int)std::min<size_t>(kThreads / 32, room / (offsets * sizeof(float)) - 1) : kThreads / 32;
-    const Tiling u = tile_rows(c.tokens(), warps * 32, 1, lanes_of(D));
-    smem = rest + offsets * sizeof(float) * (g.part ? 1 + u.threads / 32 : 1);
-    if (!g.part) g.groups = (int)std::min<long long>(c.windows() * u.tiles, 0x7fffffff / c.heads);
-    ESC_TRY(allow_smem(grad_q<D>, smem));
-    grad_q<D><<<(unsigned)(g.groups * c.heads), u.threads, smem, st>>>(m, g, u.tiles);
+    const SumsPlan p = sums_plan(c, D, g.part != nullptr);
+    g.groups = p.groups;
+    ESC_TRY(allow_smem(grad_q<D>, p.smem));
+    grad_q<D><<<(unsigned)(g.groups * c.heads), p.t.threads, p.smem, st>>>(m, g, p.t.tiles);
     return launched();
 }
 

@@ -114,9 +114,8 @@ template <typename T> __device__ __forceinline__ void stage_table(const Maps<T>&
 // Bound: the FP32 pipe, 2 D multiply-adds per pair of query and key (two at a time: they issue in half the slots, at the same rate)
 // next to about 10 other instructions.
 namespace f32 {
-constexpr int kThreads = 128, kKeys = 32, kStep = 8;
+constexpr int kThreads = 128, kKeys = 32, kStep = 4;
 
-__host__ __device__ constexpr int queries_of(int D) { return D <= 16 ? 2 : 1; }
 
 template <int D> __device__ __forceinline__ void load_row(const float* __restrict__ src, int d, float* f) {
 #pragma unroll
@@ -145,10 +144,9 @@ __device__ __forceinline__ void stage_rows(const Maps<float>& m, const float* __
     }
 }
 
-template <int D>
+template <int D, int Q>
 __global__ void __launch_bounds__(kThreads)
 forward(Maps<float> m, int tiles, float* __restrict__ out, float* __restrict__ lse) {
-    constexpr int Q = queries_of(D);
     extern __shared__ __align__(16) float smem[];
     float *ks = smem, *vs = ks + kKeys * D;
     int* bs = reinterpret_cast<int*>(vs + kKeys * D);

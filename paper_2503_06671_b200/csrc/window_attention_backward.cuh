@@ -152,12 +152,20 @@ grad_kv(Maps<float> m, Grads<float> g, int tiles) {
             dots[r] = i < n ? g.dots[p] : 0.0f;
         }
         __syncthreads();
-        const int rows = min(kRows, n - row);
-        for (int r = 0; r < rows; ++r) {
-            const float s = L::dot(k, qs + r * D) + table[as[r] - b];
-            const float p = ex2(fmaf(s, c, base[r])), dp = L::dot(v, gs + r * D);
-            L::add(gv, gs + r * D, p);
-            L::add(gk, qs + r * D, p * (dp + dots[r]));
+        // rows behind the last have p = 0; four at a time, so that their sums of products run side by side
+#pragma unroll 1
+        for (int r = 0; r < kRows; r += 4) {
+            float p[4], ds[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                p[u] = ex2(fmaf(L::dot(k, qs + (r + u) * D) + table[as[r + u] - b], c, base[r + u]));
+                ds[u] = p[u] * (L::dot(v, gs + (r + u) * D) + dots[r + u]);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                L::add(gv, gs + (r + u) * D, p[u]);
+                L::add(gk, qs + (r + u) * D, ds[u]);
+            }
         }
     }
     if (first + L::row() < n) {
@@ -169,7 +177,7 @@ grad_kv(Maps<float> m, Grads<float> g, int tiles) {
 // Also the sums for the table's gradient: a block keeps one copy of the head's offsets for each warp over all tiles of queries that
 // it takes.  At one step the lanes of a warp have different queries and one key, so all their offsets differ.
 template <int D>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, D <= 16 ? 4 : 2)
 grad_q(Maps<float> m, Grads<float> g, int tiles) {
     using L = Lane<D>;
     extern __shared__ __align__(16) float smem[];
@@ -206,13 +214,25 @@ grad_q(Maps<float> m, Grads<float> g, int tiles) {
             }
             __syncthreads();
             const int rows = min(kRows, n - key);
-            for (int r = 0; r < rows; ++r) {
-                const int o = a - bs[r];
-                const float s = L::dot(q, ks + r * D) + table[o];
-                const float p = ex2(fmaf(s, c, base)), ds = p * (L::dot(go, vs + r * D) + dot);
-                L::add(gq, ks + r * D, ds);
-                if (g.part && own && L::first() == 0) mine[o] += ds;
-                __syncwarp();                      // the next key's offsets are the neighbours'
+#pragma unroll 1
+            for (int r = 0; r < rows; r += 4) {
+                float ds[4];
+                int o[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    o[u] = a - bs[r + u];
+                    const float p = r + u < rows ? ex2(fmaf(L::dot(q, ks + (r + u) * D) + table[o[u]], c, base)) : 0.0f;
+                    ds[u] = p * (L::dot(go, vs + (r + u) * D) + dot);
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) L::add(gq, ks + (r + u) * D, ds[u]);
+                if (g.part) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        if (own && L::first() == 0 && r + u < rows) mine[o[u]] += ds[u];
+                        __syncwarp();              // the next key's offsets are the neighbours'
+                    }
+                }
             }
         }
         if (own) L::store(g.g_q + at, m.d, gq, m.scale);

@@ -46,6 +46,9 @@ SHAPES = [
     (1, 1, 700, 1, 16, 1, 333),      # two whole windows and a rest of 34
     (1, 9, 3, 2, 1, 4, 2),           # one channel
     (1, 6, 6, 9, 3, 3, 3),           # many narrow heads: nothing is aligned
+    (1, 40, 66, 1, 64, 64, 64),      # the largest square window: little shared memory is left beside its table
+    (1, 1, 900, 1, 16, 1, 8192),     # the longest sequence's table
+    (1, 3, 37, 2, 20, 64, 2),        # tall narrow windows
 ]
 
 
@@ -107,6 +110,13 @@ def compare(got, x, shape, scale, dtype):
 def test_attention(pkg, shape, dtype):
     x = inputs(shape, dtype, sum(shape))
     compare(run(pkg, x, shape, shape[4] ** -0.5), x, shape, shape[4] ** -0.5, dtype)
+
+
+def test_many_windows_of_one_block(pkg):
+    """More windows than a block of the table's gradient lists at a time, whole ones and cut ones: 300 heads leave a block all of them."""
+    shape = (1, 8 * 15 + 3, 8 * 10 + 5, 300, 2, 8, 8)
+    x = inputs(shape, "bf16", 21)
+    compare(run(pkg, x, shape, 0.7), x, shape, 0.7, "bf16")
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
