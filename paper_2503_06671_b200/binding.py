@@ -495,20 +495,33 @@ def esc_convattn_device_status(workspace, stream=None) -> int:
 _HERE = contextlib.nullcontext()
 
 
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+def _stream_address(stream):
+    import torch
+
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
 def _on_device(first, *others):
     """The tensors' one device, made current for the call that follows: kernels run where the data are."""
     import torch
 
     device = first.device
-    if device.type != "cuda" or any(t is not None and t.device != device for t in others):
-        raise ValueError("the tensors of a call have to be on one CUDA device")
+    for t in others:
+        if t is not None and t.device != device:
+            raise ValueError("the tensors of a call have to be on one CUDA device")
+    if device.type != "cuda":
+        raise ValueError("the tensors of a call have to be on a CUDA device")
     return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
 
 def _dense(name, t, shape, dtype):
     if t is None:
         return
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{name} has to be a contiguous {tuple(shape)} tensor of {dtype}, not {tuple(t.shape)} of {t.dtype}")
 
 
@@ -528,7 +541,7 @@ def esc_relpos_bias_forward(table, bucket, win_h, win_w, bias, stream=None):
     _dense("bias", bias, (heads, win_h * win_w, win_h * win_w), table.dtype)
     _bucket_arg(bucket, win_h, win_w)
     with _on_device(table, bucket, bias):
-        _check(lib().esc_relpos_bias_forward(_ptr(table), _ptr(bucket), n, heads, win_h, win_w, _ptr(bias), _dtype_code(table), _stream(stream)),
+        _check(lib().esc_relpos_bias_forward(_address(table), _address(bucket), n, heads, win_h, win_w, _address(bias), _dtype_code(table), _stream_address(stream)),
                "esc_relpos_bias_forward")
     return bias
 
@@ -557,27 +570,33 @@ def esc_relpos_bias_backward(grad_bias, bucket, win_h, win_w, grad_table, worksp
     with _on_device(grad_bias, bucket, grad_table, workspace):
         if workspace is None:
             workspace = new_relpos_bias_workspace(heads, win_h, win_w)
-        _check(lib().esc_relpos_bias_backward(_ptr(grad_bias), _ptr(bucket), n, heads, win_h, win_w, _ptr(grad_table), _dtype_code(grad_bias),
-                                              _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+        _check(lib().esc_relpos_bias_backward(_address(grad_bias), _address(bucket), n, heads, win_h, win_w, _address(grad_table), _dtype_code(grad_bias),
+                                              _address(workspace), workspace.numel() * workspace.element_size(), _stream_address(stream)),
                "esc_relpos_bias_backward")
     return grad_table
 
 
-def _pixels(heads, **maps):
+def _pixel_step(t):
+    """Values between neighbouring pixels of a map [B, H, W, C]; ValueError where they are not evenly spaced, or dense in their channels."""
+    B, H, W, C = t.shape
+    b, h, w, c = t.stride()
+    step = w if W > 1 else h if H > 1 else b if B > 1 else C                # from the innermost axis that has more than one entry
+    if (C > 1 and c != 1) or (W > 1 and w != step) or (H > 1 and h != step * W) or (B > 1 and b != step * W * H):
+        raise ValueError("pixels have to be dense in their channels and evenly spaced")
+    return step
+
+
+def _pixels(heads, first, *others):
     """(B, H, W, head_dim, pixel stride) of maps [B, H, W, heads * head_dim] that are laid out alike."""
-    first = None
-    for name, t in maps.items():
-        if t.dim() != 4 or t.shape[3] % heads != 0:
-            raise ValueError(f"{name} has to be [B, H, W, heads * head_dim]")
-        B, H, W, C = (int(x) for x in t.shape)
-        # the pixels' distance: from the innermost axis that has more than one entry
-        step = t.stride(2) if W > 1 else t.stride(1) if H > 1 else t.stride(0) if B > 1 else C
-        got = (B, H, W, C // heads, int(step)), t.dtype
-        ok = (C == 1 or t.stride(3) == 1) and (W == 1 or t.stride(2) == step) and (H == 1 or t.stride(1) == step * W) and (B == 1 or t.stride(0) == step * W * H)
-        if not ok or got != (first or got):
-            raise ValueError(f"{name}: pixels have to be dense in their channels, evenly spaced, and alike in all of {', '.join(maps)}")
-        first = got
-    return first[0]
+    shape, strides, dtype = first.shape, first.stride(), first.dtype
+    if len(shape) != 4 or heads < 1 or shape[3] % heads != 0:
+        raise ValueError("the maps have to be [B, H, W, heads * head_dim]")
+    step = _pixel_step(first)
+    for t in others:
+        if t.shape != shape or t.dtype != dtype or (t.stride() != strides and _pixel_step(t) != step):
+            raise ValueError("q, k, v and their gradients have to be of one shape and type, with pixels alike")
+    B, H, W, C = shape
+    return B, H, W, C // heads, step
 
 
 def esc_window_attention_forward(q, k, v, heads, win_h, win_w, table, bucket, scale, out, lse=None, stream=None):
@@ -587,15 +606,15 @@ def esc_window_attention_forward(q, k, v, heads, win_h, win_w, table, bucket, sc
     [n_buckets, heads] with the bucket of every offset (None: one row per offset), or None for no bias."""
     import torch
 
-    B, H, W, d, step = _pixels(heads, q=q, k=k, v=v)
+    B, H, W, d, step = _pixels(heads, q, k, v)
     _dense("out", out, (B, H, W, heads * d), q.dtype)
     _dense("lse", lse, (B, heads, H, W), torch.float32)
     n = 0 if table is None else int(table.shape[0])
     _dense("table", table, (n, heads), q.dtype)
     _bucket_arg(bucket, win_h, win_w)
     with _on_device(q, k, v, table, bucket, out, lse):
-        _check(lib().esc_window_attention_forward(_ptr(q), _ptr(k), _ptr(v), B, heads, d, H, W, step, win_h, win_w, _ptr(table), _ptr(bucket), n, scale,
-                                                  _ptr(out), _ptr(lse), _dtype_code(q), _stream(stream)),
+        _check(lib().esc_window_attention_forward(_address(q), _address(k), _address(v), B, heads, d, H, W, step, win_h, win_w, _address(table), _address(bucket), n, scale,
+                                                  _address(out), _address(lse), _dtype_code(q), _stream_address(stream)),
                "esc_window_attention_forward")
     return out
 
@@ -619,7 +638,7 @@ def esc_window_attention_backward(q, k, v, heads, win_h, win_w, table, bucket, s
     """Gradients of esc_window_attention_forward; grad_q, grad_k, grad_v are laid out like q, k, v."""
     import torch
 
-    B, H, W, d, step = _pixels(heads, q=q, k=k, v=v, grad_q=grad_q, grad_k=grad_k, grad_v=grad_v)
+    B, H, W, d, step = _pixels(heads, q, k, v, grad_q, grad_k, grad_v)
     _dense("out", out, (B, H, W, heads * d), q.dtype)
     _dense("grad_out", grad_out, (B, H, W, heads * d), q.dtype)
     _dense("lse", lse, (B, heads, H, W), torch.float32)
@@ -630,9 +649,9 @@ def esc_window_attention_backward(q, k, v, heads, win_h, win_w, table, bucket, s
     with _on_device(q, k, v, table, bucket, out, lse, grad_out, grad_q, grad_k, grad_v, grad_table, workspace):
         if workspace is None:
             workspace = new_window_attention_workspace(B, heads, d, H, W, win_h, win_w)
-        _check(lib().esc_window_attention_backward(_ptr(q), _ptr(k), _ptr(v), B, heads, d, H, W, step, win_h, win_w, _ptr(table), _ptr(bucket), n, scale,
-                                                   _ptr(out), _ptr(lse), _ptr(grad_out), _ptr(grad_q), _ptr(grad_k), _ptr(grad_v), _ptr(grad_table),
-                                                   _dtype_code(q), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+        _check(lib().esc_window_attention_backward(_address(q), _address(k), _address(v), B, heads, d, H, W, step, win_h, win_w, _address(table), _address(bucket), n, scale,
+                                                   _address(out), _address(lse), _address(grad_out), _address(grad_q), _address(grad_k), _address(grad_v), _address(grad_table),
+                                                   _dtype_code(q), _address(workspace), workspace.numel() * workspace.element_size(), _stream_address(stream)),
                "esc_window_attention_backward")
     return grad_q, grad_k, grad_v, grad_table
 
@@ -688,8 +707,8 @@ def esc_adamw_plan_init(params, grads, exp_avgs, exp_avg_sqs, avg_scales=None, s
         if bytes_ == 0:
             raise ValueError("invalid sizes")
         table = torch.empty(bytes_, dtype=torch.uint8, device="cuda")
-        _check(lib().esc_adamw_plan_init(n, (ctypes.c_longlong * n)(*sizes), *arrays, _dtype_code(params[0]), _dtype_code(grads[0]), states, _ptr(table), bytes_,
-                                         ctypes.byref(chunks), _stream(stream)), "esc_adamw_plan_init")
+        _check(lib().esc_adamw_plan_init(n, (ctypes.c_longlong * n)(*sizes), *arrays, _dtype_code(params[0]), _dtype_code(grads[0]), states, _address(table), bytes_,
+                                         ctypes.byref(chunks), _stream_address(stream)), "esc_adamw_plan_init")
     return AdamwPlan(table, chunks.value, _dtype_code(params[0]), _dtype_code(grads[0]), states, every)
 
 
@@ -712,5 +731,5 @@ def esc_adamw_step(plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_deca
     if skip is not None and (skip.numel() != 1 or skip.dtype != torch.int32):
         raise ValueError("skip has to be one int32")
     with _on_device(plan.table, scalars, skip):
-        _check(lib().esc_adamw_step(_ptr(plan.table), plan.n_chunks, plan.param_dtype, plan.grad_dtype, plan.states, int(step), lr, beta1, beta2, eps,
-                                    weight_decay, grad_scale, _ptr(scalars), _ptr(skip), _stream(stream)), "esc_adamw_step")
+        _check(lib().esc_adamw_step(_address(plan.table), plan.n_chunks, plan.param_dtype, plan.grad_dtype, plan.states, int(step), lr, beta1, beta2, eps,
+                                    weight_decay, grad_scale, _address(scalars), _address(skip), _stream_address(stream)), "esc_adamw_step")

@@ -31,7 +31,7 @@ __device__ __forceinline__ float table_at(const T* __restrict__ table, const int
 // are therefore staged in V planes, entry p in plane p % V: for one of its V values every lane of the warp reads the same plane, at
 // neighbouring places, and the planes' order is the row's alone.  Elsewhere a lane's piece can run over the end of a row of keys: it is
 // walked entry by entry, with a hole behind every eighth entry of the strip (`skew`) against the banks.
-// 6 x 2304 x 2304 bf16 (64 MB): 24.6 us with the walk, planes PLANES_US.
+// 6 x 2304 x 2304 bf16 (64 MB): 24.6 us with the walk, 15.6 by planes (4.1 TB/s).
 constexpr int kRows = 16, kFillThreads = 256;
 __host__ __device__ __forceinline__ int skew(int p) { return p + (p >> 3); }
 __host__ __device__ __forceinline__ int round_to(int v, int to) { return (v + to - 1) / to * to; }

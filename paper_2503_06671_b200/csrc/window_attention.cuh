@@ -275,13 +275,24 @@ forward(Maps<float> m, int tiles, float* __restrict__ out, float* __restrict__ l
 }  // namespace f32
 
 // ---- bf16: tensor cores ---------------------------------------------------------------------------------------------------
-// A warp has 32 queries (two tiles of 16) as A operands in registers; the block's keys and values pass by in staged tiles of 64.  s and
-// p never leave the registers: the accumulators of q k^T are, rounded to bf16, the A operand of p v.
+// A warp has 16 or 32 queries (tiles of 16) as A operands in registers; the block's keys and values pass by in staged tiles of 128, copied ahead.
+// s and p never leave the registers: the accumulators of q k^T, which start from the bias, are, rounded to bf16, the A operand of p v.
+// p is rounded as an operand only: out is off by at most 2^-8 of sum p |v| more; the sum that divides it is of the fp32 values.
+//
+// Bound: the exponentials, 16 a clock and SM (measured; a row's other arithmetic runs beside them), then the issue slots.  640x360,
+// windows of 32, 4 heads of 16 (0.93e9 pairs, 59 GFLOP, 118 MB): exponentials 206 us, products 103 at mma.sync's 955 multiply-adds
+// a clock and SM, bytes 18; 400 us, 8 pairs a clock and SM, 9.7 instructions each and 0.65 of them issued per clock and scheduler.
+// mma.sync and not tcgen05 because at 16 channels the products are not the limit: a kernel with s in tensor memory, a query per thread and
+// p through shared memory, two groups of 128 queries per block, took 554 us here and 580 for 48 x 48 windows of 6 heads of 32 (449).
+// Measured on the way, us: rescaling at every step 528; a base that moves seldom, places walked instead of divided 468; everything that a
+// window decides once outside the loop and three blocks an SM with steps of 16 keys 400 (two blocks, 32 keys: 445).
 namespace tc {
 using bf16 = __nv_bfloat16;
 constexpr int kKeys = 128, kMaxWarps = 8;          // keys of a staged tile
-__host__ __device__ constexpr int row_tiles(int D) { return D <= 32 ? 2 : 1; }   // tiles of 16 queries of a warp
-__host__ __device__ constexpr int blocks_of(int D) { return D <= 16 ? 3 : 2; }      // on an SM
+// Tiles of 16 queries of a warp: two halve the reads of keys and values per product.  One where that leaves SMs without work, or the registers
+// no room for more than 64 channels' worth.
+__host__ __device__ constexpr int most_tiles(int D) { return D <= 32 ? 2 : 1; }
+__host__ __device__ constexpr int blocks_of(int D, int MT) { return D <= 16 ? (MT == 1 ? 4 : 3) : 2; }   // on an SM
 __host__ __device__ constexpr int step_of(int D) { return D <= 16 ? 16 : 32; }      // keys of a step
 
 // The table in shared memory backwards, so that neighbouring keys read upwards, with rows of 2 ww entries: entry (key j, query i) is at
@@ -330,15 +341,15 @@ __device__ __forceinline__ void stage_piece(const bf16* p, uint32_t at, bool rea
         asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
     }
 }
-// ROWS rows of D channels of two tensors into a staged tile each, from the pixels (in [0, end), others give zeros) behind their first.
+// ROWS rows of D channels of two tensors into a staged tile each, from the pixels (a negative one gives zeros) behind their first.
 template <int D, int ROWS> struct Rows {
     using T = wmma16::Tile<D>;
     static __device__ __forceinline__ void stage(const bf16* __restrict__ one, long long stride1, bool wide1, uint32_t dst1, const bf16* __restrict__ two_, long long stride2,
-                                                 bool wide2, uint32_t dst2, int d, const long long* pixel, long long end = 0x7fffffffffffffffLL) {
+                                                 bool wide2, uint32_t dst2, int d, const long long* pixel) {
         for (int e = threadIdx.x; e < ROWS * T::kPieces; e += blockDim.x) {
             const int r = e / T::kPieces, c = e % T::kPieces;
             long long px = pixel[r];
-            const bool real = px >= 0 && px < end && c * 8 < d;
+            const bool real = px >= 0 && c * 8 < d;
             px = real ? px : 0;
             const int ch = real ? c * 8 : 0;
             stage_piece(one + px * stride1 + ch, dst1 + T::at(r, c), real, d - ch, wide1);
@@ -414,11 +425,11 @@ __device__ __forceinline__ void store_pair(bf16* to, int ch, int d, float u, flo
     }
 }
 
-template <int D, bool TWICE>
-__global__ void __launch_bounds__(kMaxWarps * 32, blocks_of(D))
+template <int D, bool TWICE, int MT>
+__global__ void __launch_bounds__(kMaxWarps * 32, blocks_of(D, MT))
 forward(Maps<bf16> m, int tiles, bf16* __restrict__ out, float* __restrict__ lse) {
     using namespace wmma16;
-    constexpr int KC = D / 16, kStep = step_of(D), NT = kStep / 8, ON = D / 8, MT = row_tiles(D), R = 2 * MT;          // steps along the channels, tiles of 8 keys, of 8 channels of out
+    constexpr int KC = D / 16, kStep = step_of(D), NT = kStep / 8, ON = D / 8, R = 2 * MT;          // steps along the channels, tiles of 8 keys, of 8 channels of out
     constexpr int kTile = Smem<D>::kTile;
     extern __shared__ __align__(128) unsigned char raw[];
     long long* pixels = reinterpret_cast<long long*>(raw + 4 * kTile);

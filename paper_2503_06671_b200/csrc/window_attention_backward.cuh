@@ -251,7 +251,11 @@ grad_q(Maps<float> m, Grads<float> g, int tiles) {
 // ---- bf16: tensor cores ---------------------------------------------------------------------------------------------------
 // Three kernels that each make p and dp anew from products of registers and staged tiles, so that every sum has one owner: the first
 // with rows of keys (g_k, g_v), the second with rows of queries (g_q), the third with a tile of query-key pairs that all windows pass
-// by (the table's gradient: the pairs' sums over the windows stay in registers, and go to their offsets once).
+// by (the table's gradient: the pairs' sums over the windows stay in registers, and go to their offsets once).  One pass would need g_q
+// added up across the warps and 1e9 additions to a table whose neighbouring pairs share entries; p and ds as an operand are rounded
+// to bf16 (2^-8 of each term), D is of the rounded out, the sums of ds for the table are of the fp32 values.
+// Bound: the exponentials, three times 206 us for the pairs of 64 patches of 64x64 in windows of 32, 4 heads of 16 (1.07e9: 238 each),
+// and the issue slots.  There: 625 + 502 + 630 us (rows of keys, of queries, table) beside 474 of the forward pass.
 namespace tc {
 using namespace winatt::tc;
 constexpr int kCols = 128;                                          // staged columns: queries for rows of keys, keys for rows of queries

@@ -150,6 +150,32 @@ def test_no_bias(pkg, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+def test_no_gradient_of_the_table_and_two_streams(pkg, dtype):
+    """Without grad_table the others are the same bits; two backward calls at once on two streams, each with its workspace."""
+    shape = (2, 30, 40, 2, 16, 12, 16)
+    B, H, W, heads, d, wh, ww = shape
+    x = inputs(shape, dtype, 30)
+    want = run(pkg, x, shape, 0.25)
+    q, k, v, go, table = (x[n].cuda() for n in ("q", "k", "v", "go", "table"))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    torch.cuda.synchronize()
+    for i, s in enumerate(streams):
+        with torch.cuda.stream(s):
+            g = [torch.full_like(q, 7.0) for _ in range(3)]
+            gt = torch.full_like(table, 7.0) if i else None
+            out, lse = torch.empty_like(q), torch.empty(B, heads, H, W, device="cuda")
+            for _ in range(3):
+                pkg.esc_window_attention_forward(q, k, v, heads, wh, ww, table, None, 0.25, out, lse)
+                pkg.esc_window_attention_backward(q, k, v, heads, wh, ww, table, None, 0.25, out, lse, go, *g, gt)
+            got.append((out, lse, *g, gt))
+    torch.cuda.synchronize()
+    for r in got:
+        for n, t in zip(("out", "lse", "g_q", "g_k", "g_v", "g_table"), r):
+            assert t is None or torch.equal(t.contiguous(), want[n].contiguous()), n
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("mask", ["inf", "lowest", "-10000"])
 @pytest.mark.parametrize("kind", ["ahead", "all", "some rows"])
 def test_masks(pkg, dtype, kind, mask):
