@@ -427,8 +427,7 @@ int esc_window_attention_forward(const void* q, const void* k, const void* v, in
  * Its backward pass.  out and lse are the forward call's.
  *   grad_out              [B,H,W,heads,head_dim] dense, 16-byte aligned
  *   grad_q, grad_k, grad_v   laid out like q, k, v, with the same pixel_stride (what lies between is left as it is)
- *   grad_table            [n_buckets, heads] of the table's type, or NULL: with bf16 tensors the sums are made from p and out
- *                         as rounded for the products, so bits beyond bf16 would say nothing
+ *   grad_table            [n_buckets, heads] of the table's type, or NULL: fp32 sums over all windows and images, rounded once
  *   workspace             esc_window_attention_backward_workspace_bytes(...) bytes, 256-byte aligned, no preparation needed
  * Every sum has a fixed order: the same input gives the same bits.
  */

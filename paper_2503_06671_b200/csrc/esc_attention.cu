@@ -109,7 +109,7 @@ int check_sizes(int B, int heads, int d, int H, int W, int wh, int ww) {
     if ((long double)std::min(wh, H) * W > 2.0e9L) return ESC_ERR_UNSUPPORTED;   // a pixel's distance from its window's first
     // one block per window, head and tile of queries (at least 32 of them)
     const long double blocks = (long double)B * ((H + wh - 1) / wh) * ((W + ww - 1) / ww) * heads * ((std::min(wh, H) * std::min(ww, W) + 31) / 32);
-    return blocks > 2.0e9L ? ESC_ERR_UNSUPPORTED : ESC_OK;
+    return blocks > 1.0e9L ? ESC_ERR_UNSUPPORTED : ESC_OK;
 }
 
 int check_call(const Call& c) {
@@ -256,8 +256,8 @@ template <int D, bool KEYS, bool TWICE> int grad_rows_bf16(const Call& c, const 
 template <int D> int backward_bf16(const Call& c, wa::bwd::Grads<bf16> g, cudaStream_t st) {
     using namespace wa::bwd::tc;
     const bool twice = RowSmem<D>::bytes(Bias(c.wh, c.ww), true) <= (D <= 16 ? 112 : 224) * 1024;
+    ESC_TRY(twice ? (grad_rows_bf16<D, false, true>(c, g, st)) : (grad_rows_bf16<D, false, false>(c, g, st)));   // first: it makes D exact
     ESC_TRY(twice ? (grad_rows_bf16<D, true, true>(c, g, st)) : (grad_rows_bf16<D, true, false>(c, g, st)));
-    ESC_TRY(twice ? (grad_rows_bf16<D, false, true>(c, g, st)) : (grad_rows_bf16<D, false, false>(c, g, st)));
     if (!g.part) return ESC_OK;
     g.groups = pair_groups(c);
     const int offsets = (int)rp::offsets_of(c.wh, c.ww);

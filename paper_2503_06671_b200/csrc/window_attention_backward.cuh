@@ -45,7 +45,8 @@ row_terms(const T* __restrict__ go, const T* __restrict__ out, const float* __re
 // What the backward kernels need beyond Maps.
 template <typename T> struct Grads {
     const T* go;                                   // dense
-    const float *bases, *dots;
+    const float* bases;
+    float* dots;
     T *g_q, *g_k, *g_v;                            // pixels `stride` values apart
     float* part;                                   // [slices][heads][offsets] sums of ds, or null
     int windows, groups;
@@ -250,12 +251,12 @@ grad_q(Maps<float> m, Grads<float> g, int tiles) {
 
 // ---- bf16: tensor cores ---------------------------------------------------------------------------------------------------
 // Three kernels that each make p and dp anew from products of registers and staged tiles, so that every sum has one owner: the first
-// with rows of keys (g_k, g_v), the second with rows of queries (g_q), the third with a tile of query-key pairs that all windows pass
+// with rows of queries (g_q), the second with rows of keys (g_k, g_v), the third with a tile of query-key pairs that all windows pass
 // by (the table's gradient: the pairs' sums over the windows stay in registers, and go to their offsets once).  One pass would need g_q
 // added up across the warps and 1e9 additions to a table whose neighbouring pairs share entries; p and ds as an operand are rounded
-// to bf16 (2^-8 of each term), D is of the rounded out, the sums of ds for the table are of the fp32 values.
+// to bf16 (2^-8 of each term), D is of the rounded out in g_q alone, the sums of ds for the table are of the fp32 values.
 // Bound: the exponentials, three times 206 us for the pairs of 64 patches of 64x64 in windows of 32, 4 heads of 16 (1.07e9: 238 each),
-// and the issue slots.  There: 625 + 502 + 630 us (rows of keys, of queries, table) beside 474 of the forward pass.
+// and the issue slots.  There: 515 + 625 + 630 us (rows of queries, of keys, table) beside 474 of the forward pass.
 namespace tc {
 using namespace winatt::tc;
 constexpr int kCols = 128;                                          // staged columns: queries for rows of keys, keys for rows of queries
@@ -279,7 +280,8 @@ __device__ __forceinline__ void stage_terms(const Grads<bf16>& gr, long long row
 }
 
 // KEYS: rows are keys (operands k and v), columns queries (q and go): g_k += ds^T q, g_v += p^T go.
-// Else: rows are queries (q and go), columns keys (k and v): g_q += ds k.
+// Else: rows are queries (q and go), columns keys (k and v): g_q += ds k.  Here a row's ds add up to what D of the rounded out is off
+// (sum_j p (dp - D) would be zero), so its dots are put right for the kernels that follow; g_q itself has D of the rounded out.
 template <int D, bool KEYS, bool TWICE>
 __global__ void __launch_bounds__(kMaxWarps * 32, grad_blocks(D))
 grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
@@ -336,7 +338,9 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
         dot[r] = KEYS ? 0.0f : gr.dots[row0 + px];
     }
     const float c = m.scale * kLog2e;
-    float acc1[MT][ON][4], acc2[KEYS ? MT : 1][ON][4];
+    float acc1[MT][ON][4], acc2[KEYS ? MT : 1][ON][4], rest[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) rest[r] = 0.0f;
 #pragma unroll
     for (int x = 0; x < ON; ++x)
 #pragma unroll
@@ -396,7 +400,10 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
                         if (j + 1 >= left) v = 0.0f;
                     }
                     if (KEYS) pp[a][2 * x + e] = pack(u, v);
-                    pd[a][2 * x + e] = pack(u * dp[a][x][2 * e], v * dp[a][x][2 * e + 1]);
+                    u *= dp[a][x][2 * e];
+                    v *= dp[a][x][2 * e + 1];
+                    if (!KEYS) rest[2 * a + e] += u + v;
+                    pd[a][2 * x + e] = pack(u, v);
                 }
 #pragma unroll
         for (int k = 0; k < KC; ++k) {
@@ -435,8 +442,12 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int i = first + 8 * r + g, a = r >> 1, e = 2 * (r & 1);
+        float more = rest[r];
+        more += __shfl_xor_sync(0xffffffffu, more, 1);
+        more += __shfl_xor_sync(0xffffffffu, more, 2);
         if (i >= n) continue;
-        const long long to = pixel_of(m, w, i) * m.stride + off;
+        const long long pixel = pixel_of(m, w, i), to = pixel * m.stride + off;
+        if (!KEYS && t == 0) gr.dots[row_of(m, w, head, pixel)] = dot[r] - more;
 #pragma unroll
         for (int x = 0; x < ON; ++x) {
             store_pair((KEYS ? gr.g_k : gr.g_q) + to, 8 * x + 2 * t, m.d, acc1[a][x][e] * m.scale, acc1[a][x][e + 1] * m.scale);
