@@ -11,7 +11,8 @@
 // zero (2^-9 of the scale instead): a zero would divide the next update by eps alone.  Rounding is to nearest, a value off by at most
 // 2^-4 of itself.  The update of p is made from the moments before they are rounded.
 //
-// Bound: HBM.  Bytes per value: fp32 states 28 (p, m, v read and written, g read), 8 bits 16 (12 + 4 + 8/256 of scales).
+// Bound: HBM.  Bytes per value: fp32 states 28 (p, m, v read and written, g read), 8 bits 16 (12 + 4 + 8/256 of scales).  100 million
+// values in 300 tensors: 412 us (6.8 TB/s) and 278 (5.8 TB/s; 500 with exact quotients and every value's place looked at).
 #pragma once
 #include <cuda_fp8.h>
 #include "common.cuh"

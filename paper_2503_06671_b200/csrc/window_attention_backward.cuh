@@ -59,7 +59,8 @@ template <typename T> __device__ __forceinline__ long long row_of(const Maps<T>&
 // ---- fp32: CUDA cores -----------------------------------------------------------------------------------------------------
 // Two kernels, so that every gradient is a sum in one thread's registers: in the first a thread has a key (k, v and their gradients
 // in registers) and the queries pass by, in the second it has a query.  A row of 64 channels is shared by two neighbouring lanes.
-// Bound: the FP32 pipe, 7 D multiply-adds per pair.
+// Bound: the FP32 pipe, 7 D multiply-adds per pair.  4 x 64x64, windows of 24, 3 heads of 16: 153 and 187 us, one round of blocks whose threads
+// walk 576 rows, four at a time (two blocks an SM instead of four for the second kernel: 234).
 namespace f32 {
 using winatt::f32::kThreads;
 using winatt::f32::stage_rows;
