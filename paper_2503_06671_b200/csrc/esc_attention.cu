@@ -19,10 +19,10 @@ bool known(int dtype) { return dtype == ESC_F32 || dtype == ESC_BF16; }
 
 constexpr size_t kMostSmem = 227 * 1024;           // of a block
 
-// Shared memory beyond 48 KB, once more for every call: the attribute belongs to the current device, and setting it again
-// is cheaper than remembering which devices have it.
+// Shared memory beyond 48 KB, once more for every call: the attribute belongs to the kernel on the current device, and setting it
+// again is cheaper than remembering which devices have it.  Always the same value: another thread may be between this and its launch.
 template <typename K> int allow_smem(K kernel, size_t bytes) {
-    if (bytes > 48 * 1024) ESC_ABI_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    if (bytes > 48 * 1024) ESC_ABI_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem));
     return ESC_OK;
 }
 #define ESC_TRY(call)                    \
