@@ -94,8 +94,8 @@ struct Call {
     long long pixels() const { return (long long)B * H * W; }
     size_t dense_bytes() const { return (size_t)pixels() * heads * d * es(); }
     size_t strided_bytes() const { return ((size_t)(pixels() - 1) * stride + (size_t)heads * d) * es(); }
-    int ny() const { return (H + wh - 1) / wh; }
-    int nx() const { return (W + ww - 1) / ww; }
+    int ny() const { return (int)(((long long)H + wh - 1) / wh); }   // H + wh can be more than an int holds
+    int nx() const { return (int)(((long long)W + ww - 1) / ww); }
     long long windows() const { return (long long)B * ny() * nx(); }
     int tokens() const { return std::min(wh, H) * std::min(ww, W); }   // of the largest window
 };
@@ -108,7 +108,7 @@ int check_sizes(int B, int heads, int d, int H, int W, int wh, int ww) {
     if (n * d > 1.0e15L) return ESC_ERR_SHAPE;
     if ((long double)std::min(wh, H) * W > 2.0e9L) return ESC_ERR_UNSUPPORTED;   // a pixel's distance from its window's first
     // one block per window, head and tile of queries (at least 32 of them)
-    const long double blocks = (long double)B * ((H + wh - 1) / wh) * ((W + ww - 1) / ww) * heads * ((std::min(wh, H) * std::min(ww, W) + 31) / 32);
+    const long double blocks = (long double)B * (((long long)H + wh - 1) / wh) * (((long long)W + ww - 1) / ww) * heads * ((std::min(wh, H) * std::min(ww, W) + 31) / 32);
     return blocks > 1.0e9L ? ESC_ERR_UNSUPPORTED : ESC_OK;
 }
 

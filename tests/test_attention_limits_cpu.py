@@ -1,0 +1,23 @@
+"""What the attention, bias and AdamW entry points do on the host at the ends of their ranges, before anything could be launched."""
+import pytest
+
+UNSUPPORTED = 3
+Q, K, V, O, T = (0x10000000000 * i for i in range(1, 6))   # never dereferenced
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2503_06671_b200 import build, lib
+
+    build.build()
+    return lib()
+
+
+def test_maps_as_high_as_an_int_can_say(L):
+    """One column of 2^31 - 1 pixels: the number of windows is rounded up without leaving 32 bits on the way."""
+    size = L.esc_window_attention_backward_workspace_bytes
+    rows = 2 ** 31 - 1
+    assert size(1, 1, 1, rows, 1, 2, 1) == size(1, 1, 1, rows, 1, 1, 1) == 0           # 2^30 and 2^31 windows: more than 1e9 blocks
+    assert 2 * 4 * rows <= size(1, 1, 1, rows, 1, 64, 1) <= 2 * 4 * rows + (64 << 20)   # two fp32 values a row, and the table's sums
+    fwd = lambda wh: L.esc_window_attention_forward(Q, K, V, 1, 1, 1, rows, 1, 1, wh, 1, T, None, 2 * wh - 1, 1.0, O, None, 1, None)   # noqa: E731
+    assert fwd(1) == fwd(2) == UNSUPPORTED
