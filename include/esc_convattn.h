@@ -385,7 +385,7 @@ int esc_conv_fuse_backward(const void* cat, const void* grad_out, int B, int C, 
  *
  *   bias[h, i, j] = table[bucket[o], h],   o = (yi - yj + win_h - 1) (2 win_w - 1) + (xi - xj + win_w - 1)
  *
- *   table    [n_buckets, heads], the type of the call; -inf masks
+ *   table    [n_buckets, heads], the type of the call; -inf masks; n_buckets above 2^30: ESC_ERR_UNSUPPORTED
  *   bucket   [(2 win_h - 1)(2 win_w - 1)] int32 (device), the bucket of every offset; NULL: every offset has its own row of the
  *            table (n_buckets has to be their number).  An entry outside [0, n_buckets) gives no bias and takes no gradient.
  *   (2 win_h - 1)(2 win_w - 1) is at most 16384 (windows of 64 x 64, sequences of 8192 with win_h = 1), else ESC_ERR_UNSUPPORTED.

@@ -45,6 +45,7 @@ int check_window(int heads, int win_h, int win_w) {
 }
 int check_buckets(const int* bucket, int n_buckets, int win_h, int win_w) {
     if (n_buckets <= 0 || (!bucket && n_buckets != rp::offsets_of(win_h, win_w))) return ESC_ERR_SHAPE;
+    if (n_buckets > 1 << 30) return ESC_ERR_UNSUPPORTED;   // sum_buckets numbers them in an int, 32 to a block
     if (!abi::aligned(bucket, 4)) return ESC_ERR_ALIGN;
     return ESC_OK;
 }

@@ -21,3 +21,12 @@ def test_maps_as_high_as_an_int_can_say(L):
     assert 2 * 4 * rows <= size(1, 1, 1, rows, 1, 64, 1) <= 2 * 4 * rows + (64 << 20)   # two fp32 values a row, and the table's sums
     fwd = lambda wh: L.esc_window_attention_forward(Q, K, V, 1, 1, 1, rows, 1, 1, wh, 1, T, None, 2 * wh - 1, 1.0, O, None, 1, None)   # noqa: E731
     assert fwd(1) == fwd(2) == UNSUPPORTED
+
+
+def test_more_buckets_than_the_kernels_can_number(L):
+    """The kernels count buckets by 32 in an int; a table of more than 2^30 rows is refused."""
+    B, WS, many = 0x60000000000, 0x70000000000, 2 ** 30 + 1
+    for n in (many, 2 ** 31 - 1):
+        assert L.esc_relpos_bias_forward(T, B, n, 1, 2, 2, O, 0, None) == UNSUPPORTED
+        assert L.esc_relpos_bias_backward(O, B, n, 1, 2, 2, T, 0, WS, 1 << 20, None) == UNSUPPORTED
+        assert L.esc_window_attention_forward(Q, K, V, 1, 1, 1, 4, 4, 1, 2, 2, T, B, n, 1.0, O, None, 1, None) == UNSUPPORTED
