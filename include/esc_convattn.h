@@ -458,7 +458,8 @@ int esc_window_attention_backward(const void* q, const void* k, const void* v, i
  *   plan                  esc_adamw_plan_bytes(...) bytes of device memory, 256-byte aligned
  *   n_chunks              out: what esc_adamw_step has to be told
  * Pointers aligned to four values are read four at a time, others one by one.  esc_adamw_plan_init waits for its copy to the device;
- * it is refused (ESC_ERR_UNSUPPORTED) while `stream` is being captured.
+ * it is refused (ESC_ERR_UNSUPPORTED) while `stream` is being captured.  Memory that a step writes may be in the lists once only (a
+ * tensor of two names goes in once): ESC_ERR_ALIAS; gradients may share theirs with one another.
  */
 enum { ESC_STATES_F32 = 0, ESC_STATES_E4M3 = 1 };
 size_t esc_adamw_plan_bytes(int n_tensors, const long long* sizes);        /* 0 for invalid arguments */
@@ -472,7 +473,7 @@ int esc_adamw_plan_init(int n_tensors, const long long* sizes, void* const* para
  *   scalars  device, 4 floats as esc_adamw_scalars gives them, or NULL.  They replace step, lr, weight_decay and grad_scale in
  *            the kernel: a captured graph takes what they hold when it is replayed, where the arguments would stay what they were.
  *   skip     device int or NULL: not zero, and the call changes nothing (gradients that overflowed)
- * Two steps of one plan, or two plans that share tensors, must not overlap on the GPU; no tensor may be in a list twice.
+ * Two steps of one plan, or two plans that share tensors, must not overlap on the GPU.
  */
 int esc_adamw_step(const void* plan, long long n_chunks, int param_dtype, int grad_dtype, int states, long long step, double lr,
                    double beta1, double beta2, double eps, double weight_decay, double grad_scale, const float* scalars,

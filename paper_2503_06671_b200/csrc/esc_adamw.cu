@@ -1,6 +1,7 @@
 // C ABI of the optimiser's step: argument checks, the plan of a list of tensors, launches.
 #include "abi.h"
 
+#include <algorithm>
 #include <cmath>
 #include <new>
 #include <vector>
@@ -20,6 +21,19 @@ long long count_chunks(int n_tensors, const long long* sizes) {   // -1: a size 
         n += (sizes[i] + kChunk - 1) / kChunk;
     }
     return n <= 0x7fffffffLL ? n : -1;
+}
+
+// The memory that a step touches.  Every value is read, changed and written by one thread, in no order: what is written has to be nobody else's.
+struct Range { uintptr_t from, to; bool written; };
+bool shared(std::vector<Range>& ranges) {
+    std::sort(ranges.begin(), ranges.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
+    uintptr_t end = 0, end_written = 0;             // of those that start earlier
+    for (const Range& r : ranges) {
+        if (r.from < (r.written ? end : end_written)) return true;
+        end = std::max(end, r.to);
+        if (r.written) end_written = std::max(end_written, r.to);
+    }
+    return false;
 }
 
 template <typename P, typename G>
@@ -59,6 +73,12 @@ int esc_adamw_plan_init(int n_tensors, const long long* sizes, void* const* para
     try {
         std::vector<Chunk> chunks;
         chunks.reserve((size_t)n);
+        std::vector<Range> ranges;
+        ranges.reserve((size_t)n_tensors * 7 + 1);
+        auto touch = [&](const void* p, size_t bytes, bool written) {
+            if (p) ranges.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, written});
+        };
+        touch(plan, esc_adamw_plan_bytes(n_tensors, sizes), false);
         for (int i = 0; i < n_tensors; ++i) {
             if (sizes[i] == 0) continue;
             if (!params[i] || !grads[i] || !exp_avgs[i] || !exp_avg_sqs[i]) return ESC_ERR_NULL;
@@ -69,6 +89,13 @@ int esc_adamw_plan_init(int n_tensors, const long long* sizes, void* const* para
             if (eight && (!esc::abi::aligned(avg_scales[i], 4) || !esc::abi::aligned(sq_scales[i], 4))) return ESC_ERR_ALIGN;
             const bool wide = esc::abi::aligned(params[i], 4 * ps) && esc::abi::aligned(grads[i], 4 * gs) && esc::abi::aligned(exp_avgs[i], 4 * ss) &&
                               esc::abi::aligned(exp_avg_sqs[i], 4 * ss) && esc::abi::aligned(copy, 8);
+            const size_t count = (size_t)sizes[i], scales = (count + kQuant - 1) / kQuant * sizeof(float);
+            touch(params[i], count * ps, true);
+            touch(grads[i], count * gs, false);
+            touch(exp_avgs[i], count * ss, true);
+            touch(exp_avg_sqs[i], count * ss, true);
+            touch(copy, count * 2, true);
+            if (eight) { touch(avg_scales[i], scales, true); touch(sq_scales[i], scales, true); }
             for (long long at = 0; at < sizes[i]; at += kChunk) {
                 Chunk c;
                 c.p = static_cast<char*>(params[i]) + at * ps;
@@ -83,6 +110,7 @@ int esc_adamw_plan_init(int n_tensors, const long long* sizes, void* const* para
                 chunks.push_back(c);
             }
         }
+        if (shared(ranges)) return ESC_ERR_ALIAS;
         // the copy comes from this function's own memory, so it has to be over before the function is
         cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
         ESC_ABI_CUDA(cudaStreamIsCapturing(st, &capture));

@@ -1,4 +1,6 @@
 """What the attention, bias and AdamW entry points do on the host at the ends of their ranges, before anything could be launched."""
+import ctypes
+
 import pytest
 
 UNSUPPORTED = 3
@@ -30,3 +32,23 @@ def test_more_buckets_than_the_kernels_can_number(L):
         assert L.esc_relpos_bias_forward(T, B, n, 1, 2, 2, O, 0, None) == UNSUPPORTED
         assert L.esc_relpos_bias_backward(O, B, n, 1, 2, 2, T, 0, WS, 1 << 20, None) == UNSUPPORTED
         assert L.esc_window_attention_forward(Q, K, V, 1, 1, 1, 4, 4, 1, 2, 2, T, B, n, 1.0, O, None, 1, None) == UNSUPPORTED
+
+
+def test_adamw_plans_with_a_tensor_twice(L):
+    """A parameter of two names, states that overlap, a copy over its own parameter, a plan inside a tensor: two threads would change one value."""
+    ALIAS, n = 5, ctypes.c_longlong()
+    sizes = (ctypes.c_longlong * 3)(1000, 0, 5000)
+    names = dict(p=0x10000000, g=0x20000000, m=0x30000000, v=0x40000000, ms=0x50000000, vs=0x60000000, c=0x70000000)
+
+    def init(eight=False, plan=0x80000000, **other):
+        lists = {k: [base, None, base + 0x100000] for k, base in names.items()}
+        for k, (i, at) in other.items():
+            lists[k][i] = at
+        arr = {k: (ctypes.c_void_p * 3)(*x) for k, x in lists.items()}
+        return L.esc_adamw_plan_init(3, sizes, arr["p"], arr["g"], arr["m"], arr["v"], arr["ms"] if eight else None, arr["vs"] if eight else None, arr["c"],
+                                     0, 0, int(eight), plan, 1 << 20, ctypes.byref(n), None)
+
+    assert init(p=(2, names["p"])) == init(p=(2, names["p"] + 3996)) == init(m=(2, names["m"])) == init(v=(0, names["m"])) == ALIAS
+    assert init(c=(0, names["p"])) == init(c=(2, names["c"] + 1996)) == init(g=(2, names["p"] + 16)) == init(m=(0, names["g"] + 0x100000 + 19996)) == ALIAS
+    assert init(True, ms=(2, names["ms"] + 12)) == init(True, vs=(0, names["ms"])) == init(True, m=(2, names["m"] + 996)) == ALIAS
+    assert init(plan=names["v"] + 256) == init(plan=names["p"]) == ALIAS   # four runs of 64 bytes

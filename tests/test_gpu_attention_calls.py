@@ -49,3 +49,17 @@ def test_threads_with_windows_of_two_sizes(pkg):
     torch.cuda.synchronize()
     assert all(c == {0} for c in codes), codes
     assert all(torch.equal(want, out) for _, want, out, _ in work)
+
+
+def test_a_plan_over_slices_of_one_buffer(pkg):
+    """Tensors that touch but do not overlap, and gradients that are one tensor, are a plan; a parameter of two names is not."""
+    flat, g = torch.zeros(3000, device="cuda"), torch.ones(1000, device="cuda")
+    m, v = torch.zeros(3000, device="cuda"), torch.zeros(3000, device="cuda")
+    cut = lambda t: [t[i * 1000:(i + 1) * 1000] for i in range(3)]   # noqa: E731
+    pkg.esc_adamw_step(pkg.new_adamw_plan(cut(flat), [g] * 3, cut(m), cut(v)), 1, 0.5, weight_decay=0.0)
+    torch.cuda.synchronize()
+    assert ((flat + 0.5).abs() <= 1e-6).all()                            # the first step is the gradient's sign: 0.5 / (1 + 1e-8)
+    with pytest.raises(pkg.EscError):
+        pkg.new_adamw_plan([flat[:1000], flat[500:1500]], [g] * 2, cut(m)[:2], cut(v)[:2])
+    with pytest.raises(pkg.EscError):
+        pkg.new_adamw_plan([flat[:1000]] * 2, [g] * 2, cut(m)[:2], cut(v)[:2])
