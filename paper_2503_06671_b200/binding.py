@@ -505,6 +505,20 @@ def _stream_address(stream):
     return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
 
 
+def _allocating_for(stream, device):
+    """torch allocates for `stream` within: what a call on it uses for itself has to come from, and go back to, memory that this stream's
+    order covers.  None: the current stream."""
+    import torch
+
+    if stream is None:
+        return _HERE
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+    if stream.device != device:
+        raise ValueError(f"the stream of a call has to be of its tensors' device {device}, not of {stream.device}")
+    return torch.cuda.stream(stream)
+
+
 def _on_device(first, *others):
     """The tensors' one device, made current for the call that follows: kernels run where the data are."""
     import torch
@@ -569,7 +583,8 @@ def esc_relpos_bias_backward(grad_bias, bucket, win_h, win_w, grad_table, worksp
     _bucket_arg(bucket, win_h, win_w)
     with _on_device(grad_bias, bucket, grad_table, workspace):
         if workspace is None:
-            workspace = new_relpos_bias_workspace(heads, win_h, win_w)
+            with _allocating_for(stream, grad_bias.device):
+                workspace = new_relpos_bias_workspace(heads, win_h, win_w)
         _check(lib().esc_relpos_bias_backward(_address(grad_bias), _address(bucket), n, heads, win_h, win_w, _address(grad_table), _dtype_code(grad_bias),
                                               _address(workspace), workspace.numel() * workspace.element_size(), _stream_address(stream)),
                "esc_relpos_bias_backward")
@@ -648,7 +663,8 @@ def esc_window_attention_backward(q, k, v, heads, win_h, win_w, table, bucket, s
     _bucket_arg(bucket, win_h, win_w)
     with _on_device(q, k, v, table, bucket, out, lse, grad_out, grad_q, grad_k, grad_v, grad_table, workspace):
         if workspace is None:
-            workspace = new_window_attention_workspace(B, heads, d, H, W, win_h, win_w)
+            with _allocating_for(stream, q.device):
+                workspace = new_window_attention_workspace(B, heads, d, H, W, win_h, win_w)
         _check(lib().esc_window_attention_backward(_address(q), _address(k), _address(v), B, heads, d, H, W, step, win_h, win_w, _address(table), _address(bucket), n, scale,
                                                    _address(out), _address(lse), _address(grad_out), _address(grad_q), _address(grad_k), _address(grad_v), _address(grad_table),
                                                    _dtype_code(q), _address(workspace), workspace.numel() * workspace.element_size(), _stream_address(stream)),

@@ -63,3 +63,64 @@ def test_a_plan_over_slices_of_one_buffer(pkg):
         pkg.new_adamw_plan([flat[:1000], flat[500:1500]], [g] * 2, cut(m)[:2], cut(v)[:2])
     with pytest.raises(pkg.EscError):
         pkg.new_adamw_plan([flat[:1000]] * 2, [g] * 2, cut(m)[:2], cut(v)[:2])
+
+
+class Blocks:
+    """Where a call's own scratch lies in memory, and which blocks the current stream's pool hands out around it."""
+
+    def __init__(self, monkeypatch, name):
+        from paper_2503_06671_b200 import binding
+
+        self.seen, plain = [], getattr(binding, name)
+
+        def look(t):
+            if t is not None and t.dtype == torch.uint8:
+                self.seen.append((t.data_ptr(), t.numel()))
+            return plain(t)
+
+        monkeypatch.setattr(binding, name, look)
+
+    def around(self, call, size, side):
+        """`call` runs on `side`, which is busy for some time; the current stream has work pending on a block of that size that it has given back."""
+        pending = torch.empty(size, dtype=torch.uint8, device="cuda")
+        before = pending.data_ptr()
+        torch.cuda._sleep(10_000_000)                                    # some 5 ms
+        pending.fill_(1)
+        del pending
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        call()
+        after = [torch.empty(size, dtype=torch.uint8, device="cuda").fill_(0xFF) for _ in range(4)]
+        torch.cuda.synchronize()
+        (at, n), = self.seen
+        assert n >= size
+        assert not before <= at < before + size, "the call's scratch is memory that the current stream still writes"
+        assert not any(t.data_ptr() <= at < t.data_ptr() + size for t in after), "the call's scratch went to the current stream while the call was pending"
+
+
+def test_scratch_of_the_attention_on_another_stream(pkg, monkeypatch):
+    """stream= alone, without making it the current one, and no workspace."""
+    B, H, W, heads, d, win = 2, 64, 64, 2, 16, 16
+    g = torch.Generator().manual_seed(2)
+    q, k, v, go = (torch.randn(B, H, W, heads * d, generator=g).cuda() for _ in range(4))
+    table = torch.randn((2 * win - 1) ** 2, heads, generator=g).cuda()
+    out, lse, side = torch.empty_like(q), torch.empty(B, heads, H, W, device="cuda"), torch.cuda.Stream()
+    pkg.esc_window_attention_forward(q, k, v, heads, win, win, table, None, 0.25, out, lse)
+    grads = [[torch.zeros_like(q) for _ in range(3)] + [torch.zeros_like(table)] for _ in range(2)]
+    size = pkg.esc_window_attention_backward_workspace_bytes(B, heads, d, H, W, win, win)
+    pkg.esc_window_attention_backward(q, k, v, heads, win, win, table, None, 0.25, out, lse, go, *grads[0], pkg.new_window_attention_workspace(B, heads, d, H, W, win, win))
+    torch.cuda.synchronize()
+    Blocks(monkeypatch, "_address").around(
+        lambda: pkg.esc_window_attention_backward(q, k, v, heads, win, win, table, None, 0.25, out, lse, go, *grads[1], stream=side), size, side)
+    assert all(torch.equal(a, b) for a, b in zip(*grads))
+
+
+def test_scratch_of_the_bias_on_another_stream(pkg, monkeypatch):
+    heads, win = 2, 32
+    grad = torch.randn(heads, win * win, win * win, device="cuda")
+    tables, side = [torch.zeros((2 * win - 1) ** 2, heads, device="cuda") for _ in range(2)], torch.cuda.Stream()
+    size = pkg.esc_relpos_bias_workspace_bytes(heads, win, win)
+    pkg.esc_relpos_bias_backward(grad, None, win, win, tables[0], pkg.new_relpos_bias_workspace(heads, win, win))
+    torch.cuda.synchronize()
+    Blocks(monkeypatch, "_address").around(lambda: pkg.esc_relpos_bias_backward(grad, None, win, win, tables[1], stream=side), size, side)
+    assert torch.equal(*tables)
