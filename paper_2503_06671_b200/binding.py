@@ -415,7 +415,8 @@ def esc_conv_fuse_backward(cat, grad_out, w_fuse, grad_cat, grad_w_fuse, grad_b_
         n = esc_conv_fuse_backward_workspace_bytes(B, C, H, W)
         if n == 0:
             raise EscError(3, "esc_conv_fuse_backward_workspace_bytes")
-        workspace = torch.empty(n, dtype=torch.uint8, device=cat.device)
+        with _allocating_for(stream, cat.device):
+            workspace = torch.empty(n, dtype=torch.uint8, device=cat.device)
     _check(lib().esc_conv_fuse_backward(_ptr(cat), _ptr(grad_out), B, C, H, W, _ptr(w_fuse), _ptr(grad_cat), _ptr(grad_w_fuse),
                                         _ptr(grad_b_fuse), _dtype_code(cat), layout, _ptr(workspace),
                                         workspace.numel() * workspace.element_size(), _stream(stream)),

@@ -124,3 +124,22 @@ def test_scratch_of_the_bias_on_another_stream(pkg, monkeypatch):
     torch.cuda.synchronize()
     Blocks(monkeypatch, "_address").around(lambda: pkg.esc_relpos_bias_backward(grad, None, win, win, tables[1], stream=side), size, side)
     assert torch.equal(*tables)
+
+
+def test_scratch_of_the_closing_convolution_on_another_stream(pkg, monkeypatch):
+    B, C, H, W = 2, 64, 48, 40
+    cat, go, w = torch.randn(B, H, W, C, device="cuda"), torch.randn(B, H, W, C, device="cuda"), torch.randn(C, C, device="cuda")
+    got = [[torch.zeros_like(cat), torch.zeros(C, C, device="cuda"), torch.zeros(C, device="cuda")] for _ in range(2)]
+    size, side = pkg.esc_conv_fuse_backward_workspace_bytes(B, C, H, W), torch.cuda.Stream()
+    pkg.esc_conv_fuse_backward(cat, go, w, *got[0], pkg.ESC_NHWC, torch.empty(size, dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    Blocks(monkeypatch, "_ptr").around(lambda: pkg.esc_conv_fuse_backward(cat, go, w, *got[1], pkg.ESC_NHWC, stream=side), size, side)
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_a_stream_of_another_device_is_refused_before_anything_runs(pkg):
+    """The check is made on the stream's own word, so a stand-in shows it on a machine with one GPU."""
+    from paper_2503_06671_b200 import binding
+
+    with pytest.raises(ValueError):
+        binding._allocating_for(torch.cuda.current_stream(), torch.device("cuda", 1))
