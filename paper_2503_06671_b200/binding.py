@@ -506,6 +506,14 @@ def _stream_address(stream):
     return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
 
 
+def _torch_stream(stream, device):
+    import torch
+
+    if stream is None:
+        return torch.cuda.current_stream(device)
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+
+
 def _allocating_for(stream, device):
     """torch allocates for `stream` within: what a call on it uses for itself has to come from, and go back to, memory that this stream's
     order covers.  None: the current stream."""
@@ -513,8 +521,7 @@ def _allocating_for(stream, device):
 
     if stream is None:
         return _HERE
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+    stream = _torch_stream(stream, device)
     if stream.device != device:
         raise ValueError(f"the stream of a call has to be of its tensors' device {device}, not of {stream.device}")
     return torch.cuda.stream(stream)
@@ -682,7 +689,8 @@ def esc_adamw_plan_bytes(sizes) -> int:
 
 
 class AdamwPlan:
-    """A list of tensors in device memory, as esc_adamw_step takes it.  It keeps the tensors."""
+    """A list of tensors in device memory, as esc_adamw_step takes it.  It keeps the tensors.  A graph that has captured its steps needs it as
+    long as it is replayed."""
 
     def __init__(self, table, n_chunks, param_dtype, grad_dtype, states, tensors):
         self.table, self.n_chunks, self.param_dtype, self.grad_dtype, self.states, self.tensors = table, n_chunks, param_dtype, grad_dtype, states, tensors
@@ -723,7 +731,8 @@ def esc_adamw_plan_init(params, grads, exp_avgs, exp_avg_sqs, avg_scales=None, s
         bytes_ = esc_adamw_plan_bytes(sizes)
         if bytes_ == 0:
             raise ValueError("invalid sizes")
-        table = torch.empty(bytes_, dtype=torch.uint8, device="cuda")
+        with _allocating_for(stream, params[0].device):                 # the copy of the addresses waits for nobody else's work
+            table = torch.empty(bytes_, dtype=torch.uint8, device="cuda")
         _check(lib().esc_adamw_plan_init(n, (ctypes.c_longlong * n)(*sizes), *arrays, _dtype_code(params[0]), _dtype_code(grads[0]), states, _address(table), bytes_,
                                          ctypes.byref(chunks), _stream_address(stream)), "esc_adamw_plan_init")
     return AdamwPlan(table, chunks.value, _dtype_code(params[0]), _dtype_code(grads[0]), states, every)

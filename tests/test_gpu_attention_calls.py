@@ -143,3 +143,14 @@ def test_a_stream_of_another_device_is_refused_before_anything_runs(pkg):
 
     with pytest.raises(ValueError):
         binding._allocating_for(torch.cuda.current_stream(), torch.device("cuda", 1))
+
+
+def test_a_plan_made_for_another_stream(pkg, monkeypatch):
+    """The table of addresses is no memory that the current stream still writes: AdamW would write wherever that says."""
+    p, g, m, v = (torch.zeros(5000, device="cuda") + (i == 1) for i in range(4))
+    size, side, plans = pkg.esc_adamw_plan_bytes([5000]), torch.cuda.Stream(), []
+    torch.cuda.synchronize()
+    Blocks(monkeypatch, "_address").around(lambda: plans.append(pkg.new_adamw_plan([p], [g], [m], [v], stream=side)), size, side)
+    pkg.esc_adamw_step(plans[0], 1, 0.5, weight_decay=0.0, stream=side)
+    torch.cuda.synchronize()
+    assert ((p + 0.5).abs() <= 1e-6).all()
