@@ -692,8 +692,9 @@ class AdamwPlan:
     """A list of tensors in device memory, as esc_adamw_step takes it.  It keeps the tensors.  A graph that has captured its steps needs it as
     long as it is replayed."""
 
-    def __init__(self, table, n_chunks, param_dtype, grad_dtype, states, tensors):
+    def __init__(self, table, n_chunks, param_dtype, grad_dtype, states, tensors, stream=None):
         self.table, self.n_chunks, self.param_dtype, self.grad_dtype, self.states, self.tensors = table, n_chunks, param_dtype, grad_dtype, states, tensors
+        self.stream = stream   # address of the stream that the table was allocated for
 
 
 def esc_adamw_plan_init(params, grads, exp_avgs, exp_avg_sqs, avg_scales=None, sq_scales=None, copies=None, stream=None):
@@ -735,7 +736,8 @@ def esc_adamw_plan_init(params, grads, exp_avgs, exp_avg_sqs, avg_scales=None, s
             table = torch.empty(bytes_, dtype=torch.uint8, device="cuda")
         _check(lib().esc_adamw_plan_init(n, (ctypes.c_longlong * n)(*sizes), *arrays, _dtype_code(params[0]), _dtype_code(grads[0]), states, _address(table), bytes_,
                                          ctypes.byref(chunks), _stream_address(stream)), "esc_adamw_plan_init")
-    return AdamwPlan(table, chunks.value, _dtype_code(params[0]), _dtype_code(grads[0]), states, every)
+        at = _stream_address(stream)
+    return AdamwPlan(table, chunks.value, _dtype_code(params[0]), _dtype_code(grads[0]), states, every, at)
 
 
 new_adamw_plan = esc_adamw_plan_init
@@ -757,5 +759,8 @@ def esc_adamw_step(plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_deca
     if skip is not None and (skip.numel() != 1 or skip.dtype != torch.int32):
         raise ValueError("skip has to be one int32")
     with _on_device(plan.table, scalars, skip):
+        at = _stream_address(stream)
+        if at != plan.stream:                                           # a plan that is dropped keeps its memory until this step is over
+            plan.table.record_stream(_torch_stream(stream, plan.table.device))
         _check(lib().esc_adamw_step(_address(plan.table), plan.n_chunks, plan.param_dtype, plan.grad_dtype, plan.states, int(step), lr, beta1, beta2, eps,
-                                    weight_decay, grad_scale, _address(scalars), _address(skip), _stream_address(stream)), "esc_adamw_step")
+                                    weight_decay, grad_scale, _address(scalars), _address(skip), at), "esc_adamw_step")

@@ -154,3 +154,21 @@ def test_a_plan_made_for_another_stream(pkg, monkeypatch):
     pkg.esc_adamw_step(plans[0], 1, 0.5, weight_decay=0.0, stream=side)
     torch.cuda.synchronize()
     assert ((p + 0.5).abs() <= 1e-6).all()
+
+
+def test_a_plan_dropped_behind_a_step_on_another_stream(pkg):
+    """Its table is nobody else's until the step has read it, whatever stream the step runs on."""
+    p, g, m, v = (torch.zeros(5000, device="cuda") + (i == 1) for i in range(4))
+    size, side = pkg.esc_adamw_plan_bytes([5000]), torch.cuda.Stream()
+    plan = pkg.new_adamw_plan([p], [g], [m], [v])
+    at = plan.table.data_ptr()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+    pkg.esc_adamw_step(plan, 1, 0.5, weight_decay=0.0, stream=side)
+    del plan
+    after = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(64)]   # not written: only where they lie is asked
+    where = [t.data_ptr() for t in after]
+    torch.cuda.synchronize()
+    assert at not in where
+    assert ((p + 0.5).abs() <= 1e-6).all()
