@@ -410,8 +410,9 @@ int esc_relpos_bias_backward(const void* grad_bias, const int* bucket, int n_buc
  *   q, k, v  [B,H,W,heads,head_dim], a pixel's heads*head_dim values dense, pixels `pixel_stride` values apart (rows and images
  *            dense behind one another): tensors of their own, or slices of the output of one projection.  head_dim <= 64.
  *            Fastest where the pointers are 16-byte aligned and head_dim and pixel_stride are multiples of 16 bytes.
- *   table, bucket, n_buckets   the bias as above; table NULL: none.  An entry of -9984 or less (-10000 in bf16, a type's lowest value)
- *            masks its offset as -inf does: such a key has no weight, also where all others of the row are masked
+ *   table, bucket, n_buckets   the bias as above; table NULL: none.  An entry of -9984 or less (-10000 in bf16, a type's lowest value) is a
+ *            mask, as -inf is: such a key has no weight, and a row that has no other keys gives zeros, where softmax of the finite
+ *            numbers would be a distribution.  (esc_relpos_bias_forward writes such entries as they are.)
  *   scale    in [1e-6, 1e6]
  *   out      [B,H,W,heads,head_dim] dense, 16-byte aligned
  *   lse      [B,heads,H,W] fp32, log of the sum of exp per row, which the backward pass takes; may be NULL.  A row whose keys

@@ -5,8 +5,10 @@
 //   s[i,j] = scale q[i] . k[j] + bias[i,j]      lse[i] = log sum_j exp s[i,j]      p[i,j] = exp(s[i,j] - lse[i])
 //   out[i] = sum_j p[i,j] v[j]
 //
-// A table's entry of kMasked or less counts as -inf, and a query that all keys are masked for gets out = 0 and lse = -inf: the backward
-// pass has p from s - lse alone, which holds nothing more of s where all of a row is that far from zero.
+// A table's entry of kMasked or less counts as -inf, and a query that all keys are masked for gets out = 0 and lse = -inf: the masks that
+// programs write (-inf, -10000, a type's lowest value) mean one thing, also where a row has nothing else.  That is an agreement, not
+// arithmetic: softmax of a row of -10000 alone would be a distribution, and the entries above kMasked are taken as the numbers that they
+// are (fp32 is 2^-10 apart at 10^4, so p there is good to about 1e-3, forward and backward).
 //
 // The running maximum and sum of a row stay in registers while the keys pass by (one pass, nothing of s is stored).  The table
 // of one head is expanded once per block into shared memory, divided by the scale: it is then where the sum q . k starts from, and
