@@ -1,6 +1,7 @@
 """Builds the CUDA library in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
 from __future__ import annotations
 
+import hashlib
 import os
 import re
 import shutil
@@ -45,8 +46,18 @@ def _newest(src: Path) -> float:
     return max(p.stat().st_mtime for p in _includes(src.resolve(), set()))
 
 
+def _object(src: Path) -> Path:
+    """Its object file: another one where the compiler is given other flags."""
+    return OBJ_DIR / f"{src.stem}.{hashlib.sha256(' '.join(NVCC_FLAGS).encode()).hexdigest()[:8]}.o"
+
+
+def _left_over() -> list:
+    """Object files of other flags, or of sources that are gone."""
+    return [o for o in OBJ_DIR.glob("*.o") if ".tmp" not in o.name and o not in {_object(s) for s in sources()}]
+
+
 def needs_build() -> bool:
-    if not LIB.exists():
+    if not LIB.exists() or _left_over():
         return True
     t = LIB.stat().st_mtime
     deps = list(CSRC.glob("*.cu")) + list(CSRC.glob("*.cuh")) + list(CSRC.glob("*.h")) + list(INCLUDE.glob("*.h"))
@@ -56,7 +67,8 @@ def needs_build() -> bool:
 def build(force: bool = False, verbose: bool = False) -> Path:
     """Compile every .cu under csrc/ (side by side) and link lib/libesc_convattn.so.
 
-    Without `force` an object file newer than its source and everything that one includes is taken as it is."""
+    Without `force` an object file of these flags, newer than its source and everything that one includes, is taken as it is;
+    `verbose` prints the registers of what is compiled."""
     if not force and not needs_build():
         return LIB
     LIB_DIR.mkdir(exist_ok=True)
@@ -64,7 +76,7 @@ def build(force: bool = False, verbose: bool = False) -> Path:
     flags = [*NVCC_FLAGS, *(["-Xptxas=-v"] if verbose else []), "-I", str(INCLUDE)]
 
     def compiled(src: Path) -> Path:
-        obj = OBJ_DIR / (src.stem + ".o")
+        obj = _object(src)
         if force or not obj.exists() or obj.stat().st_mtime <= _newest(src):
             tmp = obj.with_suffix(".tmp%d.o" % os.getpid())
             subprocess.check_call([_nvcc(), *flags, "-c", "-o", str(tmp), str(src)])
@@ -76,6 +88,8 @@ def build(force: bool = False, verbose: bool = False) -> Path:
     tmp = LIB.with_suffix(".so.tmp%d" % os.getpid())
     subprocess.check_call([_nvcc(), *NVCC_FLAGS, "-shared", "-o", str(tmp), *map(str, objects)])
     os.replace(tmp, LIB)
+    for old in _left_over():
+        old.unlink(missing_ok=True)
     return LIB
 
 
