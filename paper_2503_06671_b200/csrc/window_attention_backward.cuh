@@ -255,9 +255,10 @@ grad_q(Maps<float> m, Grads<float> g, int tiles) {
 // with rows of queries (g_q), the second with rows of keys (g_k, g_v), the third with a tile of query-key pairs that all windows pass
 // by (the table's gradient: the pairs' sums over the windows stay in registers, and go to their offsets once).  One pass would need g_q
 // added up across the warps and 1e9 additions to a table whose neighbouring pairs share entries; p and ds as an operand are rounded
-// to bf16 (2^-8 of each term), D is of the rounded out in g_q alone, the sums of ds for the table are of the fp32 values.
-// Bound: the exponentials, three times 206 us for the pairs of 64 patches of 64x64 in windows of 32, 4 heads of 16 (1.07e9: 238 each),
-// and the issue slots.  There: 515 + 625 + 630 us (rows of queries, of keys, table) beside 474 of the forward pass.
+// to bf16 (2^-8 of each term), D is put right by the rows' own sums, the sums of ds for the table are of the fp32 values.
+// Bound: the exponentials, three times 238 us for the pairs of 64 patches of 64x64 in windows of 32, 4 heads of 16 (1.07e9),
+// and the issue slots.  There: 618 + 621 + 605 us (rows of queries, of keys, table) beside 476 of the forward pass.  Rows of queries took 515
+// with D of the rounded out in g_q, without sum p k.
 namespace tc {
 using namespace winatt::tc;
 constexpr int kCols = 128;                                          // staged columns: queries for rows of keys, keys for rows of queries
@@ -282,7 +283,8 @@ __device__ __forceinline__ void stage_terms(const Grads<bf16>& gr, long long row
 
 // KEYS: rows are keys (operands k and v), columns queries (q and go): g_k += ds^T q, g_v += p^T go.
 // Else: rows are queries (q and go), columns keys (k and v): g_q += ds k.  Here a row's ds add up to what D of the rounded out is off
-// (sum_j p (dp - D) would be zero), so its dots are put right for the kernels that follow; g_q itself has D of the rounded out.
+// (sum_j p (dp - D) would be zero), so its dots are put right for the kernels that follow, and g_q by as much of sum_j p k: where few keys
+// decide a row its ds are small beside D's error, which was up to 18 times what bf16 as such costs there.
 template <int D, bool KEYS, bool TWICE>
 __global__ void __launch_bounds__(kMaxWarps * 32, grad_blocks(D))
 grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
@@ -339,7 +341,7 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
         dot[r] = KEYS ? 0.0f : gr.dots[row0 + px];
     }
     const float c = m.scale * kLog2e;
-    float acc1[MT][ON][4], acc2[KEYS ? MT : 1][ON][4], rest[R];
+    float acc1[MT][ON][4], acc2[MT][ON][4], rest[R];               // acc2: g_v, or sum p k
 #pragma unroll
     for (int r = 0; r < R; ++r) rest[r] = 0.0f;
 #pragma unroll
@@ -347,7 +349,7 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int a = 0; a < MT; ++a) { acc1[a][x][e] = 0.0f; if (KEYS) acc2[a][x][e] = 0.0f; }
+            for (int a = 0; a < MT; ++a) acc1[a][x][e] = acc2[a][x][e] = 0.0f;
 
     uint32_t plain[KC], turned[KC];
     lane_offsets<D>(lane, plain, turned);
@@ -400,7 +402,7 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
                         if (j >= left) u = 0.0f;
                         if (j + 1 >= left) v = 0.0f;
                     }
-                    if (KEYS) pp[a][2 * x + e] = pack(u, v);
+                    pp[a][2 * x + e] = pack(u, v);
                     u *= dp[a][x][2 * e];
                     v *= dp[a][x][2 * e + 1];
                     if (!KEYS) rest[2 * a + e] += u + v;
@@ -412,11 +414,9 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
             ldsm_t(f, s1 + turned[k]);
 #pragma unroll
             for (int a = 0; a < MT; ++a) { mma(acc1[a][2 * k], pd[a], f[0], f[1]); mma(acc1[a][2 * k + 1], pd[a], f[2], f[3]); }
-            if (KEYS) {
-                ldsm_t(f, s2 + turned[k]);
+            if (KEYS) ldsm_t(f, s2 + turned[k]);
 #pragma unroll
-                for (int a = 0; a < MT; ++a) { mma(acc2[a][2 * k], pp[a], f[0], f[1]); mma(acc2[a][2 * k + 1], pp[a], f[2], f[3]); }
-            }
+            for (int a = 0; a < MT; ++a) { mma(acc2[a][2 * k], pp[a], f[0], f[1]); mma(acc2[a][2 * k + 1], pp[a], f[2], f[3]); }
         }
     };
     for (int tile_col = 0, buf = 0, place = 0; tile_col < n; tile_col += kCols, buf ^= 1) {
@@ -451,7 +451,9 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
         if (!KEYS && t == 0) gr.dots[row_of(m, w, head, pixel)] = dot[r] - more;
 #pragma unroll
         for (int x = 0; x < ON; ++x) {
-            store_pair((KEYS ? gr.g_k : gr.g_q) + to, 8 * x + 2 * t, m.d, acc1[a][x][e] * m.scale, acc1[a][x][e + 1] * m.scale);
+            float u = acc1[a][x][e], v = acc1[a][x][e + 1];
+            if (!KEYS) { u = fmaf(-more, acc2[a][x][e], u); v = fmaf(-more, acc2[a][x][e + 1], v); }
+            store_pair((KEYS ? gr.g_k : gr.g_q) + to, 8 * x + 2 * t, m.d, u * m.scale, v * m.scale);
             if (KEYS) store_pair(gr.g_v + to, 8 * x + 2 * t, m.d, acc2[a][x][e], acc2[a][x][e + 1]);
         }
     }
