@@ -392,7 +392,8 @@ int esc_conv_fuse_backward(const void* cat, const void* grad_out, int B, int C, 
  *
  * esc_relpos_bias_forward writes it as a matrix [heads, N, N] with N = win_h win_w (16-byte aligned), for an attention that takes
  * one.  esc_relpos_bias_backward sums a gradient of that shape into grad_table [n_buckets, heads], fp32; a bucket that no
- * offset has gets zero.  The order of the additions is fixed: the same input gives the same bits.
+ * offset has gets zero.  The order of the additions is fixed: the same input gives the same bits.  Calls, or graphs, that may run at the
+ * same time need a workspace each.
  */
 int esc_relpos_bias_forward(const void* table, const int* bucket, int n_buckets, int heads, int win_h, int win_w, void* bias,
                             int dtype, void* stream);
@@ -430,7 +431,7 @@ int esc_window_attention_forward(const void* q, const void* k, const void* v, in
  *   grad_q, grad_k, grad_v   laid out like q, k, v, with the same pixel_stride (what lies between is left as it is)
  *   grad_table            [n_buckets, heads] of the table's type, or NULL: fp32 sums over all windows and images, rounded once
  *   workspace             esc_window_attention_backward_workspace_bytes(...) bytes, 256-byte aligned, no preparation needed
- * Every sum has a fixed order: the same input gives the same bits.
+ * Every sum has a fixed order: the same input gives the same bits.  Calls, or graphs, that may run at the same time need a workspace each.
  */
 size_t esc_window_attention_backward_workspace_bytes(int B, int heads, int head_dim, int H, int W, int win_h, int win_w);
 int esc_window_attention_backward(const void* q, const void* k, const void* v, int B, int heads, int head_dim, int H, int W,

@@ -11,7 +11,7 @@
 // zero (2^-9 of the scale instead): a zero would divide the next update by eps alone.  Rounding is to nearest, a value off by at most
 // 2^-4 of itself.  The update of p is made from the moments before they are rounded.
 //
-// Bound: HBM.  Bytes per value: fp32 states 28 (p, m, v read and written, g read), 8 bits 16 (12 + 4 + 8/256 of scales).  100 million
+// Bound: HBM.  Bytes per value: fp32 states 28 (p, m, v read and written, g read), 8 bits 16 (12 + 4, and 16/256 of scales).  100 million
 // values in 300 tensors: 412 us (6.8 TB/s) and 278 (5.8 TB/s; 500 with exact quotients and every value's place looked at).
 #pragma once
 #include <cuda_fp8.h>
@@ -112,7 +112,8 @@ template <bool WHOLE, typename T> __device__ __forceinline__ void out(T* base, i
     }
 }
 
-// The largest magnitude of a warp's values.  Infinities do not count (they are stored as the largest value), nor does NaN, which stays.
+// The largest magnitude of a warp's values.  Infinities do not count (they are stored as the largest value; as NaN where the run's scale is
+// zero), nor does NaN, which stays.
 __device__ __forceinline__ float largest(const float* x, bool finite_only) {
     float top = 0.0f;
 #pragma unroll

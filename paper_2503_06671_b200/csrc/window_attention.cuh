@@ -114,7 +114,7 @@ template <typename T> __device__ __forceinline__ void stage_table(const Maps<T>&
 // A thread has Q queries (their channels, accumulators, running maxima and sums in registers); the block's keys and values are
 // staged kKeys at a time as rows of D channels, which all threads read at the same address.  D: d rounded up, the rest is zero.
 // Bound: the FP32 pipe, 2 D multiply-adds per pair of query and key (two at a time: they issue in half the slots, at the same rate)
-// next to about 10 other instructions.  427x240, windows of 24, 4 heads of 16: 596 us, 0.17 of that pipe, for 12 warps an SM and sums that wait
+// next to about 10 other instructions.  427x240, windows of 24, 4 heads of 16: 596 us, 0.34 of that pipe, for 12 warps an SM and sums that wait
 // on one another.  Steps of 4 keys or 8: 593, 606; 64 threads a block instead of 128: 652.
 namespace f32 {
 constexpr int kThreads = 128, kKeys = 32, kStep = 4;
@@ -283,7 +283,7 @@ forward(Maps<float> m, int tiles, float* __restrict__ out, float* __restrict__ l
 // p is rounded as an operand only: out is off by at most 2^-8 of sum p |v| more; the sum that divides it is of the fp32 values.
 //
 // Bound: the exponentials, 16 a clock and SM (measured; a row's other arithmetic runs beside them), then the issue slots.  640x360,
-// windows of 32, 4 heads of 16 (0.93e9 pairs, 59 GFLOP, 118 MB): exponentials 206 us, products 103 at mma.sync's 955 multiply-adds
+// windows of 32, 4 heads of 16 (0.93e9 pairs, 59 GFLOP, 118 MB): exponentials 204 us, products 103 at mma.sync's 955 multiply-adds
 // a clock and SM, bytes 18; 400 us, 8 pairs a clock and SM, 9.7 instructions each and 0.65 of them issued per clock and scheduler.
 // mma.sync and not tcgen05 because at 16 channels the products are not the limit: a kernel with s in tensor memory, a query per thread and
 // p through shared memory, two groups of 128 queries per block, took 554 us here and 580 for 48 x 48 windows of 6 heads of 32 (449).

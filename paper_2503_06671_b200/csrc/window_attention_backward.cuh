@@ -256,7 +256,7 @@ grad_q(Maps<float> m, Grads<float> g, int tiles) {
 // by (the table's gradient: the pairs' sums over the windows stay in registers, and go to their offsets once).  One pass would need g_q
 // added up across the warps and 1e9 additions to a table whose neighbouring pairs share entries; p and ds as an operand are rounded
 // to bf16 (2^-8 of each term), D is put right by the rows' own sums, the sums of ds for the table are of the fp32 values.
-// Bound: the exponentials, three times 238 us for the pairs of 64 patches of 64x64 in windows of 32, 4 heads of 16 (1.07e9),
+// Bound: the exponentials, three times 236 us for the pairs of 64 patches of 64x64 in windows of 32, 4 heads of 16 (1.07e9),
 // and the issue slots.  There: 618 + 621 + 605 us (rows of queries, of keys, table) beside 476 of the forward pass.  Rows of queries took 515
 // with D of the rounded out in g_q, without sum p k.
 namespace tc {
