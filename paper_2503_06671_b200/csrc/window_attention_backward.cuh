@@ -5,7 +5,8 @@
 //   g_q[i]   = scale sum_j ds[i,j] k[j]            g_k[j]  = scale sum_i ds[i,j] q[i]
 //   g_v[j]   = sum_i p[i,j] go[i]                  g_table[b,h] = sum of ds over all windows' pairs of bucket b
 //
-// Every sum has a fixed order.  A query without keys (lse = -inf) has p = 0 and so takes and gives nothing.
+// Every sum has a fixed order.  A query without keys (lse = -inf) has p = 0 and so takes and gives nothing.  In a window of one pixel p is 1 whatever
+// the score is: ds is zero, and is not left to the difference of dp and D, which are two roundings of one number.
 #pragma once
 #include "window_attention.cuh"
 
@@ -51,6 +52,8 @@ template <typename T> struct Grads {
     float* part;                                   // [slices][heads][offsets] sums of ds, or null
     int windows, groups;
 };
+// The scale of g_q and g_k in a window of n pixels.
+template <typename T> __device__ __forceinline__ float score_scale(const Maps<T>& m, int n) { return n > 1 ? m.scale : 0.0f; }
 template <typename T> __device__ __forceinline__ long long row_of(const Maps<T>& m, const Window& w, int head, long long pixel) {
     const long long hw = (long long)m.H * m.W;
     return ((long long)w.b * m.heads + head) * hw + pixel - w.b * hw;
@@ -171,7 +174,7 @@ grad_kv(Maps<float> m, Grads<float> g, int tiles) {
         }
     }
     if (first + L::row() < n) {
-        L::store(g.g_k + at, m.d, gk, m.scale);
+        L::store(g.g_k + at, m.d, gk, score_scale(m, n));
         L::store(g.g_v + at, m.d, gv, 1.0f);
     }
 }
@@ -197,7 +200,7 @@ grad_q(Maps<float> m, Grads<float> g, int tiles) {
         const Window w = window_at(m, unit / tiles);
         const int n = w.tokens(), first = unit % tiles * L::rows();
         if (first >= n) continue;
-        const bool own = first + L::row() < n;
+        const bool own = first + L::row() < n, adds = own && L::first() == 0 && n > 1;   // adds: to the table's sums
         const int i = min(first + L::row(), n - 1);
         const long long pixel = pixel_of(m, w, i), at = pixel * m.stride + (long long)head * m.d, row = row_of(m, w, head, pixel);
         const int a = (i / w.w + m.wh - 1) * pitch + i % w.w + m.ww - 1;
@@ -231,13 +234,13 @@ grad_q(Maps<float> m, Grads<float> g, int tiles) {
                 if (g.part) {
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
-                        if (own && L::first() == 0 && r + u < rows) mine[o[u]] += ds[u];
+                        if (adds && r + u < rows) mine[o[u]] += ds[u];
                         __syncwarp();              // the next key's offsets are the neighbours'
                     }
                 }
             }
         }
-        if (own) L::store(g.g_q + at, m.d, gq, m.scale);
+        if (own) L::store(g.g_q + at, m.d, gq, score_scale(m, n));
     }
     if (!g.part) return;
     __syncthreads();
@@ -453,7 +456,7 @@ grad_rows(Maps<bf16> m, Grads<bf16> gr, int tiles) {
         for (int x = 0; x < ON; ++x) {
             float u = acc1[a][x][e], v = acc1[a][x][e + 1];
             if (!KEYS) { u = fmaf(-more, acc2[a][x][e], u); v = fmaf(-more, acc2[a][x][e + 1], v); }
-            store_pair((KEYS ? gr.g_k : gr.g_q) + to, 8 * x + 2 * t, m.d, u * m.scale, v * m.scale);
+            store_pair((KEYS ? gr.g_k : gr.g_q) + to, 8 * x + 2 * t, m.d, u * score_scale(m, n), v * score_scale(m, n));
             if (KEYS) store_pair(gr.g_v + to, 8 * x + 2 * t, m.d, acc2[a][x][e], acc2[a][x][e + 1]);
         }
     }
@@ -504,7 +507,7 @@ grad_table(Maps<bf16> m, Grads<bf16> gr, int key_tiles, int parts, bool staged) 
         const int per_row = kind & 1 ? (rest_x > 0) : full_x, width = kind & 1 ? rest_x : m.ww, per_col = kind & 2 ? (rest_y > 0) : full_y, height = kind & 2 ? rest_y : m.wh;
         const int count = m.B * per_col * per_row, tokens = height * width;
         const int mine = group < count ? (count - group + gr.groups - 1) / gr.groups : 0;
-        if (mine == 0 || key0 >= tokens) continue;
+        if (mine == 0 || key0 >= tokens || tokens == 1) continue;
         auto look = [&](int i) {                                    // the group's windows i .. i + kList - 1 into the list
             if (tid < kList && i + tid < mine) {
                 const int at = group + (i + tid) * gr.groups, line = at / per_row, b = line / per_col;

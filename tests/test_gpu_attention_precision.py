@@ -68,3 +68,17 @@ def test_gradients_of_rows_that_few_keys_decide(pkg, shape, spread):
     val, far = tight(x, shape, scale)
     for n in val:
         check(got[n], val[n], far[n], n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("shape", [(2, 1, 50, 3, 16, 1, 1), (1, 1, 1, 2, 32, 8, 8), (3, 5, 9, 2, 24, 4, 8), (1, 7, 7, 2, 64, 3, 6)], ids=lambda s: "x".join(map(str, s)))
+def test_windows_of_one_pixel_have_no_gradient_of_scores(pkg, shape, dtype):
+    """p is 1 whatever the score is: zeros, not the difference of two roundings of one number.  Whole windows of one pixel, a map of one, and the
+    corner that the border leaves of a larger window."""
+    B, H, W, heads, d, wh, ww = shape
+    x = inputs(shape, dtype, 60)
+    got = run(pkg, x, shape, 0.25)
+    corner = {n: got[n][:, H - 1:, W - 1:] for n in ("g_q", "g_k")}          # the last pixel is a window of its own in all of these
+    assert all((t == 0).all() for t in corner.values())
+    if wh * ww == 1 or H * W == 1:
+        assert all((got[n] == 0).all() for n in ("g_q", "g_k", "g_table"))
