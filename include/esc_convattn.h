@@ -484,6 +484,64 @@ int esc_adamw_scalars(long long step, double lr, double beta1, double beta2, dou
                       float* scalars_host);                                /* host: 4 floats */
 
 /*
+ * ---- the block's layer norms (Eq. 3) ----
+ *
+ *   y = (x - mean) / sqrt(var + eps) * weight + bias      per row of C channels, var = mean of (x - mean)^2
+ *
+ *   x        [rows, C], rows `x_stride` values apart (a channels-last map: rows = B H W; or a slice of a wider tensor)
+ *   weight, bias   [C] of x's type; NULL: ones, zeros
+ *   eps      finite, not negative.  With eps = 0 a row of equal values gives NaN.
+ *   y        [rows, C], rows `y_stride` values apart; what lies between them is left as it is
+ * rows may be 0, C is at most 2^20.  Arithmetic in fp32, one rounding.  Fastest where pointers and strides are multiples of 16 bytes.
+ */
+int esc_layer_norm_forward(const void* x, long long x_stride, const void* weight, const void* bias, float eps, void* y,
+                           long long y_stride, long long rows, int C, int dtype, void* stream);
+
+/*
+ * Its gradients; mean and var are worked out anew from x.
+ *   grad_y       [rows, C] dense
+ *   grad_skip    [rows, C] dense or NULL: added to grad_x, unnormed (the gradient that came past the layer, of a block x + f(norm(x)))
+ *   grad_x       [rows, C] dense
+ *   grad_weight, grad_bias   [C] of grad_dtype, either may be NULL: fp32 sums over all rows, rounded once; zeros where there are no rows
+ *   workspace    esc_layer_norm_backward_workspace_bytes(...) bytes, 256-byte aligned, no preparation needed
+ * Every sum has a fixed order: the same input gives the same bits.  Calls, or graphs, that may run at the same time need a workspace each.
+ */
+size_t esc_layer_norm_backward_workspace_bytes(long long rows, int C);     /* 0 for invalid arguments */
+int esc_layer_norm_backward(const void* x, long long x_stride, const void* weight, float eps, const void* grad_y,
+                            const void* grad_skip, void* grad_x, void* grad_weight, void* grad_bias, long long rows, int C,
+                            int dtype, int grad_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * ---- the block's linear layers: projections to q, k, v and back, the 1x1 convolutions of the feed-forward network ----
+ *
+ *   z[r, n] = sum_k x[r, k] weight[n, k] + bias[n];      out = act(z) + residual
+ *
+ *   x          [rows, K], rows `x_stride` values apart
+ *   weight     [N, K] dense (row = output);  bias [N] or NULL
+ *   activation ESC_ACT_NONE, ESC_ACT_RELU, ESC_ACT_GELU (z Phi(z) with the exact normal distribution function)
+ *   residual   [rows, N] dense or NULL
+ *   out        [rows, N] dense;  z [rows, N] dense or NULL: z as it is, rounded to the type, for the backward pass (act takes the
+ *              unrounded z)
+ * rows may be 0 and is below 2^31 - 4096; K and N are at most 2^20.  Sums in fp32, one rounding per output.
+ */
+enum { ESC_ACT_NONE = 0, ESC_ACT_RELU = 1, ESC_ACT_GELU = 2 };
+int esc_linear_forward(const void* x, long long x_stride, const void* weight, const void* bias, int activation,
+                       const void* residual, void* out, void* z, long long rows, int K, int N, int dtype, void* stream);
+
+/*
+ * Its gradients, with g = grad_out act'(z):  grad_x = g weight,  grad_weight = g^T x,  grad_bias = sum over rows of g.
+ *   z          what the forward pass wrote; not read, and may be NULL, with ESC_ACT_NONE.  act'(0) of ESC_ACT_RELU is 0.
+ *   grad_out   [rows, N] dense (also the residual's gradient, as it is)
+ *   grad_x     [rows, K] dense;  grad_weight [N, K] and grad_bias [N] of grad_dtype; each may be NULL.  No rows: zeros.
+ *   workspace  esc_linear_backward_workspace_bytes(...) bytes, 256-byte aligned, no preparation needed
+ * Every sum has a fixed order: the same input gives the same bits.  Calls, or graphs, that may run at the same time need a workspace each.
+ */
+size_t esc_linear_backward_workspace_bytes(long long rows, int K, int N, int activation, int dtype);   /* 0 for invalid arguments */
+int esc_linear_backward(const void* x, long long x_stride, const void* weight, const void* z, int activation,
+                        const void* grad_out, void* grad_x, void* grad_weight, void* grad_bias, long long rows, int K, int N,
+                        int dtype, int grad_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Self-test of the error path that every device-side wait of this library shares: launches one thread that waits, with
  * the kernels' own bounded waits, for a count that nothing raises and then on a barrier that nothing signals.  Each wait gives up
  * after its poll limit (about one second); the second, if the first one's record was right, records ESC_DEV_TIMEOUT in the status word of `workspace` (any initialised forward or backward workspace, device)
@@ -556,7 +614,7 @@ int esc_convattn_last_tile_width(void);
  * Returns ESC_ERR_UNSUPPORTED for any other value.  For tests and tuning. */
 int esc_convattn_set_tile_width(int tile_width);
 
-/* Number of kernels the last forward / stage / backward / attention / bias / AdamW call on this thread launched. */
+/* Number of kernels the last forward / stage / backward / attention / bias / AdamW / norm / linear call on this thread launched. */
 int esc_convattn_last_launches(void);
 
 const char* esc_status_string(int status);

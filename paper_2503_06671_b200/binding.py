@@ -86,6 +86,14 @@ def lib():
         L.esc_adamw_plan_init.argtypes = [i, vp, vp, vp, vp, vp, vp, vp, vp, i, i, i, vp, sz, vp, vp]
         L.esc_adamw_step.argtypes = [vp, ll, i, i, i, ll, dbl, dbl, dbl, dbl, dbl, dbl, vp, vp, vp]
         L.esc_adamw_scalars.argtypes = [ll, dbl, dbl, dbl, dbl, dbl, vp]
+        L.esc_layer_norm_forward.argtypes = [vp, ll, vp, vp, f, vp, ll, ll, i, i, vp]
+        L.esc_layer_norm_backward_workspace_bytes.argtypes = [ll, i]
+        L.esc_layer_norm_backward_workspace_bytes.restype = sz
+        L.esc_layer_norm_backward.argtypes = [vp, ll, vp, f, vp, vp, vp, vp, vp, ll, i, i, i, vp, sz, vp]
+        L.esc_linear_forward.argtypes = [vp, ll, vp, vp, i, vp, vp, vp, ll, i, i, i, vp]
+        L.esc_linear_backward_workspace_bytes.argtypes = [ll, i, i, i, i]
+        L.esc_linear_backward_workspace_bytes.restype = sz
+        L.esc_linear_backward.argtypes = [vp, ll, vp, vp, i, vp, vp, vp, vp, ll, i, i, i, i, vp, sz, vp]
         L.esc_convattn_set_tile_width.argtypes = [i]
         L.esc_convattn_set_stencil_engine.argtypes = [i]
         L.esc_convattn_set_fused_stage1.argtypes = [i]
@@ -97,6 +105,7 @@ def lib():
                      "esc_convattn_dynkernel", "esc_convattn_dynkernel_static", "esc_convattn_forward_mlp", "esc_convattn_dynkernel_mlp", "esc_convattn_forward_pw", "esc_convattn_stencil_pw", "esc_convattn_forward_dense", "esc_convattn_stencil_dense", "esc_convattn_forward_variant", "esc_convattn_backward", "esc_convattn_backward_mlp", "esc_convattn_backward_pw", "esc_convattn_backward_dense", "esc_convattn_backward_variant", "esc_conv_fuse_backward", "esc_convattn_stencil", "esc_convattn_forward_host", "esc_convattn_forward_host_submit", "esc_convattn_forward_host_wait",
                      "esc_relpos_bias_forward", "esc_relpos_bias_backward", "esc_window_attention_forward", "esc_window_attention_backward",
                      "esc_adamw_plan_init", "esc_adamw_step", "esc_adamw_scalars",
+                     "esc_layer_norm_forward", "esc_layer_norm_backward", "esc_linear_forward", "esc_linear_backward",
                      "esc_convattn_device_status", "esc_convattn_last_path", "esc_convattn_last_tile_width", "esc_convattn_set_tile_width", "esc_convattn_set_stencil_engine", "esc_convattn_set_fused_stage1", "esc_convattn_set_dense_engine", "esc_convattn_last_launches",
                      "esc_version"):
             getattr(L, name).restype = i
@@ -764,3 +773,150 @@ def esc_adamw_step(plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_deca
             plan.table.record_stream(_torch_stream(stream, plan.table.device))
         _check(lib().esc_adamw_step(_address(plan.table), plan.n_chunks, plan.param_dtype, plan.grad_dtype, plan.states, int(step), lr, beta1, beta2, eps,
                                     weight_decay, grad_scale, _address(scalars), _address(skip), at), "esc_adamw_step")
+
+
+# ---- layer norm and linear layers ---------------------------------------------------------------------------------------------
+
+
+ESC_ACT_NONE, ESC_ACT_RELU, ESC_ACT_GELU = 0, 1, 2
+
+
+def _rows_of(name, t):
+    """(rows, channels, values between rows) of a tensor [..., channels] whose rows are dense and evenly spaced."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) < 1 or shape[-1] < 1:
+        raise ValueError(f"{name} has to be [..., channels], not {tuple(shape)}")
+    C, rows, step = shape[-1], 1, None
+    even = strides[-1] == 1 or C == 1
+    for n, s in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+        if n != 1 and step is None:
+            step = s                                                    # the innermost axis that has more than one entry
+        elif n > 1:
+            even = even and s == step * rows
+        rows *= n
+    step = C if step is None or rows <= 1 else step
+    if rows and (not even or step < C):
+        raise ValueError(f"the rows of {name} have to be dense in their channels, evenly spaced and apart")
+    return rows, C, max(step, C)
+
+
+def _like_rows(name, t, shape, dtype):
+    """A dense tensor of as many rows as x, of the given width."""
+    if t is None:
+        return
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} has to be a contiguous {tuple(shape)} tensor of {dtype}, not {tuple(t.shape)} of {t.dtype}")
+
+
+def _grad_code(*grads):
+    """Type of the weights' gradients; they have one."""
+    types = {g.dtype for g in grads if g is not None}
+    if len(types) > 1:
+        raise ValueError("the weights' gradients have to be of one type")
+    return next((_dtype_code(g) for g in grads if g is not None), ESC_F32)
+
+
+def esc_layer_norm_forward(x, weight, bias, eps, y, stream=None):
+    """y = (x - mean) / sqrt(var + eps) * weight + bias over the last axis of x [..., C]; weight and bias [C], or None.  Rows of x and y may be
+    slices of wider tensors."""
+    rows, C, step = _rows_of("x", x)
+    y_rows, _, y_step = _rows_of("y", y)
+    if y.shape != x.shape or y.dtype != x.dtype:
+        raise ValueError("y has to be of x's shape and type")
+    _dense("weight", weight, (C,), x.dtype)
+    _dense("bias", bias, (C,), x.dtype)
+    with _on_device(x, weight, bias, y):
+        _check(lib().esc_layer_norm_forward(_address(x), step, _address(weight), _address(bias), eps, _address(y), y_step, rows, C, _dtype_code(x),
+                                            _stream_address(stream)), "esc_layer_norm_forward")
+    return y
+
+
+def esc_layer_norm_backward_workspace_bytes(rows, C) -> int:
+    return int(lib().esc_layer_norm_backward_workspace_bytes(rows, C))
+
+
+def new_layer_norm_workspace(rows, C, device="cuda"):
+    """Scratch of esc_layer_norm_backward."""
+    import torch
+
+    n = esc_layer_norm_backward_workspace_bytes(rows, C)
+    if n == 0:
+        raise ValueError("invalid problem size")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def esc_layer_norm_backward(x, weight, eps, grad_y, grad_x, grad_weight=None, grad_bias=None, grad_skip=None, workspace=None, stream=None):
+    """Gradients of esc_layer_norm_forward; grad_skip (like x, or None) is added to grad_x.  grad_weight, grad_bias: fp32 or bf16."""
+    rows, C, step = _rows_of("x", x)
+    _dense("weight", weight, (C,), x.dtype)
+    for name, t in (("grad_y", grad_y), ("grad_x", grad_x), ("grad_skip", grad_skip)):
+        _like_rows(name, t, x.shape, x.dtype)
+    for name, t in (("grad_weight", grad_weight), ("grad_bias", grad_bias)):
+        _dense(name, t, (C,), None if t is None else t.dtype)
+    with _on_device(x, weight, grad_y, grad_x, grad_weight, grad_bias, grad_skip, workspace):
+        if workspace is None:
+            with _allocating_for(stream, x.device):
+                workspace = new_layer_norm_workspace(rows, C)
+        _check(lib().esc_layer_norm_backward(_address(x), step, _address(weight), eps, _address(grad_y), _address(grad_skip), _address(grad_x), _address(grad_weight),
+                                             _address(grad_bias), rows, C, _dtype_code(x), _grad_code(grad_weight, grad_bias), _address(workspace),
+                                             workspace.numel() * workspace.element_size(), _stream_address(stream)), "esc_layer_norm_backward")
+    return grad_x, grad_weight, grad_bias
+
+
+def esc_linear_forward(x, weight, bias, activation, out, residual=None, z=None, stream=None):
+    """out = act(x weight^T + bias) + residual for x [..., K], weight [N, K], bias [N] (or None), residual like out [..., N] (or None); z (like out,
+    or None) gets x weight^T + bias, which esc_linear_backward takes where there is an activation."""
+    rows, K, step = _rows_of("x", x)
+    N = int(weight.shape[0])
+    _dense("weight", weight, (N, K), x.dtype)
+    _dense("bias", bias, (N,), x.dtype)
+    shape = x.shape[:-1] + (N,)
+    for name, t in (("out", out), ("residual", residual), ("z", z)):
+        _like_rows(name, t, shape, x.dtype)
+    with _on_device(x, weight, bias, out, residual, z):
+        _check(lib().esc_linear_forward(_address(x), step, _address(weight), _address(bias), activation, _address(residual), _address(out), _address(z),
+                                        rows, K, N, _dtype_code(x), _stream_address(stream)), "esc_linear_forward")
+    return out
+
+
+def _code_of(dtype):
+    import torch
+
+    codes = {torch.float32: ESC_F32, torch.bfloat16: ESC_BF16}
+    if dtype not in codes:
+        raise TypeError(f"unsupported dtype {dtype}")
+    return codes[dtype]
+
+
+def esc_linear_backward_workspace_bytes(rows, K, N, activation, dtype) -> int:
+    return int(lib().esc_linear_backward_workspace_bytes(rows, K, N, activation, _code_of(dtype)))
+
+
+def new_linear_workspace(rows, K, N, activation, dtype, device="cuda"):
+    """Scratch of esc_linear_backward for tensors of this (torch) type."""
+    import torch
+
+    n = esc_linear_backward_workspace_bytes(rows, K, N, activation, dtype)
+    if n == 0:
+        raise ValueError("invalid problem size")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def esc_linear_backward(x, weight, z, activation, grad_out, grad_x=None, grad_weight=None, grad_bias=None, workspace=None, stream=None):
+    """Gradients of esc_linear_forward; z is what that call wrote (None without an activation), grad_out is the residual's gradient too.
+    grad_weight, grad_bias: fp32 or bf16; any of the gradients may be None."""
+    rows, K, step = _rows_of("x", x)
+    N = int(weight.shape[0])
+    _dense("weight", weight, (N, K), x.dtype)
+    for name, t, width in (("z", z, N), ("grad_out", grad_out, N), ("grad_x", grad_x, K)):
+        _like_rows(name, t, x.shape[:-1] + (width,), x.dtype)
+    _dense("grad_weight", grad_weight, (N, K), None if grad_weight is None else grad_weight.dtype)
+    _dense("grad_bias", grad_bias, (N,), None if grad_bias is None else grad_bias.dtype)
+    with _on_device(x, weight, z, grad_out, grad_x, grad_weight, grad_bias, workspace):
+        if workspace is None:
+            with _allocating_for(stream, x.device):
+                workspace = new_linear_workspace(rows, K, N, activation, x.dtype)
+        _check(lib().esc_linear_backward(_address(x), step, _address(weight), _address(z), activation, _address(grad_out), _address(grad_x), _address(grad_weight),
+                                         _address(grad_bias), rows, K, N, _dtype_code(x), _grad_code(grad_weight, grad_bias), _address(workspace),
+                                         workspace.numel() * workspace.element_size(), _stream_address(stream)), "esc_linear_backward")
+    return grad_x, grad_weight, grad_bias
