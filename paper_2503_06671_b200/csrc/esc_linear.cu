@@ -3,12 +3,13 @@
 
 #include <algorithm>
 
-#include "linear.cuh"
+#include "linear_umma.cuh"
 
 namespace {
 
 namespace abi = esc::abi;
 namespace lin = esc::linear;
+namespace um = esc::linear::umma;
 using namespace esc::rows;
 using bf16 = __nv_bfloat16;
 
@@ -47,59 +48,152 @@ template <typename T> lin::Layer<T> layer_of(const Call& c) {
     p.x_stride = c.x_stride; p.rows = c.rows; p.K = c.K; p.N = c.N; p.act = c.act;
     return p;
 }
-unsigned tiles(long long n) { return (unsigned)((n + lin::kTile - 1) / lin::kTile); }
 
-// The weights' gradient is summed over as many runs of rows as fill the SMs twice, of 256 rows or more.
-int grad_splits(const Call& c) {
-    const long long blocks = (long long)tiles(c.N) * tiles(c.K);
-    return (int)std::max(1LL, std::min((2LL * abi::sm_count() + blocks - 1) / blocks, (c.rows + 255) / 256));
+// ---- tensor-core products ----------------------------------------------------------------------------------------------------
+
+// What a product is cut into.  Times in cycles of an SM, from the rates below; the cheapest width of a tile and number of runs of rows.
+struct Cut {
+    int tiles_i, tiles_j, bn, splits, stages, grid;
+    bool resident;
+    size_t smem;
+};
+constexpr double kLoadRate = 35, kStoreRate = 20;   // bytes per cycle of one SM: from L2 into its ring, to memory
+Cut cut(lin::Role role, long long I, int J, long long depth, size_t es) {
+    const int sms = abi::sm_count(), step = role == lin::kForward ? 16 : 64, most = es == 4 ? um::most_columns<float> : um::most_columns<bf16>;
+    const int parts = es == 4 ? 3 : 1, products = es == 4 ? 6 : 1;
+    const long long blocks = (depth + um::kBlockC - 1) / um::kBlockC, tiles_i = (I + um::kBlockI - 1) / um::kBlockI;
+    const size_t fixed = um::kStageBytes + 512, out_es = role == lin::kGradW ? 4 : es;
+    Cut best{};
+    double least = 1e300;
+    for (int bn = std::min(most, (J + step - 1) / step * step); bn >= step; bn -= step) {
+        const long long tiles_j = ((long long)J + bn - 1) / bn;
+        const double rows = (double)std::min<long long>(I, um::kBlockI);
+        const double mma = 4.0 * products * std::max(40.0, bn / 2.0), load = (rows + bn) * um::kBlockC * es / kLoadRate, store = rows * bn * out_es / kStoreRate;
+        // runs of rows: one, or as many as fill the SMs one to four times
+        for (int fill = 0; fill <= (role == lin::kGradW ? 4 : 0); ++fill) {
+            const long long splits = fill == 0 ? 1 : std::min<long long>(blocks, (long long)fill * sms / (tiles_i * tiles_j));
+            const long long units = tiles_i * tiles_j * splits, waves = (units + sms - 1) / sms;
+            if (splits < 1 || units > 0x7fffffffLL) continue;
+            const double body = (double)((blocks + splits - 1) / splits) * std::max(mma, load);
+            double cost = (double)waves * (std::max(body, store) + 200) + std::min(body, store) + 1500;
+            if (role == lin::kGradW) cost += 2.0 * splits * I * J * 4 / (kStoreRate * sms);
+            if (cost < least * 0.995) {
+                least = cost;
+                best = Cut{(int)tiles_i, (int)tiles_j, bn, (int)splits, 0, (int)std::min<long long>(units, sms), false, 0};
+            }
+        }
+    }
+    if (best.bn == 0) return best;
+    const size_t b_bytes = (size_t)best.bn * 128 * parts, a_bytes = (size_t)um::kABytes * parts;
+    // the weights stay where they leave room for a ring of rows and a block has several tiles
+    best.resident = role != lin::kGradW && blocks * b_bytes <= 96 * 1024 && best.tiles_j <= sms && (long long)best.tiles_i * best.tiles_j >= 2LL * sms;
+    if (best.resident) best.grid = sms / best.tiles_j * best.tiles_j;
+    const size_t kept = best.resident ? blocks * b_bytes : 0, stage = a_bytes + (best.resident ? 0 : b_bytes);
+    best.stages = (int)std::min<size_t>(um::kMaxStages, (um::kMostSmem - fixed - kept) / stage);
+    best.smem = best.stages * stage + kept + fixed;
+    return best;
 }
-int bias_parts(const Call& c) {
-    const long long across = (c.N + 31) / 32;
-    return (int)std::max(1LL, std::min((8LL * abi::sm_count() + across - 1) / across, (c.rows + 63) / 64));
+
+bool map_rows(CUtensorMap* m, const void* base, long long rows, long long width, long long stride, int box_rows) {
+    const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, ones[2] = {1, 1};
+    um::EncodeTiledFn fn = um::encode_fn();
+    return fn && fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-struct LinearWs { float *part, *bias; size_t bytes; };
+
+// Operands as they lie: a is [a_rows, a_width] with rows a_ld apart, b likewise.
+struct Operand { const void* p; long long rows, width, ld; };
+bool whole_pieces(const Operand& o) { return abi::aligned(o.p, 16) && o.ld % 8 == 0; }
+
+template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, const Operand& a, const Operand& b, const Cut& c, cudaStream_t st) {
+    p.tiles_i = c.tiles_i; p.tiles_j = c.tiles_j; p.bn = c.bn; p.splits = c.splits; p.stages = c.stages; p.resident = c.resident;
+    p.units = (long long)c.tiles_i * c.tiles_j * c.splits;
+    p.a = static_cast<const T*>(a.p); p.b = static_cast<const T*>(b.p); p.a_ld = a.ld; p.b_ld = b.ld;
+    CUtensorMap ma{}, mb{};
+    auto launch = [&](auto kernel, int warps) {
+        ESC_ABI_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)um::kMostSmem));   // the same for every call
+        kernel<<<(unsigned)c.grid, 32 * warps, c.smem, st>>>(ma, mb, p);
+        return launched();
+    };
+    if constexpr (sizeof(T) == 2) {
+        constexpr bool a_mn = ROLE == lin::kGradW, b_mn = ROLE != lin::kForward;
+        if (!p.kept && whole_pieces(a) && whole_pieces(b) && map_rows(&ma, a.p, a.rows, a.width, a.ld, a_mn ? um::kBlockC : um::kBlockI) &&
+            map_rows(&mb, b.p, b.rows, b.width, b.ld, b_mn ? um::kBlockC : c.bn))
+            return launch(um::product_umma<T, ROLE, true>, um::kFirstFill);
+    }
+    return launch(um::product_umma<T, ROLE, false>, um::kFirstFill + um::kFillWarps);
+}
+
+// Partial sums of grad_bias: as many blocks as fill the SMs four times.
+struct BiasCut { int across, parts; };
+BiasCut bias_cut(const Call& c, bool pieces) {
+    const long long wide = pieces ? std::min(c.N / 8, 32) * 8 : 32, across = (c.N + wide - 1) / wide;
+    return {(int)across, (int)std::max(1LL, std::min((4LL * abi::sm_count() + across - 1) / across, (c.rows + 31) / 32))};
+}
+struct LinearWs { float *part, *bias; bf16* g; size_t bytes; };
 LinearWs carve(void* ws, const Call& c) {
     LinearWs w;
     char* base = static_cast<char*>(ws);
     size_t off = 0;
     auto take = [&](size_t bytes) { char* p = base + off; off += abi::round_up(bytes, 256); return p; };
-    w.part = reinterpret_cast<float*>(take((size_t)grad_splits(c) * c.N * c.K * sizeof(float)));
-    w.bias = reinterpret_cast<float*>(take((size_t)bias_parts(c) * c.N * sizeof(float)));
+    w.part = reinterpret_cast<float*>(take((size_t)cut(lin::kGradW, c.N, c.K, std::max(c.rows, 1LL), c.es()).splits * c.N * c.K * sizeof(float)));
+    w.bias = reinterpret_cast<float*>(take((size_t)std::max(bias_cut(c, false).parts, c.N % 8 ? 0 : bias_cut(c, true).parts) * c.N * sizeof(float)));
+    w.g = reinterpret_cast<bf16*>(take(c.dtype == ESC_BF16 && c.act != ESC_ACT_NONE && c.N % 8 == 0 ? (size_t)c.rows * c.N * sizeof(bf16) : 0));
     w.bytes = off;
     return w;
 }
 
-template <typename T> int linear_forward_t(const lin::Layer<T>& p, cudaStream_t st) {
-    lin::product<T, lin::kForward><<<dim3(tiles(p.rows), tiles(p.N)), 256, 0, st>>>(p);
-    return launched();
+template <typename T> int linear_forward_t(const Call& c, const lin::Layer<T>& l, cudaStream_t st) {
+    um::Args<T> p{};
+    p.I = c.rows; p.J = c.N; p.depth = c.K; p.act = c.act;
+    p.bias = l.b; p.residual = l.residual; p.out = l.out; p.z = l.z;
+    p.pieces = c.N % esc::Elem<T>::kVec == 0 && abi::aligned(l.b, 16) && abi::aligned(l.residual, 16) && abi::aligned(l.out, 16) && abi::aligned(l.z, 16);
+    return launch_product<T, lin::kForward>(p, {c.x, c.rows, c.K, c.x_stride}, {c.w, c.N, c.K, c.K}, cut(lin::kForward, c.rows, c.N, c.K, c.es()), st);
 }
 
-template <typename G> int launch_sum_parts(const float* part, int parts, long long count, void* out, cudaStream_t st) {
-    lin::sum_parts<G><<<(unsigned)std::min<long long>((count + 255) / 256, 8LL * abi::sm_count()), 256, 0, st>>>(part, parts, count, static_cast<G*>(out));
+template <typename G> int launch_sums(const float* part, int parts, long long count, void* out, cudaStream_t st) {
+    if (parts <= 8) lin::sum_few_parts<G><<<(unsigned)std::min<long long>((count + 1023) / 1024, 16LL * abi::sm_count()), 256, 0, st>>>(part, parts, count, static_cast<G*>(out));
+    else lin::sum_parts<G><<<(unsigned)((count + 31) / 32), 256, 0, st>>>(part, parts, count, static_cast<G*>(out));
     return launched();
 }
 int sum_to(const float* part, int parts, long long count, void* out, int grad_dtype, cudaStream_t st) {
-    return grad_dtype == ESC_F32 ? launch_sum_parts<float>(part, parts, count, out, st) : launch_sum_parts<bf16>(part, parts, count, out, st);
+    return grad_dtype == ESC_F32 ? launch_sums<float>(part, parts, count, out, st) : launch_sums<bf16>(part, parts, count, out, st);
 }
 
-template <typename T> int linear_backward_t(const Call& c, lin::Layer<T> p, void* gw, void* gb, int grad_dtype, const LinearWs& w, cudaStream_t st) {
-    if (p.gx) {
-        lin::product<T, lin::kGradX><<<dim3(tiles(p.rows), tiles(p.K)), 256, 0, st>>>(p);
+template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& l, void* gw, void* gb, int grad_dtype, const LinearWs& w, cudaStream_t st) {
+    const T *go = l.go, *kept = c.act == ESC_ACT_NONE ? nullptr : l.kept;
+    bool sums_there = false;
+    if constexpr (sizeof(T) == 2) {
+        if (c.N % 8 == 0 && abi::aligned(go, 16) && abi::aligned(kept, 16) && (kept || gb)) {
+            const BiasCut b = bias_cut(c, true);
+            bf16* g = kept && (l.gx || gw) ? w.g : nullptr;
+            lin::grad_z_pieces<<<dim3(b.across, b.parts), 256, 0, st>>>(l, g, gb ? w.bias : nullptr);
+            ESC_TRY(launched());
+            if (gb) ESC_TRY(sum_to(w.bias, b.parts, c.N, gb, grad_dtype, st));
+            if (g) { go = g; kept = nullptr; }
+            sums_there = true;
+        }
+    }
+    if (gb && !sums_there) {
+        const BiasCut b = bias_cut(c, false);
+        lin::grad_bias_parts<T><<<dim3(b.across, b.parts), 256, 0, st>>>(l, w.bias);
         ESC_TRY(launched());
+        ESC_TRY(sum_to(w.bias, b.parts, c.N, gb, grad_dtype, st));
+    }
+    if (l.gx) {
+        um::Args<T> p{};
+        p.I = c.rows; p.J = c.K; p.depth = c.N; p.act = c.act; p.kept = kept; p.out = l.gx;
+        p.pieces = c.K % esc::Elem<T>::kVec == 0 && abi::aligned(l.gx, 16);
+        ESC_TRY((launch_product<T, lin::kGradX>(p, {go, c.rows, c.N, c.N}, {c.w, c.N, c.K, c.K}, cut(lin::kGradX, c.rows, c.K, c.N, c.es()), st)));
     }
     if (gw) {
-        const int splits = grad_splits(c);
-        p.part = w.part;
-        lin::product<T, lin::kGradW><<<dim3(tiles(p.N), tiles(p.K), splits), 256, 0, st>>>(p);
-        ESC_TRY(launched());
-        ESC_TRY(sum_to(w.part, splits, (long long)p.N * p.K, gw, grad_dtype, st));
-    }
-    if (gb) {
-        const int parts = bias_parts(c);
-        lin::grad_bias_parts<T><<<dim3((p.N + 31) / 32, parts), 256, 0, st>>>(p, w.bias);
-        ESC_TRY(launched());
-        ESC_TRY(sum_to(w.bias, parts, p.N, gb, grad_dtype, st));
+        const Cut k = cut(lin::kGradW, c.N, c.K, c.rows, c.es());
+        um::Args<T> p{};
+        p.I = c.N; p.J = c.K; p.depth = c.rows; p.act = c.act; p.kept = kept; p.part = w.part;
+        p.pieces = c.K % 4 == 0;
+        ESC_TRY((launch_product<T, lin::kGradW>(p, {go, c.rows, c.N, c.N}, {c.x, c.rows, c.K, c.x_stride}, k, st)));
+        ESC_TRY(sum_to(w.part, k.splits, (long long)c.N * c.K, gw, grad_dtype, st));
     }
     return ESC_OK;
 }
@@ -127,7 +221,7 @@ int esc_linear_forward(const void* x, long long x_stride, const void* weight, co
         lin::Layer<T> p = layer_of<T>(c);
         p.b = static_cast<const T*>(bias); p.residual = static_cast<const T*>(residual);
         p.out = static_cast<T*>(out); p.z = static_cast<T*>(z);
-        return linear_forward_t<T>(p, st);
+        return linear_forward_t<T>(c, p, st);
     };
     return dtype == ESC_F32 ? go(float{}) : go(bf16{});
 }

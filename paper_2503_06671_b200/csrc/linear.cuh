@@ -25,7 +25,6 @@ template <typename T> struct Layer {
     T *out, *z;                         // [rows, N]; z may be null
     const T *go, *kept;                 // backward: [rows, N]; kept: z of the forward pass (null without an activation)
     T* gx;
-    float* part;                        // [splits][N][K]
 };
 
 template <typename T> __device__ __forceinline__ float grad_z(const Layer<T>& p, long long row, int n) {
@@ -34,68 +33,6 @@ template <typename T> __device__ __forceinline__ float grad_z(const Layer<T>& p,
 }
 
 enum Role { kForward, kGradX, kGradW };
-
-// D[i][j] = sum over c of A(i, c) B(j, c): 64 x 64 of D to a block, 4 x 4 to a thread.  kGradW splits the rows over blockIdx.z.
-constexpr int kTile = 64, kDepth = 16;
-template <typename T, Role ROLE> __global__ void __launch_bounds__(256) product(const Layer<T> p)
-{
-    __shared__ float as[kDepth][kTile + 4], bs[kDepth][kTile + 4];
-    const long long I = ROLE == kGradW ? p.N : p.rows, c_all = ROLE == kForward ? p.K : ROLE == kGradX ? p.N : p.rows;
-    const int J = ROLE == kForward ? p.N : p.K;
-    const long long i0 = (long long)blockIdx.x * kTile;
-    const int j0 = blockIdx.y * kTile, tid = threadIdx.x, ti = tid / 16, tj = tid % 16;
-    const long long c_begin = c_all * blockIdx.z / gridDim.z, c_end = c_all * (blockIdx.z + 1) / gridDim.z;
-    float acc[4][4] = {};
-    for (long long c0 = c_begin; c0 < c_end; c0 += kDepth) {
-        for (int e = tid; e < kTile * kDepth; e += 256) {
-            // neighbouring threads read neighbouring values
-            const int i = ROLE == kGradW ? e % kTile : e / kDepth, ca = ROLE == kGradW ? e / kTile : e % kDepth;
-            const int j = ROLE == kForward ? e / kDepth : e % kTile, cb = ROLE == kForward ? e % kDepth : e / kTile;
-            float a = 0.f, b = 0.f;
-            if (i0 + i < I && c0 + ca < c_end) {
-                if (ROLE == kForward) a = Elem<T>::to_f32(p.x[(i0 + i) * p.x_stride + c0 + ca]);
-                else a = ROLE == kGradX ? grad_z(p, i0 + i, (int)(c0 + ca)) : grad_z(p, c0 + ca, (int)(i0 + i));
-            }
-            if (j0 + j < J && c0 + cb < c_end) {
-                if (ROLE == kGradW) b = Elem<T>::to_f32(p.x[(c0 + cb) * p.x_stride + j0 + j]);
-                else b = Elem<T>::to_f32(ROLE == kForward ? p.w[(long long)(j0 + j) * p.K + c0 + cb] : p.w[(c0 + cb) * p.K + j0 + j]);
-            }
-            as[ca][i] = a;
-            bs[cb][j] = b;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int c = 0; c < kDepth; ++c) {
-            float a[4], b[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) { a[u] = as[c][ti * 4 + u]; b[u] = bs[c][tj * 4 + u]; }
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) acc[u][v] += a[u] * b[v];
-        }
-        __syncthreads();
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const long long i = i0 + ti * 4 + u;
-        if (i >= I) break;
-        for (int v = 0; v < 4; ++v) {
-            const int j = j0 + tj * 4 + v;
-            if (j >= J) break;
-            float d = acc[u][v];
-            if (ROLE == kGradW) p.part[((long long)blockIdx.z * p.N + i) * p.K + j] = d;
-            else if (ROLE == kGradX) p.gx[i * p.K + j] = Elem<T>::from_f32(d);
-            else {
-                if (p.b) d += Elem<T>::to_f32(p.b[j]);
-                if (p.z) p.z[i * p.N + j] = Elem<T>::from_f32(d);
-                d = act_of(p.act, d);
-                if (p.residual) d += Elem<T>::to_f32(p.residual[i * p.N + j]);
-                p.out[i * p.N + j] = Elem<T>::from_f32(d);
-            }
-        }
-    }
-}
 
 // Column sums of g: a block has 32 columns and every gridDim.y-th run of eight rows; part [gridDim.y][N].
 template <typename T> __global__ void __launch_bounds__(256) grad_bias_parts(const Layer<T> p, float* part)
@@ -113,14 +50,86 @@ template <typename T> __global__ void __launch_bounds__(256) grad_bias_parts(con
     part[(size_t)blockIdx.y * p.N + n] = s;
 }
 
-// out[e] = sum over `parts` of part[.][e], in order.
+// The same for bf16 rows of whole 16-byte pieces, and g itself where `g` is given: rounded to bf16, as the operand that two products read.
+// (The sums are of the unrounded g.)  A thread has eight columns and every so many rows; a block min(N / 8, 32) such pieces of a row.
+__global__ void __launch_bounds__(256) grad_z_pieces(const Layer<__nv_bfloat16> p, __nv_bfloat16* g, float* part)
+{
+    using bf16 = __nv_bfloat16;
+    __shared__ float acc[256 * 8];
+    const int all = p.N / 8, across = all < 32 ? all : 32, down = 256 / across;
+    const int col = threadIdx.x % across, v = blockIdx.x * across + col, r = threadIdx.x / across;
+    float sum[8] = {};
+    if (r < down && v < all) {
+#pragma unroll 2
+        for (long long row = (long long)blockIdx.y * down + r; row < p.rows; row += (long long)gridDim.y * down) {
+            const long long at = row * p.N + v * 8;
+            float f[8];
+            unpack16<bf16>(*reinterpret_cast<const uint4*>(p.go + at), f);
+            if (p.act != kActNone) {
+                float z[8];
+                unpack16<bf16>(*reinterpret_cast<const uint4*>(p.kept + at), z);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] *= act_slope(p.act, z[e]);
+            }
+            if (g) {
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
+                    w[e] = *reinterpret_cast<const uint32_t*>(&h);
+                }
+                *reinterpret_cast<uint4*>(g + at) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += f[e];
+        }
+    }
+    if (!part) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e * 256 + threadIdx.x] = sum[e];
+    __syncthreads();
+    for (int c = threadIdx.x; c < across * 8; c += 256) {
+        const int n = blockIdx.x * across * 8 + c;
+        if (n >= p.N) break;
+        float s = 0.f;
+        for (int q = 0; q < down; ++q) s += acc[c % 8 * 256 + q * across + c / 8];
+        part[(size_t)blockIdx.y * p.N + n] = s;
+    }
+}
+
+// out[e] = sum over `parts` of part[.][e]: 32 of them to a block, a warp takes every eighth part, the warps are added in order.
 template <typename G> __global__ void __launch_bounds__(256) sum_parts(const float* part, int parts, long long count, G* out)
 {
-    for (long long e = (long long)blockIdx.x * 256 + threadIdx.x; e < count; e += (long long)gridDim.x * 256) {
-        float s = 0.f;
+    __shared__ float acc[8][32];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const long long e = (long long)blockIdx.x * 32 + lane;
+    float s = 0.f;
+    if (e < count) {
 #pragma unroll 8
-        for (int i = 0; i < parts; ++i) s += __ldcg(part + (size_t)i * count + e);
-        out[e] = Elem<G>::from_f32(s);
+        for (int i = warp; i < parts; i += 8) s += __ldcg(part + (size_t)i * count + e);
+    }
+    acc[warp][lane] = s;
+    __syncthreads();
+    if (warp != 0 || e >= count) return;
+#pragma unroll
+    for (int v = 1; v < 8; ++v) s += acc[v][lane];
+    out[e] = Elem<G>::from_f32(s);
+}
+// The same for few parts of many sums: a thread has four of them.
+template <typename G> __global__ void __launch_bounds__(256) sum_few_parts(const float* part, int parts, long long count, G* out)
+{
+    for (long long e = ((long long)blockIdx.x * 256 + threadIdx.x) * 4; e < count; e += (long long)gridDim.x * 1024) {
+        float s[4] = {};
+        for (int i = 0; i < parts; ++i) {
+            const float* at = part + (size_t)i * count + e;
+            if (count % 4 == 0) {
+                const float4 v = __ldcg(reinterpret_cast<const float4*>(at));
+                s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
+            } else {
+                for (int q = 0; q < 4 && e + q < count; ++q) s[q] += __ldcg(at + q);
+            }
+        }
+        for (int q = 0; q < 4 && e + q < count; ++q) out[e + q] = Elem<G>::from_f32(s[q]);
     }
 }
 
