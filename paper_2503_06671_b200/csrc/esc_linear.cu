@@ -53,22 +53,34 @@ template <typename T> lin::Layer<T> layer_of(const Call& c) {
 
 // What a product is cut into.  Times in cycles of an SM, from the rates below; the cheapest width of a tile and number of runs of rows.
 struct Cut {
-    int tiles_i, tiles_j, bn, splits, stages, grid;
+    int tiles_i, tiles_j, bn, splits, stages, grid, slots;
     bool resident;
     size_t smem;
 };
+constexpr size_t kBarBytes = 1024 + um::kMostEpi * 256;        // barriers and strips
 constexpr double kLoadRate = 35, kStoreRate = 20;   // bytes per cycle of one SM: from L2 into its ring, to memory
-Cut cut(lin::Role role, long long I, int J, long long depth, size_t es) {
+Cut cut(lin::Role role, long long I, int J, long long depth, size_t es, bool tma, bool third = false) {
     const int sms = abi::sm_count(), step = role == lin::kForward ? 16 : 64, most = es == 4 ? um::most_columns<float> : um::most_columns<bf16>;
     const int parts = es == 4 ? 3 : 1, products = es == 4 ? 6 : 1;
     const long long blocks = (depth + um::kBlockC - 1) / um::kBlockC, tiles_i = (I + um::kBlockI - 1) / um::kBlockI;
-    const size_t fixed = um::kStageBytes + 512, out_es = role == lin::kGradW ? 4 : es;
+    const size_t out_es = role == lin::kGradW ? 4 : es, slot_bytes = (size_t)(tma ? um::epi_warps<true> : um::epi_warps<false>) * um::kSlotBytes;
+    const int unit = (int)(128 / out_es);                          // columns that leave together
     Cut best{};
     double least = 1e300;
     for (int bn = std::min(most, (J + step - 1) / step * step); bn >= step; bn -= step) {
         const long long tiles_j = ((long long)J + bn - 1) / bn;
-        const double rows = (double)std::min<long long>(I, um::kBlockI);
-        const double mma = 4.0 * products * std::max(40.0, bn / 2.0), load = (rows + bn) * um::kBlockC * es / kLoadRate, store = rows * bn * out_es / kStoreRate;
+        if (tiles_j > 1 && bn > unit && bn % unit != 0) continue;
+        // w stays where it leaves room for a ring of rows and a block has several tiles; results then have two slots, else the ring has the room
+        const size_t b_bytes = (size_t)bn * 128 * parts, a_bytes = (size_t)um::kABytes * parts;
+        const int two = tma ? 1 : 2;                               // 16 epilogue warps have a slot each, four have two
+        const long long most_kept = (long long)um::kMostSmem - (long long)((two + third) * slot_bytes + kBarBytes + 3 * a_bytes);
+        const bool resident = role != lin::kGradW && (long long)(blocks * b_bytes) <= most_kept && tiles_j <= sms && tiles_i * tiles_j >= 2LL * sms;
+        const int slots = resident ? two : 1;
+        const size_t fixed = (slots + third) * slot_bytes + kBarBytes, kept = resident ? blocks * b_bytes : 0, stage = a_bytes + (resident ? 0 : b_bytes);
+        const int stages = (int)std::min<long long>(um::kMaxStages, ((long long)um::kMostSmem - (long long)(fixed + kept)) / (long long)stage);
+        if (stages < 1 || (stages < 2 && bn > step)) continue;
+        const double rows = (double)std::min<long long>(I, um::kBlockI), b_rows = resident ? 0 : bn;
+        const double mma = 4.0 * products * std::max(40.0, bn / 2.0), load = (rows + b_rows) * um::kBlockC * es / kLoadRate, store = rows * bn * out_es / kStoreRate;
         // runs of rows: one, or as many as fill the SMs one to four times
         for (int fill = 0; fill <= (role == lin::kGradW ? 4 : 0); ++fill) {
             const long long splits = fill == 0 ? 1 : std::min<long long>(blocks, (long long)fill * sms / (tiles_i * tiles_j));
@@ -79,50 +91,59 @@ Cut cut(lin::Role role, long long I, int J, long long depth, size_t es) {
             if (role == lin::kGradW) cost += 2.0 * splits * I * J * 4 / (kStoreRate * sms);
             if (cost < least * 0.995) {
                 least = cost;
-                best = Cut{(int)tiles_i, (int)tiles_j, bn, (int)splits, 0, (int)std::min<long long>(units, sms), false, 0};
+                best = Cut{(int)tiles_i, (int)tiles_j, bn, (int)splits, stages, resident ? (int)(sms / tiles_j * tiles_j) : (int)std::min<long long>(units, sms), slots, resident,
+                           stages * stage + kept + fixed};
             }
         }
     }
-    if (best.bn == 0) return best;
-    const size_t b_bytes = (size_t)best.bn * 128 * parts, a_bytes = (size_t)um::kABytes * parts;
-    // the weights stay where they leave room for a ring of rows and a block has several tiles
-    best.resident = role != lin::kGradW && blocks * b_bytes <= 96 * 1024 && best.tiles_j <= sms && (long long)best.tiles_i * best.tiles_j >= 2LL * sms;
-    if (best.resident) best.grid = sms / best.tiles_j * best.tiles_j;
-    const size_t kept = best.resident ? blocks * b_bytes : 0, stage = a_bytes + (best.resident ? 0 : b_bytes);
-    best.stages = (int)std::min<size_t>(um::kMaxStages, (um::kMostSmem - fixed - kept) / stage);
-    best.smem = best.stages * stage + kept + fixed;
     return best;
 }
 
-bool map_rows(CUtensorMap* m, const void* base, long long rows, long long width, long long stride, int box_rows) {
-    const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
-    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, ones[2] = {1, 1};
+// Matrices [batch, rows, width] whose rows are `ld` values apart, in boxes of 128 bytes of `box_rows` rows.
+template <typename T> bool map_of(CUtensorMap* m, const void* base, long long batch, long long rows, long long width, long long ld, int box_rows) {
+    constexpr size_t es = sizeof(T);
+    const bool flat = batch == 0;                                  // two dimensions
+    const cuuint64_t dims[3] = {(cuuint64_t)width, (cuuint64_t)rows, (cuuint64_t)batch}, strides[2] = {(cuuint64_t)ld * es, (cuuint64_t)rows * ld * es};
+    const cuuint32_t box[3] = {128 / es, (cuuint32_t)box_rows, 1}, ones[3] = {1, 1, 1};
     um::EncodeTiledFn fn = um::encode_fn();
-    return fn && fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                    CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return fn && fn(m, es == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, flat ? 2 : 3, const_cast<void*>(base), dims, strides, box, ones,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+bool whole_pieces(const void* p, long long ld, size_t es) { return abi::aligned(p, 16) && (size_t)ld * es % 16 == 0; }
 
-// Operands as they lie: a is [a_rows, a_width] with rows a_ld apart, b likewise.
-struct Operand { const void* p; long long rows, width, ld; };
-bool whole_pieces(const Operand& o) { return abi::aligned(o.p, 16) && o.ld % 8 == 0; }
-
-template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, const Operand& a, const Operand& b, const Cut& c, cudaStream_t st) {
-    p.tiles_i = c.tiles_i; p.tiles_j = c.tiles_j; p.bn = c.bn; p.splits = c.splits; p.stages = c.stages; p.resident = c.resident;
-    p.units = (long long)c.tiles_i * c.tiles_j * c.splits;
-    p.a = static_cast<const T*>(a.p); p.b = static_cast<const T*>(b.p); p.a_ld = a.ld; p.b_ld = b.ld;
-    CUtensorMap ma{}, mb{};
+// The result lies in memory as O [splits, I, J].  Returns the number of splits through `splits`.
+template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long long depth, cudaStream_t st, int* splits = nullptr) {
+    using O = typename um::Result<T, ROLE>::type;
+    constexpr bool a_mn = ROLE == lin::kGradW, b_mn = ROLE != lin::kForward;
+    constexpr int V = esc::Elem<T>::kVec;
+    const bool a_pieces = whole_pieces(p.a.p, p.a.ld, sizeof(T)), b_pieces = whole_pieces(p.b.p, p.b.ld, sizeof(T));
+    CUtensorMap ma{}, mb{}, mo{}, mr{}, mz{};
+    p.a_rows = (int)std::min<long long>(um::kBlockI, (p.I + 7) / 8 * 8);
+    bool tma = sizeof(T) == 2 && !p.a.kept && a_pieces && b_pieces && map_of<T>(&ma, p.a.p, 0, p.a.rows, p.a.width, p.a.ld, a_mn ? um::kBlockC : p.a_rows);
+    Cut c = cut(ROLE, p.I, p.J, depth, sizeof(T), tma, p.z && p.residual);
+    if (tma && !map_of<T>(&mb, p.b.p, 0, p.b.rows, p.b.width, p.b.ld, b_mn ? um::kBlockC : c.bn)) {
+        tma = false;
+        c = cut(ROLE, p.I, p.J, depth, sizeof(T), tma, p.z && p.residual);
+    }
+    p.tiles_i = c.tiles_i; p.tiles_j = c.tiles_j; p.bn = c.bn; p.splits = c.splits; p.stages = c.stages; p.resident = c.resident; p.slots = c.slots;
+    p.blocks = (int)((depth + um::kBlockC - 1) / um::kBlockC);
+    p.units = (unsigned)((long long)c.tiles_i * c.tiles_j * c.splits);
+    if (splits) *splits = c.splits;
+    const void* out = p.out;
+    if constexpr (ROLE == lin::kGradW) out = p.part;
+    p.by_tma = (c.tiles_j == 1 || c.bn % (int)(128 / sizeof(O)) == 0) && whole_pieces(out, p.J, sizeof(O)) && map_of<O>(&mo, out, c.splits, p.I, p.J, p.J, 32) &&
+               abi::aligned(p.bias, 16) && (!p.residual || (whole_pieces(p.residual, p.J, sizeof(T)) && map_of<T>(&mr, p.residual, 1, p.I, p.J, p.J, 32))) &&
+               (!p.z || (whole_pieces(p.z, p.J, sizeof(T)) && map_of<T>(&mz, p.z, 1, p.I, p.J, p.J, 32)));
+    p.a.pieces = a_pieces && p.a.width % V == 0 && abi::aligned(p.a.kept, 16);
+    p.b.pieces = b_pieces && p.b.width % V == 0;
     auto launch = [&](auto kernel, int warps) {
         ESC_ABI_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)um::kMostSmem));   // the same for every call
-        kernel<<<(unsigned)c.grid, 32 * warps, c.smem, st>>>(ma, mb, p);
+        kernel<<<(unsigned)c.grid, 32 * warps, c.smem, st>>>(ma, mb, mo, mr, mz, p);
         return launched();
     };
-    if constexpr (sizeof(T) == 2) {
-        constexpr bool a_mn = ROLE == lin::kGradW, b_mn = ROLE != lin::kForward;
-        if (!p.kept && whole_pieces(a) && whole_pieces(b) && map_rows(&ma, a.p, a.rows, a.width, a.ld, a_mn ? um::kBlockC : um::kBlockI) &&
-            map_rows(&mb, b.p, b.rows, b.width, b.ld, b_mn ? um::kBlockC : c.bn))
-            return launch(um::product_umma<T, ROLE, true>, um::kFirstFill);
-    }
-    return launch(um::product_umma<T, ROLE, false>, um::kFirstFill + um::kFillWarps);
+    if constexpr (sizeof(T) == 2)
+        if (tma) return launch(um::product_umma<T, ROLE, true>, um::all_warps<true>);
+    return launch(um::product_umma<T, ROLE, false>, um::all_warps<false>);
 }
 
 // Partial sums of grad_bias: as many blocks as fill the SMs four times.
@@ -137,19 +158,24 @@ LinearWs carve(void* ws, const Call& c) {
     char* base = static_cast<char*>(ws);
     size_t off = 0;
     auto take = [&](size_t bytes) { char* p = base + off; off += abi::round_up(bytes, 256); return p; };
-    w.part = reinterpret_cast<float*>(take((size_t)cut(lin::kGradW, c.N, c.K, std::max(c.rows, 1LL), c.es()).splits * c.N * c.K * sizeof(float)));
+    w.part = reinterpret_cast<float*>(take((size_t)std::max(cut(lin::kGradW, c.N, c.K, std::max(c.rows, 1LL), c.es(), false).splits, cut(lin::kGradW, c.N, c.K, std::max(c.rows, 1LL), c.es(), true).splits) *
+                                          c.N * c.K * sizeof(float)));
     w.bias = reinterpret_cast<float*>(take((size_t)std::max(bias_cut(c, false).parts, c.N % 8 ? 0 : bias_cut(c, true).parts) * c.N * sizeof(float)));
     w.g = reinterpret_cast<bf16*>(take(c.dtype == ESC_BF16 && c.act != ESC_ACT_NONE && c.N % 8 == 0 ? (size_t)c.rows * c.N * sizeof(bf16) : 0));
     w.bytes = off;
     return w;
 }
 
+template <typename T> um::Source<T> source(const void* p, long long rows, long long width, long long ld, const T* kept = nullptr, int act = 0) {
+    return um::Source<T>{static_cast<const T*>(p), kept, rows, width, ld, act, false};
+}
+
 template <typename T> int linear_forward_t(const Call& c, const lin::Layer<T>& l, cudaStream_t st) {
     um::Args<T> p{};
-    p.I = c.rows; p.J = c.N; p.depth = c.K; p.act = c.act;
+    p.I = c.rows; p.J = c.N; p.act = c.act;
+    p.a = source<T>(c.x, c.rows, c.K, c.x_stride); p.b = source<T>(c.w, c.N, c.K, c.K);
     p.bias = l.b; p.residual = l.residual; p.out = l.out; p.z = l.z;
-    p.pieces = c.N % esc::Elem<T>::kVec == 0 && abi::aligned(l.b, 16) && abi::aligned(l.residual, 16) && abi::aligned(l.out, 16) && abi::aligned(l.z, 16);
-    return launch_product<T, lin::kForward>(p, {c.x, c.rows, c.K, c.x_stride}, {c.w, c.N, c.K, c.K}, cut(lin::kForward, c.rows, c.N, c.K, c.es()), st);
+    return launch_product<T, lin::kForward>(p, c.K, st);
 }
 
 template <typename G> int launch_sums(const float* part, int parts, long long count, void* out, cudaStream_t st) {
@@ -181,19 +207,20 @@ template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& 
         ESC_TRY(launched());
         ESC_TRY(sum_to(w.bias, b.parts, c.N, gb, grad_dtype, st));
     }
+    const um::Source<T> g = source<T>(go, c.rows, c.N, c.N, kept, c.act);
     if (l.gx) {
         um::Args<T> p{};
-        p.I = c.rows; p.J = c.K; p.depth = c.N; p.act = c.act; p.kept = kept; p.out = l.gx;
-        p.pieces = c.K % esc::Elem<T>::kVec == 0 && abi::aligned(l.gx, 16);
-        ESC_TRY((launch_product<T, lin::kGradX>(p, {go, c.rows, c.N, c.N}, {c.w, c.N, c.K, c.K}, cut(lin::kGradX, c.rows, c.K, c.N, c.es()), st)));
+        p.I = c.rows; p.J = c.K;
+        p.a = g; p.b = source<T>(c.w, c.N, c.K, c.K); p.out = l.gx;
+        ESC_TRY((launch_product<T, lin::kGradX>(p, c.N, st)));
     }
     if (gw) {
-        const Cut k = cut(lin::kGradW, c.N, c.K, c.rows, c.es());
         um::Args<T> p{};
-        p.I = c.N; p.J = c.K; p.depth = c.rows; p.act = c.act; p.kept = kept; p.part = w.part;
-        p.pieces = c.K % 4 == 0;
-        ESC_TRY((launch_product<T, lin::kGradW>(p, {go, c.rows, c.N, c.N}, {c.x, c.rows, c.K, c.x_stride}, k, st)));
-        ESC_TRY(sum_to(w.part, k.splits, (long long)c.N * c.K, gw, grad_dtype, st));
+        p.I = c.N; p.J = c.K;
+        p.a = g; p.b = source<T>(c.x, c.rows, c.K, c.x_stride); p.part = w.part;
+        int splits;
+        ESC_TRY((launch_product<T, lin::kGradW>(p, c.rows, st, &splits)));
+        ESC_TRY(sum_to(w.part, splits, (long long)c.N * c.K, gw, grad_dtype, st));
     }
     return ESC_OK;
 }

@@ -28,8 +28,11 @@ namespace esc { namespace linear { namespace umma {
 
 constexpr int kBlockI = 128, kBlockC = 64;
 constexpr int kABytes = kBlockI * kBlockC * 2;                     // of one part
-constexpr int kEpiWarps = 8, kFillWarps = 8, kFirstEpi = 4, kFirstFill = kFirstEpi + kEpiWarps;
-constexpr int kStageBytes = kEpiWarps * 32 * 32 * 4;               // staging of the epilogue
+constexpr int kFillWarps = 16, kGroupWarps = 8, kFirstEpi = 4;         // a group fills every other block
+template <bool TMA> constexpr int epi_warps = TMA ? 16 : 4;
+template <bool TMA> constexpr int all_warps = kFirstEpi + epi_warps<TMA> + (TMA ? 0 : kFillWarps);
+constexpr int kMostEpi = 16;
+constexpr int kSlotBytes = 32 * 128;                               // staging of an epilogue warp: 128 bytes of 32 rows; two or three of them
 constexpr int kMaxStages = 8;
 constexpr size_t kMostSmem = 227 * 1024;
 constexpr int kTmemBuffer = 256;                                   // columns of one tile's sums
@@ -52,6 +55,15 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, unsigned parity, unsigne
     if (threadIdx.x % 32 == 0) { atomicExch(&wait_status[0], kDevTimeout); atomicExch(&wait_status[1], where); }
     return false;
 }
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                  ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
@@ -78,214 +90,287 @@ __device__ __forceinline__ void commit(uint32_t bar) {
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
-                   "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-                 : "r"(at) : "memory");
+__device__ __forceinline__ void tmem_ld(uint32_t at, float (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]),
+                   "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tmem_ld(uint32_t at, float (&r)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]) : "r"(at) : "memory");
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
+// Loads that stay where they are written: a batch of them is under way before the first value is used.
+__device__ __forceinline__ uint4 ld_piece(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ float ld_value(const float* p) {
+    float v;
+    asm volatile("ld.global.nc.b32 %0, [%1];" : "=f"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ __nv_bfloat16 ld_value(const __nv_bfloat16* p) {
+    unsigned short v;
+    asm volatile("ld.global.nc.b16 %0, [%1];" : "=h"(v) : "l"(p));
+    return __ushort_as_bfloat16(v);
+}
+
+// What a warp group loads of one operand: rows of `width` values, `ld` apart; `pieces`: rows are whole aligned 16-byte pieces.
+template <typename T> struct Source {
+    const T *p, *kept;
+    long long rows, width, ld;
+    int act;
+    bool pieces;
+};
+
 template <typename T> struct Args {
-    long long I, depth;
-    int J, tiles_i, tiles_j, bn, splits, stages;
+    long long I;
+    int J, tiles_i, tiles_j, bn, blocks, splits, stages;   // blocks: of c
     bool resident;                      // B stays in shared memory; a block keeps its tile of j
-    long long units;
-    const T *a, *b;                     // as they lie: rows of a_ld, b_ld values
-    long long a_ld, b_ld;
-    const T* kept;                      // with an activation: A = a act'(kept), laid out like a (plain loads only)
+    unsigned units;
+    Source<T> a, b;                     // plain loads; a.kept: A = a act'(kept)
+    int a_rows;                         // lines of A that TMA brings (K-major; the others' sums go nowhere)
     int act;
     const T *bias, *residual;
     T *out, *z;
     float* part;                        // kGradW: [splits][I][J]
-    bool pieces;                        // rows of the result, the bias and the residual are whole 16-byte pieces
+    bool by_tma;                        // results leave and residuals come by TMA: rows of whole aligned 16-byte pieces
+    int slots;                          // of an epilogue warp for residuals and results: one or two; z beside a residual has another
 };
 
 template <typename T> constexpr int parts_of = sizeof(T) == 4 ? 3 : 1;
 template <typename T> constexpr int most_columns = sizeof(T) == 4 ? 128 : 256;
 
-struct Unit { int i, j, split; long long c0, c1; bool live; };
-template <typename T> __device__ __forceinline__ Unit unit_of(const Args<T>& p, long long n) {
-    Unit u{};
-    const long long blocks = (p.depth + kBlockC - 1) / kBlockC;
-    if (p.resident) {
-        const long long i = blockIdx.x / p.tiles_j + n * (gridDim.x / p.tiles_j);
-        u.live = i < p.tiles_i;
-        u.i = (int)i; u.j = (int)(blockIdx.x % p.tiles_j); u.c0 = 0; u.c1 = blocks;
-        return u;
-    }
-    const long long t = blockIdx.x + n * gridDim.x;
-    u.live = t < p.units;
-    u.j = (int)(t % p.tiles_j);
-    u.i = (int)(t / p.tiles_j % p.tiles_i);
-    u.split = (int)(t / p.tiles_j / p.tiles_i);
-    u.c0 = blocks * u.split / p.splits; u.c1 = blocks * (u.split + 1) / p.splits;
-    return u;
+// A block's tiles, in the order of its loops.  32-bit arithmetic: a warp that does little else spends a tile's time on divisions.
+struct Walk {
+    unsigned t, step;                   // resident: tiles of i; else units
+    int i, j, split, c0, c1;
+    bool live;
+};
+template <typename T> __device__ __forceinline__ void place(Walk& w, const Args<T>& p) {
+    w.live = w.t < (p.resident ? (unsigned)p.tiles_i : p.units);
+    if (p.resident) { w.i = (int)w.t; return; }
+    const unsigned r = p.tiles_j == 1 ? w.t : w.t / (unsigned)p.tiles_j;
+    w.j = (int)(w.t - r * (unsigned)p.tiles_j);
+    w.split = (int)(r / (unsigned)p.tiles_i);
+    w.i = (int)(r - (unsigned)w.split * (unsigned)p.tiles_i);
+    w.c0 = (int)((long long)p.blocks * w.split / p.splits);
+    w.c1 = (int)((long long)p.blocks * (w.split + 1) / p.splits);
 }
+template <typename T> __device__ __forceinline__ Walk walk(const Args<T>& p) {
+    Walk w{blockIdx.x, gridDim.x, 0, 0, 0, 0, p.blocks, false};
+    if (p.resident) { w.step /= (unsigned)p.tiles_j; w.t /= (unsigned)p.tiles_j; w.j = (int)(blockIdx.x % (unsigned)p.tiles_j); }
+    place(w, p);
+    return w;
+}
+template <typename T> __device__ __forceinline__ void next(Walk& w, const Args<T>& p) { w.t += w.step; place(w, p); }
 
 // ---- plain loads into swizzled lines ------------------------------------------------------------------------------------------
 
-struct Pair { float lo, hi; };
-__device__ __forceinline__ Pair load_pair(const float* p, int n, bool even) {
-    Pair v{0.f, 0.f};
-    if (n >= 2 && even) { const float2 f = *reinterpret_cast<const float2*>(p); v.lo = f.x; v.hi = f.y; return v; }
-    if (n >= 1) v.lo = p[0];
-    if (n >= 2) v.hi = p[1];
-    return v;
-}
-__device__ __forceinline__ Pair load_pair(const __nv_bfloat16* p, int n, bool) {
-    Pair v{0.f, 0.f};
-    if (n >= 2 && (reinterpret_cast<uintptr_t>(p) & 3) == 0) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
-        v.lo = __uint_as_float(w << 16); v.hi = __uint_as_float(w & 0xffff0000u);
-        return v;
-    }
-    if (n >= 1) v.lo = __bfloat162float(p[0]);
-    if (n >= 2) v.hi = __bfloat162float(p[1]);
-    return v;
-}
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 __device__ __forceinline__ void st_shared(uint32_t at, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
-__device__ __forceinline__ Pair less(Pair v, uint32_t part) { return Pair{v.lo - __uint_as_float(part << 16), v.hi - __uint_as_float(part & 0xffff0000u)}; }
+__device__ __forceinline__ void st_shared(uint32_t at, uint32_t v, uint32_t w) { asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(v), "r"(w) : "memory"); }
+__device__ __forceinline__ void st_shared(uint32_t at, uint4 v) { asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); }
+// The three bf16 parts of two values; the differences are exact.
+__device__ __forceinline__ void split(float a, float b, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+    hi = pack(a, b);
+    a -= __uint_as_float(hi << 16); b -= __uint_as_float(hi & 0xffff0000u);
+    mid = pack(a, b);
+    a -= __uint_as_float(mid << 16); b -= __uint_as_float(mid & 0xffff0000u);
+    lo = pack(a, b);
+}
 
-// One operand's block: `lines` lines of 64 values, a warp a line, a lane two values of it.  Line L: K-major row mn0 + L, columns from c0;
-// MN-major row c0 + L % 64, columns from mn0 + L / 64 * 64.  The parts of fp32 lie `part_bytes` apart.
-template <typename T, bool MN> __device__ __forceinline__ void fill(uint32_t dst, int lines, uint32_t part_bytes, const T* src, long long ld, const T* kept, int act,
-                                                                     long long mn0, long long mn_all, long long c0, long long c_all, int warp, int lane) {
-    constexpr int kBatch = 8;
-    const bool even = sizeof(T) == 4 && ld % 2 == 0 && (reinterpret_cast<uintptr_t>(src) & 7) == 0;
-    const bool even_kept = even && (reinterpret_cast<uintptr_t>(kept) & 7) == 0;
-    for (int first = warp; first < lines; first += kFillWarps * kBatch) {
-        Pair v[kBatch];
+
+// One operand's block: `lines` lines of 64 values.  Line L is row r0 + L from column c0 on (K-major), or row r0 + L % 64 from column
+// c0 + L / 64 * 64 on (MN-major).  What lies outside the matrix is zero.  Every load of a batch is issued before the first is used, none
+// is conditional (one that has nothing to read reads the matrix' first value).  The parts of fp32 lie `part_bytes` apart.
+template <typename T, bool MN, bool KEPT> __device__ __forceinline__ void fill_values(uint32_t dst, int lines, uint32_t part_bytes, const Source<T>& s, long long r0, long long c0, int warp, int lane) {
+    constexpr int kBatch = KEPT ? 2 : 4;
+    for (int first = warp; first < lines; first += kGroupWarps * kBatch) {
+        T lo[kBatch], hi[kBatch], zl[KEPT ? kBatch : 1], zh[KEPT ? kBatch : 1];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const int L = first + u * kFillWarps;
-            const long long row = MN ? c0 + L % kBlockC : mn0 + L, col = (MN ? mn0 + L / kBlockC * kBlockC : c0) + 2 * lane;
-            const long long left = (MN ? mn_all : c_all) - col;
-            const int n = L < lines && row < (MN ? c_all : mn_all) ? (left >= 2 ? 2 : left == 1 ? 1 : 0) : 0;
-            v[u] = load_pair(src + row * ld + col, n, even);
-            if (kept) {
-                const Pair z = load_pair(kept + row * ld + col, n, even_kept);
-                v[u].lo *= act_slope(act, z.lo);
-                v[u].hi *= act_slope(act, z.hi);
-            }
+            const int L = first + u * kGroupWarps;
+            const long long row = r0 + (MN ? L % kBlockC : L), col = c0 + (MN ? L / kBlockC * kBlockC : 0) + 2 * lane, at = row * s.ld + col;
+            const bool in = L < lines && row < s.rows, one = in && col < s.width, two = in && col + 1 < s.width;
+            lo[u] = ld_value(s.p + (one ? at : 0));
+            hi[u] = ld_value(s.p + (two ? at + 1 : 0));
+            if (KEPT) { zl[u] = ld_value(s.kept + (one ? at : 0)); zh[u] = ld_value(s.kept + (two ? at + 1 : 0)); }
+            if (!one) lo[u] = Elem<T>::from_f32(0.f);
+            if (!two) hi[u] = Elem<T>::from_f32(0.f);
         }
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const int L = first + u * kFillWarps;
+            const int L = first + u * kGroupWarps;
             if (L >= lines) break;
+            float a = Elem<T>::to_f32(lo[u]), b = Elem<T>::to_f32(hi[u]);
+            if (KEPT) {
+                float x = Elem<T>::to_f32(zl[u]), y = Elem<T>::to_f32(zh[u]);
+                slope_pair(s.act, x, y);
+                const bool in = r0 + (MN ? L % kBlockC : L) < s.rows;   // a slope that is not a number may be another value's
+                const long long col = c0 + (MN ? L / kBlockC * kBlockC : 0) + 2 * lane;
+                a = in && col < s.width ? a * x : 0.f;
+                b = in && col + 1 < s.width ? b * y : 0.f;
+            }
             const uint32_t at = dst + L * 128 + (((lane >> 2) ^ (L & 7)) << 4) + (lane & 3) * 4;
-            const uint32_t hi = pack(v[u].lo, v[u].hi);
-            st_shared(at, hi);
             if (sizeof(T) == 4) {
-                const Pair r = less(v[u], hi);
-                const uint32_t mid = pack(r.lo, r.hi);
-                st_shared(at + part_bytes, mid);
-                const Pair q = less(r, mid);
-                st_shared(at + 2 * part_bytes, pack(q.lo, q.hi));
+                uint32_t h, m, l;
+                split(a, b, h, m, l);
+                st_shared(at, h);
+                st_shared(at + part_bytes, m);
+                st_shared(at + 2 * part_bytes, l);
+            } else {
+                st_shared(at, pack(a, b));
             }
         }
     }
+}
+template <typename T, bool MN, bool KEPT> __device__ __forceinline__ void fill_pieces(uint32_t dst, int lines, uint32_t part_bytes, const Source<T>& s, long long r0, long long c0, int warp, int lane) {
+    constexpr int V = Elem<T>::kVec, per_line = 64 / V, at_once = 32 / per_line, kBatch = KEPT ? 2 : 4;
+    const int col0 = lane % per_line * V;
+    for (int first = warp * at_once + lane / per_line; first - lane / per_line < lines; first += kGroupWarps * at_once * kBatch) {
+        uint4 v[kBatch], z[KEPT ? kBatch : 1];
+        bool in[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int L = first + u * kGroupWarps * at_once;
+            const long long row = r0 + (MN ? L % kBlockC : L), col = c0 + (MN ? L / kBlockC * kBlockC : 0) + col0;
+            in[u] = L < lines && row < s.rows && col < s.width;
+            const long long at = in[u] ? row * s.ld + col : 0;
+            v[u] = ld_piece(s.p + at);
+            if (KEPT) z[u] = ld_piece(s.kept + at);
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int L = first + u * kGroupWarps * at_once;
+            if (L >= lines) break;
+            float f[V];
+            unpack16<T>(v[u], f);
+            if (KEPT) {
+                float x[V];
+                unpack16<T>(z[u], x);
+#pragma unroll
+                for (int e = 0; e < V; e += 2) {
+                    slope_pair(s.act, x[e], x[e + 1]);
+                    f[e] *= x[e]; f[e + 1] *= x[e + 1];
+                }
+            }
+            if (!in[u])
+#pragma unroll
+                for (int e = 0; e < V; ++e) f[e] = 0.f;
+            const uint32_t at = dst + L * 128 + ((((col0 * 2) >> 4) ^ (L & 7)) << 4) + (col0 * 2 & 15);
+            if (sizeof(T) == 4) {
+                uint32_t h[2], m[2], l[2];
+                split(f[0], f[1], h[0], m[0], l[0]);
+                split(f[2], f[3], h[1], m[1], l[1]);
+                st_shared(at, h[0], h[1]);
+                st_shared(at + part_bytes, m[0], m[1]);
+                st_shared(at + 2 * part_bytes, l[0], l[1]);
+            } else {
+                st_shared(at, make_uint4(pack(f[0], f[1]), pack(f[2], f[3]), pack(f[4 % V], f[5 % V]), pack(f[6 % V], f[7 % V])));
+            }
+        }
+    }
+}
+template <typename T, bool MN, bool KEPT> __device__ __forceinline__ void fill(uint32_t dst, int lines, uint32_t part_bytes, const Source<T>& s, long long r0, long long c0, int warp, int lane) {
+    if (s.pieces) fill_pieces<T, MN, KEPT>(dst, lines, part_bytes, s, r0, c0, warp, lane);
+    else fill_values<T, MN, KEPT>(dst, lines, part_bytes, s, r0, c0, warp, lane);
 }
 
 // ---- epilogue ---------------------------------------------------------------------------------------------------------------
 
-// Eight (bf16) or four (fp32) neighbouring columns of one row, which is a 16-byte piece of it.
-template <typename T> __device__ __forceinline__ void store16(T* p, const float* f);
-template <> __device__ __forceinline__ void store16<float>(float* p, const float* f) { *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]); }
-template <> __device__ __forceinline__ void store16<__nv_bfloat16>(__nv_bfloat16* p, const float* f) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack(f[0], f[1]), pack(f[2], f[3]), pack(f[4], f[5]), pack(f[6], f[7]));
+__device__ __forceinline__ uint4 ld_shared(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+template <typename O> __device__ __forceinline__ uint4 pack16(const float* f);
+template <> __device__ __forceinline__ uint4 pack16<float>(const float* f) { return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])); }
+template <> __device__ __forceinline__ uint4 pack16<__nv_bfloat16>(const float* f) { return make_uint4(pack(f[0], f[1]), pack(f[2], f[3]), pack(f[4], f[5]), pack(f[6], f[7])); }
+template <typename T, Role ROLE> struct Result { using type = T; };
+template <typename T> struct Result<T, kGradW> { using type = float; };
+
+template <typename T> __device__ __forceinline__ void add_piece(float* f, uint4 v);
+template <> __device__ __forceinline__ void add_piece<float>(float* f, uint4 v) {
+    un2(add2(f2(f[0], f[1]), f2(__uint_as_float(v.x), __uint_as_float(v.y))), f[0], f[1]);
+    un2(add2(f2(f[2], f[3]), f2(__uint_as_float(v.z), __uint_as_float(v.w))), f[2], f[3]);
+}
+template <> __device__ __forceinline__ void add_piece<__nv_bfloat16>(float* f, uint4 v) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) un2(add2(f2(f[2 * q], f[2 * q + 1]), f2(__uint_as_float(w[q] << 16), __uint_as_float(w[q] & 0xffff0000u))), f[2 * q], f[2 * q + 1]);
 }
 
-// 32 rows x 32 columns that this warp has staged, from row i0 and column j0 on; rows below `rows`, columns below `cols` of them are real.
-// O: type of the result; the epilogue of kForward adds bias, activation and residual.
-template <typename T, typename O, Role ROLE> __device__ __forceinline__ void write_chunk(const float* st, const Args<T>& p, O* out, long long i0, int rows, int j0, int cols, int lane) {
-    constexpr int V = Elem<O>::kVec, per_row = 32 / V, at_once = 32 / per_row, turns = 32 / at_once;
-    const float4* st4 = reinterpret_cast<const float4*>(st);
-    if (p.pieces) {
-        const int c = lane % per_row * V;
-        if (c >= cols) return;
-        float bias[V];
-        if (ROLE == kForward && p.bias) unpack16<T>(*reinterpret_cast<const uint4*>(p.bias + j0 + c), bias);
-        uint4 res[turns];
-        if (ROLE == kForward && p.residual)
+// Staged rows of 128 bytes: the 16-byte pieces of row r are exchanged by r % 8, so that eight rows' pieces of a column lie in different
+// banks.  Byte b of row r:
+__device__ __forceinline__ uint32_t staged(int r, uint32_t b) { return r * 128 + (b ^ ((uint32_t)(r & 7) << 4)); }
+
+__device__ __forceinline__ void st_value(uint32_t at, float v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "f"(v) : "memory"); }
+__device__ __forceinline__ void st_value(uint32_t at, __nv_bfloat16 v) { asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(__bfloat16_as_ushort(v)) : "memory"); }
+__device__ __forceinline__ float get_value(uint32_t at, float) {
+    float v;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ __nv_bfloat16 get_value(uint32_t at, __nv_bfloat16) {
+    unsigned short v;
+    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(at) : "memory");
+    return __ushort_as_bfloat16(v);
+}
+// Where rows are not whole aligned 16-byte pieces: 32 staged rows, the first `rows` of them and `cols` values of each, from or to a matrix.
+template <typename T> __device__ __forceinline__ void rows_in(uint32_t slot, const T* src, long long ld, int rows, int cols, int lane) {
+    constexpr int per_lane = 128 / sizeof(T) / 32;
+    for (int r = 0; r < rows; r += 4) {
+        T v[4][per_lane];
 #pragma unroll
-            for (int t = 0; t < turns; ++t) {
-                const int r = t * at_once + lane / per_row;
-                if (r < rows) res[t] = *reinterpret_cast<const uint4*>(p.residual + (i0 + r) * p.J + j0 + c);
-            }
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int t = 0; t < turns; ++t) {
-            const int r = t * at_once + lane / per_row;
-            if (r >= rows) break;
-            float f[V];
+            for (int q = 0; q < per_lane; ++q) v[u][q] = ld_value(src + (r + u < rows && lane + 32 * q < cols ? (r + u) * ld + lane + 32 * q : 0));
 #pragma unroll
-            for (int q = 0; q < V / 4; ++q) {
-                const float4 v = st4[r * 8 + ((c / 4 + q) ^ (r & 7))];
-                f[4 * q] = v.x; f[4 * q + 1] = v.y; f[4 * q + 2] = v.z; f[4 * q + 3] = v.w;
-            }
-            const long long at = (i0 + r) * p.J + j0 + c;
-            if (ROLE == kForward) {
-                if (p.bias)
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
-                    for (int e = 0; e < V; ++e) f[e] += bias[e];
-                if (p.z) store16<T>(p.z + at, f);
-                if (p.act != kActNone)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) f[e] = act_of(p.act, f[e]);
-                if (p.residual) {
-                    float rf[V];
-                    unpack16<T>(res[t], rf);
-#pragma unroll
-                    for (int e = 0; e < V; ++e) f[e] += rf[e];
-                }
-            }
-            store16<O>(out + at, f);
-        }
-        return;
+            for (int q = 0; q < per_lane; ++q) st_value(slot + staged(r + u, (lane + 32 * q) * sizeof(T)), v[u][q]);
     }
-    if (lane >= cols) return;
-    const float bias = ROLE == kForward && p.bias ? Elem<T>::to_f32(p.bias[j0 + lane]) : 0.f;
+}
+template <typename T> __device__ __forceinline__ void rows_out(uint32_t slot, T* dst, long long ld, int rows, int cols, int lane) {
+    constexpr int per_lane = 128 / sizeof(T) / 32;
 #pragma unroll 4
-    for (int r = 0; r < rows; ++r) {
-        float f = st[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)];
-        const long long at = (i0 + r) * p.J + j0 + lane;
-        if (ROLE == kForward) {
-            f += bias;
-            if (p.z) p.z[at] = Elem<T>::from_f32(f);
-            f = act_of(p.act, f);
-            if (p.residual) f += Elem<T>::to_f32(p.residual[at]);
-        }
-        out[at] = Elem<O>::from_f32(f);
-    }
+    for (int r = 0; r < rows; ++r, dst += ld)
+#pragma unroll
+        for (int q = 0; q < per_lane; ++q)
+            if (lane + 32 * q < cols) dst[lane + 32 * q] = get_value(slot + staged(r, (lane + 32 * q) * sizeof(T)), T{});
 }
 
 // ---- the kernel ---------------------------------------------------------------------------------------------------------------
 
 template <typename T, Role ROLE, bool TMA>
-__global__ void __launch_bounds__(32 * (TMA ? kFirstFill : kFirstFill + kFillWarps), 1)
-product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Args<T> p)
+__global__ void __launch_bounds__(32 * all_warps<TMA>, 1)
+product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
+             const __grid_constant__ CUtensorMap map_res, const __grid_constant__ CUtensorMap map_z, const __grid_constant__ Args<T> p)
 {
     constexpr bool A_MN = ROLE == kGradW, B_MN = ROLE != kForward;
-    constexpr int PARTS = parts_of<T>;
+    constexpr int PARTS = parts_of<T>, EPI = epi_warps<TMA>, kFirstFill = kFirstEpi + EPI;
     static_assert(!TMA || PARTS == 1, "TMA brings bf16 as it is");
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t base = smem_u32(smem);
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
-    const long long blocks = (p.depth + kBlockC - 1) / kBlockC;
     const uint32_t b_part = (uint32_t)p.bn * 128, b_bytes = b_part * PARTS, stage_bytes = kABytes * PARTS + (p.resident ? 0 : b_bytes);
     const uint32_t resident = base + p.stages * stage_bytes;
-    const uint32_t staging = resident + (p.resident ? (uint32_t)blocks * b_bytes : 0), bars = staging + kStageBytes;
-    const uint32_t full = bars, empty = full + 8 * kMaxStages, acc_full = empty + 8 * kMaxStages, acc_empty = acc_full + 16, b_full = acc_empty + 16, slot = b_full + 8;
+    const uint32_t staging = resident + (p.resident ? (uint32_t)p.blocks * b_bytes : 0), slots = p.slots + (p.z && p.residual ? 1 : 0);
+    const uint32_t strips = staging + EPI * slots * kSlotBytes;    // of an epilogue warp: the bias of its columns
+    const uint32_t full = strips + EPI * 256, empty = full + 8 * kMaxStages, acc_full = empty + 8 * kMaxStages, acc_empty = acc_full + 16,
+                   b_full = acc_empty + 16, res_full = b_full + 8, slot = res_full + 16 * kMostEpi;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8 * s, TMA ? 1 : kFillWarps); mbar_init(empty + 8 * s, 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(acc_full + 8 * s, 1); mbar_init(acc_empty + 8 * s, kEpiWarps); }
+        for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8 * s, TMA ? 1 : kGroupWarps); mbar_init(empty + 8 * s, 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(acc_full + 8 * s, 1); mbar_init(acc_empty + 8 * s, EPI); }
         mbar_init(b_full, TMA ? 1 : kFillWarps);
+        for (int s = 0; s < 2 * EPI; ++s) mbar_init(res_full + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) {
@@ -299,85 +384,85 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
 
     bool alive = true;
-    if (TMA ? warp == 0 : warp >= kFirstFill) {
-        // ---- fill the ring --------------------------------------------------------------------------------------------------
-        unsigned k = 0;                                            // blocks so far
-        for (long long n = 0; alive; ++n) {
-            const Unit u = unit_of(p, n);
-            if (!u.live) break;
-            const long long i0 = (long long)u.i * kBlockI;
-            const int j0 = u.j * p.bn;
-            if (TMA) {
-                if (p.resident && n == 0 && lane == 0) {
-                    mbar_expect(b_full, (unsigned)(blocks * b_bytes));
-                    for (int c = 0; c < blocks; ++c) {
-                        if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(resident + c * b_bytes + m * 128, &map_b, b_full, j0 + m, c * kBlockC);
-                        else tma_load_2d(resident + c * b_bytes, &map_b, b_full, c * kBlockC, j0);
+    unsigned k = 0;                                                // blocks of c, tiles so far
+    int n = 0;
+    if (TMA && warp == 0) {
+        // ---- the ring, by TMA -------------------------------------------------------------------------------------------------
+        for (Walk u = walk(p); u.live && alive; next(u, p), ++n) {
+            const int i0 = u.i * kBlockI, j0 = u.j * p.bn;
+            if (p.resident && n == 0 && lane == 0) {
+                mbar_expect(b_full, (unsigned)p.blocks * b_bytes);
+                for (int c = 0; c < p.blocks; ++c) {
+                    if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(resident + c * b_bytes + m * 128, &map_b, b_full, j0 + m, c * kBlockC);
+                    else tma_load_2d(resident + c * b_bytes, &map_b, b_full, c * kBlockC, j0);
+                }
+            }
+            __syncwarp();
+            for (int c = u.c0; c < u.c1; ++c, ++k) {
+                const unsigned s = k % (unsigned)p.stages, round = k / (unsigned)p.stages;
+                if (round > 0) alive = wait_warp(empty + 8 * s, (round - 1) & 1, 0x10000000u | k);
+                if (!alive) break;
+                if (lane == 0) {
+                    const uint32_t at = base + s * stage_bytes, bar = full + 8 * s;
+                    const int c0 = c * kBlockC;
+                    mbar_expect(bar, stage_bytes - (A_MN ? 0 : (kBlockI - p.a_rows) * 128));
+                    if (A_MN) for (int m = 0; m < kBlockI; m += 64) tma_load_2d(at + m * 128, &map_a, bar, i0 + m, c0);
+                    else tma_load_2d(at, &map_a, bar, c0, i0);
+                    if (!p.resident) {
+                        if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(at + kABytes + m * 128, &map_b, bar, j0 + m, c0);
+                        else tma_load_2d(at + kABytes, &map_b, bar, c0, j0);
                     }
                 }
                 __syncwarp();
-                for (long long c = u.c0; c < u.c1; ++c, ++k) {
-                    const int s = (int)(k % p.stages);
-                    if (k >= (unsigned)p.stages) alive = wait_warp(empty + 8 * s, (k / p.stages - 1) & 1, 0x10000000u | k);
-                    if (!alive) break;
-                    if (lane == 0) {
-                        const uint32_t at = base + s * stage_bytes, bar = full + 8 * s;
-                        const int c0 = (int)(c * kBlockC);
-                        mbar_expect(bar, stage_bytes);
-                        if (A_MN) for (int m = 0; m < kBlockI; m += 64) tma_load_2d(at + m * 128, &map_a, bar, (int)i0 + m, c0);
-                        else tma_load_2d(at, &map_a, bar, c0, (int)i0);
-                        if (!p.resident) {
-                            if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(at + kABytes + m * 128, &map_b, bar, j0 + m, c0);
-                            else tma_load_2d(at + kABytes, &map_b, bar, c0, j0);
-                        }
-                    }
-                    __syncwarp();
-                }
-                if (!alive)                                        // what is still on its way here lands before the block goes
-                    for (unsigned q = k > (unsigned)p.stages ? k - p.stages : 0; q < k; ++q) wait_warp(full + 8 * (q % p.stages), (q / p.stages) & 1, 0x70000000u | q);
-            } else {
-                const int w = warp - kFirstFill;
-                if (p.resident && n == 0) {
-                    for (int c = 0; c < blocks; ++c)
-                        fill<T, B_MN>(resident + c * b_bytes, p.bn, b_part, p.b, p.b_ld, nullptr, 0, j0, p.J, (long long)c * kBlockC, p.depth, w, lane);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(b_full);
-                }
-                for (long long c = u.c0; c < u.c1; ++c, ++k) {
-                    const int s = (int)(k % p.stages);
-                    if (k >= (unsigned)p.stages) alive = wait_warp(empty + 8 * s, (k / p.stages - 1) & 1, 0x20000000u | k);
-                    if (!alive) break;
-                    const uint32_t at = base + s * stage_bytes;
-                    fill<T, A_MN>(at, kBlockI, kABytes, p.a, p.a_ld, p.kept, p.act, i0, p.I, c * kBlockC, p.depth, w, lane);
-                    if (!p.resident) fill<T, B_MN>(at + PARTS * kABytes, p.bn, b_part, p.b, p.b_ld, nullptr, 0, j0, p.J, c * kBlockC, p.depth, w, lane);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(full + 8 * s);
-                }
+            }
+        }
+        if (!alive)                                                // what is still on its way here lands before the block goes
+            for (unsigned q = k > (unsigned)p.stages ? k - p.stages : 0; q < k; ++q) wait_warp(full + 8 * (q % p.stages), (q / p.stages) & 1, 0x70000000u | q);
+    } else if (!TMA && warp >= kFirstFill) {
+        // ---- the ring, by plain loads -------------------------------------------------------------------------------------------
+        const int group = (warp - kFirstFill) / kGroupWarps, w = (warp - kFirstFill) % kGroupWarps;
+        for (Walk u = walk(p); u.live && alive; next(u, p), ++n) {
+            const long long i0 = (long long)u.i * kBlockI, j0 = u.j * p.bn;
+            if (p.resident && n == 0) {
+                for (int c = group; c < p.blocks; c += kFillWarps / kGroupWarps)
+                    fill<T, B_MN, false>(resident + c * b_bytes, p.bn, b_part, p.b, B_MN ? c * kBlockC : j0, B_MN ? j0 : c * kBlockC, w, lane);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_full);
+            }
+            for (int c = u.c0; c < u.c1; ++c, ++k) {
+                if (k % (kFillWarps / kGroupWarps) != (unsigned)group) continue;
+                const unsigned s = k % (unsigned)p.stages, round = k / (unsigned)p.stages;
+                if (round > 0) alive = wait_warp(empty + 8 * s, (round - 1) & 1, 0x20000000u | k);
+                if (!alive) break;
+                const uint32_t at = base + s * stage_bytes;
+                const long long c0 = (long long)c * kBlockC;
+                if (ROLE != kForward && p.a.kept) fill<T, A_MN, true>(at, kBlockI, kABytes, p.a, A_MN ? c0 : i0, A_MN ? i0 : c0, w, lane);
+                else fill<T, A_MN, false>(at, kBlockI, kABytes, p.a, A_MN ? c0 : i0, A_MN ? i0 : c0, w, lane);
+                if (!p.resident) fill<T, B_MN, false>(at + PARTS * kABytes, p.bn, b_part, p.b, B_MN ? c0 : j0, B_MN ? j0 : c0, w, lane);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(full + 8 * s);
             }
         }
     } else if (warp == 1) {
-        // ---- issue ------------------------------------------------------------------------------------------------------------
+        // ---- issue --------------------------------------------------------------------------------------------------------------
         const uint32_t idesc = instr_desc<A_MN, B_MN>(p.bn);
-        unsigned k = 0;
-        for (long long n = 0; alive; ++n) {
-            const Unit u = unit_of(p, n);
-            if (!u.live) break;
-            const int buf = (int)(n & 1);
+        for (Walk u = walk(p); u.live && alive; next(u, p), ++n) {
+            const int buf = n & 1;
             if (n >= 2) alive = wait_warp(acc_empty + 8 * buf, (unsigned)((n >> 1) - 1) & 1, 0x30000000u | (unsigned)n);
             if (alive && p.resident && n == 0) alive = wait_warp(b_full, 0, 0x40000000u);
             if (!alive) break;
             fence_after();
             const uint32_t d = tmem + buf * kTmemBuffer;
-            for (long long c = u.c0; c < u.c1; ++c, ++k) {
-                const int s = (int)(k % p.stages);
-                alive = wait_warp(full + 8 * s, (k / p.stages) & 1, 0x50000000u | k);
+            for (int c = u.c0; c < u.c1; ++c, ++k) {
+                const unsigned s = k % (unsigned)p.stages;
+                alive = wait_warp(full + 8 * s, (k / (unsigned)p.stages) & 1, 0x50000000u | k);
                 if (!alive) break;
                 fence_after();
                 const uint32_t a_at = base + s * stage_bytes, b_at = p.resident ? resident + (uint32_t)c * b_bytes : a_at + PARTS * kABytes;
                 const unsigned long long da = smem_desc<A_MN>(a_at), db = smem_desc<B_MN>(b_at);
-#pragma unroll
+#pragma unroll 1
                 for (int t = 0; t < kBlockC / 16; ++t) {
                     const unsigned long long at = da + t * (step16<A_MN> >> 4), bt = db + t * (step16<B_MN> >> 4);
                     const bool add = c > u.c0 || t > 0;
@@ -398,49 +483,129 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         }
     } else if (warp >= kFirstEpi && warp < kFirstFill) {
         // ---- write out ------------------------------------------------------------------------------------------------------
-        const int e = warp - kFirstEpi, quarter = warp & 3;
-        const uint32_t mine = staging + e * 4096;
-        const float* st = reinterpret_cast<const float*>(smem + (mine - base));
-        for (long long n = 0; alive; ++n) {
-            const Unit u = unit_of(p, n);
-            if (!u.live) break;
-            const int buf = (int)(n & 1);
+        // A unit: 128 bytes of 32 rows.  The warps of a quarter of the lanes take units in turn, over the tiles.
+        using O = typename Result<T, ROLE>::type;
+        constexpr int UC = 128 / sizeof(O), V = Elem<O>::kVec, TEAM = EPI / 4;
+        const int e = warp - kFirstEpi, quarter = warp & 3, member = e / 4, per_tile = (p.bn + UC - 1) / UC;
+        const uint32_t mine = staging + e * slots * kSlotBytes, res_bar = res_full + e * 16;
+        const uint32_t lane_at = lane * 128 + ((lane & 7) << 4), strip = strips + e * 256;   // a piece q of this lane's row: xor q << 4
+        const unsigned two = p.slots - 1;
+        const bool has_z = ROLE == kForward && p.z, has_res = ROLE == kForward && p.residual, has_bias = ROLE == kForward && p.bias;
+        unsigned uses = 0;                                         // of the slots that residuals and results lie in
+        // the residual of this warp's next unit, from unit c of tile u on, into the slot that it will have; `turn` is whose c is
+        auto fetch = [&](Walk u, int c, int turn) {
+            for (; u.live; next(u, p), c = 0) {
+                const int i0 = u.i * kBlockI + quarter * 32, j0 = u.j * p.bn, wide = min(p.J - j0, p.bn);
+                for (; c < per_tile; ++c) {
+                    const bool ours = turn == member && c * UC < wide && i0 < p.I;
+                    turn = turn + 1 == TEAM ? 0 : turn + 1;
+                    if (!ours) continue;
+                    mbar_expect(res_bar + (uses & two) * 8, kSlotBytes);
+                    tma_load_3d(mine + (uses & two) * kSlotBytes, &map_res, res_bar + (uses & two) * 8, j0 + c * UC, i0, 0);
+                    return;
+                }
+            }
+        };
+        Walk u = walk(p);
+        if (p.by_tma && has_res && lane == 0) fetch(u, 0, 0);
+        __syncwarp();
+        int turn = 0;                                              // which member of the team has the next unit
+        for (; u.live && alive; next(u, p), ++n) {
+            const int buf = n & 1;
             alive = wait_warp(acc_full + 8 * buf, (unsigned)(n >> 1) & 1, 0x60000000u | (unsigned)n);
             if (!alive) break;
             fence_after();
-            const long long i0 = (long long)u.i * kBlockI + quarter * 32;
-            const int rows = (int)(p.I - i0 < 32 ? p.I - i0 : 32);
-            const int j0 = u.j * p.bn, wide = p.J - j0 < p.bn ? p.J - j0 : p.bn;
+            const int i0 = u.i * kBlockI + quarter * 32, j0 = u.j * p.bn, wide = min(p.J - j0, p.bn), rows = (int)min(p.I - i0, 32LL);
             const uint32_t d = tmem + buf * kTmemBuffer + ((uint32_t)(quarter * 32) << 16);
-            for (int c = e / 4 * 32; c < wide; c += 64) {
-                uint32_t acc[32];
-                tmem_ld32(d + c, acc);
-                tmem_wait_ld();
-                if (PARTS == 3) {
-                    uint32_t small[32];
-                    tmem_ld32(d + kTmemBuffer / 2 + c, small);
-                    tmem_wait_ld();
+            for (int c = 0; c < per_tile; ++c) {
+                const bool ours = turn == member && c * UC < wide && rows > 0;
+                turn = turn + 1 == TEAM ? 0 : turn + 1;
+                if (!ours) continue;
+                const uint32_t at = mine + (uses & two) * kSlotBytes, z_at = mine + p.slots * kSlotBytes;
+                const int col = j0 + c * UC, cols = min(wide - c * UC, UC);
+                if (has_bias)
 #pragma unroll
-                    for (int q = 0; q < 32; ++q) acc[q] = __float_as_uint(__uint_as_float(acc[q]) + __uint_as_float(small[q]));
+                    for (int v = lane; v < UC; v += 32) st_value(strip + v * 4, v < cols ? Elem<T>::to_f32(ld_value(p.bias + col + v)) : 0.f);
+                if (p.by_tma) {
+                    if (lane == 0) { if (two) bulk_wait_read<1>(); else bulk_wait_read<0>(); }   // the slots have been read
+                    if (has_res) alive = wait_warp(res_bar + (uses & two) * 8, (uses >> two) & 1, 0x80000000u | (unsigned)n);
+                    if (!alive) break;
+                } else if (has_res) {
+                    if constexpr (ROLE == kForward) rows_in<T>(at, p.residual + (long long)i0 * p.J + col, p.J, rows, cols, lane);
                 }
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(mine + lane * 128 + ((q ^ (lane & 7)) << 4)),
-                                 "r"(acc[4 * q]), "r"(acc[4 * q + 1]), "r"(acc[4 * q + 2]), "r"(acc[4 * q + 3]) : "memory");
                 __syncwarp();
-                const int cols = wide - c < 32 ? wide - c : 32;
-                if (rows > 0) {
-                    if (ROLE == kGradW) {
-                        write_chunk<T, float, ROLE>(st, p, p.part + u.split * p.I * p.J, i0, rows, j0 + c, cols, lane);
-                    } else {
-                        write_chunk<T, T, ROLE>(st, p, p.out, i0, rows, j0 + c, cols, lane);
+                // Loops that stay loops: a role's code has to stay in the instruction cache beside the others' (unrolled, waiting for
+                // instructions was most of this kernel's time).  z without a residual leaves first, through the same slot.
+#pragma unroll 1
+                for (int pass = has_z && !has_res ? 0 : 1; pass < 2; ++pass) {
+#pragma unroll 1
+                    for (int q = 0; q < 8; q += 2) {
+                        float f[2 * V];
+                        tmem_ld(d + c * UC + q * V, f);
+                        tmem_wait_ld();
+                        if (PARTS == 3) {
+                            float small[2 * V];
+                            tmem_ld(d + kTmemBuffer / 2 + c * UC + q * V, small);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int v = 0; v < 2 * V; ++v) f[v] += small[v];
+                        }
+                        const uint32_t left = lane_at ^ (uint32_t)(q << 4), right = lane_at ^ (uint32_t)((q + 1) << 4);
+                        if (has_bias)
+#pragma unroll
+                            for (int v = 0; v < 2 * V; v += 4) add_piece<float>(f + v, ld_shared(strip + (q * V + v) * 4));
+                        if (has_z && has_res) {
+                            st_shared(z_at + left, pack16<O>(f));
+                            st_shared(z_at + right, pack16<O>(f + V));
+                        }
+                        if (ROLE == kForward && pass == 1) {
+                            if (p.act == kActGelu)
+#pragma unroll
+                                for (int v = 0; v < 2 * V; v += 2) act_pair(kActGelu, f[v], f[v + 1]);
+                            else if (p.act == kActRelu)
+#pragma unroll
+                                for (int v = 0; v < 2 * V; v += 2) act_pair(kActRelu, f[v], f[v + 1]);
+                            if (has_res) {
+                                add_piece<O>(f, ld_shared(at + left));
+                                add_piece<O>(f + V, ld_shared(at + right));
+                            }
+                        }
+                        st_shared(at + left, pack16<O>(f));
+                        st_shared(at + right, pack16<O>(f + V));
                     }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (ROLE == kForward && p.z && (pass == 0 || has_res)) {
+                        const uint32_t from = pass == 0 ? at : z_at;
+                        if (p.by_tma) {
+                            if (lane == 0) { tma_store_3d(&map_z, from, col, i0, 0); bulk_commit(); if (pass == 0) bulk_wait_read<0>(); }
+                        } else {
+                            if constexpr (ROLE == kForward) rows_out<T>(from, p.z + (long long)i0 * p.J + col, p.J, rows, cols, lane);
+                        }
+                        __syncwarp();
+                    }
+                }
+                ++uses;
+                if (p.by_tma) {
+                    if (lane == 0) {
+                        tma_store_3d(&map_out, at, col, i0, u.split); bulk_commit();
+                        if (has_res) {                             // the next one into its slot, once that has been read
+                            if (!two) bulk_wait_read<0>(); else if (has_z) bulk_wait_read<2>(); else bulk_wait_read<1>();
+                            fetch(u, c + 1, turn);
+                        }
+                    }
+                } else {
+                    O* out;
+                    if constexpr (ROLE == kGradW) out = p.part + u.split * p.I * p.J; else out = p.out;
+                    rows_out<O>(at, out + (long long)i0 * p.J + col, p.J, rows, cols, lane);
                 }
                 __syncwarp();
             }
+            if (!alive) break;
             fence_before();
             if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
         }
+        if (lane == 0) bulk_wait_read<0>();                        // shared memory outlives what is read from it
     }
     fence_before();
     __syncthreads();
