@@ -53,13 +53,13 @@ template <typename T> lin::Layer<T> layer_of(const Call& c) {
 
 // What a product is cut into.  Times in cycles of an SM, from the rates below; the cheapest width of a tile and number of runs of rows.
 struct Cut {
-    int tiles_i, tiles_j, bn, splits, stages, grid, slots;
+    int tiles_i, tiles_j, bn, splits, stages, grid;
     bool resident;
     size_t smem;
 };
 constexpr size_t kBarBytes = 1024 + um::kMostEpi * 256;        // barriers and strips
 constexpr double kLoadRate = 35, kStoreRate = 20;   // bytes per cycle of one SM: from L2 into its ring, to memory
-Cut cut(lin::Role role, long long I, int J, long long depth, size_t es, bool tma, bool third = false) {
+Cut cut(lin::Role role, long long I, int J, long long depth, size_t es, bool tma) {
     const int sms = abi::sm_count(), step = role == lin::kForward ? 16 : 64, most = es == 4 ? um::most_columns<float> : um::most_columns<bf16>;
     const int parts = es == 4 ? 3 : 1, products = es == 4 ? 6 : 1;
     const long long blocks = (depth + um::kBlockC - 1) / um::kBlockC, tiles_i = (I + um::kBlockI - 1) / um::kBlockI;
@@ -70,13 +70,10 @@ Cut cut(lin::Role role, long long I, int J, long long depth, size_t es, bool tma
     for (int bn = std::min(most, (J + step - 1) / step * step); bn >= step; bn -= step) {
         const long long tiles_j = ((long long)J + bn - 1) / bn;
         if (tiles_j > 1 && bn > unit && bn % unit != 0) continue;
-        // w stays where it leaves room for a ring of rows and a block has several tiles; results then have two slots, else the ring has the room
-        const size_t b_bytes = (size_t)bn * 128 * parts, a_bytes = (size_t)um::kABytes * parts;
-        const int two = tma ? 1 : 2;                               // 16 epilogue warps have a slot each, four have two
-        const long long most_kept = (long long)um::kMostSmem - (long long)((two + third) * slot_bytes + kBarBytes + 3 * a_bytes);
-        const bool resident = role != lin::kGradW && (long long)(blocks * b_bytes) <= most_kept && tiles_j <= sms && tiles_i * tiles_j >= 2LL * sms;
-        const int slots = resident ? two : 1;
-        const size_t fixed = (slots + third) * slot_bytes + kBarBytes, kept = resident ? blocks * b_bytes : 0, stage = a_bytes + (resident ? 0 : b_bytes);
+        // w stays where it leaves room for a ring of rows and a block has several tiles
+        const size_t b_bytes = (size_t)bn * 128 * parts, a_bytes = (size_t)um::kABytes * parts, fixed = slot_bytes + kBarBytes;
+        const bool resident = role != lin::kGradW && blocks * b_bytes + fixed + 3 * a_bytes <= um::kMostSmem && tiles_j <= sms && tiles_i * tiles_j >= 2LL * sms;
+        const size_t kept = resident ? blocks * b_bytes : 0, stage = a_bytes + (resident ? 0 : b_bytes);
         const int stages = (int)std::min<long long>(um::kMaxStages, ((long long)um::kMostSmem - (long long)(fixed + kept)) / (long long)stage);
         if (stages < 1 || (stages < 2 && bn > step)) continue;
         const double rows = (double)std::min<long long>(I, um::kBlockI), b_rows = resident ? 0 : bn;
@@ -91,7 +88,7 @@ Cut cut(lin::Role role, long long I, int J, long long depth, size_t es, bool tma
             if (role == lin::kGradW) cost += 2.0 * splits * I * J * 4 / (kStoreRate * sms);
             if (cost < least * 0.995) {
                 least = cost;
-                best = Cut{(int)tiles_i, (int)tiles_j, bn, (int)splits, stages, resident ? (int)(sms / tiles_j * tiles_j) : (int)std::min<long long>(units, sms), slots, resident,
+                best = Cut{(int)tiles_i, (int)tiles_j, bn, (int)splits, stages, resident ? (int)(sms / tiles_j * tiles_j) : (int)std::min<long long>(units, sms), resident,
                            stages * stage + kept + fixed};
             }
         }
@@ -119,13 +116,16 @@ template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long lon
     const bool a_pieces = whole_pieces(p.a.p, p.a.ld, sizeof(T)), b_pieces = whole_pieces(p.b.p, p.b.ld, sizeof(T));
     CUtensorMap ma{}, mb{}, mo{}, mr{}, mz{};
     p.a_rows = (int)std::min<long long>(um::kBlockI, (p.I + 7) / 8 * 8);
-    bool tma = sizeof(T) == 2 && !p.a.kept && a_pieces && b_pieces && map_of<T>(&ma, p.a.p, 0, p.a.rows, p.a.width, p.a.ld, a_mn ? um::kBlockC : p.a_rows);
-    Cut c = cut(ROLE, p.I, p.J, depth, sizeof(T), tma, p.z && p.residual);
-    if (tma && !map_of<T>(&mb, p.b.p, 0, p.b.rows, p.b.width, p.b.ld, b_mn ? um::kBlockC : c.bn)) {
-        tma = false;
-        c = cut(ROLE, p.I, p.J, depth, sizeof(T), tma, p.z && p.residual);
+    p.a_tma = sizeof(T) == 2 && !p.a.kept && a_pieces && map_of<T>(&ma, p.a.p, 0, p.a.rows, p.a.width, p.a.ld, a_mn ? um::kBlockC : p.a_rows);
+    const auto cut_for = [&] { return cut(ROLE, p.I, p.J, depth, sizeof(T), p.a_tma && p.b_tma); };
+    p.b_tma = sizeof(T) == 2 && b_pieces;
+    Cut c = cut_for();
+    if (p.b_tma && !map_of<T>(&mb, p.b.p, 0, p.b.rows, p.b.width, p.b.ld, b_mn ? um::kBlockC : c.bn)) {
+        p.b_tma = false;
+        c = cut_for();
     }
-    p.tiles_i = c.tiles_i; p.tiles_j = c.tiles_j; p.bn = c.bn; p.splits = c.splits; p.stages = c.stages; p.resident = c.resident; p.slots = c.slots;
+    const bool tma = p.a_tma && p.b_tma;
+    p.tiles_i = c.tiles_i; p.tiles_j = c.tiles_j; p.bn = c.bn; p.splits = c.splits; p.stages = c.stages; p.resident = c.resident;
     p.blocks = (int)((depth + um::kBlockC - 1) / um::kBlockC);
     p.units = (unsigned)((long long)c.tiles_i * c.tiles_j * c.splits);
     if (splits) *splits = c.splits;

@@ -7,76 +7,58 @@ namespace esc { namespace linear {
 
 constexpr int kActNone = 0, kActRelu = 1, kActGelu = 2;
 
-// Activations of two values at a time.  With x = |z|, e = exp(-z^2 / 2) and Q(x) = Phi(-x) / e, which falls smoothly from 1/2:
+// With x = |z|, e = exp(-z^2 / 2) and Q(x) = Phi(-x) / e, which falls smoothly from 1/2:
 //
 //   GELU      z Phi(z) = max(z, 0) - x e Q(x)
 //   its slope Phi(z) + z phi(z) = [z >= 0] + sign(z) e (x / sqrt(2 pi) - Q(x))
 //
 // Q is a polynomial in t = 1 / (1 + p x) without a constant term (the form that Hastings gave the error function), fitted here by least
-// squares with Lawson's weights to erfcx(x / sqrt 2) / 2 on [0, 15]: 2.6e-8 relative at most, in the left tail too.  fp32 arithmetic in
-// pairs, one 2^x and one reciprocal a value: against erfcf and expf a third of the instructions (320x180 from 192 to 384 channels and the
-// gradients of 64 x 64x64 were bound by those: 86 us each).
-typedef unsigned long long F2;
-__device__ __forceinline__ F2 f2(float lo, float hi) { F2 v; asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi)); return v; }
-__device__ __forceinline__ F2 f2(float v) { return f2(v, v); }
-__device__ __forceinline__ void un2(F2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
-__device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
-__device__ __forceinline__ F2 add2(F2 a, F2 b) { F2 d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
-__device__ __forceinline__ float pow2(float v) { float r; asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
-__device__ __forceinline__ float inverse(float v) { float r; asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+// squares with Lawson's weights to erfcx(x / sqrt 2) / 2 on [0, 15]: nine terms, 2.6e-8 relative at most, in the left tail too.  One 2^x and
+// one reciprocal a value: against erfcf and expf a third of the instructions (320x180 from 192 to 384 channels and the gradients of
+// 64 x 64x64 were bound by those, 86 us each).  GELU that is rounded to bf16 takes six terms: 1e-5 relative at most, less than the 2^-16 by
+// which half a step of bf16 above a power of two falls short of 2^-8.
+__device__ __forceinline__ float pow2(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+__device__ __forceinline__ float inverse(float v) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 __device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float min_nan(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 
-struct Gauss { F2 x, e, q; };
-__device__ __forceinline__ Gauss gauss(float a, float b) {
-    // beyond 30 e is zero in fp32; bounded so that 0 times infinity does not come up
+struct Gauss { float x, e, q; };
+template <bool NINE> __device__ __forceinline__ Gauss gauss(float z) {
     Gauss g;
-    g.x = f2(min_nan(fabsf(a), 30.f), min_nan(fabsf(b), 30.f));
-    float lo, hi;
-    un2(mul2(mul2(g.x, g.x), f2(-0.72134752044f)), lo, hi);
-    g.e = f2(pow2(lo), pow2(hi));
-    un2(fma2(g.x, f2(0.345f), f2(1.f)), lo, hi);
-    const F2 t = f2(inverse(lo), inverse(hi));
-    F2 q = f2(-0.0279335122f);
-    q = fma2(q, t, f2(0.143238278f));
-    q = fma2(q, t, f2(-0.267236026f));
-    q = fma2(q, t, f2(0.183022695f));
-    q = fma2(q, t, f2(-0.0349471461f));
-    q = fma2(q, t, f2(0.110766168f));
-    q = fma2(q, t, f2(0.117478006f));
-    q = fma2(q, t, f2(0.137990677f));
-    q = fma2(q, t, f2(0.137620871f));
-    g.q = mul2(q, t);
+    g.x = min_nan(fabsf(z), 30.f);                                 // beyond, e is zero in fp32: 0 times infinity does not come up
+    g.e = pow2(g.x * g.x * -0.72134752044f);
+    const float t = inverse(fmaf(g.x, NINE ? 0.345f : 0.31f, 1.f));
+    float q;
+    if (NINE) {
+        q = fmaf(-0.0279335122f, t, 0.143238278f);
+        q = fmaf(q, t, -0.267236026f);
+        q = fmaf(q, t, 0.183022695f);
+        q = fmaf(q, t, -0.0349471461f);
+        q = fmaf(q, t, 0.110766168f);
+        q = fmaf(q, t, 0.117478006f);
+        q = fmaf(q, t, 0.137990677f);
+        q = fmaf(q, t, 0.137620871f);
+    } else {
+        q = fmaf(-0.073929169f, t, 0.180450428f);
+        q = fmaf(q, t, 0.0157446193f);
+        q = fmaf(q, t, 0.133429833f);
+        q = fmaf(q, t, 0.120441264f);
+        q = fmaf(q, t, 0.123860703f);
+    }
+    g.q = q * t;
     return g;
 }
-__device__ __forceinline__ void act_pair(int act, float& a, float& b) {
-    if (act == kActRelu) { a = max_nan(a, 0.f); b = max_nan(b, 0.f); }
-    if (act == kActGelu) {
-        const Gauss g = gauss(a, b);
-        float lo, hi;
-        un2(mul2(g.x, mul2(g.e, g.q)), lo, hi);
-        a = max_nan(a, 0.f) - lo;
-        b = max_nan(b, 0.f) - hi;
-    }
+// GELU for results of type T.
+template <typename T> __device__ __forceinline__ float gelu(float z) {
+    const Gauss g = gauss<sizeof(T) == 4>(z);
+    return fmaf(-g.x, g.e * g.q, max_nan(z, 0.f));
 }
-__device__ __forceinline__ void slope_pair(int act, float& a, float& b) {
-    if (act == kActRelu) { a = a > 0.f ? 1.f : 0.f; b = b > 0.f ? 1.f : 0.f; }
-    if (act == kActGelu) {
-        const Gauss g = gauss(a, b);
-        float lo, hi;
-        un2(mul2(g.q, f2(-1.f)), lo, hi);
-        un2(mul2(g.e, fma2(g.x, f2(0.39894228040f), f2(lo, hi))), lo, hi);
-        a = a >= 0.f ? 1.f + lo : -lo;
-        b = b >= 0.f ? 1.f + hi : -hi;
-    }
-    if (act == kActNone) a = b = 1.f;
+__device__ __forceinline__ float gelu_slope(float z) {
+    const Gauss g = gauss<true>(z);
+    const float h = g.e * fmaf(g.x, 0.39894228040f, -g.q);
+    return z >= 0.f ? 1.f + h : -h;
 }
-__device__ __forceinline__ float act_slope(int act, float z) {
-    float other = z;
-    slope_pair(act, z, other);
-    return z;
-}
+__device__ __forceinline__ float act_slope(int act, float z) { return act == kActGelu ? gelu_slope(z) : act == kActRelu ? (z > 0.f ? 1.f : 0.f) : 1.f; }
 
 template <typename T> struct Layer {
     const T *x, *w, *b;                 // [rows, K], [N, K], [N] or null
@@ -121,7 +103,7 @@ __global__ void __launch_bounds__(256) grad_z_pieces(const Layer<__nv_bfloat16> 
     const int col = threadIdx.x % across, v = blockIdx.x * across + col, r = threadIdx.x / across;
     float sum[8] = {};
     if (r < down && v < all) {
-#pragma unroll 2
+#pragma unroll 1
         for (long long row = (long long)blockIdx.y * down + r; row < p.rows; row += (long long)gridDim.y * down) {
             const long long at = row * p.N + v * 8;
             float f[8];
@@ -130,11 +112,7 @@ __global__ void __launch_bounds__(256) grad_z_pieces(const Layer<__nv_bfloat16> 
                 float z[8];
                 unpack16<bf16>(*reinterpret_cast<const uint4*>(p.kept + at), z);
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    slope_pair(p.act, z[e], z[e + 1]);
-                    f[e] *= z[e];
-                    f[e + 1] *= z[e + 1];
-                }
+                for (int e = 0; e < 8; ++e) f[e] *= act_slope(p.act, z[e]);
             }
             if (g) {
                 uint32_t w[4];

@@ -29,10 +29,10 @@ namespace esc { namespace linear { namespace umma {
 constexpr int kBlockI = 128, kBlockC = 64;
 constexpr int kABytes = kBlockI * kBlockC * 2;                     // of one part
 constexpr int kFillWarps = 16, kGroupWarps = 8, kFirstEpi = 4;         // a group fills every other block
-template <bool TMA> constexpr int epi_warps = TMA ? 16 : 4;
+template <bool TMA> constexpr int epi_warps = TMA ? 16 : 8;
 template <bool TMA> constexpr int all_warps = kFirstEpi + epi_warps<TMA> + (TMA ? 0 : kFillWarps);
 constexpr int kMostEpi = 16;
-constexpr int kSlotBytes = 32 * 128;                               // staging of an epilogue warp: 128 bytes of 32 rows; two or three of them
+constexpr int kSlotBytes = 32 * 128;                               // staging of an epilogue warp: 128 bytes of 32 rows
 constexpr int kMaxStages = 8;
 constexpr size_t kMostSmem = 227 * 1024;
 constexpr int kTmemBuffer = 256;                                   // columns of one tile's sums
@@ -55,6 +55,23 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, unsigned parity, unsigne
     if (threadIdx.x % 32 == 0) { atomicExch(&wait_status[0], kDevTimeout); atomicExch(&wait_status[1], where); }
     return false;
 }
+// The same of one lane.
+__device__ __forceinline__ bool wait_lane(uint32_t bar, unsigned parity, unsigned where) {
+    for (unsigned n = 0; n < kPolls; ++n) {
+        unsigned ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity), "r"(kHintNs) : "memory");
+        if (ok) return true;
+    }
+    atomicExch(&wait_status[0], kDevTimeout);
+    atomicExch(&wait_status[1], where);
+    return false;
+}
+// A place in the ring, and how often it came round.
+struct Ring {
+    unsigned s, round;
+    __device__ __forceinline__ void next(int stages) { if (++s == (unsigned)stages) { s = 0; ++round; } }
+};
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                  ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
@@ -133,12 +150,12 @@ template <typename T> struct Args {
     unsigned units;
     Source<T> a, b;                     // plain loads; a.kept: A = a act'(kept)
     int a_rows;                         // lines of A that TMA brings (K-major; the others' sums go nowhere)
+    bool a_tma, b_tma;                  // beside plain loads: this operand comes by TMA
     int act;
     const T *bias, *residual;
     T *out, *z;
     float* part;                        // kGradW: [splits][I][J]
     bool by_tma;                        // results leave and residuals come by TMA: rows of whole aligned 16-byte pieces
-    int slots;                          // of an epilogue warp for residuals and results: one or two; z beside a residual has another
 };
 
 template <typename T> constexpr int parts_of = sizeof(T) == 4 ? 3 : 1;
@@ -187,100 +204,125 @@ __device__ __forceinline__ void split(float a, float b, uint32_t& hi, uint32_t& 
 }
 
 
-// One operand's block: `lines` lines of 64 values.  Line L is row r0 + L from column c0 on (K-major), or row r0 + L % 64 from column
-// c0 + L / 64 * 64 on (MN-major).  What lies outside the matrix is zero.  Every load of a batch is issued before the first is used, none
-// is conditional (one that has nothing to read reads the matrix' first value).  The parts of fp32 lie `part_bytes` apart.
-template <typename T, bool MN, bool KEPT> __device__ __forceinline__ void fill_values(uint32_t dst, int lines, uint32_t part_bytes, const Source<T>& s, long long r0, long long c0, int warp, int lane) {
-    constexpr int kBatch = KEPT ? 2 : 4;
-    for (int first = warp; first < lines; first += kGroupWarps * kBatch) {
-        T lo[kBatch], hi[kBatch], zl[KEPT ? kBatch : 1], zh[KEPT ? kBatch : 1];
+// Staged rows of 128 bytes: the 16-byte pieces of row r are exchanged by r % 8, so that eight rows' pieces of a column lie in different
+// banks.  Byte b of row r:
+__device__ __forceinline__ uint32_t staged(int r, uint32_t b) { return r * 128 + (b ^ ((uint32_t)(r & 7) << 4)); }
+
+// 64 lines of 64 values: line l is row r0 + l from column c0 on.  What lies outside the matrix is zero.  Every load is issued before the first
+// is used, none is conditional (one that has nothing to read reads the matrix' first value).  The parts of fp32 lie `part_bytes` apart.
+// fill_values: a warp a line, a lane two values of it; fill_pieces: a lane 16 bytes.
+template <typename T, bool KEPT> __device__ __forceinline__ void fill_values(uint32_t dst, int lines, uint32_t part_bytes, const Source<T>& s, long long r0, long long c0, int warp, int lane) {
+    constexpr int kStep = kGroupWarps, kTurns = kBlockC / kStep, kBatch = KEPT ? 2 : sizeof(T) == 4 ? 4 : 8;
+    const long long col = c0 + 2 * lane, left = s.rows - r0 - warp;
+    const bool one = col < s.width, two = col + 1 < s.width;
+    const int rows = (int)min(left, (long long)(lines - warp));    // of this warp's: line warp + u kStep is there for u kStep < rows
+    const long long step = s.ld * kStep;
+    const T* p = s.p + (r0 + warp) * s.ld + col;
+    const T* z = s.kept + (r0 + warp) * s.ld + col;
+    const uint32_t at = dst + staged(warp, lane * 4);
+#pragma unroll 1
+    for (int turn = 0; turn < kTurns; turn += kBatch) {
+        if (turn * kStep + warp >= lines) break;
+        T lo[kBatch], hi[kBatch], zl[kBatch], zh[kBatch];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const int L = first + u * kGroupWarps;
-            const long long row = r0 + (MN ? L % kBlockC : L), col = c0 + (MN ? L / kBlockC * kBlockC : 0) + 2 * lane, at = row * s.ld + col;
-            const bool in = L < lines && row < s.rows, one = in && col < s.width, two = in && col + 1 < s.width;
-            lo[u] = ld_value(s.p + (one ? at : 0));
-            hi[u] = ld_value(s.p + (two ? at + 1 : 0));
-            if (KEPT) { zl[u] = ld_value(s.kept + (one ? at : 0)); zh[u] = ld_value(s.kept + (two ? at + 1 : 0)); }
-            if (!one) lo[u] = Elem<T>::from_f32(0.f);
-            if (!two) hi[u] = Elem<T>::from_f32(0.f);
+            const bool in = (turn + u) * kStep < rows;
+            lo[u] = ld_value(in && one ? p : s.p);
+            hi[u] = ld_value(in && two ? p + 1 : s.p);
+            if (KEPT) { zl[u] = ld_value(in && one ? z : s.kept); zh[u] = ld_value(in && two ? z + 1 : s.kept); z += step; }
+            p += step;
         }
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const int L = first + u * kGroupWarps;
-            if (L >= lines) break;
-            float a = Elem<T>::to_f32(lo[u]), b = Elem<T>::to_f32(hi[u]);
-            if (KEPT) {
-                float x = Elem<T>::to_f32(zl[u]), y = Elem<T>::to_f32(zh[u]);
-                slope_pair(s.act, x, y);
-                const bool in = r0 + (MN ? L % kBlockC : L) < s.rows;   // a slope that is not a number may be another value's
-                const long long col = c0 + (MN ? L / kBlockC * kBlockC : 0) + 2 * lane;
-                a = in && col < s.width ? a * x : 0.f;
-                b = in && col + 1 < s.width ? b * y : 0.f;
-            }
-            const uint32_t at = dst + L * 128 + (((lane >> 2) ^ (L & 7)) << 4) + (lane & 3) * 4;
-            if (sizeof(T) == 4) {
-                uint32_t h, m, l;
-                split(a, b, h, m, l);
-                st_shared(at, h);
-                st_shared(at + part_bytes, m);
-                st_shared(at + 2 * part_bytes, l);
+            const bool in = (turn + u) * kStep < rows;
+            static_assert(kStep % 8 == 0, "the pieces of these lines are exchanged alike");
+            const uint32_t to = at + (turn + u) * kStep * 128;
+            if ((turn + u) * kStep + warp >= lines) break;
+            if constexpr (sizeof(T) == 2 && !KEPT) {               // as it is
+                const uint32_t v = (uint32_t)__bfloat16_as_ushort(lo[u]) | ((uint32_t)__bfloat16_as_ushort(hi[u]) << 16);
+                st_shared(to, in ? v & ((one ? 0xffffu : 0u) | (two ? 0xffff0000u : 0u)) : 0u);
             } else {
-                st_shared(at, pack(a, b));
+                float a = Elem<T>::to_f32(lo[u]), b = Elem<T>::to_f32(hi[u]);
+                if (KEPT) {
+                    a *= act_slope(s.act, Elem<T>::to_f32(zl[u]));
+                    b *= act_slope(s.act, Elem<T>::to_f32(zh[u]));
+                }
+                a = in && one ? a : 0.f;
+                b = in && two ? b : 0.f;
+                if (sizeof(T) == 4) {
+                    uint32_t h, m, l;
+                    split(a, b, h, m, l);
+                    st_shared(to, h);
+                    st_shared(to + part_bytes, m);
+                    st_shared(to + 2 * part_bytes, l);
+                } else {
+                    st_shared(to, pack(a, b));
+                }
             }
         }
     }
 }
-template <typename T, bool MN, bool KEPT> __device__ __forceinline__ void fill_pieces(uint32_t dst, int lines, uint32_t part_bytes, const Source<T>& s, long long r0, long long c0, int warp, int lane) {
-    constexpr int V = Elem<T>::kVec, per_line = 64 / V, at_once = 32 / per_line, kBatch = KEPT ? 2 : 4;
-    const int col0 = lane % per_line * V;
-    for (int first = warp * at_once + lane / per_line; first - lane / per_line < lines; first += kGroupWarps * at_once * kBatch) {
-        uint4 v[kBatch], z[KEPT ? kBatch : 1];
-        bool in[kBatch];
+template <typename T, bool KEPT> __device__ __forceinline__ void fill_pieces(uint32_t dst, int lines, uint32_t part_bytes, const Source<T>& s, long long r0, long long c0, int warp, int lane) {
+    constexpr int V = Elem<T>::kVec, per_line = 64 / V, at_once = 32 / per_line, kStep = kGroupWarps * at_once, kTurns = kBlockC / kStep, kBatch = KEPT ? 2 : kTurns;
+    const int line = warp * at_once + lane / per_line, byte = lane % per_line * V * 2;
+    const long long col = c0 + lane % per_line * V, left = s.rows - r0 - line;
+    const int rows = col < s.width ? (int)min(left, (long long)(lines - line)) : 0;
+    const long long step = s.ld * kStep;
+    const T* p = s.p + (r0 + line) * s.ld + col;
+    const T* z = s.kept + (r0 + line) * s.ld + col;
+    const uint32_t at = dst + staged(line, byte);
+#pragma unroll 1
+    for (int turn = 0; turn < kTurns; turn += kBatch) {
+        uint4 v[kBatch], w[kBatch];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const int L = first + u * kGroupWarps * at_once;
-            const long long row = r0 + (MN ? L % kBlockC : L), col = c0 + (MN ? L / kBlockC * kBlockC : 0) + col0;
-            in[u] = L < lines && row < s.rows && col < s.width;
-            const long long at = in[u] ? row * s.ld + col : 0;
-            v[u] = ld_piece(s.p + at);
-            if (KEPT) z[u] = ld_piece(s.kept + at);
+            const bool in = (turn + u) * kStep < rows;
+            v[u] = ld_piece(in ? p : s.p);
+            if (KEPT) { w[u] = ld_piece(in ? z : s.kept); z += step; }
+            p += step;
         }
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const int L = first + u * kGroupWarps * at_once;
-            if (L >= lines) break;
+            if (!((turn + u) * kStep < rows)) v[u] = make_uint4(0, 0, 0, 0);
+            static_assert(kStep % 8 == 0, "the pieces of these lines are exchanged alike");
+            const uint32_t to = at + (turn + u) * kStep * 128;
+            if ((turn + u) * kStep + line >= lines) break;
+            if constexpr (sizeof(T) == 2 && !KEPT) {
+                st_shared(to, v[u]);
+                continue;
+            }
             float f[V];
             unpack16<T>(v[u], f);
             if (KEPT) {
                 float x[V];
-                unpack16<T>(z[u], x);
+                unpack16<T>(w[u], x);
 #pragma unroll
-                for (int e = 0; e < V; e += 2) {
-                    slope_pair(s.act, x[e], x[e + 1]);
-                    f[e] *= x[e]; f[e + 1] *= x[e + 1];
-                }
+                for (int e = 0; e < V; ++e) f[e] *= act_slope(s.act, x[e]);
+                if (!((turn + u) * kStep < rows))                  // a slope that is not a number may be another value's
+#pragma unroll
+                    for (int e = 0; e < V; ++e) f[e] = 0.f;
             }
-            if (!in[u])
-#pragma unroll
-                for (int e = 0; e < V; ++e) f[e] = 0.f;
-            const uint32_t at = dst + L * 128 + ((((col0 * 2) >> 4) ^ (L & 7)) << 4) + (col0 * 2 & 15);
             if (sizeof(T) == 4) {
                 uint32_t h[2], m[2], l[2];
                 split(f[0], f[1], h[0], m[0], l[0]);
                 split(f[2], f[3], h[1], m[1], l[1]);
-                st_shared(at, h[0], h[1]);
-                st_shared(at + part_bytes, m[0], m[1]);
-                st_shared(at + 2 * part_bytes, l[0], l[1]);
+                st_shared(to, h[0], h[1]);
+                st_shared(to + part_bytes, m[0], m[1]);
+                st_shared(to + 2 * part_bytes, l[0], l[1]);
             } else {
-                st_shared(at, make_uint4(pack(f[0], f[1]), pack(f[2], f[3]), pack(f[4 % V], f[5 % V]), pack(f[6 % V], f[7 % V])));
+                st_shared(to, make_uint4(pack(f[0], f[1]), pack(f[2], f[3]), pack(f[4 % V], f[5 % V]), pack(f[6 % V], f[7 % V])));
             }
         }
     }
 }
+// One operand's block of `lines` lines (a multiple of 16).  Line L: K-major row r0 + L from column c0 on; MN-major row r0 + L % 64 from column
+// c0 + L / 64 * 64 on.
 template <typename T, bool MN, bool KEPT> __device__ __forceinline__ void fill(uint32_t dst, int lines, uint32_t part_bytes, const Source<T>& s, long long r0, long long c0, int warp, int lane) {
-    if (s.pieces) fill_pieces<T, MN, KEPT>(dst, lines, part_bytes, s, r0, c0, warp, lane);
-    else fill_values<T, MN, KEPT>(dst, lines, part_bytes, s, r0, c0, warp, lane);
+#pragma unroll 1
+    for (int L = 0; L < lines; L += kBlockC) {
+        if (s.pieces) fill_pieces<T, KEPT>(dst + L * 128, lines - L, part_bytes, s, MN ? r0 : r0 + L, MN ? c0 + L : c0, warp, lane);
+        else fill_values<T, KEPT>(dst + L * 128, lines - L, part_bytes, s, MN ? r0 : r0 + L, MN ? c0 + L : c0, warp, lane);
+    }
 }
 
 // ---- epilogue ---------------------------------------------------------------------------------------------------------------
@@ -296,20 +338,12 @@ template <> __device__ __forceinline__ uint4 pack16<__nv_bfloat16>(const float* 
 template <typename T, Role ROLE> struct Result { using type = T; };
 template <typename T> struct Result<T, kGradW> { using type = float; };
 
-template <typename T> __device__ __forceinline__ void add_piece(float* f, uint4 v);
-template <> __device__ __forceinline__ void add_piece<float>(float* f, uint4 v) {
-    un2(add2(f2(f[0], f[1]), f2(__uint_as_float(v.x), __uint_as_float(v.y))), f[0], f[1]);
-    un2(add2(f2(f[2], f[3]), f2(__uint_as_float(v.z), __uint_as_float(v.w))), f[2], f[3]);
-}
-template <> __device__ __forceinline__ void add_piece<__nv_bfloat16>(float* f, uint4 v) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+template <typename T> __device__ __forceinline__ void add_piece(float* f, uint4 v) {
+    float g[Elem<T>::kVec];
+    unpack16<T>(v, g);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) un2(add2(f2(f[2 * q], f[2 * q + 1]), f2(__uint_as_float(w[q] << 16), __uint_as_float(w[q] & 0xffff0000u))), f[2 * q], f[2 * q + 1]);
+    for (int e = 0; e < Elem<T>::kVec; ++e) f[e] += g[e];
 }
-
-// Staged rows of 128 bytes: the 16-byte pieces of row r are exchanged by r % 8, so that eight rows' pieces of a column lie in different
-// banks.  Byte b of row r:
-__device__ __forceinline__ uint32_t staged(int r, uint32_t b) { return r * 128 + (b ^ ((uint32_t)(r & 7) << 4)); }
 
 __device__ __forceinline__ void st_value(uint32_t at, float v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "f"(v) : "memory"); }
 __device__ __forceinline__ void st_value(uint32_t at, __nv_bfloat16 v) { asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(__bfloat16_as_ushort(v)) : "memory"); }
@@ -325,15 +359,16 @@ __device__ __forceinline__ __nv_bfloat16 get_value(uint32_t at, __nv_bfloat16) {
 }
 // Where rows are not whole aligned 16-byte pieces: 32 staged rows, the first `rows` of them and `cols` values of each, from or to a matrix.
 template <typename T> __device__ __forceinline__ void rows_in(uint32_t slot, const T* src, long long ld, int rows, int cols, int lane) {
-    constexpr int per_lane = 128 / sizeof(T) / 32;
-    for (int r = 0; r < rows; r += 4) {
-        T v[4][per_lane];
+    constexpr int per_lane = 128 / sizeof(T) / 32, kBatch = 8;
+#pragma unroll 1
+    for (int r = 0; r < rows; r += kBatch) {
+        T v[kBatch][per_lane];
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < kBatch; ++u)
 #pragma unroll
             for (int q = 0; q < per_lane; ++q) v[u][q] = ld_value(src + (r + u < rows && lane + 32 * q < cols ? (r + u) * ld + lane + 32 * q : 0));
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < kBatch; ++u)
 #pragma unroll
             for (int q = 0; q < per_lane; ++q) st_value(slot + staged(r + u, (lane + 32 * q) * sizeof(T)), v[u][q]);
     }
@@ -362,15 +397,15 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const uint32_t b_part = (uint32_t)p.bn * 128, b_bytes = b_part * PARTS, stage_bytes = kABytes * PARTS + (p.resident ? 0 : b_bytes);
     const uint32_t resident = base + p.stages * stage_bytes;
-    const uint32_t staging = resident + (p.resident ? (uint32_t)p.blocks * b_bytes : 0), slots = p.slots + (p.z && p.residual ? 1 : 0);
-    const uint32_t strips = staging + EPI * slots * kSlotBytes;    // of an epilogue warp: the bias of its columns
+    const uint32_t staging = resident + (p.resident ? (uint32_t)p.blocks * b_bytes : 0);
+    const uint32_t strips = staging + EPI * kSlotBytes;    // of an epilogue warp: the bias of its columns
     const uint32_t full = strips + EPI * 256, empty = full + 8 * kMaxStages, acc_full = empty + 8 * kMaxStages, acc_empty = acc_full + 16,
-                   b_full = acc_empty + 16, res_full = b_full + 8, slot = res_full + 16 * kMostEpi;
+                   b_full = acc_empty + 16, res_full = b_full + 8, slot = res_full + 8 * kMostEpi;
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8 * s, TMA ? 1 : kGroupWarps); mbar_init(empty + 8 * s, 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(acc_full + 8 * s, 1); mbar_init(acc_empty + 8 * s, EPI); }
         mbar_init(b_full, TMA ? 1 : kFillWarps);
-        for (int s = 0; s < 2 * EPI; ++s) mbar_init(res_full + 8 * s, 1);
+        for (int s = 0; s < EPI; ++s) mbar_init(res_full + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) {
@@ -382,30 +417,31 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+    tmem = __shfl_sync(0xffffffffu, tmem, 0);                      // known to be uniform, as an instruction's operands have to be
 
     bool alive = true;
-    unsigned k = 0;                                                // blocks of c, tiles so far
-    int n = 0;
+    int n = 0;                                                     // tiles so far
     if (TMA && warp == 0) {
+        const uint32_t a_expect = stage_bytes - (A_MN ? 0 : (kBlockI - p.a_rows) * 128);
         // ---- the ring, by TMA -------------------------------------------------------------------------------------------------
-        for (Walk u = walk(p); u.live && alive; next(u, p), ++n) {
-            const int i0 = u.i * kBlockI, j0 = u.j * p.bn;
-            if (p.resident && n == 0 && lane == 0) {
-                mbar_expect(b_full, (unsigned)p.blocks * b_bytes);
-                for (int c = 0; c < p.blocks; ++c) {
-                    if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(resident + c * b_bytes + m * 128, &map_b, b_full, j0 + m, c * kBlockC);
-                    else tma_load_2d(resident + c * b_bytes, &map_b, b_full, c * kBlockC, j0);
+        // by one lane: a block of c takes little more than its loads' issue
+        if (lane == 0) {
+            Ring r{};
+            for (Walk u = walk(p); u.live && alive; next(u, p), ++n) {
+                const int i0 = u.i * kBlockI, j0 = u.j * p.bn;
+                if (p.resident && n == 0) {
+                    mbar_expect(b_full, (unsigned)p.blocks * b_bytes);
+                    for (int c = 0; c < p.blocks; ++c) {
+                        if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(resident + c * b_bytes + m * 128, &map_b, b_full, j0 + m, c * kBlockC);
+                        else tma_load_2d(resident + c * b_bytes, &map_b, b_full, c * kBlockC, j0);
+                    }
                 }
-            }
-            __syncwarp();
-            for (int c = u.c0; c < u.c1; ++c, ++k) {
-                const unsigned s = k % (unsigned)p.stages, round = k / (unsigned)p.stages;
-                if (round > 0) alive = wait_warp(empty + 8 * s, (round - 1) & 1, 0x10000000u | k);
-                if (!alive) break;
-                if (lane == 0) {
-                    const uint32_t at = base + s * stage_bytes, bar = full + 8 * s;
+                for (int c = u.c0; c < u.c1; ++c, r.next(p.stages)) {
+                    if (r.round > 0) alive = wait_lane(empty + 8 * r.s, (r.round - 1) & 1, 0x10000000u | r.round);
+                    if (!alive) break;
+                    const uint32_t at = base + r.s * stage_bytes, bar = full + 8 * r.s;
                     const int c0 = c * kBlockC;
-                    mbar_expect(bar, stage_bytes - (A_MN ? 0 : (kBlockI - p.a_rows) * 128));
+                    mbar_expect(bar, a_expect);
                     if (A_MN) for (int m = 0; m < kBlockI; m += 64) tma_load_2d(at + m * 128, &map_a, bar, i0 + m, c0);
                     else tma_load_2d(at, &map_a, bar, c0, i0);
                     if (!p.resident) {
@@ -413,41 +449,67 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                         else tma_load_2d(at + kABytes, &map_b, bar, c0, j0);
                     }
                 }
-                __syncwarp();
             }
+            if (!alive)                                            // what is still on its way here lands before the block goes
+                for (unsigned s = 0; s < (unsigned)p.stages; ++s)
+                    if (r.round > 0 || s < r.s) wait_lane(full + 8 * s, (s < r.s ? r.round : r.round - 1) & 1, 0x70000000u | s);
         }
-        if (!alive)                                                // what is still on its way here lands before the block goes
-            for (unsigned q = k > (unsigned)p.stages ? k - p.stages : 0; q < k; ++q) wait_warp(full + 8 * (q % p.stages), (q / p.stages) & 1, 0x70000000u | q);
+        __syncwarp();
     } else if (!TMA && warp >= kFirstFill) {
         // ---- the ring, by plain loads -------------------------------------------------------------------------------------------
         const int group = (warp - kFirstFill) / kGroupWarps, w = (warp - kFirstFill) % kGroupWarps;
+        static_assert(kFillWarps == 2 * kGroupWarps, "groups take turns");
+        Ring r{};
+        int turn = 0;
         for (Walk u = walk(p); u.live && alive; next(u, p), ++n) {
             const long long i0 = (long long)u.i * kBlockI, j0 = u.j * p.bn;
             if (p.resident && n == 0) {
-                for (int c = group; c < p.blocks; c += kFillWarps / kGroupWarps)
-                    fill<T, B_MN, false>(resident + c * b_bytes, p.bn, b_part, p.b, B_MN ? c * kBlockC : j0, B_MN ? j0 : c * kBlockC, w, lane);
+                const bool asks = PARTS == 1 && p.b_tma && group == 0 && w == 0 && lane == 0;
+                if (asks) {
+                    mbar_expect(b_full, (unsigned)p.blocks * b_bytes);
+                    for (int c = 0; c < p.blocks; ++c) {
+                        if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(resident + c * b_bytes + m * 128, &map_b, b_full, (int)j0 + m, c * kBlockC);
+                        else tma_load_2d(resident + c * b_bytes, &map_b, b_full, c * kBlockC, (int)j0);
+                    }
+                }
+                if (PARTS == 3 || !p.b_tma)
+                    for (int c = group; c < p.blocks; c += kFillWarps / kGroupWarps)
+                        fill<T, B_MN, false>(resident + c * b_bytes, p.bn, b_part, p.b, B_MN ? c * kBlockC : j0, B_MN ? j0 : c * kBlockC, w, lane);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(b_full);
+                if (lane == 0 && !asks) mbar_arrive(b_full);
             }
-            for (int c = u.c0; c < u.c1; ++c, ++k) {
-                if (k % (kFillWarps / kGroupWarps) != (unsigned)group) continue;
-                const unsigned s = k % (unsigned)p.stages, round = k / (unsigned)p.stages;
-                if (round > 0) alive = wait_warp(empty + 8 * s, (round - 1) & 1, 0x20000000u | k);
+            for (int c = u.c0; c < u.c1; ++c, r.next(p.stages), turn ^= 1) {
+                if (turn != group) continue;
+                if (r.round > 0) alive = wait_warp(empty + 8 * r.s, (r.round - 1) & 1, 0x20000000u | r.round);
                 if (!alive) break;
-                const uint32_t at = base + s * stage_bytes;
+                const uint32_t at = base + r.s * stage_bytes;
                 const long long c0 = (long long)c * kBlockC;
+                const bool ta = PARTS == 1 && p.a_tma, tb = PARTS == 1 && p.b_tma;
+                const bool asks = (ta || (tb && !p.resident)) && w == 0 && lane == 0;
+                if (asks) {                                        // its arrival at the barrier, with the bytes that it asks for
+                    mbar_expect(full + 8 * r.s, (ta ? (A_MN ? kABytes : p.a_rows * 128) : 0) + (tb && !p.resident ? b_bytes : 0));
+                    if (ta) {
+                        if (A_MN) for (int m = 0; m < kBlockI; m += 64) tma_load_2d(at + m * 128, &map_a, full + 8 * r.s, (int)i0 + m, (int)c0);
+                        else tma_load_2d(at, &map_a, full + 8 * r.s, (int)c0, (int)i0);
+                    }
+                    if (tb && !p.resident) {
+                        if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(at + kABytes + m * 128, &map_b, full + 8 * r.s, (int)j0 + m, (int)c0);
+                        else tma_load_2d(at + kABytes, &map_b, full + 8 * r.s, (int)c0, (int)j0);
+                    }
+                }
                 if (ROLE != kForward && p.a.kept) fill<T, A_MN, true>(at, kBlockI, kABytes, p.a, A_MN ? c0 : i0, A_MN ? i0 : c0, w, lane);
-                else fill<T, A_MN, false>(at, kBlockI, kABytes, p.a, A_MN ? c0 : i0, A_MN ? i0 : c0, w, lane);
-                if (!p.resident) fill<T, B_MN, false>(at + PARTS * kABytes, p.bn, b_part, p.b, B_MN ? c0 : j0, B_MN ? j0 : c0, w, lane);
+                else if (!ta) fill<T, A_MN, false>(at, kBlockI, kABytes, p.a, A_MN ? c0 : i0, A_MN ? i0 : c0, w, lane);
+                if (!p.resident && !tb) fill<T, B_MN, false>(at + PARTS * kABytes, p.bn, b_part, p.b, B_MN ? c0 : j0, B_MN ? j0 : c0, w, lane);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(full + 8 * s);
+                if (lane == 0 && !asks) mbar_arrive(full + 8 * r.s);
             }
         }
     } else if (warp == 1) {
         // ---- issue --------------------------------------------------------------------------------------------------------------
         const uint32_t idesc = instr_desc<A_MN, B_MN>(p.bn);
+        Ring r{};
         for (Walk u = walk(p); u.live && alive; next(u, p), ++n) {
             const int buf = n & 1;
             if (n >= 2) alive = wait_warp(acc_empty + 8 * buf, (unsigned)((n >> 1) - 1) & 1, 0x30000000u | (unsigned)n);
@@ -455,14 +517,13 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             if (!alive) break;
             fence_after();
             const uint32_t d = tmem + buf * kTmemBuffer;
-            for (int c = u.c0; c < u.c1; ++c, ++k) {
-                const unsigned s = k % (unsigned)p.stages;
-                alive = wait_warp(full + 8 * s, (k / (unsigned)p.stages) & 1, 0x50000000u | k);
+            for (int c = u.c0; c < u.c1; ++c, r.next(p.stages)) {
+                alive = wait_warp(full + 8 * r.s, r.round & 1, 0x50000000u | r.round);
                 if (!alive) break;
                 fence_after();
-                const uint32_t a_at = base + s * stage_bytes, b_at = p.resident ? resident + (uint32_t)c * b_bytes : a_at + PARTS * kABytes;
+                const uint32_t a_at = base + r.s * stage_bytes, b_at = p.resident ? resident + (uint32_t)c * b_bytes : a_at + PARTS * kABytes;
                 const unsigned long long da = smem_desc<A_MN>(a_at), db = smem_desc<B_MN>(b_at);
-#pragma unroll 1
+#pragma unroll
                 for (int t = 0; t < kBlockC / 16; ++t) {
                     const unsigned long long at = da + t * (step16<A_MN> >> 4), bt = db + t * (step16<B_MN> >> 4);
                     const bool add = c > u.c0 || t > 0;
@@ -477,7 +538,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                         mma(d2, at, bt + pb, idesc, true);
                     }
                 }
-                commit(empty + 8 * s);
+                commit(empty + 8 * r.s);
             }
             commit(acc_full + 8 * buf);
         }
@@ -487,12 +548,11 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         using O = typename Result<T, ROLE>::type;
         constexpr int UC = 128 / sizeof(O), V = Elem<O>::kVec, TEAM = EPI / 4;
         const int e = warp - kFirstEpi, quarter = warp & 3, member = e / 4, per_tile = (p.bn + UC - 1) / UC;
-        const uint32_t mine = staging + e * slots * kSlotBytes, res_bar = res_full + e * 16;
+        const uint32_t mine = staging + e * kSlotBytes, res_bar = res_full + e * 8;
         const uint32_t lane_at = lane * 128 + ((lane & 7) << 4), strip = strips + e * 256;   // a piece q of this lane's row: xor q << 4
-        const unsigned two = p.slots - 1;
         const bool has_z = ROLE == kForward && p.z, has_res = ROLE == kForward && p.residual, has_bias = ROLE == kForward && p.bias;
-        unsigned uses = 0;                                         // of the slots that residuals and results lie in
-        // the residual of this warp's next unit, from unit c of tile u on, into the slot that it will have; `turn` is whose c is
+        unsigned units = 0;                                        // of this warp so far
+        // the residual of this warp's next unit, from unit c of tile u on, into its slot; `turn` is whose c is
         auto fetch = [&](Walk u, int c, int turn) {
             for (; u.live; next(u, p), c = 0) {
                 const int i0 = u.i * kBlockI + quarter * 32, j0 = u.j * p.bn, wide = min(p.J - j0, p.bn);
@@ -500,14 +560,14 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     const bool ours = turn == member && c * UC < wide && i0 < p.I;
                     turn = turn + 1 == TEAM ? 0 : turn + 1;
                     if (!ours) continue;
-                    mbar_expect(res_bar + (uses & two) * 8, kSlotBytes);
-                    tma_load_3d(mine + (uses & two) * kSlotBytes, &map_res, res_bar + (uses & two) * 8, j0 + c * UC, i0, 0);
+                    mbar_expect(res_bar, kSlotBytes);
+                    tma_load_3d(mine, &map_res, res_bar, j0 + c * UC, i0, 0);
                     return;
                 }
             }
         };
         Walk u = walk(p);
-        if (p.by_tma && has_res && lane == 0) fetch(u, 0, 0);
+        if (p.by_tma && has_res && !has_z && lane == 0) fetch(u, 0, 0);
         __syncwarp();
         int turn = 0;                                              // which member of the team has the next unit
         for (; u.live && alive; next(u, p), ++n) {
@@ -521,25 +581,28 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 const bool ours = turn == member && c * UC < wide && rows > 0;
                 turn = turn + 1 == TEAM ? 0 : turn + 1;
                 if (!ours) continue;
-                const uint32_t at = mine + (uses & two) * kSlotBytes, z_at = mine + p.slots * kSlotBytes;
                 const int col = j0 + c * UC, cols = min(wide - c * UC, UC);
                 if (has_bias)
 #pragma unroll
                     for (int v = lane; v < UC; v += 32) st_value(strip + v * 4, v < cols ? Elem<T>::to_f32(ld_value(p.bias + col + v)) : 0.f);
-                if (p.by_tma) {
-                    if (lane == 0) { if (two) bulk_wait_read<1>(); else bulk_wait_read<0>(); }   // the slots have been read
-                    if (has_res) alive = wait_warp(res_bar + (uses & two) * 8, (uses >> two) & 1, 0x80000000u | (unsigned)n);
-                    if (!alive) break;
-                } else if (has_res) {
-                    if constexpr (ROLE == kForward) rows_in<T>(at, p.residual + (long long)i0 * p.J + col, p.J, rows, cols, lane);
-                }
+                if (p.by_tma && lane == 0) bulk_wait_read<0>();    // the slot has been read
                 __syncwarp();
                 // Loops that stay loops: a role's code has to stay in the instruction cache beside the others' (unrolled, waiting for
-                // instructions was most of this kernel's time).  z without a residual leaves first, through the same slot.
+                // instructions was most of this kernel's time).  z leaves first, through the same slot.
 #pragma unroll 1
-                for (int pass = has_z && !has_res ? 0 : 1; pass < 2; ++pass) {
+                for (int pass = has_z ? 0 : 1; pass < 2; ++pass) {
+                    if (pass == 1 && has_res) {
+                        if (!p.by_tma) {
+                            if constexpr (ROLE == kForward) rows_in<T>(mine, p.residual + (long long)i0 * p.J + col, p.J, rows, cols, lane);
+                            __syncwarp();
+                        } else {
+                            if (has_z && lane == 0) fetch(u, c, member);
+                            alive = wait_warp(res_bar, units & 1, 0x80000000u | (unsigned)n);
+                            if (!alive) break;
+                        }
+                    }
 #pragma unroll 1
-                    for (int q = 0; q < 8; q += 2) {
+                    for (int q = 0; q * V < cols; q += 2) {
                         float f[2 * V];
                         tmem_ld(d + c * UC + q * V, f);
                         tmem_wait_ld();
@@ -554,50 +617,46 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                         if (has_bias)
 #pragma unroll
                             for (int v = 0; v < 2 * V; v += 4) add_piece<float>(f + v, ld_shared(strip + (q * V + v) * 4));
-                        if (has_z && has_res) {
-                            st_shared(z_at + left, pack16<O>(f));
-                            st_shared(z_at + right, pack16<O>(f + V));
-                        }
                         if (ROLE == kForward && pass == 1) {
                             if (p.act == kActGelu)
 #pragma unroll
-                                for (int v = 0; v < 2 * V; v += 2) act_pair(kActGelu, f[v], f[v + 1]);
+                                for (int v = 0; v < 2 * V; ++v) f[v] = gelu<O>(f[v]);
                             else if (p.act == kActRelu)
 #pragma unroll
-                                for (int v = 0; v < 2 * V; v += 2) act_pair(kActRelu, f[v], f[v + 1]);
+                                for (int v = 0; v < 2 * V; ++v) f[v] = max_nan(f[v], 0.f);
                             if (has_res) {
-                                add_piece<O>(f, ld_shared(at + left));
-                                add_piece<O>(f + V, ld_shared(at + right));
+                                add_piece<O>(f, ld_shared(mine + left));
+                                add_piece<O>(f + V, ld_shared(mine + right));
                             }
                         }
-                        st_shared(at + left, pack16<O>(f));
-                        st_shared(at + right, pack16<O>(f + V));
+                        st_shared(mine + left, pack16<O>(f));
+                        st_shared(mine + right, pack16<O>(f + V));
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-                    if (ROLE == kForward && p.z && (pass == 0 || has_res)) {
-                        const uint32_t from = pass == 0 ? at : z_at;
+                    if (pass == 0) {
                         if (p.by_tma) {
-                            if (lane == 0) { tma_store_3d(&map_z, from, col, i0, 0); bulk_commit(); if (pass == 0) bulk_wait_read<0>(); }
+                            if (lane == 0) { tma_store_3d(&map_z, mine, col, i0, 0); bulk_commit(); bulk_wait_read<0>(); }
                         } else {
-                            if constexpr (ROLE == kForward) rows_out<T>(from, p.z + (long long)i0 * p.J + col, p.J, rows, cols, lane);
+                            if constexpr (ROLE == kForward) rows_out<T>(mine, p.z + (long long)i0 * p.J + col, p.J, rows, cols, lane);
                         }
                         __syncwarp();
                     }
                 }
-                ++uses;
+                if (!alive) break;
+                ++units;
                 if (p.by_tma) {
                     if (lane == 0) {
-                        tma_store_3d(&map_out, at, col, i0, u.split); bulk_commit();
-                        if (has_res) {                             // the next one into its slot, once that has been read
-                            if (!two) bulk_wait_read<0>(); else if (has_z) bulk_wait_read<2>(); else bulk_wait_read<1>();
+                        tma_store_3d(&map_out, mine, col, i0, u.split); bulk_commit();
+                        if (has_res && !has_z) {
+                            bulk_wait_read<0>();
                             fetch(u, c + 1, turn);
                         }
                     }
                 } else {
                     O* out;
                     if constexpr (ROLE == kGradW) out = p.part + u.split * p.I * p.J; else out = p.out;
-                    rows_out<O>(at, out + (long long)i0 * p.J + col, p.J, rows, cols, lane);
+                    rows_out<O>(mine, out + (long long)i0 * p.J + col, p.J, rows, cols, lane);
                 }
                 __syncwarp();
             }
