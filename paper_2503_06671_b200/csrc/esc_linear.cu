@@ -116,7 +116,7 @@ template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long lon
     const bool a_pieces = whole_pieces(p.a.p, p.a.ld, sizeof(T)), b_pieces = whole_pieces(p.b.p, p.b.ld, sizeof(T));
     CUtensorMap ma{}, mb{}, mo{}, mr{}, mz{};
     p.a_rows = (int)std::min<long long>(um::kBlockI, (p.I + 7) / 8 * 8);
-    p.a_tma = sizeof(T) == 2 && !p.a.kept && a_pieces && map_of<T>(&ma, p.a.p, 0, p.a.rows, p.a.width, p.a.ld, a_mn ? um::kBlockC : p.a_rows);
+    p.a_tma = sizeof(T) == 2 && a_pieces && map_of<T>(&ma, p.a.p, 0, p.a.rows, p.a.width, p.a.ld, a_mn ? um::kBlockC : p.a_rows);
     const auto cut_for = [&] { return cut(ROLE, p.I, p.J, depth, sizeof(T), p.a_tma && p.b_tma); };
     p.b_tma = sizeof(T) == 2 && b_pieces;
     Cut c = cut_for();
@@ -134,7 +134,7 @@ template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long lon
     p.by_tma = (c.tiles_j == 1 || c.bn % (int)(128 / sizeof(O)) == 0) && whole_pieces(out, p.J, sizeof(O)) && map_of<O>(&mo, out, c.splits, p.I, p.J, p.J, 32) &&
                abi::aligned(p.bias, 16) && (!p.residual || (whole_pieces(p.residual, p.J, sizeof(T)) && map_of<T>(&mr, p.residual, 1, p.I, p.J, p.J, 32))) &&
                (!p.z || (whole_pieces(p.z, p.J, sizeof(T)) && map_of<T>(&mz, p.z, 1, p.I, p.J, p.J, 32)));
-    p.a.pieces = a_pieces && p.a.width % V == 0 && abi::aligned(p.a.kept, 16);
+    p.a.pieces = a_pieces && p.a.width % V == 0;
     p.b.pieces = b_pieces && p.b.width % V == 0;
     auto launch = [&](auto kernel, int warps) {
         ESC_ABI_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)um::kMostSmem));   // the same for every call
@@ -146,13 +146,15 @@ template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long lon
     return launch(um::product_umma<T, ROLE, false>, um::all_warps<false>);
 }
 
-// Partial sums of grad_bias: as many blocks as fill the SMs four times.
+// grad_z_sums: pieces of a row to a block, and as many blocks as fill the SMs four times, which leave a partial sum each.
 struct BiasCut { int across, parts; };
-BiasCut bias_cut(const Call& c, bool pieces) {
-    const long long wide = pieces ? std::min(c.N / 8, 32) * 8 : 32, across = (c.N + wide - 1) / wide;
-    return {(int)across, (int)std::max(1LL, std::min((4LL * abi::sm_count() + across - 1) / across, (c.rows + 31) / 32))};
+BiasCut bias_cut(const Call& c, int vec) {
+    const int all = c.N / vec, wide = std::min(all, 32), across = (all + wide - 1) / wide;
+    return {across, (int)std::max(1LL, std::min((4LL * abi::sm_count() + across - 1) / across, (c.rows + 31) / 32))};
 }
-struct LinearWs { float *part, *bias; bf16* g; size_t bytes; };
+// g lies in rows of whole 16-byte pieces, whatever N is.
+long long g_stride(const Call& c) { return (long long)abi::round_up(c.N, 16 / c.es()); }
+struct LinearWs { float *part, *bias; void* g; size_t bytes; };
 LinearWs carve(void* ws, const Call& c) {
     LinearWs w;
     char* base = static_cast<char*>(ws);
@@ -160,14 +162,15 @@ LinearWs carve(void* ws, const Call& c) {
     auto take = [&](size_t bytes) { char* p = base + off; off += abi::round_up(bytes, 256); return p; };
     w.part = reinterpret_cast<float*>(take((size_t)std::max(cut(lin::kGradW, c.N, c.K, std::max(c.rows, 1LL), c.es(), false).splits, cut(lin::kGradW, c.N, c.K, std::max(c.rows, 1LL), c.es(), true).splits) *
                                           c.N * c.K * sizeof(float)));
-    w.bias = reinterpret_cast<float*>(take((size_t)std::max(bias_cut(c, false).parts, c.N % 8 ? 0 : bias_cut(c, true).parts) * c.N * sizeof(float)));
-    w.g = reinterpret_cast<bf16*>(take(c.dtype == ESC_BF16 && c.act != ESC_ACT_NONE && c.N % 8 == 0 ? (size_t)c.rows * c.N * sizeof(bf16) : 0));
+    const int vec = 16 / (int)c.es();
+    w.bias = reinterpret_cast<float*>(take((size_t)std::max(bias_cut(c, 1).parts, c.N < vec ? 0 : bias_cut(c, vec).parts) * c.N * sizeof(float)));
+    w.g = take(c.act != ESC_ACT_NONE ? (size_t)c.rows * g_stride(c) * c.es() : 0);
     w.bytes = off;
     return w;
 }
 
-template <typename T> um::Source<T> source(const void* p, long long rows, long long width, long long ld, const T* kept = nullptr, int act = 0) {
-    return um::Source<T>{static_cast<const T*>(p), kept, rows, width, ld, act, false};
+template <typename T> um::Source<T> source(const void* p, long long rows, long long width, long long ld) {
+    return um::Source<T>{static_cast<const T*>(p), rows, width, ld, false};
 }
 
 template <typename T> int linear_forward_t(const Call& c, const lin::Layer<T>& l, cudaStream_t st) {
@@ -188,26 +191,21 @@ int sum_to(const float* part, int parts, long long count, void* out, int grad_dt
 }
 
 template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& l, void* gw, void* gb, int grad_dtype, const LinearWs& w, cudaStream_t st) {
-    const T *go = l.go, *kept = c.act == ESC_ACT_NONE ? nullptr : l.kept;
-    bool sums_there = false;
-    if constexpr (sizeof(T) == 2) {
-        if (c.N % 8 == 0 && abi::aligned(go, 16) && abi::aligned(kept, 16) && (kept || gb)) {
-            const BiasCut b = bias_cut(c, true);
-            bf16* g = kept && (l.gx || gw) ? w.g : nullptr;
-            lin::grad_z_pieces<<<dim3(b.across, b.parts), 256, 0, st>>>(l, g, gb ? w.bias : nullptr);
-            ESC_TRY(launched());
-            if (gb) ESC_TRY(sum_to(w.bias, b.parts, c.N, gb, grad_dtype, st));
-            if (g) { go = g; kept = nullptr; }
-            sums_there = true;
-        }
-    }
-    if (gb && !sums_there) {
-        const BiasCut b = bias_cut(c, false);
-        lin::grad_bias_parts<T><<<dim3(b.across, b.parts), 256, 0, st>>>(l, w.bias);
+    constexpr int V = esc::Elem<T>::kVec;
+    um::Source<T> g = source<T>(l.go, c.rows, c.N, c.N);
+    const bool acts = c.act != ESC_ACT_NONE && (l.gx || gw);
+    if (acts || gb) {
+        T* to = acts ? static_cast<T*>(w.g) : nullptr;
+        const long long ld = g_stride(c);
+        const bool pieces = c.N % V == 0 && abi::aligned(l.go, 16) && (c.act == ESC_ACT_NONE || abi::aligned(l.kept, 16));
+        const BiasCut b = bias_cut(c, pieces ? V : 1);
+        const dim3 grid(b.across, b.parts);
+        if (pieces) lin::grad_z_sums<T, V><<<grid, 256, 0, st>>>(l, to, ld, gb ? w.bias : nullptr);
+        else lin::grad_z_sums<T, 1><<<grid, 256, 0, st>>>(l, to, ld, gb ? w.bias : nullptr);
         ESC_TRY(launched());
-        ESC_TRY(sum_to(w.bias, b.parts, c.N, gb, grad_dtype, st));
+        if (gb) ESC_TRY(sum_to(w.bias, b.parts, c.N, gb, grad_dtype, st));
+        if (acts) g = source<T>(to, c.rows, c.N, ld);
     }
-    const um::Source<T> g = source<T>(go, c.rows, c.N, c.N, kept, c.act);
     if (l.gx) {
         um::Args<T> p{};
         p.I = c.rows; p.J = c.K;

@@ -70,72 +70,61 @@ template <typename T> struct Layer {
     T* gx;
 };
 
-template <typename T> __device__ __forceinline__ float grad_z(const Layer<T>& p, long long row, int n) {
-    const float g = Elem<T>::to_f32(p.go[row * p.N + n]);
-    return p.act == kActNone ? g : g * act_slope(p.act, Elem<T>::to_f32(p.kept[row * p.N + n]));
-}
-
 enum Role { kForward, kGradX, kGradW };
 
-// Column sums of g: a block has 32 columns and every gridDim.y-th run of eight rows; part [gridDim.y][N].
-template <typename T> __global__ void __launch_bounds__(256) grad_bias_parts(const Layer<T> p, float* part)
-{
-    __shared__ float acc[8][32];
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, n = blockIdx.x * 32 + lane;
-    float s = 0.f;
-    if (n < p.N)
-        for (long long row = (long long)blockIdx.y * 8 + warp; row < p.rows; row += (long long)gridDim.y * 8) s += grad_z(p, row, n);
-    acc[warp][lane] = s;
-    __syncthreads();
-    if (warp != 0 || n >= p.N) return;
-#pragma unroll
-    for (int v = 1; v < 8; ++v) s += acc[v][lane];
-    part[(size_t)blockIdx.y * p.N + n] = s;
+// g = go act'(z) and its column sums, as far as they are asked for: g [rows, g_ld] of the type (rounded: the operand that two products
+// read), part [gridDim.y][N] fp32 sums of the unrounded g.  A thread has V neighbouring columns and every so many rows; a block has
+// min(N / V, 32) such pieces of a row.  V > 1: rows are whole aligned pieces.
+template <typename T, int V> __device__ __forceinline__ void load_values(const T* p, float* f) {
+    if constexpr (V == 1) f[0] = Elem<T>::to_f32(*p);
+    else unpack16<T>(*reinterpret_cast<const uint4*>(p), f);
 }
-
-// The same for bf16 rows of whole 16-byte pieces, and g itself where `g` is given: rounded to bf16, as the operand that two products read.
-// (The sums are of the unrounded g.)  A thread has eight columns and every so many rows; a block min(N / 8, 32) such pieces of a row.
-__global__ void __launch_bounds__(256) grad_z_pieces(const Layer<__nv_bfloat16> p, __nv_bfloat16* g, float* part)
+template <typename T, int V> __global__ void __launch_bounds__(256) grad_z_sums(const Layer<T> p, T* g, long long g_ld, float* part)
 {
-    using bf16 = __nv_bfloat16;
-    __shared__ float acc[256 * 8];
-    const int all = p.N / 8, across = all < 32 ? all : 32, down = 256 / across;
+    __shared__ float acc[256 * V];
+    const int all = p.N / V, across = all < 32 ? all : 32, down = 256 / across;
     const int col = threadIdx.x % across, v = blockIdx.x * across + col, r = threadIdx.x / across;
-    float sum[8] = {};
+    float sum[V] = {};
     if (r < down && v < all) {
-#pragma unroll 1
-        for (long long row = (long long)blockIdx.y * down + r; row < p.rows; row += (long long)gridDim.y * down) {
-            const long long at = row * p.N + v * 8;
-            float f[8];
-            unpack16<bf16>(*reinterpret_cast<const uint4*>(p.go + at), f);
+        const long long step = (long long)gridDim.y * down;
+#pragma unroll 2
+        for (long long row = (long long)blockIdx.y * down + r; row < p.rows; row += step) {
+            const long long at = row * p.N + v * V;
+            float f[V];
+            load_values<T, V>(p.go + at, f);
             if (p.act != kActNone) {
-                float z[8];
-                unpack16<bf16>(*reinterpret_cast<const uint4*>(p.kept + at), z);
+                float z[V];
+                load_values<T, V>(p.kept + at, z);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] *= act_slope(p.act, z[e]);
+                for (int e = 0; e < V; ++e) f[e] *= act_slope(p.act, z[e]);
             }
             if (g) {
-                uint32_t w[4];
+                T* to = g + row * g_ld + v * V;
+                if constexpr (V == 1) *to = Elem<T>::from_f32(f[0]);
+                else if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = make_float4(f[0], f[1], f[2], f[3]);
+                else {
+                    uint32_t w[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
-                    w[e] = *reinterpret_cast<const uint32_t*>(&h);
+                    for (int e = 0; e < 4; ++e) {
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
+                        w[e] = *reinterpret_cast<const uint32_t*>(&h);
+                    }
+                    *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
-                *reinterpret_cast<uint4*>(g + at) = make_uint4(w[0], w[1], w[2], w[3]);
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += f[e];
+            for (int e = 0; e < V; ++e) sum[e] += f[e];
         }
     }
     if (!part) return;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e * 256 + threadIdx.x] = sum[e];
+    for (int e = 0; e < V; ++e) acc[e * 256 + threadIdx.x] = sum[e];
     __syncthreads();
-    for (int c = threadIdx.x; c < across * 8; c += 256) {
-        const int n = blockIdx.x * across * 8 + c;
+    for (int c = threadIdx.x; c < across * V; c += 256) {
+        const int n = blockIdx.x * across * V + c;
         if (n >= p.N) break;
         float s = 0.f;
-        for (int q = 0; q < down; ++q) s += acc[c % 8 * 256 + q * across + c / 8];
+        for (int q = 0; q < down; ++q) s += acc[c % V * 256 + q * across + c / V];
         part[(size_t)blockIdx.y * p.N + n] = s;
     }
 }

@@ -43,6 +43,8 @@ __device__ unsigned wait_status[2];                                // ESC_DEV_TI
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void mbar_init(uint32_t bar, unsigned count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void mbar_expect(uint32_t bar, unsigned bytes) { asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory"); }
+// Bytes alone: who asks for them arrives later.
+__device__ __forceinline__ void mbar_bytes(uint32_t bar, unsigned bytes) { asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory"); }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 // Bounded wait of a whole warp; all lanes get the same answer.
 __device__ __forceinline__ bool wait_warp(uint32_t bar, unsigned parity, unsigned where) {
@@ -129,6 +131,12 @@ __device__ __forceinline__ float ld_value(const float* p) {
     asm volatile("ld.global.nc.b32 %0, [%1];" : "=f"(v) : "l"(p));
     return v;
 }
+__device__ __forceinline__ uint32_t ld_bits(const float* p) { return __float_as_uint(ld_value(p)); }
+__device__ __forceinline__ uint32_t ld_bits(const __nv_bfloat16* p) {
+    unsigned short v;
+    asm volatile("ld.global.nc.b16 %0, [%1];" : "=h"(v) : "l"(p));
+    return v;
+}
 __device__ __forceinline__ __nv_bfloat16 ld_value(const __nv_bfloat16* p) {
     unsigned short v;
     asm volatile("ld.global.nc.b16 %0, [%1];" : "=h"(v) : "l"(p));
@@ -137,9 +145,8 @@ __device__ __forceinline__ __nv_bfloat16 ld_value(const __nv_bfloat16* p) {
 
 // What a warp group loads of one operand: rows of `width` values, `ld` apart; `pieces`: rows are whole aligned 16-byte pieces.
 template <typename T> struct Source {
-    const T *p, *kept;
+    const T* p;
     long long rows, width, ld;
-    int act;
     bool pieces;
 };
 
@@ -148,7 +155,7 @@ template <typename T> struct Args {
     int J, tiles_i, tiles_j, bn, blocks, splits, stages;   // blocks: of c
     bool resident;                      // B stays in shared memory; a block keeps its tile of j
     unsigned units;
-    Source<T> a, b;                     // plain loads; a.kept: A = a act'(kept)
+    Source<T> a, b;
     int a_rows;                         // lines of A that TMA brings (K-major; the others' sums go nowhere)
     bool a_tma, b_tma;                  // beside plain loads: this operand comes by TMA
     int act;
@@ -208,122 +215,82 @@ __device__ __forceinline__ void split(float a, float b, uint32_t& hi, uint32_t& 
 // banks.  Byte b of row r:
 __device__ __forceinline__ uint32_t staged(int r, uint32_t b) { return r * 128 + (b ^ ((uint32_t)(r & 7) << 4)); }
 
-// 64 lines of 64 values: line l is row r0 + l from column c0 on.  What lies outside the matrix is zero.  Every load is issued before the first
-// is used, none is conditional (one that has nothing to read reads the matrix' first value).  The parts of fp32 lie `part_bytes` apart.
-// fill_values: a warp a line, a lane two values of it; fill_pieces: a lane 16 bytes.
-template <typename T, bool KEPT> __device__ __forceinline__ void fill_values(uint32_t dst, int lines, uint32_t part_bytes, const Source<T>& s, long long r0, long long c0, int warp, int lane) {
-    constexpr int kStep = kGroupWarps, kTurns = kBlockC / kStep, kBatch = KEPT ? 2 : sizeof(T) == 4 ? 4 : 8;
-    const long long col = c0 + 2 * lane, left = s.rows - r0 - warp;
-    const bool one = col < s.width, two = col + 1 < s.width;
-    const int rows = (int)min(left, (long long)(lines - warp));    // of this warp's: line warp + u kStep is there for u kStep < rows
-    const long long step = s.ld * kStep;
-    const T* p = s.p + (r0 + warp) * s.ld + col;
-    const T* z = s.kept + (r0 + warp) * s.ld + col;
-    const uint32_t at = dst + staged(warp, lane * 4);
-#pragma unroll 1
-    for (int turn = 0; turn < kTurns; turn += kBatch) {
-        if (turn * kStep + warp >= lines) break;
-        T lo[kBatch], hi[kBatch], zl[kBatch], zh[kBatch];
+// 64 lines of 64 values of an operand: line l is row r0 + l from column c0 on.  What lies outside the matrix is zero, lines from `lines` on
+// are left out.  The warps of a group take every kGroupWarps-th line, a lane two values of it, or 16 bytes where rows allow that.
+template <typename T> struct Chunk {
+    static constexpr int V = Elem<T>::kVec, kLanes = 64 / V, kStep = kGroupWarps * (32 / kLanes), kTurns = kBlockC / kStep;   // of pieces
+    static_assert(kGroupWarps == 8, "the pieces of a lane's lines are exchanged alike");
+    uint32_t v[16];
+    uint32_t to;
+    int rows, lines;                    // below a lane's first line
+    bool pieces, one, two;              // values: which of a lane's two lie inside
+
+    // Loads are issued here and used in `put`, another chunk's in between: none is conditional (one that has nothing to read reads the
+    // matrix' first value).
+    __device__ __forceinline__ void get(const Source<T>& s, uint32_t dst, int left_lines, long long r0, long long c0, int warp, int lane) {
+        pieces = s.pieces;
+        const int line = pieces ? warp * (32 / kLanes) + lane / kLanes : warp, col = pieces ? lane % kLanes * V : 2 * lane;
+        one = c0 + col < s.width;
+        two = c0 + col + 1 < s.width;
+        lines = left_lines - line;
+        rows = (int)min(s.rows - r0 - line, (long long)lines);
+        if (pieces && !one) rows = 0;
+        to = dst + staged(line, col * 2);
+        const T* p = s.p + (r0 + line) * s.ld + c0 + col;
+        if (pieces) {
+            const long long step = s.ld * kStep;
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const bool in = (turn + u) * kStep < rows;
-            lo[u] = ld_value(in && one ? p : s.p);
-            hi[u] = ld_value(in && two ? p + 1 : s.p);
-            if (KEPT) { zl[u] = ld_value(in && one ? z : s.kept); zh[u] = ld_value(in && two ? z + 1 : s.kept); z += step; }
-            p += step;
+            for (int u = 0; u < kTurns; ++u, p += step) {
+                const uint4 w = ld_piece(u * kStep < rows ? p : s.p);
+                v[4 * u] = w.x; v[4 * u + 1] = w.y; v[4 * u + 2] = w.z; v[4 * u + 3] = w.w;
+            }
+        } else {
+            const long long step = s.ld * kGroupWarps;
+#pragma unroll
+            for (int u = 0; u < 8; ++u, p += step) {
+                const bool in = u * kGroupWarps < rows;
+                v[2 * u] = ld_bits(in && one ? p : s.p);
+                v[2 * u + 1] = ld_bits(in && two ? p + 1 : s.p);
+            }
         }
+    }
+    __device__ __forceinline__ void put(uint32_t part_bytes) {
+        if (pieces) {
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const bool in = (turn + u) * kStep < rows;
-            static_assert(kStep % 8 == 0, "the pieces of these lines are exchanged alike");
-            const uint32_t to = at + (turn + u) * kStep * 128;
-            if ((turn + u) * kStep + warp >= lines) break;
-            if constexpr (sizeof(T) == 2 && !KEPT) {               // as it is
-                const uint32_t v = (uint32_t)__bfloat16_as_ushort(lo[u]) | ((uint32_t)__bfloat16_as_ushort(hi[u]) << 16);
-                st_shared(to, in ? v & ((one ? 0xffffu : 0u) | (two ? 0xffff0000u : 0u)) : 0u);
-            } else {
-                float a = Elem<T>::to_f32(lo[u]), b = Elem<T>::to_f32(hi[u]);
-                if (KEPT) {
-                    a *= act_slope(s.act, Elem<T>::to_f32(zl[u]));
-                    b *= act_slope(s.act, Elem<T>::to_f32(zh[u]));
-                }
-                a = in && one ? a : 0.f;
-                b = in && two ? b : 0.f;
-                if (sizeof(T) == 4) {
-                    uint32_t h, m, l;
-                    split(a, b, h, m, l);
-                    st_shared(to, h);
-                    st_shared(to + part_bytes, m);
-                    st_shared(to + 2 * part_bytes, l);
+            for (int u = 0; u < kTurns; ++u) {
+                if (u * kStep >= lines) break;
+                const uint4 w = u * kStep < rows ? make_uint4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]) : make_uint4(0, 0, 0, 0);
+                const uint32_t at = to + u * kStep * 128;
+                if constexpr (sizeof(T) == 2) {
+                    st_shared(at, w);
                 } else {
-                    st_shared(to, pack(a, b));
+                    uint32_t h[2], m[2], l[2];
+                    split(__uint_as_float(w.x), __uint_as_float(w.y), h[0], m[0], l[0]);
+                    split(__uint_as_float(w.z), __uint_as_float(w.w), h[1], m[1], l[1]);
+                    st_shared(at, h[0], h[1]);
+                    st_shared(at + part_bytes, m[0], m[1]);
+                    st_shared(at + 2 * part_bytes, l[0], l[1]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                if (u * kGroupWarps >= lines) break;
+                const bool in = u * kGroupWarps < rows;
+                const uint32_t a = in && one ? v[2 * u] : 0u, b = in && two ? v[2 * u + 1] : 0u, at = to + u * kGroupWarps * 128;
+                if constexpr (sizeof(T) == 2) {
+                    st_shared(at, a | (b << 16));
+                } else {
+                    uint32_t h, m, l;
+                    split(__uint_as_float(a), __uint_as_float(b), h, m, l);
+                    st_shared(at, h);
+                    st_shared(at + part_bytes, m);
+                    st_shared(at + 2 * part_bytes, l);
                 }
             }
         }
     }
-}
-template <typename T, bool KEPT> __device__ __forceinline__ void fill_pieces(uint32_t dst, int lines, uint32_t part_bytes, const Source<T>& s, long long r0, long long c0, int warp, int lane) {
-    constexpr int V = Elem<T>::kVec, per_line = 64 / V, at_once = 32 / per_line, kStep = kGroupWarps * at_once, kTurns = kBlockC / kStep, kBatch = KEPT ? 2 : kTurns;
-    const int line = warp * at_once + lane / per_line, byte = lane % per_line * V * 2;
-    const long long col = c0 + lane % per_line * V, left = s.rows - r0 - line;
-    const int rows = col < s.width ? (int)min(left, (long long)(lines - line)) : 0;
-    const long long step = s.ld * kStep;
-    const T* p = s.p + (r0 + line) * s.ld + col;
-    const T* z = s.kept + (r0 + line) * s.ld + col;
-    const uint32_t at = dst + staged(line, byte);
-#pragma unroll 1
-    for (int turn = 0; turn < kTurns; turn += kBatch) {
-        uint4 v[kBatch], w[kBatch];
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const bool in = (turn + u) * kStep < rows;
-            v[u] = ld_piece(in ? p : s.p);
-            if (KEPT) { w[u] = ld_piece(in ? z : s.kept); z += step; }
-            p += step;
-        }
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            if (!((turn + u) * kStep < rows)) v[u] = make_uint4(0, 0, 0, 0);
-            static_assert(kStep % 8 == 0, "the pieces of these lines are exchanged alike");
-            const uint32_t to = at + (turn + u) * kStep * 128;
-            if ((turn + u) * kStep + line >= lines) break;
-            if constexpr (sizeof(T) == 2 && !KEPT) {
-                st_shared(to, v[u]);
-                continue;
-            }
-            float f[V];
-            unpack16<T>(v[u], f);
-            if (KEPT) {
-                float x[V];
-                unpack16<T>(w[u], x);
-#pragma unroll
-                for (int e = 0; e < V; ++e) f[e] *= act_slope(s.act, x[e]);
-                if (!((turn + u) * kStep < rows))                  // a slope that is not a number may be another value's
-#pragma unroll
-                    for (int e = 0; e < V; ++e) f[e] = 0.f;
-            }
-            if (sizeof(T) == 4) {
-                uint32_t h[2], m[2], l[2];
-                split(f[0], f[1], h[0], m[0], l[0]);
-                split(f[2], f[3], h[1], m[1], l[1]);
-                st_shared(to, h[0], h[1]);
-                st_shared(to + part_bytes, m[0], m[1]);
-                st_shared(to + 2 * part_bytes, l[0], l[1]);
-            } else {
-                st_shared(to, make_uint4(pack(f[0], f[1]), pack(f[2], f[3]), pack(f[4 % V], f[5 % V]), pack(f[6 % V], f[7 % V])));
-            }
-        }
-    }
-}
-// One operand's block of `lines` lines (a multiple of 16).  Line L: K-major row r0 + L from column c0 on; MN-major row r0 + L % 64 from column
-// c0 + L / 64 * 64 on.
-template <typename T, bool MN, bool KEPT> __device__ __forceinline__ void fill(uint32_t dst, int lines, uint32_t part_bytes, const Source<T>& s, long long r0, long long c0, int warp, int lane) {
-#pragma unroll 1
-    for (int L = 0; L < lines; L += kBlockC) {
-        if (s.pieces) fill_pieces<T, KEPT>(dst + L * 128, lines - L, part_bytes, s, MN ? r0 : r0 + L, MN ? c0 + L : c0, warp, lane);
-        else fill_values<T, KEPT>(dst + L * 128, lines - L, part_bytes, s, MN ? r0 : r0 + L, MN ? c0 + L : c0, warp, lane);
-    }
-}
+};
 
 // ---- epilogue ---------------------------------------------------------------------------------------------------------------
 
@@ -457,53 +424,75 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         __syncwarp();
     } else if (!TMA && warp >= kFirstFill) {
         // ---- the ring, by plain loads -------------------------------------------------------------------------------------------
+        // A group walks its blocks' operands in chunks; a chunk's loads are under way while the one before is stored.
         const int group = (warp - kFirstFill) / kGroupWarps, w = (warp - kFirstFill) % kGroupWarps;
         static_assert(kFillWarps == 2 * kGroupWarps, "groups take turns");
+        const bool ta = PARTS == 1 && p.a_tma, tb = PARTS == 1 && p.b_tma;
+        const int a_chunks = ta ? 0 : kBlockI / kBlockC, b_chunks = tb ? 0 : (p.bn + kBlockC - 1) / kBlockC;
+        // chunk q of the block c of tile u (of B alone: q from a_chunks on), to `at`
+        auto get = [&](Chunk<T>& x, int q, const Walk& u, int c, uint32_t a_at, uint32_t b_at) {
+            const bool of_b = q >= a_chunks, mn = of_b ? B_MN : A_MN;
+            const int L = (of_b ? q - a_chunks : q) * kBlockC;
+            const long long m0 = of_b ? (long long)u.j * p.bn : (long long)u.i * kBlockI, c0 = (long long)c * kBlockC;
+            x.get(of_b ? p.b : p.a, (of_b ? b_at : a_at) + L * 128, of_b ? p.bn - L : kBlockI - L, mn ? c0 : m0 + L, mn ? m0 + L : c0, w, lane);
+        };
+        auto put = [&](Chunk<T>& x, int q) { x.put(q >= a_chunks ? b_part : (uint32_t)kABytes); };
         Ring r{};
         int turn = 0;
         for (Walk u = walk(p); u.live && alive; next(u, p), ++n) {
-            const long long i0 = (long long)u.i * kBlockI, j0 = u.j * p.bn;
+            const int i0 = u.i * kBlockI, j0 = u.j * p.bn;
             if (p.resident && n == 0) {
-                const bool asks = PARTS == 1 && p.b_tma && group == 0 && w == 0 && lane == 0;
-                if (asks) {
-                    mbar_expect(b_full, (unsigned)p.blocks * b_bytes);
+                if (tb && group == 0 && w == 0 && lane == 0) {
+                    mbar_bytes(b_full, (unsigned)p.blocks * b_bytes);
                     for (int c = 0; c < p.blocks; ++c) {
-                        if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(resident + c * b_bytes + m * 128, &map_b, b_full, (int)j0 + m, c * kBlockC);
-                        else tma_load_2d(resident + c * b_bytes, &map_b, b_full, c * kBlockC, (int)j0);
+                        if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(resident + c * b_bytes + m * 128, &map_b, b_full, j0 + m, c * kBlockC);
+                        else tma_load_2d(resident + c * b_bytes, &map_b, b_full, c * kBlockC, j0);
                     }
                 }
-                if (PARTS == 3 || !p.b_tma)
-                    for (int c = group; c < p.blocks; c += kFillWarps / kGroupWarps)
-                        fill<T, B_MN, false>(resident + c * b_bytes, p.bn, b_part, p.b, B_MN ? c * kBlockC : j0, B_MN ? j0 : c * kBlockC, w, lane);
+                for (int c = group; c < p.blocks; c += kFillWarps / kGroupWarps)
+                    for (int q = a_chunks; q < a_chunks + b_chunks; ++q) {
+                        Chunk<T> x;
+                        get(x, q, u, c, 0, resident + c * b_bytes);
+                        put(x, q);
+                    }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0 && !asks) mbar_arrive(b_full);
+                if (lane == 0) mbar_arrive(b_full);
             }
+            const int chunks = a_chunks + (p.resident ? 0 : b_chunks);
             for (int c = u.c0; c < u.c1; ++c, r.next(p.stages), turn ^= 1) {
                 if (turn != group) continue;
+                const uint32_t at = base + r.s * stage_bytes;
+                Chunk<T> x;
+                if (chunks > 0) get(x, 0, u, c, at, at + PARTS * kABytes);
                 if (r.round > 0) alive = wait_warp(empty + 8 * r.s, (r.round - 1) & 1, 0x20000000u | r.round);
                 if (!alive) break;
-                const uint32_t at = base + r.s * stage_bytes;
-                const long long c0 = (long long)c * kBlockC;
-                const bool ta = PARTS == 1 && p.a_tma, tb = PARTS == 1 && p.b_tma;
-                const bool asks = (ta || (tb && !p.resident)) && w == 0 && lane == 0;
-                if (asks) {                                        // its arrival at the barrier, with the bytes that it asks for
-                    mbar_expect(full + 8 * r.s, (ta ? (A_MN ? kABytes : p.a_rows * 128) : 0) + (tb && !p.resident ? b_bytes : 0));
+                if ((ta || (tb && !p.resident)) && w == 0 && lane == 0) {
+                    mbar_bytes(full + 8 * r.s, (ta ? (A_MN ? kABytes : p.a_rows * 128) : 0) + (tb && !p.resident ? b_bytes : 0));
                     if (ta) {
-                        if (A_MN) for (int m = 0; m < kBlockI; m += 64) tma_load_2d(at + m * 128, &map_a, full + 8 * r.s, (int)i0 + m, (int)c0);
-                        else tma_load_2d(at, &map_a, full + 8 * r.s, (int)c0, (int)i0);
+                        if (A_MN) for (int m = 0; m < kBlockI; m += 64) tma_load_2d(at + m * 128, &map_a, full + 8 * r.s, i0 + m, c * kBlockC);
+                        else tma_load_2d(at, &map_a, full + 8 * r.s, c * kBlockC, i0);
                     }
                     if (tb && !p.resident) {
-                        if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(at + kABytes + m * 128, &map_b, full + 8 * r.s, (int)j0 + m, (int)c0);
-                        else tma_load_2d(at + kABytes, &map_b, full + 8 * r.s, (int)c0, (int)j0);
+                        if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(at + kABytes + m * 128, &map_b, full + 8 * r.s, j0 + m, c * kBlockC);
+                        else tma_load_2d(at + kABytes, &map_b, full + 8 * r.s, c * kBlockC, j0);
                     }
                 }
-                if (ROLE != kForward && p.a.kept) fill<T, A_MN, true>(at, kBlockI, kABytes, p.a, A_MN ? c0 : i0, A_MN ? i0 : c0, w, lane);
-                else if (!ta) fill<T, A_MN, false>(at, kBlockI, kABytes, p.a, A_MN ? c0 : i0, A_MN ? i0 : c0, w, lane);
-                if (!p.resident && !tb) fill<T, B_MN, false>(at + PARTS * kABytes, p.bn, b_part, p.b, B_MN ? c0 : j0, B_MN ? j0 : c0, w, lane);
+#pragma unroll 1
+                for (int q = 0; q < chunks; ++q) {
+                    if constexpr (PARTS == 3) {                    // another chunk's loads meanwhile; bf16 has no registers for that
+                        Chunk<T> y;
+                        if (q + 1 < chunks) get(y, q + 1, u, c, at, at + PARTS * kABytes);
+                        put(x, q);
+                        x = y;
+                    } else {
+                        put(x, q);
+                        if (q + 1 < chunks) get(x, q + 1, u, c, at, at + PARTS * kABytes);
+                    }
+                }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0 && !asks) mbar_arrive(full + 8 * r.s);
+                if (lane == 0) mbar_arrive(full + 8 * r.s);
             }
         }
     } else if (warp == 1) {
