@@ -3,13 +3,14 @@
 
 #include <algorithm>
 
-#include "linear_umma.cuh"
+#include "linear_backward_small.cuh"
 
 namespace {
 
 namespace abi = esc::abi;
 namespace lin = esc::linear;
 namespace um = esc::linear::umma;
+namespace sm = esc::linear::small;
 using namespace esc::rows;
 using bf16 = __nv_bfloat16;
 
@@ -160,10 +161,12 @@ LinearWs carve(void* ws, const Call& c) {
     char* base = static_cast<char*>(ws);
     size_t off = 0;
     auto take = [&](size_t bytes) { char* p = base + off; off += abi::round_up(bytes, 256); return p; };
-    w.part = reinterpret_cast<float*>(take((size_t)std::max(cut(lin::kGradW, c.N, c.K, std::max(c.rows, 1LL), c.es(), false).splits, cut(lin::kGradW, c.N, c.K, std::max(c.rows, 1LL), c.es(), true).splits) *
-                                          c.N * c.K * sizeof(float)));
+    const long long rows = std::max(c.rows, 1LL);
+    const int fused = c.dtype == ESC_BF16 ? sm::plan(rows, c.K, c.N, c.act != ESC_ACT_NONE, abi::sm_count()).grid : 0;   // its blocks leave a part each
+    const int splits = std::max({cut(lin::kGradW, c.N, c.K, rows, c.es(), false).splits, cut(lin::kGradW, c.N, c.K, rows, c.es(), true).splits, fused});
+    w.part = reinterpret_cast<float*>(take((size_t)splits * c.N * c.K * sizeof(float)));
     const int vec = 16 / (int)c.es();
-    w.bias = reinterpret_cast<float*>(take((size_t)std::max(bias_cut(c, 1).parts, c.N < vec ? 0 : bias_cut(c, vec).parts) * c.N * sizeof(float)));
+    w.bias = reinterpret_cast<float*>(take((size_t)std::max({bias_cut(c, 1).parts, c.N < vec ? 0 : bias_cut(c, vec).parts, fused}) * c.N * sizeof(float)));
     w.g = take(c.act != ESC_ACT_NONE ? (size_t)c.rows * g_stride(c) * c.es() : 0);
     w.bytes = off;
     return w;
@@ -181,18 +184,43 @@ template <typename T> int linear_forward_t(const Call& c, const lin::Layer<T>& l
     return launch_product<T, lin::kForward>(p, c.K, st);
 }
 
-template <typename G> int launch_sums(const float* part, int parts, long long count, void* out, cudaStream_t st) {
-    if (parts <= 8) lin::sum_few_parts<G><<<(unsigned)std::min<long long>((count + 1023) / 1024, 16LL * abi::sm_count()), 256, 0, st>>>(part, parts, count, static_cast<G*>(out));
-    else lin::sum_parts<G><<<(unsigned)((count + 31) / 32), 256, 0, st>>>(part, parts, count, static_cast<G*>(out));
+// The partial sums of the weights' and the bias' gradients, in one launch.
+template <typename G> int launch_sums(const lin::Parts& w, const lin::Parts& b, void* gw, void* gb, cudaStream_t st) {
+    lin::sum_parts<G><<<(unsigned)(lin::sum_blocks(w) + lin::sum_blocks(b)), 256, 0, st>>>(w, b, static_cast<G*>(gw), static_cast<G*>(gb));
     return launched();
 }
-int sum_to(const float* part, int parts, long long count, void* out, int grad_dtype, cudaStream_t st) {
-    return grad_dtype == ESC_F32 ? launch_sums<float>(part, parts, count, out, st) : launch_sums<bf16>(part, parts, count, out, st);
+int sum_to(const lin::Parts& w, const lin::Parts& b, void* gw, void* gb, int grad_dtype, cudaStream_t st) {
+    if (w.count + b.count == 0) return ESC_OK;
+    return grad_dtype == ESC_F32 ? launch_sums<float>(w, b, gw, gb, st) : launch_sums<bf16>(w, b, gw, gb, st);
+}
+
+// A small bf16 layer in one pass; kNotThis: it is not one, or its tensors are not rows of whole 16-byte pieces.
+constexpr int kNotThis = -1;
+int backward_small(const Call& c, const lin::Layer<bf16>& l, void* gw, void* gb, int grad_dtype, const LinearWs& w, cudaStream_t st) {
+    const bool act = c.act != ESC_ACT_NONE;
+    const sm::Plan d = sm::plan(c.rows, c.K, c.N, act, abi::sm_count());
+    if (d.stages == 0 || (!l.gx && !gw)) return kNotThis;
+    if (!whole_pieces(l.go, c.N, 2) || !whole_pieces(c.x, c.x_stride, 2) || !whole_pieces(c.w, c.K, 2) || (act && !whole_pieces(l.kept, c.N, 2)) ||
+        (l.gx && !whole_pieces(l.gx, c.K, 2))) return kNotThis;
+    CUtensorMap go{}, z{}, x{}, wm{}, gx{}, part{};
+    if (!map_of<bf16>(&go, l.go, 0, c.rows, c.N, c.N, sm::kRows) || !map_of<bf16>(&x, c.x, 0, c.rows, c.K, c.x_stride, sm::kRows) || !map_of<bf16>(&wm, c.w, 0, c.N, c.K, c.K, 64) ||
+        (act && !map_of<bf16>(&z, l.kept, 0, c.rows, c.N, c.N, sm::kRows)) || (l.gx && !map_of<bf16>(&gx, l.gx, 1, c.rows, c.K, c.K, 32)) ||
+        (gw && !map_of<float>(&part, w.part, d.grid, c.N, c.K, c.K, 32))) return kNotThis;
+    const sm::Args p{(int)c.rows, c.N, c.K, d.tiles, c.act, d.stages, d.nb, d.kb, d.gx_buffers, l.gx != nullptr, gw != nullptr, gb != nullptr, w.bias};
+    ESC_ABI_CUDA(cudaFuncSetAttribute(sm::backward, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)um::kMostSmem));   // the same for every call
+    sm::backward<<<(unsigned)d.grid, sm::kThreads, d.smem, st>>>(go, z, x, wm, gx, part, p);
+    ESC_TRY(launched());
+    return sum_to({w.part, d.grid, gw ? (long long)c.N * c.K : 0}, {w.bias, d.grid, gb ? c.N : 0}, gw, gb, grad_dtype, st);
 }
 
 template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& l, void* gw, void* gb, int grad_dtype, const LinearWs& w, cudaStream_t st) {
     constexpr int V = esc::Elem<T>::kVec;
+    if constexpr (sizeof(T) == 2) {
+        const int rc = backward_small(c, l, gw, gb, grad_dtype, w, st);
+        if (rc != kNotThis) return rc;
+    }
     um::Source<T> g = source<T>(l.go, c.rows, c.N, c.N);
+    lin::Parts pw{w.part, 0, 0}, pb{w.bias, 0, 0};
     const bool acts = c.act != ESC_ACT_NONE && (l.gx || gw);
     if (acts || gb) {
         T* to = acts ? static_cast<T*>(w.g) : nullptr;
@@ -203,7 +231,7 @@ template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& 
         if (pieces) lin::grad_z_sums<T, V><<<grid, 256, 0, st>>>(l, to, ld, gb ? w.bias : nullptr);
         else lin::grad_z_sums<T, 1><<<grid, 256, 0, st>>>(l, to, ld, gb ? w.bias : nullptr);
         ESC_TRY(launched());
-        if (gb) ESC_TRY(sum_to(w.bias, b.parts, c.N, gb, grad_dtype, st));
+        if (gb) pb = lin::Parts{w.bias, b.parts, c.N};
         if (acts) g = source<T>(to, c.rows, c.N, ld);
     }
     if (l.gx) {
@@ -216,11 +244,10 @@ template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& 
         um::Args<T> p{};
         p.I = c.N; p.J = c.K;
         p.a = g; p.b = source<T>(c.x, c.rows, c.K, c.x_stride); p.part = w.part;
-        int splits;
-        ESC_TRY((launch_product<T, lin::kGradW>(p, c.rows, st, &splits)));
-        ESC_TRY(sum_to(w.part, splits, (long long)c.N * c.K, gw, grad_dtype, st));
+        ESC_TRY((launch_product<T, lin::kGradW>(p, c.rows, st, &pw.parts)));
+        pw.count = (long long)c.N * c.K;
     }
-    return ESC_OK;
+    return sum_to(pw, pb, gw, gb, grad_dtype, st);
 }
 
 }  // namespace

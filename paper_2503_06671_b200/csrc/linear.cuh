@@ -129,40 +129,48 @@ template <typename T, int V> __global__ void __launch_bounds__(256) grad_z_sums(
     }
 }
 
-// out[e] = sum over `parts` of part[.][e]: 32 of them to a block, a warp takes every eighth part, the warps are added in order.
-template <typename G> __global__ void __launch_bounds__(256) sum_parts(const float* part, int parts, long long count, G* out)
+// Partial sums [parts][count], to be added up: the weights' and the bias' gradients in one launch, either may be empty.
+struct Parts { const float* p; int parts; long long count; };
+
+// Many parts: 32 sums to a block, a warp takes every eighth part, the warps are added in order.  Up to kFewParts: a thread has four sums.
+constexpr int kFewParts = 8;
+inline __host__ __device__ long long sum_blocks(const Parts& t) { return t.parts <= kFewParts ? (t.count + 1023) / 1024 : (t.count + 31) / 32; }
+template <typename G> __global__ void __launch_bounds__(256) sum_parts(const Parts w, const Parts b, G* gw, G* gb)
 {
     __shared__ float acc[8][32];
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const long long e = (long long)blockIdx.x * 32 + lane;
-    float s = 0.f;
-    if (e < count) {
-#pragma unroll 8
-        for (int i = warp; i < parts; i += 8) s += __ldcg(part + (size_t)i * count + e);
-    }
-    acc[warp][lane] = s;
-    __syncthreads();
-    if (warp != 0 || e >= count) return;
-#pragma unroll
-    for (int v = 1; v < 8; ++v) s += acc[v][lane];
-    out[e] = Elem<G>::from_f32(s);
-}
-// The same for few parts of many sums: a thread has four of them.
-template <typename G> __global__ void __launch_bounds__(256) sum_few_parts(const float* part, int parts, long long count, G* out)
-{
-    for (long long e = ((long long)blockIdx.x * 256 + threadIdx.x) * 4; e < count; e += (long long)gridDim.x * 1024) {
+    const long long ours = sum_blocks(w);
+    const bool of_b = blockIdx.x >= ours;
+    const Parts t = of_b ? b : w;
+    const long long block = blockIdx.x - (of_b ? ours : 0);
+    G* out = of_b ? gb : gw;
+    if (t.parts <= kFewParts) {
+        const long long e = block * 1024 + threadIdx.x * 4;
         float s[4] = {};
-        for (int i = 0; i < parts; ++i) {
-            const float* at = part + (size_t)i * count + e;
-            if (count % 4 == 0) {
+        for (int i = 0; i < t.parts; ++i) {
+            const float* at = t.p + (size_t)i * t.count + e;
+            if (t.count % 4 == 0 && e < t.count) {
                 const float4 v = __ldcg(reinterpret_cast<const float4*>(at));
                 s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
             } else {
-                for (int q = 0; q < 4 && e + q < count; ++q) s[q] += __ldcg(at + q);
+                for (int u = 0; u < 4 && e + u < t.count; ++u) s[u] += __ldcg(at + u);
             }
         }
-        for (int q = 0; q < 4 && e + q < count; ++q) out[e + q] = Elem<G>::from_f32(s[q]);
+        for (int u = 0; u < 4 && e + u < t.count; ++u) out[e + u] = Elem<G>::from_f32(s[u]);
+        return;
     }
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const long long e = block * 32 + lane;
+    float s = 0.f;
+    if (e < t.count) {
+#pragma unroll 8
+        for (int i = warp; i < t.parts; i += 8) s += __ldcg(t.p + (size_t)i * t.count + e);
+    }
+    acc[warp][lane] = s;
+    __syncthreads();
+    if (warp != 0 || e >= t.count) return;
+#pragma unroll
+    for (int v = 1; v < 8; ++v) s += acc[v][lane];
+    out[e] = Elem<G>::from_f32(s);
 }
 
 }}  // namespace esc::linear

@@ -1,0 +1,267 @@
+// The backward pass of a small linear layer (bf16; K and N of a few hundred at most) in one pass over its rows:
+//
+//   g = go act'(z)     gx = g w     gw = sum over rows of g^T x     gb = sum over rows of g
+//
+// Such layers are bound by memory: go, z and x are read once, gx is written once, and g never leaves shared memory.  A block takes tiles of
+// 128 rows, one after another.  TMA brings go, z and x as boxes of 128 rows x 64 columns (128 bytes a row, 128-byte swizzle); 16 warps
+// turn go into g in place and add up its columns; then the same boxes of g are the operand of both products: with 128 rows and the columns
+// as contraction (K-major) for gx, with the columns as rows of the result and 128 rows as contraction (MN-major) for gw.  w stays in shared
+// memory and the sums of gw in tensor memory for the life of the block (N / 128 x K columns beside one or two tiles of gx); each block leaves
+// one partial sum of gw and gb.  64 x 64x64 rows, 64 to 128 channels, GELU: three kernels that wrote and read g took 96 us.
+#pragma once
+#include "linear_umma.cuh"
+
+namespace esc { namespace linear { namespace small {
+
+using namespace esc::linear::umma;
+using bf16 = __nv_bfloat16;
+
+constexpr int kRows = 128, kBox = kRows * 128, kActWarps = 16, kOutWarps = 4, kFirstAct = 4, kFirstOut = kFirstAct + kActWarps, kThreads = 32 * (kFirstOut + kOutWarps);
+constexpr int kMostBoxes = 4;                                      // of go: N up to 256
+constexpr int kMostStages = 4;
+
+struct Args {
+    int rows, N, K, tiles, act, stages;
+    int nb, kb;                                                    // boxes of 64 columns of go and of x
+    int gx_buffers;
+    bool gx, gw, gb;
+    float* part_b;                                                 // [gridDim.x][N]
+};
+
+__device__ __forceinline__ unsigned long long desc(uint32_t addr, uint32_t lbo) {
+    return (unsigned long long)((addr >> 4) & 0x3FFFu) | ((unsigned long long)(lbo >> 4) << 16) | ((unsigned long long)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUtensorMap map_z, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+         const __grid_constant__ CUtensorMap map_gx, const __grid_constant__ CUtensorMap map_part, const __grid_constant__ Args p)
+{
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const uint32_t base = smem_u32(smem);
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
+    const bool has_act = p.act != kActNone;
+    // a tile: go, x, z in this order (the last rows of gw's products may come from the box behind go's, and go nowhere)
+    const uint32_t x_at = p.nb * kBox, z_at = x_at + p.kb * kBox, stage_bytes = z_at + (has_act ? p.nb * kBox : 0);
+    const uint32_t w_at = base + p.stages * stage_bytes, w_block = p.kb * 64 * 128, staging = w_at + p.nb * w_block;
+    const uint32_t full = staging + kOutWarps * kSlotBytes, ready = full + 8 * kMostStages, empty = ready + 8 * kMostStages, gx_full = empty + 8 * kMostStages,
+                   gx_empty = gx_full + 16, w_full = gx_empty + 16, gw_done = w_full + 8, gb_done = gw_done + 8, slot = gb_done + 8,
+                   strip = slot + 24;                              // [kActWarps][256] floats: columns of g
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(ready + 8 * s, kActWarps); mbar_init(empty + 8 * s, 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(gx_full + 8 * s, 1); mbar_init(gx_empty + 8 * s, kOutWarps); }
+        mbar_init(w_full, 1);
+        mbar_init(gw_done, 1);
+        mbar_init(gb_done, kActWarps);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+    tmem = __shfl_sync(0xffffffffu, tmem, 0);
+    const uint32_t columns = p.kb * 64, gw_at = tmem + p.gx_buffers * columns;   // sums: gx of one or two tiles, then gw by 128 outputs
+
+    bool alive = true;
+    int n = 0;                                                     // tiles so far
+    Ring r{};
+    if (warp == 0) {
+        if (lane == 0) {
+            mbar_expect(w_full, p.nb * w_block);
+            for (int c = 0; c < p.nb; ++c)
+                for (int m = 0; m < p.kb; ++m) tma_load_2d(w_at + c * w_block + m * 64 * 128, &map_w, w_full, m * 64, c * 64);
+            for (int t = blockIdx.x; t < p.tiles && alive; t += gridDim.x, r.next(p.stages)) {
+                if (r.round > 0) alive = wait_lane(empty + 8 * r.s, (r.round - 1) & 1, 0x11000000u | r.round);
+                if (!alive) break;
+                const uint32_t at = base + r.s * stage_bytes, bar = full + 8 * r.s;
+                mbar_expect(bar, stage_bytes);
+                for (int c = 0; c < p.nb; ++c) {
+                    tma_load_2d(at + c * kBox, &map_go, bar, c * 64, t * kRows);
+                    if (has_act) tma_load_2d(at + z_at + c * kBox, &map_z, bar, c * 64, t * kRows);
+                }
+                for (int c = 0; c < p.kb; ++c) tma_load_2d(at + x_at + c * kBox, &map_x, bar, c * 64, t * kRows);
+            }
+            if (!alive)                                            // what is still on its way here lands before the block goes
+                for (unsigned s = 0; s < (unsigned)p.stages; ++s)
+                    if (r.round > 0 || s < r.s) wait_lane(full + 8 * s, (s < r.s ? r.round : r.round - 1) & 1, 0x71000000u | s);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        const uint32_t idesc_x = instr_desc<false, true>(columns), idesc_w = instr_desc<true, true>(columns);
+        alive = wait_warp(w_full, 0, 0x41000000u);
+        for (int t = blockIdx.x; t < p.tiles && alive; t += gridDim.x, r.next(p.stages), ++n) {
+            const int buf = p.gx_buffers == 2 ? n & 1 : 0, use = p.gx_buffers == 2 ? n >> 1 : n;
+            alive = wait_warp(ready + 8 * r.s, r.round & 1, 0x51000000u | r.round);
+            if (alive && p.gx && use > 0) alive = wait_warp(gx_empty + 8 * buf, (use - 1) & 1, 0x31000000u | (unsigned)n);
+            if (!alive) break;
+            fence_after();
+            const uint32_t at = base + r.s * stage_bytes;
+            if (p.gx) {
+#pragma unroll 1
+                for (int c = 0; c < p.nb; ++c) {
+                    const unsigned long long a = desc(at + c * kBox, 16), b = desc(w_at + c * w_block, 64 * 128);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mma(tmem + buf * columns, a + k * 2, b + k * 128, idesc_x, c > 0 || k > 0);
+                }
+                commit(gx_full + 8 * buf);
+            }
+            if (p.gw) {
+#pragma unroll 1
+                for (int m = 0; m < p.nb; m += 2) {
+                    const unsigned long long a = desc(at + m * kBox, kBox), b = desc(at + x_at, kBox);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) mma(gw_at + m / 2 * columns, a + k * 128, b + k * 128, idesc_w, n > 0 || k > 0);
+                }
+            }
+            commit(empty + 8 * r.s);
+        }
+        commit(gw_done);
+    } else if (warp >= kFirstAct && warp < kFirstOut) {
+        // ---- g in place, and its columns' sums ------------------------------------------------------------------------------
+        // A lane has the eight columns of one piece in every box, a warp four rows at a time.
+        const int w = warp - kFirstAct, row = w * 4 + lane / 8, q = lane % 8;
+        float sum[kMostBoxes][8] = {};
+        for (int t = blockIdx.x; t < p.tiles && alive; t += gridDim.x, r.next(p.stages)) {
+            alive = wait_warp(full + 8 * r.s, r.round & 1, 0x21000000u | r.round);
+            if (!alive) break;
+            const uint32_t at = base + r.s * stage_bytes + staged(row, q * 16);   // rows 4 kActWarps apart are exchanged alike
+            if (has_act || p.gb) {
+#pragma unroll
+                for (int c = 0; c < kMostBoxes; ++c) {
+                    if (c >= p.nb) break;
+#pragma unroll 1
+                    for (int i = 0; i < kRows; i += 4 * kActWarps) {
+                        const uint32_t piece = at + c * kBox + i * 128;
+                        float f[8];
+                        unpack16<bf16>(ld_shared(piece), f);
+                        if (has_act) {
+                            float z[8];
+                            unpack16<bf16>(ld_shared(piece + z_at), z);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) f[e] *= act_slope(p.act, z[e]);
+                            st_shared(piece, pack16<bf16>(f));
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sum[c][e] += f[e];
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ready + 8 * r.s);
+        }
+        if (p.gb && alive) {
+            // the rows of a warp, then the warps in order
+#pragma unroll
+            for (int c = 0; c < kMostBoxes; ++c) {
+                if (c >= p.nb) break;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    sum[c][e] += __shfl_xor_sync(0xffffffffu, sum[c][e], 8);
+                    sum[c][e] += __shfl_xor_sync(0xffffffffu, sum[c][e], 16);
+                    if (lane < 8) st_value(strip + (w * 256 + c * 64 + lane * 8 + e) * 4, sum[c][e]);
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(gb_done);
+            alive = wait_warp(gb_done, 0, 0x91000000u);
+            const int col = w * 32 + lane;
+            if (alive && col < p.N) {
+                float s = 0.f;
+#pragma unroll
+                for (int v = 0; v < kActWarps; ++v) s += get_value(strip + (v * 256 + col) * 4, 0.f);
+                p.part_b[(size_t)blockIdx.x * p.N + col] = s;
+            }
+        }
+    } else if (warp >= kFirstOut) {
+        // ---- gx of each tile, gw at the end: 128 bytes of 32 rows at a time ---------------------------------------------------
+        const int e = warp - kFirstOut, quarter = warp & 3, member = e / 4;
+        const uint32_t mine = staging + e * kSlotBytes, lane_at = lane * 128 + ((lane & 7) << 4), lanes = (uint32_t)(quarter * 32) << 16;
+        if (p.gx) {
+            int turn = 0;
+            for (int t = blockIdx.x; t < p.tiles && alive; t += gridDim.x, ++n) {
+                const int buf = p.gx_buffers == 2 ? n & 1 : 0, use = p.gx_buffers == 2 ? n >> 1 : n;
+                alive = wait_warp(gx_full + 8 * buf, use & 1, 0x61000000u | (unsigned)n);
+                if (!alive) break;
+                fence_after();
+                const int i0 = t * kRows + quarter * 32;
+                for (int c = 0; c < p.kb; ++c, turn = turn + 1 == kOutWarps / 4 ? 0 : turn + 1) {
+                    if (turn != member || i0 >= p.rows) continue;
+                    if (lane == 0) bulk_wait_read<0>();
+                    __syncwarp();
+#pragma unroll 1
+                    for (int q = 0; q < 8; q += 2) {
+                        float f[16];
+                        tmem_ld(tmem + lanes + buf * columns + c * 64 + q * 8, f);
+                        tmem_wait_ld();
+                        st_shared(mine + (lane_at ^ (uint32_t)(q << 4)), pack16<bf16>(f));
+                        st_shared(mine + (lane_at ^ (uint32_t)((q + 1) << 4)), pack16<bf16>(f + 8));
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) { tma_store_3d(&map_gx, mine, c * 64, i0, 0); bulk_commit(); }
+                    __syncwarp();
+                }
+                fence_before();
+                if (lane == 0) mbar_arrive(gx_empty + 8 * buf);
+            }
+        }
+        if (p.gw && alive) alive = wait_warp(gw_done, 0, 0x81000000u);
+        if (p.gw && alive) {
+            fence_after();
+            const int across = (int)(columns / 32), units = (p.nb + 1) / 2 * across;
+            for (int v = member; v < units; v += kOutWarps / 4) {
+                const int m = v / across, c = v - m * across, n0 = m * 128 + quarter * 32;
+                if (n0 >= p.N || c * 32 >= p.K) continue;
+                if (lane == 0) bulk_wait_read<0>();
+                __syncwarp();
+#pragma unroll 1
+                for (int q = 0; q < 8; q += 2) {
+                    float f[8];
+                    tmem_ld(gw_at + lanes + m * columns + c * 32 + q * 4, f);
+                    tmem_wait_ld();
+                    st_shared(mine + (lane_at ^ (uint32_t)(q << 4)), pack16<float>(f));
+                    st_shared(mine + (lane_at ^ (uint32_t)((q + 1) << 4)), pack16<float>(f + 4));
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) { tma_store_3d(&map_part, mine, c * 32, n0, (int)blockIdx.x); bulk_commit(); }
+                __syncwarp();
+            }
+        }
+        if (lane == 0) bulk_wait_read<0>();                        // shared memory outlives what is read from it
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == 2) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
+// Sizes: whether a layer is one of these, and how its block is laid out (stages 0: it is not).
+struct Plan { int stages, gx_buffers, nb, kb, tiles, grid; size_t smem; };
+inline Plan plan(long long rows, int K, int N, bool act, int sms) {
+    Plan d{};
+    if (N > 64 * kMostBoxes || K > 256 || rows < 1 || rows > 0x7fffffffLL - kRows) return d;
+    d.nb = (N + 63) / 64; d.kb = (K + 63) / 64;
+    const int gw_columns = (d.nb + 1) / 2 * d.kb * 64;
+    d.gx_buffers = gw_columns + 2 * d.kb * 64 <= 512 ? 2 : 1;
+    if (gw_columns + d.kb * 64 > 512) return d;
+    d.tiles = (int)((rows + kRows - 1) / kRows);
+    d.grid = d.tiles < sms ? d.tiles : sms;
+    const size_t stage = (size_t)(d.nb * (act ? 2 : 1) + d.kb) * kBox, fixed = (size_t)d.nb * d.kb * 64 * 128 + kOutWarps * kSlotBytes + 1024 + kActWarps * 1024;
+    if (fixed + stage > kMostSmem) return d;
+    size_t stages = (kMostSmem - fixed) / stage;
+    if (stages > kMostStages) stages = kMostStages;
+    if (stages < 2 && d.tiles > sms) return d;                     // without a second tile on its way the three kernels are faster
+    d.stages = (int)stages;
+    d.smem = stages * stage + fixed;
+    return d;
+}
+
+}}}  // namespace esc::linear::small
