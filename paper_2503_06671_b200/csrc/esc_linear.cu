@@ -186,8 +186,7 @@ template <typename T> int linear_forward_t(const Call& c, const lin::Layer<T>& l
 
 // The partial sums of the weights' and the bias' gradients, in one launch.
 template <typename G> int launch_sums(const lin::Parts& w, const lin::Parts& b, void* gw, void* gb, cudaStream_t st) {
-    lin::sum_parts<G><<<(unsigned)(lin::sum_blocks(w) + lin::sum_blocks(b)), 256, 0, st>>>(w, b, static_cast<G*>(gw), static_cast<G*>(gb));
-    return launched();
+    return launch_behind(lin::sum_parts<G>, (unsigned)(lin::sum_blocks(w) + lin::sum_blocks(b)), lin::kSumThreads, st, w, b, static_cast<G*>(gw), static_cast<G*>(gb));
 }
 int sum_to(const lin::Parts& w, const lin::Parts& b, void* gw, void* gb, int grad_dtype, cudaStream_t st) {
     if (w.count + b.count == 0) return ESC_OK;

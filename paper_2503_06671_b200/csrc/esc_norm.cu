@@ -72,8 +72,8 @@ template <typename T, bool BACK> int launch_norm_any(const Spread& s, const ln::
     return s.g == 32 ? launch_norm_nv<T, 1, 32, BACK>(s, p, blocks, st) : launch_norm_nv<T, 1, ln::kThreads, BACK>(s, p, blocks, st);
 }
 
-constexpr int kNormBlocksPerSm = 4;                 // of the backward pass: each leaves a partial sum of every column
-int norm_parts(long long rows) { return (int)std::max(1LL, std::min<long long>(rows, (long long)kNormBlocksPerSm * abi::sm_count())); }
+// Blocks of the backward pass at most: each leaves a partial sum of every column.
+int norm_parts(long long rows, int per_sm = 4) { return (int)std::max(1LL, std::min<long long>(rows, (long long)per_sm * abi::sm_count())); }
 bool long_row(int C) { return C > ln::kThreads * 8; }   // may need the wide kernels: C odd
 size_t norm_stats_offset(long long rows, int C) { return abi::round_up((size_t)norm_parts(rows) * 2 * C * sizeof(float), 256); }
 size_t norm_ws_bytes(long long rows, int C) { return norm_stats_offset(rows, C) + (long_row(C) ? abi::round_up((size_t)rows * 2 * sizeof(float), 256) : 0); }
@@ -98,9 +98,8 @@ template <typename T> int norm_forward_t(const ln::Rows<T>& p, cudaStream_t st) 
 
 int launch_sum_columns(const float* part, int parts, int C, int grad_dtype, void* gw, void* gb, cudaStream_t st) {
     const unsigned blocks = (unsigned)((2LL * C + 31) / 32);
-    if (grad_dtype == ESC_F32) ln::sum_columns<float><<<blocks, ln::kThreads, 0, st>>>(part, parts, C, static_cast<float*>(gw), static_cast<float*>(gb));
-    else ln::sum_columns<bf16><<<blocks, ln::kThreads, 0, st>>>(part, parts, C, static_cast<bf16*>(gw), static_cast<bf16*>(gb));
-    return launched();
+    if (grad_dtype == ESC_F32) return launch_behind(ln::sum_columns<float>, blocks, ln::kSumThreads, st, part, parts, C, static_cast<float*>(gw), static_cast<float*>(gb));
+    return launch_behind(ln::sum_columns<bf16>, blocks, ln::kSumThreads, st, part, parts, C, static_cast<bf16*>(gw), static_cast<bf16*>(gb));
 }
 
 template <typename T> int norm_backward_t(ln::Rows<T> p, bool columns, int grad_dtype, void* gw, void* gb, char* ws, cudaStream_t st) {
@@ -120,7 +119,7 @@ template <typename T> int norm_backward_t(ln::Rows<T> p, bool columns, int grad_
         }
     } else {
         const long long per = ln::kThreads / s.g;
-        parts = (int)std::min<long long>((p.rows + per - 1) / per, most);
+        parts = (int)std::min<long long>((p.rows + per - 1) / per, norm_parts(p.rows, ln::back_blocks(s.vec * s.nv)));
         ESC_TRY((launch_norm_any<T, true>(s, p, parts, st)));
     }
     return columns ? launch_sum_columns(p.part, parts, p.C, grad_dtype, gw, gb, st) : ESC_OK;

@@ -19,6 +19,7 @@ namespace esc { namespace norm {
 
 constexpr int kThreads = 256;
 constexpr int kMaxChannels = 1 << 20;
+constexpr int back_blocks(int values) { return values <= 8 ? 3 : values <= 16 ? 2 : 1; }   // of an SM, by the values that a thread holds of a row: what registers allow
 
 // VEC neighbouring values as one access of VEC * sizeof(T) bytes.
 template <typename T, int VEC> struct Vec;
@@ -108,15 +109,20 @@ __global__ void __launch_bounds__(kThreads) forward(const Rows<T> p)
         if (real[i] && p.weight) w[i].load(p.weight + c);
         if (real[i] && p.bias) b[i].load(p.bias + c);
     }
-    // a warp's rows end together, so that all its lanes reach the shuffles
-    for (long long first = (long long)blockIdx.x * per_block; first < p.rows; first += (long long)gridDim.x * per_block) {
-        const long long row = first + threadIdx.x / G;
-        const bool live = row < p.rows;
-        float f[F];
-        Vec<T, VEC> x[NV];
+    // A warp's rows end together, so that all its lanes reach the shuffles.  The next row's values are under way while this one is worked on.
+    const long long step = (long long)gridDim.x * per_block;
+    long long row = (long long)blockIdx.x * per_block + threadIdx.x / G;
+    Vec<T, VEC> x[NV], ahead[NV];
+    auto load = [&](Vec<T, VEC> (&v)[NV], long long r) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (live && real[i]) x[i].load(p.x + row * p.x_stride + (i * G + in_row) * VEC);
+            if (r < p.rows && real[i]) v[i].load(p.x + r * p.x_stride + (i * G + in_row) * VEC);
+    };
+    load(x, row);
+    for (; row - threadIdx.x / G < p.rows; row += step) {
+        load(ahead, row + step);
+        const bool live = row < p.rows;
+        float f[F];
         float s[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -154,11 +160,13 @@ __global__ void __launch_bounds__(kThreads) forward(const Rows<T> p)
             }
             Vec<T, VEC>::store(p.y + row * p.y_stride + (i * G + in_row) * VEC, o);
         }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) x[i] = ahead[i];
     }
 }
 
 template <typename T, int VEC, int NV, int G>
-__global__ void __launch_bounds__(kThreads) backward(const Rows<T> p)
+__global__ void __launch_bounds__(kThreads, back_blocks(VEC * NV)) backward(const Rows<T> p)
 {
     constexpr int per_block = kThreads / G, F = VEC * NV;
     __shared__ float scratch[G > 32 ? 3 * (kThreads / 32) : 1];
@@ -175,23 +183,31 @@ __global__ void __launch_bounds__(kThreads) backward(const Rows<T> p)
     float gw[F], gb[F];
 #pragma unroll
     for (int i = 0; i < F; ++i) gw[i] = gb[i] = 0.f;
-    for (long long first = (long long)blockIdx.x * per_block; first < p.rows; first += (long long)gridDim.x * per_block) {
-        const long long row = first + threadIdx.x / G;
-        const bool live = row < p.rows;
-        Vec<T, VEC> x[NV], g[NV], k[NV];
+    // the next row's values are under way while this one is worked on, where registers allow that
+    constexpr bool kAhead = F <= 8;
+    const long long step = (long long)gridDim.x * per_block;
+    long long row = (long long)blockIdx.x * per_block + threadIdx.x / G;
+    struct Values { Vec<T, VEC> x[NV], g[NV], k[NV]; } at, ahead;
+    auto load = [&](Values& v, long long r) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (live && real[i]) {
+            if (r < p.rows && real[i]) {
                 const int c = (i * G + in_row) * VEC;
-                x[i].load(p.x + row * p.x_stride + c);
-                g[i].load(p.gy + row * p.C + c);
-                if (p.skip) k[i].load(p.skip + row * p.C + c);
+                v.x[i].load(p.x + r * p.x_stride + c);
+                v.g[i].load(p.gy + r * p.C + c);
+                if (p.skip) v.k[i].load(p.skip + r * p.C + c);
             }
+    };
+    if (kAhead) load(at, row);
+    for (; row - threadIdx.x / G < p.rows; row += step) {
+        if (kAhead) load(ahead, row + step);
+        else load(at, row);
+        const bool live = row < p.rows;
         float f[F];
         float s[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (live && real[i]) x[i].get(f + i * VEC);
+            if (live && real[i]) at.x[i].get(f + i * VEC);
             else
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) f[i * VEC + j] = 0.f;
@@ -206,7 +222,7 @@ __global__ void __launch_bounds__(kThreads) backward(const Rows<T> p)
             if (!live || !real[i]) continue;
             float wf[VEC], gf[VEC];
             if (p.weight) w[i].get(wf);
-            g[i].get(gf);
+            at.g[i].get(gf);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 const float d = f[i * VEC + j] - mu, a = p.weight ? gf[j] * wf[j] : gf[j];
@@ -221,8 +237,8 @@ __global__ void __launch_bounds__(kThreads) backward(const Rows<T> p)
             if (!live || !real[i]) continue;
             float wf[VEC], gf[VEC], kf[VEC], o[VEC];
             if (p.weight) w[i].get(wf);
-            g[i].get(gf);
-            if (p.skip) k[i].get(kf);
+            at.g[i].get(gf);
+            if (p.skip) at.k[i].get(kf);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 const float xh = f[i * VEC + j] * r, a = p.weight ? gf[j] * wf[j] : gf[j];
@@ -233,7 +249,9 @@ __global__ void __launch_bounds__(kThreads) backward(const Rows<T> p)
             }
             Vec<T, VEC>::store(p.gx + row * p.C + (i * G + in_row) * VEC, o);
         }
+        if (kAhead) at = ahead;
     }
+    pdl_launch_dependents();
     if (!p.part) return;
     float* out = p.part + (size_t)blockIdx.x * 2 * p.C;
     if constexpr (G > 32) {                                        // every column has one thread
@@ -346,22 +364,23 @@ template <typename T> __global__ void __launch_bounds__(kThreads) columns_wide(c
     p.part[(size_t)blockIdx.y * 2 * p.C + p.C + c] = gb;
 }
 
-// Column sums of `parts` partial sums [parts][2][C]: 32 columns to a block, a warp takes every eighth part, the warps are added in order.
-template <typename G> __global__ void __launch_bounds__(kThreads) sum_columns(const float* part, int parts, int C, G* gw, G* gb)
+// Column sums of `parts` partial sums [parts][2][C]: 32 columns to a block, a warp takes every 32nd part, the warps are added in order.
+constexpr int kSumThreads = 1024;
+template <typename G> __global__ void __launch_bounds__(kSumThreads) sum_columns(const float* part, int parts, int C, G* gw, G* gb)
 {
-    __shared__ float acc[kThreads / 32][32];
+    __shared__ float acc[kSumThreads / 32][32];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, c = blockIdx.x * 32 + lane;
     pdl_wait_primary();
     float s = 0.f;
     if (c < 2 * C) {
 #pragma unroll 8
-        for (int i = warp; i < parts; i += kThreads / 32) s += __ldcg(part + (size_t)i * 2 * C + c);
+        for (int i = warp; i < parts; i += kSumThreads / 32) s += __ldcg(part + (size_t)i * 2 * C + c);
     }
     acc[warp][lane] = s;
     __syncthreads();
     if (warp != 0 || c >= 2 * C) return;
 #pragma unroll
-    for (int v = 1; v < kThreads / 32; ++v) s += acc[v][lane];
+    for (int v = 1; v < kSumThreads / 32; ++v) s += acc[v][lane];
     G* out = c < C ? gw : gb;
     if (out) out[c < C ? c : c - C] = Elem<G>::from_f32(s);
 }

@@ -22,43 +22,71 @@ __device__ __forceinline__ float inverse(float v) { float r; asm("rcp.approx.ftz
 __device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float min_nan(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 
-struct Gauss { float x, e, q; };
-template <bool NINE> __device__ __forceinline__ Gauss gauss(float z) {
-    Gauss g;
-    g.x = min_nan(fabsf(z), 30.f);                                 // beyond, e is zero in fp32: 0 times infinity does not come up
-    g.e = pow2(g.x * g.x * -0.72134752044f);
-    const float t = inverse(fmaf(g.x, NINE ? 0.345f : 0.31f, 1.f));
-    float q;
-    if (NINE) {
-        q = fmaf(-0.0279335122f, t, 0.143238278f);
-        q = fmaf(q, t, -0.267236026f);
-        q = fmaf(q, t, 0.183022695f);
-        q = fmaf(q, t, -0.0349471461f);
-        q = fmaf(q, t, 0.110766168f);
-        q = fmaf(q, t, 0.117478006f);
-        q = fmaf(q, t, 0.137990677f);
-        q = fmaf(q, t, 0.137620871f);
-    } else {
-        q = fmaf(-0.073929169f, t, 0.180450428f);
-        q = fmaf(q, t, 0.0157446193f);
-        q = fmaf(q, t, 0.133429833f);
-        q = fmaf(q, t, 0.120441264f);
-        q = fmaf(q, t, 0.123860703f);
+// Two values at a time (packed fp32: half the instructions); who loops over values keeps the constants in registers, as a packed
+// instruction takes none from its own words.
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 f2(float lo, float hi) { F2 v; asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi)); return v; }
+__device__ __forceinline__ F2 held(float v) { F2 d; asm volatile("mov.b64 %0, {%1, %1};" : "=l"(d) : "f"(v)); return d; }
+__device__ __forceinline__ void un2(F2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ F2 add2(F2 a, F2 b) { F2 d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+
+template <int TERMS> struct GaussConst {
+    F2 ln, p, one, density, q[TERMS];                              // q: of -Q
+    __device__ __forceinline__ GaussConst() {
+        ln = held(-0.72134752044f); p = held(TERMS == 9 ? 0.345f : 0.31f); one = held(1.f); density = held(0.39894228040f);
+        const float nine[9] = {-0.137620871f, -0.137990677f, -0.117478006f, -0.110766168f, 0.0349471461f, -0.183022695f, 0.267236026f, -0.143238278f, 0.0279335122f};
+        const float six[6] = {-0.123860703f, -0.120441264f, -0.133429833f, -0.0157446193f, -0.180450428f, 0.073929169f};
+#pragma unroll
+        for (int i = 0; i < TERMS; ++i) q[i] = held(TERMS == 9 ? nine[i] : six[i % 6]);
     }
-    g.q = q * t;
-    return g;
+};
+template <int TERMS> struct Gauss {
+    F2 x, e, q;                                                    // q: -Q
+    __device__ __forceinline__ Gauss(const GaussConst<TERMS>& k, float a, float b) {
+        x = f2(min_nan(fabsf(a), 30.f), min_nan(fabsf(b), 30.f));  // beyond, e is zero in fp32: 0 times infinity does not come up
+        float lo, hi;
+        un2(mul2(mul2(x, x), k.ln), lo, hi);
+        e = f2(pow2(lo), pow2(hi));
+        un2(fma2(x, k.p, k.one), lo, hi);
+        const F2 t = f2(inverse(lo), inverse(hi));
+        q = k.q[TERMS - 1];
+#pragma unroll
+        for (int i = TERMS - 2; i >= 0; --i) q = fma2(q, t, k.q[i]);
+        q = mul2(q, t);
+    }
+};
+template <int TERMS> __device__ __forceinline__ void gelu_pair(const GaussConst<TERMS>& k, float& a, float& b) {
+    const Gauss<TERMS> g(k, a, b);
+    un2(fma2(g.x, mul2(g.e, g.q), f2(max_nan(a, 0.f), max_nan(b, 0.f))), a, b);
 }
-// GELU for results of type T.
-template <typename T> __device__ __forceinline__ float gelu(float z) {
-    const Gauss g = gauss<sizeof(T) == 4>(z);
-    return fmaf(-g.x, g.e * g.q, max_nan(z, 0.f));
+__device__ __forceinline__ void gelu_slope_pair(const GaussConst<9>& k, float& a, float& b) {
+    const Gauss<9> g(k, a, b);
+    float lo, hi;
+    un2(mul2(g.e, fma2(g.x, k.density, g.q)), lo, hi);
+    a = a >= 0.f ? 1.f + lo : -lo;
+    b = b >= 0.f ? 1.f + hi : -hi;
 }
-__device__ __forceinline__ float gelu_slope(float z) {
-    const Gauss g = gauss<true>(z);
-    const float h = g.e * fmaf(g.x, 0.39894228040f, -g.q);
-    return z >= 0.f ? 1.f + h : -h;
+// f *= act'(z) for V values.
+template <int V> __device__ __forceinline__ void times_slope(int act, const GaussConst<9>& k, float* f, float* z) {
+    if (act == kActGelu) {
+        if constexpr (V == 1) {
+            float other = z[0];
+            gelu_slope_pair(k, z[0], other);
+            f[0] *= z[0];
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; e += 2) {
+                gelu_slope_pair(k, z[e], z[e + 1]);
+                un2(mul2(f2(f[e], f[e + 1]), f2(z[e], z[e + 1])), f[e], f[e + 1]);
+            }
+        }
+    } else if (act == kActRelu) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[e] *= z[e] > 0.f ? 1.f : 0.f;
+    }
 }
-__device__ __forceinline__ float act_slope(int act, float z) { return act == kActGelu ? gelu_slope(z) : act == kActRelu ? (z > 0.f ? 1.f : 0.f) : 1.f; }
 
 template <typename T> struct Layer {
     const T *x, *w, *b;                 // [rows, K], [N, K], [N] or null
@@ -85,6 +113,7 @@ template <typename T, int V> __global__ void __launch_bounds__(256) grad_z_sums(
     const int all = p.N / V, across = all < 32 ? all : 32, down = 256 / across;
     const int col = threadIdx.x % across, v = blockIdx.x * across + col, r = threadIdx.x / across;
     float sum[V] = {};
+    const GaussConst<9> k;
     if (r < down && v < all) {
         const long long step = (long long)gridDim.y * down;
 #pragma unroll 2
@@ -95,8 +124,7 @@ template <typename T, int V> __global__ void __launch_bounds__(256) grad_z_sums(
             if (p.act != kActNone) {
                 float z[V];
                 load_values<T, V>(p.kept + at, z);
-#pragma unroll
-                for (int e = 0; e < V; ++e) f[e] *= act_slope(p.act, z[e]);
+                times_slope<V>(p.act, k, f, z);
             }
             if (g) {
                 T* to = g + row * g_ld + v * V;
@@ -116,6 +144,7 @@ template <typename T, int V> __global__ void __launch_bounds__(256) grad_z_sums(
             for (int e = 0; e < V; ++e) sum[e] += f[e];
         }
     }
+    pdl_launch_dependents();
     if (!part) return;
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e * 256 + threadIdx.x] = sum[e];
@@ -132,19 +161,20 @@ template <typename T, int V> __global__ void __launch_bounds__(256) grad_z_sums(
 // Partial sums [parts][count], to be added up: the weights' and the bias' gradients in one launch, either may be empty.
 struct Parts { const float* p; int parts; long long count; };
 
-// Many parts: 32 sums to a block, a warp takes every eighth part, the warps are added in order.  Up to kFewParts: a thread has four sums.
-constexpr int kFewParts = 8;
-inline __host__ __device__ long long sum_blocks(const Parts& t) { return t.parts <= kFewParts ? (t.count + 1023) / 1024 : (t.count + 31) / 32; }
-template <typename G> __global__ void __launch_bounds__(256) sum_parts(const Parts w, const Parts b, G* gw, G* gb)
+// Many parts: 32 sums to a block, a warp takes every 32nd part, the warps are added in order.  Up to kFewParts: a thread has four sums.
+constexpr int kFewParts = 8, kSumThreads = 1024;
+inline __host__ __device__ long long sum_blocks(const Parts& t) { return t.parts <= kFewParts ? (t.count + 4 * kSumThreads - 1) / (4 * kSumThreads) : (t.count + 31) / 32; }
+template <typename G> __global__ void __launch_bounds__(kSumThreads) sum_parts(const Parts w, const Parts b, G* gw, G* gb)
 {
-    __shared__ float acc[8][32];
+    __shared__ float acc[kSumThreads / 32][32];
+    pdl_wait_primary();
     const long long ours = sum_blocks(w);
     const bool of_b = blockIdx.x >= ours;
     const Parts t = of_b ? b : w;
     const long long block = blockIdx.x - (of_b ? ours : 0);
     G* out = of_b ? gb : gw;
     if (t.parts <= kFewParts) {
-        const long long e = block * 1024 + threadIdx.x * 4;
+        const long long e = block * (4 * kSumThreads) + threadIdx.x * 4;
         float s[4] = {};
         for (int i = 0; i < t.parts; ++i) {
             const float* at = t.p + (size_t)i * t.count + e;
@@ -163,13 +193,13 @@ template <typename G> __global__ void __launch_bounds__(256) sum_parts(const Par
     float s = 0.f;
     if (e < t.count) {
 #pragma unroll 8
-        for (int i = warp; i < t.parts; i += 8) s += __ldcg(t.p + (size_t)i * t.count + e);
+        for (int i = warp; i < t.parts; i += kSumThreads / 32) s += __ldcg(t.p + (size_t)i * t.count + e);
     }
     acc[warp][lane] = s;
     __syncthreads();
     if (warp != 0 || e >= t.count) return;
 #pragma unroll
-    for (int v = 1; v < 8; ++v) s += acc[v][lane];
+    for (int v = 1; v < kSumThreads / 32; ++v) s += acc[v][lane];
     out[e] = Elem<G>::from_f32(s);
 }
 

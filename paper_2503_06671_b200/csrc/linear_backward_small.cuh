@@ -3,7 +3,7 @@
 //   g = go act'(z)     gx = g w     gw = sum over rows of g^T x     gb = sum over rows of g
 //
 // Such layers are bound by memory: go, z and x are read once, gx is written once, and g never leaves shared memory.  A block takes tiles of
-// 128 rows, one after another.  TMA brings go, z and x as boxes of 128 rows x 64 columns (128 bytes a row, 128-byte swizzle); 16 warps
+// 128 rows, one after another.  TMA brings go, z and x as boxes of 128 rows x 64 columns (128 bytes a row, 128-byte swizzle); eight warps
 // turn go into g in place and add up its columns; then the same boxes of g are the operand of both products: with 128 rows and the columns
 // as contraction (K-major) for gx, with the columns as rows of the result and 128 rows as contraction (MN-major) for gw.  w stays in shared
 // memory and the sums of gw in tensor memory for the life of the block (N / 128 x K columns beside one or two tiles of gx); each block leaves
@@ -16,7 +16,7 @@ namespace esc { namespace linear { namespace small {
 using namespace esc::linear::umma;
 using bf16 = __nv_bfloat16;
 
-constexpr int kRows = 128, kBox = kRows * 128, kActWarps = 16, kOutWarps = 4, kFirstAct = 4, kFirstOut = kFirstAct + kActWarps, kThreads = 32 * (kFirstOut + kOutWarps);
+constexpr int kRows = 128, kBox = kRows * 128, kActWarps = 8, kOutWarps = 4, kFirstAct = 4, kFirstOut = kFirstAct + kActWarps, kThreads = 32 * (kFirstOut + kOutWarps);
 constexpr int kMostBoxes = 4;                                      // of go: N up to 256
 constexpr int kMostStages = 4;
 
@@ -125,6 +125,7 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
         // A lane has the eight columns of one piece in every box, a warp four rows at a time.
         const int w = warp - kFirstAct, row = w * 4 + lane / 8, q = lane % 8;
         float sum[kMostBoxes][8] = {};
+        const GaussConst<9> k;
         for (int t = blockIdx.x; t < p.tiles && alive; t += gridDim.x, r.next(p.stages)) {
             alive = wait_warp(full + 8 * r.s, r.round & 1, 0x21000000u | r.round);
             if (!alive) break;
@@ -141,8 +142,7 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
                         if (has_act) {
                             float z[8];
                             unpack16<bf16>(ld_shared(piece + z_at), z);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) f[e] *= act_slope(p.act, z[e]);
+                            times_slope<8>(p.act, k, f, z);
                             st_shared(piece, pack16<bf16>(f));
                         }
 #pragma unroll
@@ -235,6 +235,7 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
         }
         if (lane == 0) bulk_wait_read<0>();                        // shared memory outlives what is read from it
     }
+    pdl_launch_dependents();
     fence_before();
     __syncthreads();
     if (warp == 2) {

@@ -29,9 +29,9 @@ namespace esc { namespace linear { namespace umma {
 constexpr int kBlockI = 128, kBlockC = 64;
 constexpr int kABytes = kBlockI * kBlockC * 2;                     // of one part
 constexpr int kFillWarps = 16, kGroupWarps = 8, kFirstEpi = 4;         // a group fills every other block
-template <bool TMA> constexpr int epi_warps = TMA ? 16 : 8;
+template <bool TMA> constexpr int epi_warps = TMA ? 12 : 8;
 template <bool TMA> constexpr int all_warps = kFirstEpi + epi_warps<TMA> + (TMA ? 0 : kFillWarps);
-constexpr int kMostEpi = 16;
+constexpr int kMostEpi = 12;
 constexpr int kSlotBytes = 32 * 128;                               // staging of an epilogue warp: 128 bytes of 32 rows
 constexpr int kMaxStages = 8;
 constexpr size_t kMostSmem = 227 * 1024;
@@ -541,6 +541,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         const uint32_t lane_at = lane * 128 + ((lane & 7) << 4), strip = strips + e * 256;   // a piece q of this lane's row: xor q << 4
         const bool has_z = ROLE == kForward && p.z, has_res = ROLE == kForward && p.residual, has_bias = ROLE == kForward && p.bias;
         unsigned units = 0;                                        // of this warp so far
+        const GaussConst<sizeof(T) == 4 ? 9 : 6> gc;
         // the residual of this warp's next unit, from unit c of tile u on, into its slot; `turn` is whose c is
         auto fetch = [&](Walk u, int c, int turn) {
             for (; u.live; next(u, p), c = 0) {
@@ -609,7 +610,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                         if (ROLE == kForward && pass == 1) {
                             if (p.act == kActGelu)
 #pragma unroll
-                                for (int v = 0; v < 2 * V; ++v) f[v] = gelu<O>(f[v]);
+                                for (int v = 0; v < 2 * V; v += 2) gelu_pair(gc, f[v], f[v + 1]);
                             else if (p.act == kActRelu)
 #pragma unroll
                                 for (int v = 0; v < 2 * V; ++v) f[v] = max_nan(f[v], 0.f);
@@ -655,6 +656,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         }
         if (lane == 0) bulk_wait_read<0>();                        // shared memory outlives what is read from it
     }
+    pdl_launch_dependents();
     fence_before();
     __syncthreads();
     if (warp == 2) {
