@@ -783,10 +783,13 @@ ESC_ACT_NONE, ESC_ACT_RELU, ESC_ACT_GELU = 0, 1, 2
 
 def _rows_of(name, t):
     """(rows, channels, values between rows) of a tensor [..., channels] whose rows are dense and evenly spaced."""
-    shape, strides = t.shape, t.stride()
+    shape = t.shape
     if len(shape) < 1 or shape[-1] < 1:
         raise ValueError(f"{name} has to be [..., channels], not {tuple(shape)}")
-    C, rows, step = shape[-1], 1, None
+    C = shape[-1]
+    if t.is_contiguous():
+        return t.numel() // C, C, C
+    strides, rows, step = t.stride(), 1, None
     even = strides[-1] == 1 or C == 1
     for n, s in zip(reversed(shape[:-1]), reversed(strides[:-1])):
         if n != 1 and step is None:
@@ -800,6 +803,30 @@ def _rows_of(name, t):
     return rows, C, max(step, C)
 
 
+def _launch(name, tensors, stream, *args):
+    """Calls the C entry `name` with `args` and the address of the stream, on the tensors' one device: kernels run where the data are."""
+    import torch
+
+    device = None
+    for t in tensors:
+        if t is not None:
+            at = t.get_device()
+            if device is None:
+                device = at
+            elif at != device:
+                raise ValueError("the tensors of a call have to be on one CUDA device")
+    if device < 0:
+        raise ValueError("the tensors of a call have to be on a CUDA device")
+    entry = getattr(lib(), name)
+    if device == torch.cuda.current_device():
+        status = entry(*args, torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            status = entry(*args, torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream)
+    if status != 0:
+        raise EscError(status, name)
+
+
 def _like_rows(name, t, shape, dtype):
     """A dense tensor of as many rows as x, of the given width."""
     if t is None:
@@ -810,10 +837,14 @@ def _like_rows(name, t, shape, dtype):
 
 def _grad_code(*grads):
     """Type of the weights' gradients; they have one."""
-    types = {g.dtype for g in grads if g is not None}
-    if len(types) > 1:
-        raise ValueError("the weights' gradients have to be of one type")
-    return next((_dtype_code(g) for g in grads if g is not None), ESC_F32)
+    code = None
+    for g in grads:
+        if g is not None:
+            if code is None:
+                code = _dtype_code(g)
+            elif code != _dtype_code(g):
+                raise ValueError("the weights' gradients have to be of one type")
+    return ESC_F32 if code is None else code
 
 
 def esc_layer_norm_forward(x, weight, bias, eps, y, stream=None):
@@ -825,9 +856,7 @@ def esc_layer_norm_forward(x, weight, bias, eps, y, stream=None):
         raise ValueError("y has to be of x's shape and type")
     _dense("weight", weight, (C,), x.dtype)
     _dense("bias", bias, (C,), x.dtype)
-    with _on_device(x, weight, bias, y):
-        _check(lib().esc_layer_norm_forward(_address(x), step, _address(weight), _address(bias), eps, _address(y), y_step, rows, C, _dtype_code(x),
-                                            _stream_address(stream)), "esc_layer_norm_forward")
+    _launch("esc_layer_norm_forward", (x, weight, bias, y), stream, _address(x), step, _address(weight), _address(bias), eps, _address(y), y_step, rows, C, _dtype_code(x))
     return y
 
 
@@ -853,13 +882,12 @@ def esc_layer_norm_backward(x, weight, eps, grad_y, grad_x, grad_weight=None, gr
         _like_rows(name, t, x.shape, x.dtype)
     for name, t in (("grad_weight", grad_weight), ("grad_bias", grad_bias)):
         _dense(name, t, (C,), None if t is None else t.dtype)
-    with _on_device(x, weight, grad_y, grad_x, grad_weight, grad_bias, grad_skip, workspace):
-        if workspace is None:
-            with _allocating_for(stream, x.device):
-                workspace = new_layer_norm_workspace(rows, C)
-        _check(lib().esc_layer_norm_backward(_address(x), step, _address(weight), eps, _address(grad_y), _address(grad_skip), _address(grad_x), _address(grad_weight),
-                                             _address(grad_bias), rows, C, _dtype_code(x), _grad_code(grad_weight, grad_bias), _address(workspace),
-                                             workspace.numel() * workspace.element_size(), _stream_address(stream)), "esc_layer_norm_backward")
+    if workspace is None:
+        with _on_device(x), _allocating_for(stream, x.device):
+            workspace = new_layer_norm_workspace(rows, C)
+    _launch("esc_layer_norm_backward", (x, weight, grad_y, grad_x, grad_weight, grad_bias, grad_skip, workspace), stream, _address(x), step, _address(weight), eps,
+            _address(grad_y), _address(grad_skip), _address(grad_x), _address(grad_weight), _address(grad_bias), rows, C, _dtype_code(x),
+            _grad_code(grad_weight, grad_bias), _address(workspace), workspace.numel() * workspace.element_size())
     return grad_x, grad_weight, grad_bias
 
 
@@ -873,9 +901,8 @@ def esc_linear_forward(x, weight, bias, activation, out, residual=None, z=None, 
     shape = x.shape[:-1] + (N,)
     for name, t in (("out", out), ("residual", residual), ("z", z)):
         _like_rows(name, t, shape, x.dtype)
-    with _on_device(x, weight, bias, out, residual, z):
-        _check(lib().esc_linear_forward(_address(x), step, _address(weight), _address(bias), activation, _address(residual), _address(out), _address(z),
-                                        rows, K, N, _dtype_code(x), _stream_address(stream)), "esc_linear_forward")
+    _launch("esc_linear_forward", (x, weight, bias, out, residual, z), stream, _address(x), step, _address(weight), _address(bias), activation, _address(residual),
+            _address(out), _address(z), rows, K, N, _dtype_code(x))
     return out
 
 
@@ -912,11 +939,10 @@ def esc_linear_backward(x, weight, z, activation, grad_out, grad_x=None, grad_we
         _like_rows(name, t, x.shape[:-1] + (width,), x.dtype)
     _dense("grad_weight", grad_weight, (N, K), None if grad_weight is None else grad_weight.dtype)
     _dense("grad_bias", grad_bias, (N,), None if grad_bias is None else grad_bias.dtype)
-    with _on_device(x, weight, z, grad_out, grad_x, grad_weight, grad_bias, workspace):
-        if workspace is None:
-            with _allocating_for(stream, x.device):
-                workspace = new_linear_workspace(rows, K, N, activation, x.dtype)
-        _check(lib().esc_linear_backward(_address(x), step, _address(weight), _address(z), activation, _address(grad_out), _address(grad_x), _address(grad_weight),
-                                         _address(grad_bias), rows, K, N, _dtype_code(x), _grad_code(grad_weight, grad_bias), _address(workspace),
-                                         workspace.numel() * workspace.element_size(), _stream_address(stream)), "esc_linear_backward")
+    if workspace is None:
+        with _on_device(x), _allocating_for(stream, x.device):
+            workspace = new_linear_workspace(rows, K, N, activation, x.dtype)
+    _launch("esc_linear_backward", (x, weight, z, grad_out, grad_x, grad_weight, grad_bias, workspace), stream, _address(x), step, _address(weight), _address(z), activation,
+            _address(grad_out), _address(grad_x), _address(grad_weight), _address(grad_bias), rows, K, N, _dtype_code(x), _grad_code(grad_weight, grad_bias),
+            _address(workspace), workspace.numel() * workspace.element_size())
     return grad_x, grad_weight, grad_bias
