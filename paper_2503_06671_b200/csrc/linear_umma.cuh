@@ -326,7 +326,7 @@ __device__ __forceinline__ __nv_bfloat16 get_value(uint32_t at, __nv_bfloat16) {
 }
 // Where rows are not whole aligned 16-byte pieces: 32 staged rows, the first `rows` of them and `cols` values of each, from or to a matrix.
 template <typename T> __device__ __forceinline__ void rows_in(uint32_t slot, const T* src, long long ld, int rows, int cols, int lane) {
-    constexpr int per_lane = 128 / sizeof(T) / 32, kBatch = 8;
+    constexpr int per_lane = 128 / sizeof(T) / 32, kBatch = 16;
 #pragma unroll 1
     for (int r = 0; r < rows; r += kBatch) {
         T v[kBatch][per_lane];
@@ -341,12 +341,21 @@ template <typename T> __device__ __forceinline__ void rows_in(uint32_t slot, con
     }
 }
 template <typename T> __device__ __forceinline__ void rows_out(uint32_t slot, T* dst, long long ld, int rows, int cols, int lane) {
-    constexpr int per_lane = 128 / sizeof(T) / 32;
-#pragma unroll 4
-    for (int r = 0; r < rows; ++r, dst += ld)
+    constexpr int per_lane = 128 / sizeof(T) / 32, kBatch = 8;
+    dst += lane;
+#pragma unroll 1
+    for (int r = 0; r < rows; r += kBatch) {
+        T v[kBatch][per_lane];
 #pragma unroll
-        for (int q = 0; q < per_lane; ++q)
-            if (lane + 32 * q < cols) dst[lane + 32 * q] = get_value(slot + staged(r, (lane + 32 * q) * sizeof(T)), T{});
+        for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+            for (int q = 0; q < per_lane; ++q) v[u][q] = get_value(slot + staged(r + u, (lane + 32 * q) * sizeof(T)), T{});
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u, dst += ld)
+#pragma unroll
+            for (int q = 0; q < per_lane; ++q)
+                if (r + u < rows && lane + 32 * q < cols) dst[32 * q] = v[u][q];
+    }
 }
 
 // ---- the kernel ---------------------------------------------------------------------------------------------------------------
