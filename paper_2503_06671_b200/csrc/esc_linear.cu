@@ -2,6 +2,7 @@
 #include "rows.h"
 
 #include <algorithm>
+#include <type_traits>
 
 #include "linear_backward_small.cuh"
 
@@ -52,7 +53,7 @@ template <typename T> lin::Layer<T> layer_of(const Call& c) {
 
 // ---- tensor-core products ----------------------------------------------------------------------------------------------------
 
-// What a product is cut into.  Times in cycles of an SM, from the rates below; the cheapest width of a tile and number of runs of rows.
+// What a product is cut into (`runs`: its result is fp32).  Times in cycles of an SM, from the rates below; the cheapest width of a tile and number of runs of rows.
 struct Cut {
     int tiles_i, tiles_j, bn, splits, stages, grid;
     bool resident;
@@ -60,15 +61,15 @@ struct Cut {
 };
 constexpr size_t kBarBytes = 1024 + um::kMostEpi * 256;        // barriers and strips
 constexpr double kLoadRate = 35, kStoreRate = 20;   // bytes per cycle of one SM: from L2 into its ring, to memory
-Cut cut(lin::Role role, long long I, int J, long long depth, size_t es, bool tma) {
-    const int sms = abi::sm_count(), step = role == lin::kForward ? 16 : 64, most = es == 4 ? um::most_columns<float> : um::most_columns<bf16>;
+Cut cut(lin::Role role, long long I, int J, long long depth, size_t es, bool tma, bool runs) {
+    const int sms = abi::sm_count(), step = role == lin::kForward ? 16 : 64, most = es == 4 ? um::most_columns<float> : runs ? um::kMostRunColumns : um::most_columns<bf16>;
     const int parts = es == 4 ? 3 : 1, products = es == 4 ? 6 : 1;
     const long long blocks = (depth + um::kBlockC - 1) / um::kBlockC, tiles_i = (I + um::kBlockI - 1) / um::kBlockI;
     const size_t out_es = role == lin::kGradW ? 4 : es, slot_bytes = (size_t)(tma ? um::epi_warps<true> : um::epi_warps<false>) * um::kSlotBytes;
     const int unit = (int)(128 / out_es);                          // columns that leave together
     Cut best{};
     double least = 1e300;
-    for (int bn = std::min(most, (J + step - 1) / step * step); bn >= step; bn -= step) {
+    for (int bn = std::min(most / step, (J + step - 1) / step) * step; bn >= step; bn -= step) {
         const long long tiles_j = ((long long)J + bn - 1) / bn;
         if (tiles_j > 1 && bn > unit && bn % unit != 0) continue;
         // w stays where it leaves room for a ring of rows and a block has several tiles
@@ -110,7 +111,7 @@ template <typename T> bool map_of(CUtensorMap* m, const void* base, long long ba
 bool whole_pieces(const void* p, long long ld, size_t es) { return abi::aligned(p, 16) && (size_t)ld * es % 16 == 0; }
 
 // The result lies in memory as O [splits, I, J].  Returns the number of splits through `splits`.
-template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long long depth, cudaStream_t st, int* splits = nullptr) {
+template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long long depth, bool runs, cudaStream_t st, int* splits = nullptr) {
     using O = typename um::Result<T, ROLE>::type;
     constexpr bool a_mn = ROLE == lin::kGradW, b_mn = ROLE != lin::kForward;
     constexpr int V = esc::Elem<T>::kVec;
@@ -118,7 +119,7 @@ template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long lon
     CUtensorMap ma{}, mb{}, mo{}, mr{}, mz{};
     p.a_rows = (int)std::min<long long>(um::kBlockI, (p.I + 7) / 8 * 8);
     p.a_tma = sizeof(T) == 2 && a_pieces && map_of<T>(&ma, p.a.p, 0, p.a.rows, p.a.width, p.a.ld, a_mn ? um::kBlockC : p.a_rows);
-    const auto cut_for = [&] { return cut(ROLE, p.I, p.J, depth, sizeof(T), p.a_tma && p.b_tma); };
+    const auto cut_for = [&] { return cut(ROLE, p.I, p.J, depth, sizeof(T), p.a_tma && p.b_tma, runs); };
     p.b_tma = sizeof(T) == 2 && b_pieces;
     Cut c = cut_for();
     if (p.b_tma && !map_of<T>(&mb, p.b.p, 0, p.b.rows, p.b.width, p.b.ld, b_mn ? um::kBlockC : c.bn)) {
@@ -126,6 +127,7 @@ template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long lon
         c = cut_for();
     }
     const bool tma = p.a_tma && p.b_tma;
+    if (c.bn == 0) return ESC_ERR_UNSUPPORTED;                     // more tiles than a launch can count
     p.tiles_i = c.tiles_i; p.tiles_j = c.tiles_j; p.bn = c.bn; p.splits = c.splits; p.stages = c.stages; p.resident = c.resident;
     p.blocks = (int)((depth + um::kBlockC - 1) / um::kBlockC);
     p.units = (unsigned)((long long)c.tiles_i * c.tiles_j * c.splits);
@@ -142,9 +144,15 @@ template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long lon
         kernel<<<(unsigned)c.grid, 32 * warps, c.smem, st>>>(ma, mb, mo, mr, mz, p);
         return launched();
     };
+    auto pick = [&](auto by_tma) {
+        constexpr bool TMA = decltype(by_tma)::value;
+        if constexpr (sizeof(T) == 4 || ROLE == lin::kGradW)
+            if (runs && (p.blocks + c.splits - 1) / c.splits > um::kRun) return launch(um::product_umma<T, ROLE, TMA, true>, um::all_warps<TMA>);
+        return launch(um::product_umma<T, ROLE, TMA, false>, um::all_warps<TMA>);
+    };
     if constexpr (sizeof(T) == 2)
-        if (tma) return launch(um::product_umma<T, ROLE, true>, um::all_warps<true>);
-    return launch(um::product_umma<T, ROLE, false>, um::all_warps<false>);
+        if (tma) return pick(std::true_type{});
+    return pick(std::false_type{});
 }
 
 // grad_z_sums: pieces of a row to a block, and as many blocks as fill the SMs four times, which leave a partial sum each.
@@ -163,7 +171,8 @@ LinearWs carve(void* ws, const Call& c) {
     auto take = [&](size_t bytes) { char* p = base + off; off += abi::round_up(bytes, 256); return p; };
     const long long rows = std::max(c.rows, 1LL);
     const int fused = c.dtype == ESC_BF16 ? sm::plan(rows, c.K, c.N, c.act != ESC_ACT_NONE, abi::sm_count()).grid : 0;   // its blocks leave a part each
-    const int splits = std::max({cut(lin::kGradW, c.N, c.K, rows, c.es(), false).splits, cut(lin::kGradW, c.N, c.K, rows, c.es(), true).splits, fused});
+    int splits = fused;
+    for (int kind = 0; kind < 4; ++kind) splits = std::max(splits, cut(lin::kGradW, c.N, c.K, rows, c.es(), kind & 1, kind & 2).splits);   // whatever the call takes
     w.part = reinterpret_cast<float*>(take((size_t)splits * c.N * c.K * sizeof(float)));
     const int vec = 16 / (int)c.es();
     w.bias = reinterpret_cast<float*>(take((size_t)std::max({bias_cut(c, 1).parts, c.N < vec ? 0 : bias_cut(c, vec).parts, fused}) * c.N * sizeof(float)));
@@ -181,7 +190,7 @@ template <typename T> int linear_forward_t(const Call& c, const lin::Layer<T>& l
     p.I = c.rows; p.J = c.N; p.act = c.act;
     p.a = source<T>(c.x, c.rows, c.K, c.x_stride); p.b = source<T>(c.w, c.N, c.K, c.K);
     p.bias = l.b; p.residual = l.residual; p.out = l.out; p.z = l.z;
-    return launch_product<T, lin::kForward>(p, c.K, st);
+    return launch_product<T, lin::kForward>(p, c.K, sizeof(T) == 4, st);
 }
 
 // The partial sums of the weights' and the bias' gradients, in one launch.
@@ -198,7 +207,7 @@ constexpr int kNotThis = -1;
 int backward_small(const Call& c, const lin::Layer<bf16>& l, void* gw, void* gb, int grad_dtype, const LinearWs& w, cudaStream_t st) {
     const bool act = c.act != ESC_ACT_NONE;
     const sm::Plan d = sm::plan(c.rows, c.K, c.N, act, abi::sm_count());
-    if (d.stages == 0 || (!l.gx && !gw)) return kNotThis;
+    if (d.stages == 0 || (!l.gx && !gw) || (gw && grad_dtype == ESC_F32)) return kNotThis;   // its sums run over all of a block's rows (see kRun)
     if (!whole_pieces(l.go, c.N, 2) || !whole_pieces(c.x, c.x_stride, 2) || !whole_pieces(c.w, c.K, 2) || (act && !whole_pieces(l.kept, c.N, 2)) ||
         (l.gx && !whole_pieces(l.gx, c.K, 2))) return kNotThis;
     CUtensorMap go{}, z{}, x{}, wm{}, gx{}, part{};
@@ -237,13 +246,13 @@ template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& 
         um::Args<T> p{};
         p.I = c.rows; p.J = c.K;
         p.a = g; p.b = source<T>(c.w, c.N, c.K, c.K); p.out = l.gx;
-        ESC_TRY((launch_product<T, lin::kGradX>(p, c.N, st)));
+        ESC_TRY((launch_product<T, lin::kGradX>(p, c.N, sizeof(T) == 4, st)));
     }
     if (gw) {
         um::Args<T> p{};
         p.I = c.N; p.J = c.K;
         p.a = g; p.b = source<T>(c.x, c.rows, c.K, c.x_stride); p.part = w.part;
-        ESC_TRY((launch_product<T, lin::kGradW>(p, c.rows, st, &pw.parts)));
+        ESC_TRY((launch_product<T, lin::kGradW>(p, c.rows, sizeof(T) == 4 || grad_dtype == ESC_F32, st, &pw.parts)));
         pw.count = (long long)c.N * c.K;
     }
     return sum_to(pw, pb, gw, gb, grad_dtype, st);

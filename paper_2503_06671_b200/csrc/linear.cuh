@@ -22,7 +22,7 @@ __device__ __forceinline__ float inverse(float v) { float r; asm("rcp.approx.ftz
 __device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float min_nan(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 
-// Two values at a time (packed fp32: half the instructions); who loops over values keeps the constants in registers, as a packed
+// The slope two values at a time (packed fp32: half the instructions); who loops over values keeps the constants in registers, as a packed
 // instruction takes none from its own words.
 typedef unsigned long long F2;
 __device__ __forceinline__ F2 f2(float lo, float hi) { F2 v; asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi)); return v; }
@@ -32,44 +32,53 @@ __device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 d; asm("fma.rn.f32x2 %
 __device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
 __device__ __forceinline__ F2 add2(F2 a, F2 b) { F2 d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
 
-template <int TERMS> struct GaussConst {
-    F2 ln, p, one, density, q[TERMS];                              // q: of -Q
+constexpr float kLn = -0.72134752044f, kDensity = 0.39894228040f, kP9 = 0.345f, kP6 = 0.31f;
+struct GaussConst {
+    F2 ln, p, one, density, q[9];                                  // q: of -Q
     __device__ __forceinline__ GaussConst() {
-        ln = held(-0.72134752044f); p = held(TERMS == 9 ? 0.345f : 0.31f); one = held(1.f); density = held(0.39894228040f);
-        const float nine[9] = {-0.137620871f, -0.137990677f, -0.117478006f, -0.110766168f, 0.0349471461f, -0.183022695f, 0.267236026f, -0.143238278f, 0.0279335122f};
-        const float six[6] = {-0.123860703f, -0.120441264f, -0.133429833f, -0.0157446193f, -0.180450428f, 0.073929169f};
-#pragma unroll
-        for (int i = 0; i < TERMS; ++i) q[i] = held(TERMS == 9 ? nine[i] : six[i % 6]);
+        ln = held(kLn); p = held(kP9); one = held(1.f); density = held(kDensity);
+        q[0] = held(-0.137620871f); q[1] = held(-0.137990677f); q[2] = held(-0.117478006f); q[3] = held(-0.110766168f); q[4] = held(0.0349471461f);
+        q[5] = held(-0.183022695f); q[6] = held(0.267236026f); q[7] = held(-0.143238278f); q[8] = held(0.0279335122f);
     }
 };
-template <int TERMS> struct Gauss {
-    F2 x, e, q;                                                    // q: -Q
-    __device__ __forceinline__ Gauss(const GaussConst<TERMS>& k, float a, float b) {
-        x = f2(min_nan(fabsf(a), 30.f), min_nan(fabsf(b), 30.f));  // beyond, e is zero in fp32: 0 times infinity does not come up
-        float lo, hi;
-        un2(mul2(mul2(x, x), k.ln), lo, hi);
-        e = f2(pow2(lo), pow2(hi));
-        un2(fma2(x, k.p, k.one), lo, hi);
-        const F2 t = f2(inverse(lo), inverse(hi));
-        q = k.q[TERMS - 1];
-#pragma unroll
-        for (int i = TERMS - 2; i >= 0; --i) q = fma2(q, t, k.q[i]);
-        q = mul2(q, t);
-    }
-};
-template <int TERMS> __device__ __forceinline__ void gelu_pair(const GaussConst<TERMS>& k, float& a, float& b) {
-    const Gauss<TERMS> g(k, a, b);
-    un2(fma2(g.x, mul2(g.e, g.q), f2(max_nan(a, 0.f), max_nan(b, 0.f))), a, b);
-}
-__device__ __forceinline__ void gelu_slope_pair(const GaussConst<9>& k, float& a, float& b) {
-    const Gauss<9> g(k, a, b);
+__device__ __forceinline__ void gelu_slope_pair(const GaussConst& k, float& a, float& b) {
+    const F2 x = f2(min_nan(fabsf(a), 30.f), min_nan(fabsf(b), 30.f));   // beyond, e is zero in fp32: 0 times infinity does not come up
     float lo, hi;
-    un2(mul2(g.e, fma2(g.x, k.density, g.q)), lo, hi);
+    un2(mul2(mul2(x, x), k.ln), lo, hi);
+    const F2 e = f2(pow2(lo), pow2(hi));
+    un2(fma2(x, k.p, k.one), lo, hi);
+    const F2 t = f2(inverse(lo), inverse(hi));
+    F2 q = k.q[8];
+#pragma unroll
+    for (int i = 7; i >= 0; --i) q = fma2(q, t, k.q[i]);
+    un2(mul2(e, fma2(x, k.density, mul2(q, t))), lo, hi);
     a = a >= 0.f ? 1.f + lo : -lo;
     b = b >= 0.f ? 1.f + hi : -hi;
 }
+// GELU for results of type T, one value at a time (in the products' epilogue registers are scarcer than instructions).
+template <typename T> __device__ __forceinline__ float gelu(float z) {
+    const float x = min_nan(fabsf(z), 30.f), e = pow2(x * x * kLn), t = inverse(fmaf(x, sizeof(T) == 4 ? kP9 : kP6, 1.f));
+    float q;
+    if (sizeof(T) == 4) {
+        q = fmaf(0.0279335122f, t, -0.143238278f);
+        q = fmaf(q, t, 0.267236026f);
+        q = fmaf(q, t, -0.183022695f);
+        q = fmaf(q, t, 0.0349471461f);
+        q = fmaf(q, t, -0.110766168f);
+        q = fmaf(q, t, -0.117478006f);
+        q = fmaf(q, t, -0.137990677f);
+        q = fmaf(q, t, -0.137620871f);
+    } else {
+        q = fmaf(0.073929169f, t, -0.180450428f);
+        q = fmaf(q, t, -0.0157446193f);
+        q = fmaf(q, t, -0.133429833f);
+        q = fmaf(q, t, -0.120441264f);
+        q = fmaf(q, t, -0.123860703f);
+    }
+    return fmaf(x, e * (q * t), max_nan(z, 0.f));
+}
 // f *= act'(z) for V values.
-template <int V> __device__ __forceinline__ void times_slope(int act, const GaussConst<9>& k, float* f, float* z) {
+template <int V> __device__ __forceinline__ void times_slope(int act, const GaussConst& k, float* f, float* z) {
     if (act == kActGelu) {
         if constexpr (V == 1) {
             float other = z[0];
@@ -113,7 +122,7 @@ template <typename T, int V> __global__ void __launch_bounds__(256) grad_z_sums(
     const int all = p.N / V, across = all < 32 ? all : 32, down = 256 / across;
     const int col = threadIdx.x % across, v = blockIdx.x * across + col, r = threadIdx.x / across;
     float sum[V] = {};
-    const GaussConst<9> k;
+    const GaussConst k;
     if (r < down && v < all) {
         const long long step = (long long)gridDim.y * down;
 #pragma unroll 2

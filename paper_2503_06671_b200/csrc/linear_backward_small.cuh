@@ -125,7 +125,7 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
         // A lane has the eight columns of one piece in every box, a warp four rows at a time.
         const int w = warp - kFirstAct, row = w * 4 + lane / 8, q = lane % 8;
         float sum[kMostBoxes][8] = {};
-        const GaussConst<9> k;
+        const GaussConst k;
         for (int t = blockIdx.x; t < p.tiles && alive; t += gridDim.x, r.next(p.stages)) {
             alive = wait_warp(full + 8 * r.s, r.round & 1, 0x21000000u | r.round);
             if (!alive) break;

@@ -28,7 +28,8 @@ namespace esc { namespace linear { namespace umma {
 
 constexpr int kBlockI = 128, kBlockC = 64;
 constexpr int kABytes = kBlockI * kBlockC * 2;                     // of one part
-constexpr int kFillWarps = 16, kGroupWarps = 8, kFirstEpi = 4;         // a group fills every other block
+// Warps: one that asks for TMA loads, one that issues (two idle), those that write out, those that fill (a group fills every other block).
+constexpr int kFillWarps = 16, kGroupWarps = 8, kFirstEpi = 4;
 template <bool TMA> constexpr int epi_warps = TMA ? 12 : 8;
 template <bool TMA> constexpr int all_warps = kFirstEpi + epi_warps<TMA> + (TMA ? 0 : kFillWarps);
 constexpr int kMostEpi = 12;
@@ -118,6 +119,16 @@ __device__ __forceinline__ void tmem_ld(uint32_t at, float (&r)[8]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]) : "r"(at) : "memory");
 }
+__device__ __forceinline__ void tmem_st(uint32_t at, const float (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(at), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]),
+                   "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_st(uint32_t at, const float (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(at), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // Loads that stay where they are written: a batch of them is under way before the first value is used.
@@ -166,7 +177,12 @@ template <typename T> struct Args {
 };
 
 template <typename T> constexpr int parts_of = sizeof(T) == 4 ? 3 : 1;
-template <typename T> constexpr int most_columns = sizeof(T) == 4 ? 128 : 256;
+// The tensor cores add to a sum by truncation: about a quarter of a step of fp32 is lost per 16 values of c, always towards zero.  Where the
+// result is fp32 a sum therefore ends after kRun blocks of c and is added, rounded to nearest, to a running sum beside it in tensor memory
+// (4096 values: 4.4e-6 -> below 1e-6 of the result's norm; 16 x 8000: 9.1e-6 -> 3e-7).  That takes columns, so tiles are narrower.
+constexpr int kRun = 8;
+template <typename T> constexpr int most_columns = sizeof(T) == 4 ? 96 : 256;
+constexpr int kMostRunColumns = 128;                               // of bf16 with such runs
 
 // A block's tiles, in the order of its loops.  32-bit arithmetic: a warp that does little else spends a tile's time on divisions.
 struct Walk {
@@ -358,15 +374,46 @@ template <typename T> __device__ __forceinline__ void rows_out(uint32_t slot, T*
     }
 }
 
+// Columns of this run, of its small parts, and of the runs before.
+template <int PARTS, int N> __device__ __forceinline__ void sums(float (&f)[N], uint32_t d, uint32_t sum_at, bool begun) {
+    float more[N];
+    tmem_ld(d, f);
+    tmem_wait_ld();
+    if (PARTS == 3) {
+        tmem_ld(d + kTmemBuffer / 2, more);
+        tmem_wait_ld();
+#pragma unroll
+        for (int v = 0; v < N; ++v) f[v] += more[v];
+    }
+    if (begun) {
+        tmem_ld(sum_at, more);
+        tmem_wait_ld();
+#pragma unroll
+        for (int v = 0; v < N; ++v) f[v] += more[v];
+    }
+}
+// A unit's 32 columns of a run that is not its tile's last, onto the running sum.  Out of the way of the code that every tile runs.
+template <int PARTS, int N> __device__ __noinline__ void add_run(uint32_t d, uint32_t sum_at, bool begun) {
+#pragma unroll 1
+    for (int c = 0; c < 32; c += N) {
+        float f[N];
+        sums<PARTS>(f, d + c, sum_at + c, begun);
+        tmem_st(sum_at + c, f);
+    }
+    tmem_wait_st();
+}
+
 // ---- the kernel ---------------------------------------------------------------------------------------------------------------
 
-template <typename T, Role ROLE, bool TMA>
+// RUNS: the contraction is longer than kRun blocks, and the result fp32.  Of its own: the code of the running sum, though it did not run,
+// cost 427x240, 64 to 64 channels in fp32 six of 33 us.
+template <typename T, Role ROLE, bool TMA, bool RUNS>
 __global__ void __launch_bounds__(32 * all_warps<TMA>, 1)
 product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
              const __grid_constant__ CUtensorMap map_res, const __grid_constant__ CUtensorMap map_z, const __grid_constant__ Args<T> p)
 {
     constexpr bool A_MN = ROLE == kGradW, B_MN = ROLE != kForward;
-    constexpr int PARTS = parts_of<T>, EPI = epi_warps<TMA>, kFirstFill = kFirstEpi + EPI;
+    constexpr int PARTS = parts_of<T>, EPI = epi_warps<TMA>, kIssue = 1, kFirstFill = kFirstEpi + EPI;
     static_assert(!TMA || PARTS == 1, "TMA brings bf16 as it is");
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t base = smem_u32(smem);
@@ -384,7 +431,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         for (int s = 0; s < EPI; ++s) mbar_init(res_full + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 2) {
+    if (warp == kIssue) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -504,42 +551,43 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 if (lane == 0) mbar_arrive(full + 8 * r.s);
             }
         }
-    } else if (warp == 1) {
+    } else if (warp == kIssue) {
         // ---- issue --------------------------------------------------------------------------------------------------------------
         const uint32_t idesc = instr_desc<A_MN, B_MN>(p.bn);
         Ring r{};
-        for (Walk u = walk(p); u.live && alive; next(u, p), ++n) {
-            const int buf = n & 1;
-            if (n >= 2) alive = wait_warp(acc_empty + 8 * buf, (unsigned)((n >> 1) - 1) & 1, 0x30000000u | (unsigned)n);
-            if (alive && p.resident && n == 0) alive = wait_warp(b_full, 0, 0x40000000u);
-            if (!alive) break;
-            fence_after();
-            const uint32_t d = tmem + buf * kTmemBuffer;
-            for (int c = u.c0; c < u.c1; ++c, r.next(p.stages)) {
-                alive = wait_warp(full + 8 * r.s, r.round & 1, 0x50000000u | r.round);
+        if (p.resident) alive = wait_warp(b_full, 0, 0x40000000u);
+        for (Walk u = walk(p); u.live && alive; next(u, p))
+            for (int c = u.c0; c < u.c1 && alive; ++n) {           // n: runs so far
+                const int first = c, end = RUNS ? min(c + kRun, u.c1) : u.c1, buf = n & 1;
+                if (n >= 2) alive = wait_warp(acc_empty + 8 * buf, (unsigned)((n >> 1) - 1) & 1, 0x30000000u | (unsigned)n);
                 if (!alive) break;
                 fence_after();
-                const uint32_t a_at = base + r.s * stage_bytes, b_at = p.resident ? resident + (uint32_t)c * b_bytes : a_at + PARTS * kABytes;
-                const unsigned long long da = smem_desc<A_MN>(a_at), db = smem_desc<B_MN>(b_at);
+                const uint32_t d = tmem + buf * kTmemBuffer;
+                for (; c < end; ++c, r.next(p.stages)) {
+                    alive = wait_warp(full + 8 * r.s, r.round & 1, 0x50000000u | r.round);
+                    if (!alive) break;
+                    fence_after();
+                    const uint32_t a_at = base + r.s * stage_bytes, b_at = p.resident ? resident + (uint32_t)c * b_bytes : a_at + PARTS * kABytes;
+                    const unsigned long long da = smem_desc<A_MN>(a_at), db = smem_desc<B_MN>(b_at);
 #pragma unroll
-                for (int t = 0; t < kBlockC / 16; ++t) {
-                    const unsigned long long at = da + t * (step16<A_MN> >> 4), bt = db + t * (step16<B_MN> >> 4);
-                    const bool add = c > u.c0 || t > 0;
-                    mma(d, at, bt, idesc, add);
-                    if (PARTS == 3) {
-                        const unsigned long long pa = kABytes >> 4, pb = b_part >> 4;
-                        const uint32_t d2 = d + kTmemBuffer / 2;
-                        mma(d2, at + 2 * pa, bt, idesc, add);
-                        mma(d2, at + pa, bt + pb, idesc, true);
-                        mma(d2, at, bt + 2 * pb, idesc, true);
-                        mma(d2, at + pa, bt, idesc, true);
-                        mma(d2, at, bt + pb, idesc, true);
+                    for (int t = 0; t < kBlockC / 16; ++t) {
+                        const unsigned long long at = da + t * (step16<A_MN> >> 4), bt = db + t * (step16<B_MN> >> 4);
+                        const bool add = c > first || t > 0;
+                        mma(d, at, bt, idesc, add);
+                        if (PARTS == 3) {
+                            const unsigned long long pa = kABytes >> 4, pb = b_part >> 4;
+                            const uint32_t d2 = d + kTmemBuffer / 2;
+                            mma(d2, at + 2 * pa, bt, idesc, add);
+                            mma(d2, at + pa, bt + pb, idesc, true);
+                            mma(d2, at, bt + 2 * pb, idesc, true);
+                            mma(d2, at + pa, bt, idesc, true);
+                            mma(d2, at, bt + pb, idesc, true);
+                        }
                     }
+                    commit(empty + 8 * r.s);
                 }
-                commit(empty + 8 * r.s);
+                commit(acc_full + 8 * buf);
             }
-            commit(acc_full + 8 * buf);
-        }
     } else if (warp >= kFirstEpi && warp < kFirstFill) {
         // ---- write out ------------------------------------------------------------------------------------------------------
         // A unit: 128 bytes of 32 rows.  The warps of a quarter of the lanes take units in turn, over the tiles.
@@ -550,7 +598,6 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         const uint32_t lane_at = lane * 128 + ((lane & 7) << 4), strip = strips + e * 256;   // a piece q of this lane's row: xor q << 4
         const bool has_z = ROLE == kForward && p.z, has_res = ROLE == kForward && p.residual, has_bias = ROLE == kForward && p.bias;
         unsigned units = 0;                                        // of this warp so far
-        const GaussConst<sizeof(T) == 4 ? 9 : 6> gc;
         // the residual of this warp's next unit, from unit c of tile u on, into its slot; `turn` is whose c is
         auto fetch = [&](Walk u, int c, int turn) {
             for (; u.live; next(u, p), c = 0) {
@@ -565,21 +612,31 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 }
             }
         };
+        static_assert(!RUNS || sizeof(O) == 4, "see kRun");
         Walk u = walk(p);
         if (p.by_tma && has_res && !has_z && lane == 0) fetch(u, 0, 0);
         __syncwarp();
         int turn = 0;                                              // which member of the team has the next unit
-        for (; u.live && alive; next(u, p), ++n) {
+        int done = 0;                                              // blocks of c of this tile that are summed; n: runs so far
+        for (; u.live && alive; ++n) {
             const int buf = n & 1;
             alive = wait_warp(acc_full + 8 * buf, (unsigned)(n >> 1) & 1, 0x60000000u | (unsigned)n);
             if (!alive) break;
             fence_after();
+            const bool begun = RUNS && done > 0, last = !RUNS || done + kRun >= u.c1 - u.c0;
+            done = last ? 0 : done + kRun;
             const int i0 = u.i * kBlockI + quarter * 32, j0 = u.j * p.bn, wide = min(p.J - j0, p.bn), rows = (int)min(p.I - i0, 32LL);
             const uint32_t d = tmem + buf * kTmemBuffer + ((uint32_t)(quarter * 32) << 16);
+            const int tile_turn = turn;
             for (int c = 0; c < per_tile; ++c) {
                 const bool ours = turn == member && c * UC < wide && rows > 0;
                 turn = turn + 1 == TEAM ? 0 : turn + 1;
                 if (!ours) continue;
+                const uint32_t sum_at = tmem + ((uint32_t)(quarter * 32) << 16) + (PARTS == 3 ? most_columns<T> + c * (kTmemBuffer / 2) : kMostRunColumns + c * UC);
+                if (RUNS && !last) {                              // the same warp has this unit in every run
+                    add_run<PARTS, 2 * V>(d + c * UC, sum_at, begun);
+                    continue;
+                }
                 const int col = j0 + c * UC, cols = min(wide - c * UC, UC);
                 if (has_bias)
 #pragma unroll
@@ -603,15 +660,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 #pragma unroll 1
                     for (int q = 0; q * V < cols; q += 2) {
                         float f[2 * V];
-                        tmem_ld(d + c * UC + q * V, f);
-                        tmem_wait_ld();
-                        if (PARTS == 3) {
-                            float small[2 * V];
-                            tmem_ld(d + kTmemBuffer / 2 + c * UC + q * V, small);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int v = 0; v < 2 * V; ++v) f[v] += small[v];
-                        }
+                        sums<PARTS>(f, d + c * UC + q * V, sum_at + q * V, begun);
                         const uint32_t left = lane_at ^ (uint32_t)(q << 4), right = lane_at ^ (uint32_t)((q + 1) << 4);
                         if (has_bias)
 #pragma unroll
@@ -619,7 +668,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                         if (ROLE == kForward && pass == 1) {
                             if (p.act == kActGelu)
 #pragma unroll
-                                for (int v = 0; v < 2 * V; v += 2) gelu_pair(gc, f[v], f[v + 1]);
+                                for (int v = 0; v < 2 * V; ++v) f[v] = gelu<O>(f[v]);
                             else if (p.act == kActRelu)
 #pragma unroll
                                 for (int v = 0; v < 2 * V; ++v) f[v] = max_nan(f[v], 0.f);
@@ -661,14 +710,17 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             }
             if (!alive) break;
             fence_before();
+            __syncwarp();
             if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
+            if (last) next(u, p);
+            else turn = tile_turn;
         }
         if (lane == 0) bulk_wait_read<0>();                        // shared memory outlives what is read from it
     }
     pdl_launch_dependents();
     fence_before();
     __syncthreads();
-    if (warp == 2) {
+    if (warp == kIssue) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
