@@ -110,8 +110,9 @@ template <typename T> bool map_of(CUtensorMap* m, const void* base, long long ba
 }
 bool whole_pieces(const void* p, long long ld, size_t es) { return abi::aligned(p, 16) && (size_t)ld * es % 16 == 0; }
 
-// The result lies in memory as O [splits, I, J].  Returns the number of splits through `splits`.
-template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long long depth, bool runs, cudaStream_t st, int* splits = nullptr) {
+// The result lies in memory as O [splits, I, J].  Returns the number of splits through `splits`.  `beside`: the kernel before it in the stream is
+// the other product of the same g, and need not have ended.
+template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long long depth, bool runs, cudaStream_t st, int* splits = nullptr, bool beside = false) {
     using O = typename um::Result<T, ROLE>::type;
     constexpr bool a_mn = ROLE == lin::kGradW, b_mn = ROLE != lin::kForward;
     constexpr int V = esc::Elem<T>::kVec;
@@ -141,6 +142,7 @@ template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long lon
     p.b.pieces = b_pieces && p.b.width % V == 0;
     auto launch = [&](auto kernel, int warps) {
         ESC_ABI_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)um::kMostSmem));   // the same for every call
+        if (beside) return launch_behind(kernel, (unsigned)c.grid, 32 * warps, st, c.smem, ma, mb, mo, mr, mz, p);
         kernel<<<(unsigned)c.grid, 32 * warps, c.smem, st>>>(ma, mb, mo, mr, mz, p);
         return launched();
     };
@@ -195,7 +197,7 @@ template <typename T> int linear_forward_t(const Call& c, const lin::Layer<T>& l
 
 // The partial sums of the weights' and the bias' gradients, in one launch.
 template <typename G> int launch_sums(const lin::Parts& w, const lin::Parts& b, void* gw, void* gb, cudaStream_t st) {
-    return launch_behind(lin::sum_parts<G>, (unsigned)(lin::sum_blocks(w) + lin::sum_blocks(b)), lin::kSumThreads, st, w, b, static_cast<G*>(gw), static_cast<G*>(gb));
+    return launch_behind(lin::sum_parts<G>, (unsigned)(lin::sum_blocks(w) + lin::sum_blocks(b)), lin::kSumThreads, st, 0, w, b, static_cast<G*>(gw), static_cast<G*>(gb));
 }
 int sum_to(const lin::Parts& w, const lin::Parts& b, void* gw, void* gb, int grad_dtype, cudaStream_t st) {
     if (w.count + b.count == 0) return ESC_OK;
@@ -252,7 +254,7 @@ template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& 
         um::Args<T> p{};
         p.I = c.N; p.J = c.K;
         p.a = g; p.b = source<T>(c.x, c.rows, c.K, c.x_stride); p.part = w.part;
-        ESC_TRY((launch_product<T, lin::kGradW>(p, c.rows, sizeof(T) == 4 || grad_dtype == ESC_F32, st, &pw.parts)));
+        ESC_TRY((launch_product<T, lin::kGradW>(p, c.rows, sizeof(T) == 4 || grad_dtype == ESC_F32, st, &pw.parts, l.gx != nullptr)));
         pw.count = (long long)c.N * c.K;
     }
     return sum_to(pw, pb, gw, gb, grad_dtype, st);

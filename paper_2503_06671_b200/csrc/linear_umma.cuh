@@ -431,6 +431,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         for (int s = 0; s < EPI; ++s) mbar_init(res_full + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (ROLE == kGradX) pdl_launch_dependents();                   // the product of the weights' gradient may start on SMs that this one leaves
     if (warp == kIssue) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -718,6 +719,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         if (lane == 0) bulk_wait_read<0>();                        // shared memory outlives what is read from it
     }
     pdl_launch_dependents();
+    if (ROLE == kGradW) pdl_wait_primary();                        // it may have started beside the other product: what comes next waits for both
     fence_before();
     __syncthreads();
     if (warp == kIssue) {

@@ -18,13 +18,13 @@ inline int launched() {
     return ESC_OK;
 }
 
-// A kernel that starts while the one before it in the stream ends, and waits for that itself (griddepcontrol.wait) before it reads.
-template <typename... P, typename... A> int launch_behind(void (*kernel)(P...), unsigned blocks, int threads, cudaStream_t st, A... args) {
+// A kernel that may start while the one before it in the stream ends, and waits for that itself (griddepcontrol.wait).
+template <typename... P, typename... A> int launch_behind(void (*kernel)(P...), unsigned blocks, int threads, cudaStream_t st, size_t smem, A... args) {
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(threads); cfg.stream = st; cfg.attrs = &attr; cfg.numAttrs = 1;
+    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st; cfg.attrs = &attr; cfg.numAttrs = 1;
     ESC_ABI_CUDA(cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...));
     return launched();
 }
