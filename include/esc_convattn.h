@@ -522,7 +522,12 @@ int esc_layer_norm_backward(const void* x, long long x_stride, const void* weigh
  *   residual   [rows, N] dense or NULL
  *   out        [rows, N] dense;  z [rows, N] dense or NULL: z as it is, rounded to the type, for the backward pass (act takes the
  *              unrounded z)
- * rows may be 0 and is below 2^31 - 4096; K and N are at most 2^20.  Sums in fp32, one rounding per output.
+ * rows may be 0 and is below 2^31 - 4096; K and N are at most 2^20 (ESC_ERR_UNSUPPORTED beyond, and where rows N would take more than
+ * 2^31 tiles of 128 x 16).  Fastest where pointers are 16-byte aligned and K, N and x_stride multiples of 16 bytes.
+ * Arithmetic: the products run on the tensor cores.  bf16 values are multiplied exactly and added in fp32; fp32 values are three bf16 parts each
+ * (24 bits), of whose products those above 2^-26 are taken, and sums end after 512 values and are added in fp32: about as far from
+ * the exact result as fp32 multiply-adds.  An fp32 value that is not finite (or 3.39e38 or more) makes its row, in a gradient of the weights
+ * its column, NaN; with bf16 it gives what the sums give.  Each output is rounded once.
  */
 enum { ESC_ACT_NONE = 0, ESC_ACT_RELU = 1, ESC_ACT_GELU = 2 };
 int esc_linear_forward(const void* x, long long x_stride, const void* weight, const void* bias, int activation,
@@ -534,12 +539,22 @@ int esc_linear_forward(const void* x, long long x_stride, const void* weight, co
  *   grad_out   [rows, N] dense (also the residual's gradient, as it is)
  *   grad_x     [rows, K] dense;  grad_weight [N, K] and grad_bias [N] of grad_dtype; each may be NULL.  No rows: zeros.
  *   workspace  esc_linear_backward_workspace_bytes(...) bytes, 256-byte aligned, no preparation needed
+ * With bf16 tensors and an activation g is rounded to bf16, as an operand of the two products, not in grad_bias.
  * Every sum has a fixed order: the same input gives the same bits.  Calls, or graphs, that may run at the same time need a workspace each.
  */
 size_t esc_linear_backward_workspace_bytes(long long rows, int K, int N, int activation, int dtype);   /* 0 for invalid arguments */
 int esc_linear_backward(const void* x, long long x_stride, const void* weight, const void* z, int activation,
                         const void* grad_out, void* grad_x, void* grad_weight, void* grad_bias, long long rows, int K, int N,
                         int dtype, int grad_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The linear layers' kernels wait, with a limit of about a second, for their own loads and products.  Should a wait run out, the call's
+ * results are not valid; esc_linear_device_status(), which synchronises `stream`, then returns ESC_DEV_TIMEOUT once (for all streams of the
+ * current device) and clears that.  Not while `stream` is being captured (ESC_ERR_UNSUPPORTED).  The self-test launches one warp that
+ * waits in vain.
+ */
+int esc_linear_device_status(void* stream);
+int esc_linear_selftest_bounded_wait(void* stream);
 
 /*
  * Self-test of the error path that every device-side wait of this library shares: launches one thread that waits, with

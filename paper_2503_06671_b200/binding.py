@@ -94,6 +94,8 @@ def lib():
         L.esc_linear_backward_workspace_bytes.argtypes = [ll, i, i, i, i]
         L.esc_linear_backward_workspace_bytes.restype = sz
         L.esc_linear_backward.argtypes = [vp, ll, vp, vp, i, vp, vp, vp, vp, ll, i, i, i, i, vp, sz, vp]
+        L.esc_linear_device_status.argtypes = [vp]
+        L.esc_linear_selftest_bounded_wait.argtypes = [vp]
         L.esc_convattn_set_tile_width.argtypes = [i]
         L.esc_convattn_set_stencil_engine.argtypes = [i]
         L.esc_convattn_set_fused_stage1.argtypes = [i]
@@ -105,7 +107,7 @@ def lib():
                      "esc_convattn_dynkernel", "esc_convattn_dynkernel_static", "esc_convattn_forward_mlp", "esc_convattn_dynkernel_mlp", "esc_convattn_forward_pw", "esc_convattn_stencil_pw", "esc_convattn_forward_dense", "esc_convattn_stencil_dense", "esc_convattn_forward_variant", "esc_convattn_backward", "esc_convattn_backward_mlp", "esc_convattn_backward_pw", "esc_convattn_backward_dense", "esc_convattn_backward_variant", "esc_conv_fuse_backward", "esc_convattn_stencil", "esc_convattn_forward_host", "esc_convattn_forward_host_submit", "esc_convattn_forward_host_wait",
                      "esc_relpos_bias_forward", "esc_relpos_bias_backward", "esc_window_attention_forward", "esc_window_attention_backward",
                      "esc_adamw_plan_init", "esc_adamw_step", "esc_adamw_scalars",
-                     "esc_layer_norm_forward", "esc_layer_norm_backward", "esc_linear_forward", "esc_linear_backward",
+                     "esc_layer_norm_forward", "esc_layer_norm_backward", "esc_linear_forward", "esc_linear_backward", "esc_linear_device_status", "esc_linear_selftest_bounded_wait",
                      "esc_convattn_device_status", "esc_convattn_last_path", "esc_convattn_last_tile_width", "esc_convattn_set_tile_width", "esc_convattn_set_stencil_engine", "esc_convattn_set_fused_stage1", "esc_convattn_set_dense_engine", "esc_convattn_last_launches",
                      "esc_version"):
             getattr(L, name).restype = i
@@ -946,3 +948,12 @@ def esc_linear_backward(x, weight, z, activation, grad_out, grad_x=None, grad_we
             _address(grad_out), _address(grad_x), _address(grad_weight), _address(grad_bias), rows, K, N, _dtype_code(x), _grad_code(grad_weight, grad_bias),
             _address(workspace), workspace.numel() * workspace.element_size())
     return grad_x, grad_weight, grad_bias
+
+
+def esc_linear_device_status(stream=None) -> int:
+    """0, or ESC_DEV_TIMEOUT once if a wait of a linear layer's kernel ran out on this device; synchronises."""
+    return lib().esc_linear_device_status(_stream(stream))
+
+
+def esc_linear_selftest_bounded_wait(stream=None) -> None:
+    _check(lib().esc_linear_selftest_bounded_wait(_stream(stream)), "esc_linear_selftest_bounded_wait")

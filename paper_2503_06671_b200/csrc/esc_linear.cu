@@ -264,6 +264,27 @@ template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& 
 
 extern "C" {
 
+int esc_linear_device_status(void* stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    ESC_ABI_CUDA(cudaStreamIsCapturing(st, &capturing));
+    if (capturing != cudaStreamCaptureStatusNone) return ESC_ERR_UNSUPPORTED;
+    unsigned status[2] = {0, 0};
+    ESC_ABI_CUDA(cudaMemcpyFromSymbolAsync(status, um::wait_status, sizeof status, 0, cudaMemcpyDeviceToHost, st));
+    ESC_ABI_CUDA(cudaStreamSynchronize(st));
+    if (status[0] == 0) return ESC_OK;
+    const unsigned clear[2] = {0, 0};
+    ESC_ABI_CUDA(cudaMemcpyToSymbolAsync(um::wait_status, clear, sizeof clear, 0, cudaMemcpyHostToDevice, st));
+    ESC_ABI_CUDA(cudaStreamSynchronize(st));
+    return (int)status[0];
+}
+
+int esc_linear_selftest_bounded_wait(void* stream) {
+    um::wait_in_vain<<<1, 32, 0, static_cast<cudaStream_t>(stream)>>>();
+    ESC_ABI_CUDA(cudaGetLastError());
+    return ESC_OK;
+}
+
 int esc_linear_forward(const void* x, long long x_stride, const void* weight, const void* bias, int activation, const void* residual, void* out, void* z,
                        long long rows, int K, int N, int dtype, void* stream) {
     abi::launches_reset();

@@ -728,6 +728,15 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     }
 }
 
+// One warp's wait for a barrier that nothing signals: gives up after its poll limit and records that.
+__global__ void __launch_bounds__(32) wait_in_vain()
+{
+    __shared__ __align__(8) unsigned long long bar;
+    if (threadIdx.x == 0) mbar_init(smem_u32(&bar), 1);
+    __syncwarp();
+    wait_warp(smem_u32(&bar), 0, 0xA0000000u);
+}
+
 // ---- host side ------------------------------------------------------------------------------------------------------------------
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
                                   CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);

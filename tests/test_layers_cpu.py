@@ -92,6 +92,7 @@ def test_linear_refusals(L):
     assert fwd(x=X + 1) == 4 and fwd(w=W + 1) == 4 and fwd(b=B + 1) == 4 and fwd(res=GY + 1) == 4 and fwd(out=Y + 1) == 4 and fwd(z=GX + 1) == 4
     assert fwd(out=X) == 5 and fwd(out=W) == 5 and fwd(out=B) == 5 and fwd(out=GY) == 5 and fwd(z=Y) == 5 and fwd(z=X) == 5 and fwd(z=Y + 192 * 2 * 99) == 5
     assert fwd(rows=0) == 0
+    assert fwd(rows=(1 << 31) - 8192, K=8, xs=8, N=1 << 20, out=1 << 50, res=None, z=None) == 3          # more tiles than a launch can count
 
     need = L.esc_linear_backward_workspace_bytes(100, 64, 192, 2, 1)
     assert need > 0 and need % 256 == 0
