@@ -494,63 +494,73 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             x.get(of_b ? p.b : p.a, (of_b ? b_at : a_at) + L * 128, of_b ? p.bn - L : kBlockI - L, mn ? c0 : m0 + L, mn ? m0 + L : c0, w, lane);
         };
         auto put = [&](Chunk<T>& x, int q) { x.put(q >= a_chunks ? b_part : (uint32_t)kABytes); };
-        Ring r{};
-        int turn = 0;
-        for (Walk u = walk(p); u.live && alive; next(u, p), ++n) {
-            const int i0 = u.i * kBlockI, j0 = u.j * p.bn;
-            if (p.resident && n == 0) {
-                if (tb && group == 0 && w == 0 && lane == 0) {
-                    mbar_bytes(b_full, (unsigned)p.blocks * b_bytes);
-                    for (int c = 0; c < p.blocks; ++c) {
-                        if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(resident + c * b_bytes + m * 128, &map_b, b_full, j0 + m, c * kBlockC);
-                        else tma_load_2d(resident + c * b_bytes, &map_b, b_full, c * kBlockC, j0);
-                    }
+        struct Place { Walk u; int c; Ring r; };                   // a block, and its place in the ring
+        auto forth = [&](Place& k) {
+            if (++k.c >= k.u.c1) { next(k.u, p); k.c = k.u.c0; }
+            k.r.next(p.stages);
+        };
+        Place here{walk(p), 0, Ring{}};
+        here.c = here.u.c0;
+        if (p.resident) {
+            if (tb && group == 0 && w == 0 && lane == 0) {
+                mbar_bytes(b_full, (unsigned)p.blocks * b_bytes);
+                for (int c = 0; c < p.blocks; ++c) {
+                    if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(resident + c * b_bytes + m * 128, &map_b, b_full, here.u.j * p.bn + m, c * kBlockC);
+                    else tma_load_2d(resident + c * b_bytes, &map_b, b_full, c * kBlockC, here.u.j * p.bn);
                 }
-                for (int c = group; c < p.blocks; c += kFillWarps / kGroupWarps)
-                    for (int q = a_chunks; q < a_chunks + b_chunks; ++q) {
-                        Chunk<T> x;
-                        get(x, q, u, c, 0, resident + c * b_bytes);
-                        put(x, q);
-                    }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(b_full);
             }
-            const int chunks = a_chunks + (p.resident ? 0 : b_chunks);
-            for (int c = u.c0; c < u.c1; ++c, r.next(p.stages), turn ^= 1) {
-                if (turn != group) continue;
-                const uint32_t at = base + r.s * stage_bytes;
-                Chunk<T> x;
-                if (chunks > 0) get(x, 0, u, c, at, at + PARTS * kABytes);
-                if (r.round > 0) alive = wait_warp(empty + 8 * r.s, (r.round - 1) & 1, 0x20000000u | r.round);
-                if (!alive) break;
-                if ((ta || (tb && !p.resident)) && w == 0 && lane == 0) {
-                    mbar_bytes(full + 8 * r.s, (ta ? (A_MN ? kABytes : p.a_rows * 128) : 0) + (tb && !p.resident ? b_bytes : 0));
-                    if (ta) {
-                        if (A_MN) for (int m = 0; m < kBlockI; m += 64) tma_load_2d(at + m * 128, &map_a, full + 8 * r.s, i0 + m, c * kBlockC);
-                        else tma_load_2d(at, &map_a, full + 8 * r.s, c * kBlockC, i0);
-                    }
-                    if (tb && !p.resident) {
-                        if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(at + kABytes + m * 128, &map_b, full + 8 * r.s, j0 + m, c * kBlockC);
-                        else tma_load_2d(at + kABytes, &map_b, full + 8 * r.s, c * kBlockC, j0);
-                    }
+            for (int c = group; c < p.blocks; c += kFillWarps / kGroupWarps)
+                for (int q = a_chunks; q < a_chunks + b_chunks; ++q) {
+                    Chunk<T> x;
+                    get(x, q, here.u, c, 0, resident + c * b_bytes);
+                    put(x, q);
                 }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b_full);
+        }
+        const int chunks = a_chunks + (p.resident ? 0 : b_chunks);
+        if (group == 1) forth(here);
+        auto at_of = [&](const Place& k) { return base + k.r.s * stage_bytes; };
+        Chunk<T> x;
+        if (chunks > 0 && here.u.live) get(x, 0, here.u, here.c, at_of(here), at_of(here) + PARTS * kABytes);
+        while (here.u.live) {
+            Place after = here;
+            forth(after);
+            if (after.u.live) forth(after);
+            if (here.r.round > 0) alive = wait_warp(empty + 8 * here.r.s, (here.r.round - 1) & 1, 0x20000000u | here.r.round);
+            if (!alive) break;
+            const uint32_t at = at_of(here), bar = full + 8 * here.r.s;
+            if ((ta || (tb && !p.resident)) && w == 0 && lane == 0) {
+                const int i0 = here.u.i * kBlockI, j0 = here.u.j * p.bn, c0 = here.c * kBlockC;
+                mbar_bytes(bar, (ta ? (A_MN ? kABytes : p.a_rows * 128) : 0) + (tb && !p.resident ? b_bytes : 0));
+                if (ta) {
+                    if (A_MN) for (int m = 0; m < kBlockI; m += 64) tma_load_2d(at + m * 128, &map_a, bar, i0 + m, c0);
+                    else tma_load_2d(at, &map_a, bar, c0, i0);
+                }
+                if (tb && !p.resident) {
+                    if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(at + kABytes + m * 128, &map_b, bar, j0 + m, c0);
+                    else tma_load_2d(at + kABytes, &map_b, bar, c0, j0);
+                }
+            }
 #pragma unroll 1
-                for (int q = 0; q < chunks; ++q) {
-                    if constexpr (PARTS == 3) {                    // another chunk's loads meanwhile; bf16 has no registers for that
-                        Chunk<T> y;
-                        if (q + 1 < chunks) get(y, q + 1, u, c, at, at + PARTS * kABytes);
-                        put(x, q);
-                        x = y;
-                    } else {
-                        put(x, q);
-                        if (q + 1 < chunks) get(x, q + 1, u, c, at, at + PARTS * kABytes);
-                    }
+            for (int q = 0; q < chunks; ++q) {                     // the next chunk, or the next block's first, is loaded meanwhile
+                const bool more = q + 1 < chunks;
+                const Place& k = more ? here : after;
+                if constexpr (PARTS == 3) {
+                    Chunk<T> y;
+                    if (k.u.live) get(y, more ? q + 1 : 0, k.u, k.c, at_of(k), at_of(k) + PARTS * kABytes);
+                    put(x, q);
+                    x = y;
+                } else {                                           // bf16 has no registers for two
+                    put(x, q);
+                    if (k.u.live) get(x, more ? q + 1 : 0, k.u, k.c, at_of(k), at_of(k) + PARTS * kABytes);
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(full + 8 * r.s);
             }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+            here = after;
         }
     } else if (warp == kIssue) {
         // ---- issue --------------------------------------------------------------------------------------------------------------
