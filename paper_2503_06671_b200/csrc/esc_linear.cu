@@ -163,9 +163,13 @@ BiasCut bias_cut(const Call& c, int vec) {
     const int all = c.N / vec, wide = std::min(all, 32), across = (all + wide - 1) / wide;
     return {across, (int)std::max(1LL, std::min((4LL * abi::sm_count() + across - 1) / across, (c.rows + 31) / 32))};
 }
+// A copy of ragged bf16 rows to rows of whole pieces costs two passes over them and a launch; a product that takes them as they are runs at a
+// third of the speed: 70640 x 906 x 441 backward 595 us as they are.  Below a million values the launch costs more.
+bool copied(long long rows, int K) { return rows * K >= 1 << 20; }
+long long piece_stride(int K) { return (long long)abi::round_up(K, 8); }
 // g lies in rows of whole 16-byte pieces, whatever N is.
 long long g_stride(const Call& c) { return (long long)abi::round_up(c.N, 16 / c.es()); }
-struct LinearWs { float *part, *bias; void* g; size_t bytes; };
+struct LinearWs { float *part, *bias; void* g; bf16 *x, *w; size_t bytes; };
 LinearWs carve(void* ws, const Call& c) {
     LinearWs w;
     char* base = static_cast<char*>(ws);
@@ -176,15 +180,34 @@ LinearWs carve(void* ws, const Call& c) {
     int splits = fused;
     for (int kind = 0; kind < 4; ++kind) splits = std::max(splits, cut(lin::kGradW, c.N, c.K, rows, c.es(), kind & 1, kind & 2).splits);   // whatever the call takes
     w.part = reinterpret_cast<float*>(take((size_t)splits * c.N * c.K * sizeof(float)));
-    const int vec = 16 / (int)c.es();
-    w.bias = reinterpret_cast<float*>(take((size_t)std::max({bias_cut(c, 1).parts, c.N < vec ? 0 : bias_cut(c, vec).parts, fused}) * c.N * sizeof(float)));
+    int parts = fused;
+    for (int vec = 16 / (int)c.es(); vec >= 1; vec /= 2)
+        if (c.N % vec == 0) parts = std::max(parts, bias_cut(c, vec).parts);
+    w.bias = reinterpret_cast<float*>(take((size_t)parts * c.N * sizeof(float)));
     w.g = take(c.act != ESC_ACT_NONE ? (size_t)c.rows * g_stride(c) * c.es() : 0);
+    // bf16 with K that is no multiple of eight: x and the weights as rows of whole 16-byte pieces, where copying them pays
+    const bool ragged = c.dtype == ESC_BF16 && c.K % 8 != 0;
+    w.x = reinterpret_cast<bf16*>(take(ragged && copied(c.rows, c.K) ? (size_t)c.rows * piece_stride(c.K) * 2 : 0));
+    w.w = reinterpret_cast<bf16*>(take(ragged && copied(c.N, c.K) ? (size_t)c.N * piece_stride(c.K) * 2 : 0));
     w.bytes = off;
     return w;
 }
 
 template <typename T> um::Source<T> source(const void* p, long long rows, long long width, long long ld) {
     return um::Source<T>{static_cast<const T*>(p), rows, width, ld, false};
+}
+
+template <typename U> int launch_copy_of(const um::Source<bf16>& s, bf16* out, long long ld, cudaStream_t st) {
+    constexpr int values = sizeof(U) / 2;
+    const int width = (int)(s.width / values);
+    const unsigned across = (unsigned)((width + 63) / 64);
+    const long long want = (32LL * abi::sm_count() + across - 1) / across;
+    lin::copy_rows<U><<<dim3(across, (unsigned)std::min({(s.rows + 63) / 64, want, 65535LL})), 256, 0, st>>>(reinterpret_cast<const U*>(s.p), s.ld / values, s.rows, width,
+                                                                                                         reinterpret_cast<U*>(out), ld / values);
+    return launched();
+}
+int launch_copy(const um::Source<bf16>& s, bf16* out, long long ld, cudaStream_t st) {
+    return s.width % 2 == 0 && s.ld % 2 == 0 && abi::aligned(s.p, 4) ? launch_copy_of<unsigned>(s, out, ld, st) : launch_copy_of<unsigned short>(s, out, ld, st);
 }
 
 template <typename T> int linear_forward_t(const Call& c, const lin::Layer<T>& l, cudaStream_t st) {
@@ -235,25 +258,47 @@ template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& 
     if (acts || gb) {
         T* to = acts ? static_cast<T*>(w.g) : nullptr;
         const long long ld = g_stride(c);
-        const bool pieces = c.N % V == 0 && abi::aligned(l.go, 16) && (c.act == ESC_ACT_NONE || abi::aligned(l.kept, 16));
-        const BiasCut b = bias_cut(c, pieces ? V : 1);
+        // the widest piece, of 16 bytes at most, that divides the rows and their alignment
+        const auto fits = [&](int vec) {
+            return c.N % vec == 0 && abi::aligned(l.go, vec * sizeof(T)) && (c.act == ESC_ACT_NONE || abi::aligned(l.kept, vec * sizeof(T)));
+        };
+        int vec = V;
+        while (!fits(vec)) vec /= 2;
+        const BiasCut b = bias_cut(c, vec);
         const dim3 grid(b.across, b.parts);
-        if (pieces) lin::grad_z_sums<T, V><<<grid, 256, 0, st>>>(l, to, ld, gb ? w.bias : nullptr);
-        else lin::grad_z_sums<T, 1><<<grid, 256, 0, st>>>(l, to, ld, gb ? w.bias : nullptr);
+        float* sums = gb ? w.bias : nullptr;
+        if (vec == 8) { if constexpr (V == 8) lin::grad_z_sums<T, 8><<<grid, 256, 0, st>>>(l, to, ld, sums); }
+        else if (vec == 4) lin::grad_z_sums<T, 4><<<grid, 256, 0, st>>>(l, to, ld, sums);
+        else if (vec == 2) lin::grad_z_sums<T, 2><<<grid, 256, 0, st>>>(l, to, ld, sums);
+        else lin::grad_z_sums<T, 1><<<grid, 256, 0, st>>>(l, to, ld, sums);
         ESC_TRY(launched());
         if (gb) pb = lin::Parts{w.bias, b.parts, c.N};
         if (acts) g = source<T>(to, c.rows, c.N, ld);
     }
+    um::Source<T> x = source<T>(c.x, c.rows, c.K, c.x_stride), weight = source<T>(c.w, c.N, c.K, c.K);
+    if constexpr (sizeof(T) == 2) {
+        if (c.K % 8 != 0) {
+            const long long ld = piece_stride(c.K);
+            if (gw && copied(c.rows, c.K)) {
+                ESC_TRY(launch_copy(x, w.x, ld, st));
+                x = source<T>(w.x, c.rows, c.K, ld);
+            }
+            if (l.gx && copied(c.N, c.K)) {
+                ESC_TRY(launch_copy(weight, w.w, ld, st));
+                weight = source<T>(w.w, c.N, c.K, ld);
+            }
+        }
+    }
     if (l.gx) {
         um::Args<T> p{};
         p.I = c.rows; p.J = c.K;
-        p.a = g; p.b = source<T>(c.w, c.N, c.K, c.K); p.out = l.gx;
+        p.a = g; p.b = weight; p.out = l.gx;
         ESC_TRY((launch_product<T, lin::kGradX>(p, c.N, sizeof(T) == 4, st)));
     }
     if (gw) {
         um::Args<T> p{};
         p.I = c.N; p.J = c.K;
-        p.a = g; p.b = source<T>(c.x, c.rows, c.K, c.x_stride); p.part = w.part;
+        p.a = g; p.b = x; p.part = w.part;
         ESC_TRY((launch_product<T, lin::kGradW>(p, c.rows, sizeof(T) == 4 || grad_dtype == ESC_F32, st, &pw.parts, l.gx != nullptr)));
         pw.count = (long long)c.N * c.K;
     }

@@ -111,12 +111,40 @@ enum Role { kForward, kGradX, kGradW };
 
 // g = go act'(z) and its column sums, as far as they are asked for: g [rows, g_ld] of the type (rounded: the operand that two products
 // read), part [gridDim.y][N] fp32 sums of the unrounded g.  A thread has V neighbouring columns and every so many rows; a block has
-// min(N / V, 32) such pieces of a row.  V > 1: rows are whole aligned pieces.
+// min(N / V, 32) such pieces of a row, which divide the rows and their alignment.
 template <typename T, int V> __device__ __forceinline__ void load_values(const T* p, float* f) {
-    if constexpr (V == 1) f[0] = Elem<T>::to_f32(*p);
-    else unpack16<T>(*reinterpret_cast<const uint4*>(p), f);
+    constexpr int words = V * sizeof(T) / 4;
+    if constexpr (words == 0) {
+        f[0] = __uint_as_float((unsigned)*reinterpret_cast<const unsigned short*>(p) << 16);
+    } else {
+        unsigned w[words];
+        if constexpr (words == 4) { const uint4 q = *reinterpret_cast<const uint4*>(p); w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w; }
+        else if constexpr (words == 2) { const uint2 q = *reinterpret_cast<const uint2*>(p); w[0] = q.x; w[1] = q.y; }
+        else w[0] = *reinterpret_cast<const unsigned*>(p);
+#pragma unroll
+        for (int i = 0; i < words; ++i) {
+            if constexpr (sizeof(T) == 4) f[i] = __uint_as_float(w[i]);
+            else { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+        }
+    }
 }
-template <typename T, int V> __global__ void __launch_bounds__(256) grad_z_sums(const Layer<T> p, T* g, long long g_ld, float* part)
+template <typename T, int V> __device__ __forceinline__ void store_values(T* p, const float* f) {
+    constexpr int words = V * sizeof(T) / 4;
+    if constexpr (words == 0) {
+        *p = Elem<T>::from_f32(f[0]);
+    } else {
+        unsigned w[words];
+#pragma unroll
+        for (int i = 0; i < words; ++i) {
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(f[i]);
+            else { const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]); w[i] = *reinterpret_cast<const unsigned*>(&h); }
+        }
+        if constexpr (words == 4) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        else if constexpr (words == 2) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<unsigned*>(p) = w[0];
+    }
+}
+template <typename T, int V> __global__ void __launch_bounds__(256, 4) grad_z_sums(const Layer<T> p, T* g, long long g_ld, float* part)
 {
     __shared__ float acc[256 * V];
     const int all = p.N / V, across = all < 32 ? all : 32, down = 256 / across;
@@ -124,33 +152,25 @@ template <typename T, int V> __global__ void __launch_bounds__(256) grad_z_sums(
     float sum[V] = {};
     const GaussConst k;
     if (r < down && v < all) {
+        // several rows' loads before the first store
+        constexpr int kBatch = V >= 8 ? 2 : V >= 4 ? 4 : 8;
         const long long step = (long long)gridDim.y * down;
-#pragma unroll 2
-        for (long long row = (long long)blockIdx.y * down + r; row < p.rows; row += step) {
-            const long long at = row * p.N + v * V;
-            float f[V];
-            load_values<T, V>(p.go + at, f);
-            if (p.act != kActNone) {
-                float z[V];
-                load_values<T, V>(p.kept + at, z);
-                times_slope<V>(p.act, k, f, z);
-            }
-            if (g) {
-                T* to = g + row * g_ld + v * V;
-                if constexpr (V == 1) *to = Elem<T>::from_f32(f[0]);
-                else if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to) = make_float4(f[0], f[1], f[2], f[3]);
-                else {
-                    uint32_t w[4];
+        for (long long row = (long long)blockIdx.y * down + r; row < p.rows; row += step * kBatch) {
+            float f[kBatch][V], z[kBatch][V];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
-                        w[e] = *reinterpret_cast<const uint32_t*>(&h);
-                    }
-                    *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-                }
+            for (int u = 0; u < kBatch; ++u) {
+                const long long at = (row + u * step < p.rows ? row + u * step : row) * p.N + v * V;
+                load_values<T, V>(p.go + at, f[u]);
+                if (p.act != kActNone) load_values<T, V>(p.kept + at, z[u]);
             }
 #pragma unroll
-            for (int e = 0; e < V; ++e) sum[e] += f[e];
+            for (int u = 0; u < kBatch; ++u) {
+                if (row + u * step >= p.rows) break;
+                if (p.act != kActNone) times_slope<V>(p.act, k, f[u], z[u]);
+                if (g) store_values<T, V>(g + (row + u * step) * g_ld + v * V, f[u]);
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[e] += f[u][e];
+            }
         }
     }
     pdl_launch_dependents();
@@ -164,6 +184,28 @@ template <typename T, int V> __global__ void __launch_bounds__(256) grad_z_sums(
         float s = 0.f;
         for (int q = 0; q < down; ++q) s += acc[c % V * 256 + q * across + c / V];
         part[(size_t)blockIdx.y * p.N + n] = s;
+    }
+}
+
+// Rows that are not whole 16-byte pieces, copied to rows that are: 64 units of one or two bf16 values to a warp.
+template <typename U> __global__ void __launch_bounds__(256) copy_rows(const U* in, long long in_ld, long long rows, int width, U* out, long long ld)
+{
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, col = blockIdx.x * 64 + lane;
+    const bool left = col < width, right = col + 32 < width;
+    constexpr int kBatch = 8;
+    for (long long row = ((long long)blockIdx.y * 8 + warp) * kBatch; row < rows; row += (long long)gridDim.y * 8 * kBatch) {
+        U a[kBatch], b[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const U* p = in + (row + u < rows ? row + u : row) * in_ld;
+            a[u] = p[left ? col : 0];
+            b[u] = p[right ? col + 32 : 0];
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (row + u < rows && left) out[(row + u) * ld + col] = a[u];
+            if (row + u < rows && right) out[(row + u) * ld + col + 32] = b[u];
+        }
     }
 }
 
