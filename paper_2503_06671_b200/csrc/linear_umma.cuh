@@ -502,14 +502,14 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         Place here{walk(p), 0, Ring{}};
         here.c = here.u.c0;
         if (p.resident) {
-            if (tb && group == 0 && w == 0 && lane == 0) {
+            if (tb && group == 1 && w == 0 && lane == 0) {
                 mbar_bytes(b_full, (unsigned)p.blocks * b_bytes);
                 for (int c = 0; c < p.blocks; ++c) {
                     if (B_MN) for (int m = 0; m < p.bn; m += 64) tma_load_2d(resident + c * b_bytes + m * 128, &map_b, b_full, here.u.j * p.bn + m, c * kBlockC);
                     else tma_load_2d(resident + c * b_bytes, &map_b, b_full, c * kBlockC, here.u.j * p.bn);
                 }
             }
-            for (int c = group; c < p.blocks; c += kFillWarps / kGroupWarps)
+            for (int c = 1 - group; c < p.blocks; c += kFillWarps / kGroupWarps)   // of one block group 0 has none: it has the first tile
                 for (int q = a_chunks; q < a_chunks + b_chunks; ++q) {
                     Chunk<T> x;
                     get(x, q, here.u, c, 0, resident + c * b_bytes);
