@@ -135,7 +135,7 @@ template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long lon
     if (splits) *splits = c.splits;
     const void* out = p.out;
     if constexpr (ROLE == lin::kGradW) out = p.part;
-    p.by_tma = (c.tiles_j == 1 || c.bn % (int)(128 / sizeof(O)) == 0) && whole_pieces(out, p.J, sizeof(O)) && map_of<O>(&mo, out, c.splits, p.I, p.J, p.J, 32) &&
+    const bool out_tma = (c.tiles_j == 1 || c.bn % (int)(128 / sizeof(O)) == 0) && whole_pieces(out, p.J, sizeof(O)) && map_of<O>(&mo, out, c.splits, p.I, p.J, p.J, 32) &&
                abi::aligned(p.bias, 16) && (!p.residual || (whole_pieces(p.residual, p.J, sizeof(T)) && map_of<T>(&mr, p.residual, 1, p.I, p.J, p.J, 32))) &&
                (!p.z || (whole_pieces(p.z, p.J, sizeof(T)) && map_of<T>(&mz, p.z, 1, p.I, p.J, p.J, 32)));
     p.a.pieces = a_pieces && p.a.width % V == 0;
@@ -146,15 +146,17 @@ template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long lon
         kernel<<<(unsigned)c.grid, 32 * warps, c.smem, st>>>(ma, mb, mo, mr, mz, p);
         return launched();
     };
-    auto pick = [&](auto by_tma) {
-        constexpr bool TMA = decltype(by_tma)::value;
+    auto pick = [&](auto in, auto out_by) {
+        constexpr bool TMA = decltype(in)::value, OUT = decltype(out_by)::value;
         if constexpr (sizeof(T) == 4 || ROLE == lin::kGradW)
-            if (runs && (p.blocks + c.splits - 1) / c.splits > um::kRun) return launch(um::product_umma<T, ROLE, TMA, true>, um::all_warps<TMA>);
-        return launch(um::product_umma<T, ROLE, TMA, false>, um::all_warps<TMA>);
+            if (runs && (p.blocks + c.splits - 1) / c.splits > um::kRun) return launch(um::product_umma<T, ROLE, TMA, true, OUT>, um::all_warps<TMA>);
+        return launch(um::product_umma<T, ROLE, TMA, false, OUT>, um::all_warps<TMA>);
     };
+    using yes = std::true_type;
+    using no = std::false_type;
     if constexpr (sizeof(T) == 2)
-        if (tma) return pick(std::true_type{});
-    return pick(std::false_type{});
+        if (tma) return out_tma ? pick(yes{}, yes{}) : pick(yes{}, no{});
+    return out_tma ? pick(no{}, yes{}) : pick(no{}, no{});
 }
 
 // grad_z_sums: pieces of a row to a block, and as many blocks as fill the SMs four times, which leave a partial sum each.

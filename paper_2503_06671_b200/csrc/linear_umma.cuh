@@ -173,7 +173,6 @@ template <typename T> struct Args {
     const T *bias, *residual;
     T *out, *z;
     float* part;                        // kGradW: [splits][I][J]
-    bool by_tma;                        // results leave and residuals come by TMA: rows of whole aligned 16-byte pieces
 };
 
 template <typename T> constexpr int parts_of = sizeof(T) == 4 ? 3 : 1;
@@ -407,7 +406,8 @@ template <int PARTS, int N> __device__ __noinline__ void add_run(uint32_t d, uin
 
 // RUNS: the contraction is longer than kRun blocks, and the result fp32.  Of its own: the code of the running sum, though it did not run,
 // cost 427x240, 64 to 64 channels in fp32 six of 33 us.
-template <typename T, Role ROLE, bool TMA, bool RUNS>
+// OUT: results leave and residuals come by TMA: rows of whole aligned 16-byte pieces.
+template <typename T, Role ROLE, bool TMA, bool RUNS, bool OUT>
 __global__ void __launch_bounds__(32 * all_warps<TMA>, 1)
 product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
              const __grid_constant__ CUtensorMap map_res, const __grid_constant__ CUtensorMap map_z, const __grid_constant__ Args<T> p)
@@ -625,7 +625,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         };
         static_assert(!RUNS || sizeof(O) == 4, "see kRun");
         Walk u = walk(p);
-        if (p.by_tma && has_res && !has_z && lane == 0) fetch(u, 0, 0);
+        if (OUT && has_res && !has_z && lane == 0) fetch(u, 0, 0);
         __syncwarp();
         int turn = 0;                                              // which member of the team has the next unit
         int done = 0;                                              // blocks of c of this tile that are summed; n: runs so far
@@ -652,14 +652,14 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 if (has_bias)
 #pragma unroll
                     for (int v = lane; v < UC; v += 32) st_value(strip + v * 4, v < cols ? Elem<T>::to_f32(ld_value(p.bias + col + v)) : 0.f);
-                if (p.by_tma && lane == 0) bulk_wait_read<0>();    // the slot has been read
+                if (OUT && lane == 0) bulk_wait_read<0>();    // the slot has been read
                 __syncwarp();
                 // Loops that stay loops: a role's code has to stay in the instruction cache beside the others' (unrolled, waiting for
                 // instructions was most of this kernel's time).  z leaves first, through the same slot.
 #pragma unroll 1
                 for (int pass = has_z ? 0 : 1; pass < 2; ++pass) {
                     if (pass == 1 && has_res) {
-                        if (!p.by_tma) {
+                        if constexpr (!OUT) {
                             if constexpr (ROLE == kForward) rows_in<T>(mine, p.residual + (long long)i0 * p.J + col, p.J, rows, cols, lane);
                             __syncwarp();
                         } else {
@@ -694,7 +694,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (pass == 0) {
-                        if (p.by_tma) {
+                        if constexpr (OUT) {
                             if (lane == 0) { tma_store_3d(&map_z, mine, col, i0, 0); bulk_commit(); bulk_wait_read<0>(); }
                         } else {
                             if constexpr (ROLE == kForward) rows_out<T>(mine, p.z + (long long)i0 * p.J + col, p.J, rows, cols, lane);
@@ -704,7 +704,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 }
                 if (!alive) break;
                 ++units;
-                if (p.by_tma) {
+                if constexpr (OUT) {
                     if (lane == 0) {
                         tma_store_3d(&map_out, mine, col, i0, u.split); bulk_commit();
                         if (has_res && !has_z) {
