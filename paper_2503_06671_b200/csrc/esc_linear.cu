@@ -5,6 +5,7 @@
 #include <type_traits>
 
 #include "linear_backward_small.cuh"
+#include "linear_few.cuh"
 
 namespace {
 
@@ -12,6 +13,7 @@ namespace abi = esc::abi;
 namespace lin = esc::linear;
 namespace um = esc::linear::umma;
 namespace sm = esc::linear::small;
+namespace fw = esc::linear::few;
 using namespace esc::rows;
 using bf16 = __nv_bfloat16;
 
@@ -171,6 +173,9 @@ bool copied(long long rows, int K) { return rows * K >= 1 << 20; }
 long long piece_stride(int K) { return (long long)abi::round_up(K, 8); }
 // g lies in rows of whole 16-byte pieces, whatever N is.
 long long g_stride(const Call& c) { return (long long)abi::round_up(c.N, 16 / c.es()); }
+struct FewCut { int across, stretches; };
+FewCut few_cut(const Call& c, int vec);
+constexpr int kFewV = 4;
 struct LinearWs { float *part, *bias; void* g; bf16 *x, *w; size_t bytes; };
 LinearWs carve(void* ws, const Call& c) {
     LinearWs w;
@@ -181,7 +186,9 @@ LinearWs carve(void* ws, const Call& c) {
     const int fused = c.dtype == ESC_BF16 ? sm::plan(rows, c.K, c.N, c.act != ESC_ACT_NONE, abi::sm_count()).grid : 0;   // its blocks leave a part each
     int splits = fused;
     for (int kind = 0; kind < 4; ++kind) splits = std::max(splits, cut(lin::kGradW, c.N, c.K, rows, c.es(), kind & 1, kind & 2).splits);   // whatever the call takes
-    w.part = reinterpret_cast<float*>(take((size_t)splits * c.N * c.K * sizeof(float)));
+    size_t part = (size_t)splits * c.N * c.K;
+    if (rows <= fw::kMostRows) part = std::max(part, (size_t)(std::max(few_cut(c, 1).stretches, few_cut(c, kFewV).stretches) * rows * c.K));
+    w.part = reinterpret_cast<float*>(take(part * sizeof(float)));
     int parts = fused;
     for (int vec = 16 / (int)c.es(); vec >= 1; vec /= 2)
         if (c.N % vec == 0) parts = std::max(parts, bias_cut(c, vec).parts);
@@ -212,14 +219,6 @@ int launch_copy(const um::Source<bf16>& s, bf16* out, long long ld, cudaStream_t
     return s.width % 2 == 0 && s.ld % 2 == 0 && abi::aligned(s.p, 4) ? launch_copy_of<unsigned>(s, out, ld, st) : launch_copy_of<unsigned short>(s, out, ld, st);
 }
 
-template <typename T> int linear_forward_t(const Call& c, const lin::Layer<T>& l, cudaStream_t st) {
-    um::Args<T> p{};
-    p.I = c.rows; p.J = c.N; p.act = c.act;
-    p.a = source<T>(c.x, c.rows, c.K, c.x_stride); p.b = source<T>(c.w, c.N, c.K, c.K);
-    p.bias = l.b; p.residual = l.residual; p.out = l.out; p.z = l.z;
-    return launch_product<T, lin::kForward>(p, c.K, sizeof(T) == 4, st);
-}
-
 // The partial sums of the weights' and the bias' gradients, in one launch.
 template <typename G> int launch_sums(const lin::Parts& w, const lin::Parts& b, void* gw, void* gb, cudaStream_t st) {
     return launch_behind(lin::sum_parts<G>, (unsigned)(lin::sum_blocks(w) + lin::sum_blocks(b)), lin::kSumThreads, st, 0, w, b, static_cast<G*>(gw), static_cast<G*>(gb));
@@ -227,6 +226,86 @@ template <typename G> int launch_sums(const lin::Parts& w, const lin::Parts& b, 
 int sum_to(const lin::Parts& w, const lin::Parts& b, void* gw, void* gb, int grad_dtype, cudaStream_t st) {
     if (w.count + b.count == 0) return ESC_OK;
     return grad_dtype == ESC_F32 ? launch_sums<float>(w, b, gw, gb, st) : launch_sums<bf16>(w, b, gw, gb, st);
+}
+
+// ---- a few rows --------------------------------------------------------------------------------------------------------------
+
+// Whether rows of the tensors that a kernel reads in pieces of `vec` values are whole aligned ones.
+bool even(const Call& c, int vec) {
+    const size_t bytes = vec * c.es();
+    return c.K % vec == 0 && c.x_stride % vec == 0 && abi::aligned(c.x, bytes) && abi::aligned(c.w, bytes);
+}
+template <int R> using rows_is = std::integral_constant<int, R>;
+template <typename F> int for_rows(long long rows, F f) {
+    return rows <= 1 ? f(rows_is<1>{}) : rows <= 2 ? f(rows_is<2>{}) : rows <= 4 ? f(rows_is<4>{}) : rows <= 8 ? f(rows_is<8>{}) : f(rows_is<16>{});
+}
+
+// Whether a call of that many rows is one for those kernels.  They take about 8 us (a backward pass 15) and 0.15 us for a million products,
+// whichever way these lie; the tensor cores' 10 to 13 (21) and 3.5 for each thousand of inputs or, for fp32 and rows that are not whole pieces, 25.
+// Forward: 16 x 8192 to 256 in bf16 11 us here, 29 there; 16 x 1024 to 4096 15 and 10; 8 x 4096 to 4096 in fp32 39 and 116; 4 and 16 x 4001 to
+// 4001 in bf16 56 and 163, 111 there.  Backward: 4 x 1024 to 4096 in bf16 18 and 38, 16 x 1024 to 1024 25 and 23, 4 x 4001 to 4001 113 and 99, in
+// fp32 125 and 232.
+bool is_few(const Call& c, bool backward) {
+    const bool wide = c.dtype == ESC_F32, pieces = even(c, 16 / (int)c.es());
+    if (c.rows > (backward && !wide ? fw::kMostRows / 2 : fw::kMostRows)) return false;
+    const double products = (double)c.rows * c.K * c.N;
+    return (wide && pieces) || products <= (wide || (!backward && !pieces) ? 1 << 27 : 1 << 25);
+}
+
+template <typename T> int forward_few(const Call& c, const lin::Layer<T>& l, cudaStream_t st) {
+    constexpr int V = esc::Elem<T>::kVec;
+    const bool pieces = even(c, V);
+    const int step = 32 * (pieces ? V : 1);
+    // Four outputs to a warp, two where four would leave SMs short of warps (16 x 2050 to 64: 16.8 and 12.5 us; 8 x 4096 to 4096: 39 and 59).
+    // Slices of the inputs: as many as have a step each, until every SM has eight warps (32 warps: 16 x 4096 to 4096 72 -> 84 us).
+    const int columns = c.N < 4 * abi::sm_count() ? 2 : 4;
+    int slices = 1;
+    while (slices < fw::kWarps && slices * step < c.K && (long long)c.N * slices < 8LL * abi::sm_count() * columns) slices *= 2;
+    const int per_block = fw::kWarps / slices * columns;
+    const unsigned blocks = (unsigned)((c.N + per_block - 1) / per_block);
+    return for_rows(c.rows, [&](auto r) {
+        constexpr int R = decltype(r)::value;
+        auto launch = [&](auto kernel) {
+            kernel<<<blocks, 32 * fw::kWarps, 0, st>>>(l, slices);
+            return launched();
+        };
+        if (columns == 2) return pieces ? launch(fw::forward<T, V, R, 2>) : launch(fw::forward<T, 1, R, 2>);
+        return pieces ? launch(fw::forward<T, V, R, 4>) : launch(fw::forward<T, 1, R, 4>);
+    });
+}
+
+// The backward pass: tiles of 32 V inputs, and stretches of outputs, so many that the SMs have 16 warps each, of 8 at least, and so long that
+// the partial sums of gx are no more than half of w's values.
+FewCut few_cut(const Call& c, int vec) {
+    const int across = (c.K + 32 * vec - 1) / (32 * vec);
+    return {across, (int)std::max(1LL, std::min(c.N / std::max(8LL, 2 * c.rows), (16LL * abi::sm_count() + across - 1) / across))};
+}
+template <typename T, typename G> int backward_few_to(const Call& c, const lin::Layer<T>& l, G* gw, G* gb, float* part, cudaStream_t st) {
+    const int vec = even(c, kFewV) && abi::aligned(gw, kFewV * sizeof(G)) ? kFewV : 1;
+    const FewCut d = few_cut(c, vec);
+    const unsigned blocks = (unsigned)((d.across * (long long)d.stretches + 3) / 4);
+    ESC_TRY(for_rows(c.rows, [&](auto r) {
+        constexpr int R = decltype(r)::value;
+        if (vec == kFewV) fw::backward<T, G, kFewV, R><<<blocks, 128, 0, st>>>(l, d.across, d.stretches, part, gw, gb);
+        else fw::backward<T, G, 1, R><<<blocks, 128, 0, st>>>(l, d.across, d.stretches, part, gw, gb);
+        return launched();
+    }));
+    if (!l.gx) return ESC_OK;
+    const lin::Parts px{part, d.stretches, c.rows * c.K}, none{nullptr, 0, 0};
+    return launch_sums<T>(px, none, l.gx, nullptr, st);
+}
+template <typename T> int backward_few(const Call& c, const lin::Layer<T>& l, void* gw, void* gb, int grad_dtype, float* part, cudaStream_t st) {
+    return grad_dtype == ESC_F32 ? backward_few_to<T, float>(c, l, static_cast<float*>(gw), static_cast<float*>(gb), part, st)
+                                 : backward_few_to<T, bf16>(c, l, static_cast<bf16*>(gw), static_cast<bf16*>(gb), part, st);
+}
+
+template <typename T> int linear_forward_t(const Call& c, const lin::Layer<T>& l, cudaStream_t st) {
+    if (is_few(c, false)) return forward_few<T>(c, l, st);
+    um::Args<T> p{};
+    p.I = c.rows; p.J = c.N; p.act = c.act;
+    p.a = source<T>(c.x, c.rows, c.K, c.x_stride); p.b = source<T>(c.w, c.N, c.K, c.K);
+    p.bias = l.b; p.residual = l.residual; p.out = l.out; p.z = l.z;
+    return launch_product<T, lin::kForward>(p, c.K, sizeof(T) == 4, st);
 }
 
 // A small bf16 layer in one pass; kNotThis: it is not one, or its tensors are not rows of whole 16-byte pieces.
@@ -250,6 +329,7 @@ int backward_small(const Call& c, const lin::Layer<bf16>& l, void* gw, void* gb,
 
 template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& l, void* gw, void* gb, int grad_dtype, const LinearWs& w, cudaStream_t st) {
     constexpr int V = esc::Elem<T>::kVec;
+    if (is_few(c, true)) return backward_few<T>(c, l, gw, gb, grad_dtype, w.part, st);
     if constexpr (sizeof(T) == 2) {
         const int rc = backward_small(c, l, gw, gb, grad_dtype, w, st);
         if (rc != kNotThis) return rc;
