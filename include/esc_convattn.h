@@ -527,7 +527,8 @@ int esc_layer_norm_backward(const void* x, long long x_stride, const void* weigh
  * Arithmetic: the products run on the tensor cores.  bf16 values are multiplied exactly and added in fp32; fp32 values are three bf16 parts each
  * (24 bits), of whose products those above 2^-26 are taken, and sums end after 512 values and are added in fp32: about as far from
  * the exact result as fp32 multiply-adds.  An fp32 value that is not finite (or 3.39e38 or more) makes its row, in a gradient of the weights
- * its column, NaN; with bf16 it gives what the sums give.  Each output is rounded once.
+ * its column, NaN; with bf16 it gives what the sums give.  Up to 16 rows may be multiplied and added in fp32 instead.  Each output is
+ * rounded once.
  */
 enum { ESC_ACT_NONE = 0, ESC_ACT_RELU = 1, ESC_ACT_GELU = 2 };
 int esc_linear_forward(const void* x, long long x_stride, const void* weight, const void* bias, int activation,
