@@ -162,10 +162,12 @@ template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long lon
 }
 
 // grad_z_sums: pieces of a row to a block, and as many blocks as fill the SMs four times, which leave a partial sum each.
-struct BiasCut { int across, parts; };
+struct BiasCut { int blocks, across, parts; };
 BiasCut bias_cut(const Call& c, int vec) {
-    const int all = c.N / vec, wide = std::min(all, 32), across = (all + wide - 1) / wide;
-    return {across, (int)std::max(1LL, std::min((4LL * abi::sm_count() + across - 1) / across, (c.rows + 31) / 32))};
+    // 32 pieces at most, whole lines of 128 bytes where rows have them, and blocks alike (48 pieces: 24 and 24)
+    const int all = c.N / vec, line = std::max(1, (int)(128 / (vec * c.es()))), blocks = (all + 31) / 32;
+    const int across = blocks == 1 ? all : std::min(32, (int)abi::round_up((all + blocks - 1) / blocks, line));
+    return {blocks, across, (int)std::max(1LL, std::min(((long long)lin::kSumBlocks * abi::sm_count() + blocks - 1) / blocks, (c.rows + 31) / 32))};
 }
 // A copy of ragged bf16 rows to rows of whole pieces costs two passes over them and a launch; a product that takes them as they are runs at a
 // third of the speed: 70640 x 906 x 441 backward 595 us as they are.  Below a million values the launch costs more.
@@ -347,12 +349,12 @@ template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& 
         int vec = V;
         while (!fits(vec)) vec /= 2;
         const BiasCut b = bias_cut(c, vec);
-        const dim3 grid(b.across, b.parts);
+        const dim3 grid(b.blocks, b.parts);
         float* sums = gb ? w.bias : nullptr;
-        if (vec == 8) { if constexpr (V == 8) lin::grad_z_sums<T, 8><<<grid, 256, 0, st>>>(l, to, ld, sums); }
-        else if (vec == 4) lin::grad_z_sums<T, 4><<<grid, 256, 0, st>>>(l, to, ld, sums);
-        else if (vec == 2) lin::grad_z_sums<T, 2><<<grid, 256, 0, st>>>(l, to, ld, sums);
-        else lin::grad_z_sums<T, 1><<<grid, 256, 0, st>>>(l, to, ld, sums);
+        if (vec == 8) { if constexpr (V == 8) lin::grad_z_sums<T, 8><<<grid, 256, 0, st>>>(l, to, ld, sums, b.across); }
+        else if (vec == 4) lin::grad_z_sums<T, 4><<<grid, 256, 0, st>>>(l, to, ld, sums, b.across);
+        else if (vec == 2) lin::grad_z_sums<T, 2><<<grid, 256, 0, st>>>(l, to, ld, sums, b.across);
+        else lin::grad_z_sums<T, 1><<<grid, 256, 0, st>>>(l, to, ld, sums, b.across);
         ESC_TRY(launched());
         if (gb) pb = lin::Parts{w.bias, b.parts, c.N};
         if (acts) g = source<T>(to, c.rows, c.N, ld);

@@ -109,9 +109,11 @@ template <typename T> struct Layer {
 
 enum Role { kForward, kGradX, kGradW };
 
+constexpr int kSumBlocks = 4;                                      // of grad_z_sums, of an SM
+
 // g = go act'(z) and its column sums, as far as they are asked for: g [rows, g_ld] of the type (rounded: the operand that two products
 // read), part [gridDim.y][N] fp32 sums of the unrounded g.  A thread has V neighbouring columns and every so many rows; a block has
-// min(N / V, 32) such pieces of a row, which divide the rows and their alignment.
+// `across` such pieces of a row; they divide the rows and their alignment.
 template <typename T, int V> __device__ __forceinline__ void load_values(const T* p, float* f) {
     constexpr int words = V * sizeof(T) / 4;
     if constexpr (words == 0) {
@@ -144,18 +146,18 @@ template <typename T, int V> __device__ __forceinline__ void store_values(T* p, 
         else *reinterpret_cast<unsigned*>(p) = w[0];
     }
 }
-template <typename T, int V> __global__ void __launch_bounds__(256, 4) grad_z_sums(const Layer<T> p, T* g, long long g_ld, float* part)
+template <typename T, int V> __global__ void __launch_bounds__(256, kSumBlocks) grad_z_sums(const Layer<T> p, T* g, long long g_ld, float* part, int across)
 {
     __shared__ float acc[256 * V];
-    const int all = p.N / V, across = all < 32 ? all : 32, down = 256 / across;
+    const int all = p.N / V, down = 256 / across;
     const int col = threadIdx.x % across, v = blockIdx.x * across + col, r = threadIdx.x / across;
     float sum[V] = {};
     const GaussConst k;
     if (r < down && v < all) {
         // several rows' loads before the first store
         constexpr int kBatch = V >= 8 ? 2 : V >= 4 ? 4 : 8;
-        const long long step = (long long)gridDim.y * down;
-        for (long long row = (long long)blockIdx.y * down + r; row < p.rows; row += step * kBatch) {
+        const long long step = down;
+        for (long long row = (long long)blockIdx.y * down * kBatch + r; row < p.rows; row += step * kBatch * gridDim.y) {
             float f[kBatch][V], z[kBatch][V];
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
