@@ -185,7 +185,8 @@ LinearWs carve(void* ws, const Call& c) {
     size_t off = 0;
     auto take = [&](size_t bytes) { char* p = base + off; off += abi::round_up(bytes, 256); return p; };
     const long long rows = std::max(c.rows, 1LL);
-    const int fused = c.dtype == ESC_BF16 ? sm::plan(rows, c.K, c.N, c.act != ESC_ACT_NONE, abi::sm_count()).grid : 0;   // its blocks leave a part each
+    const sm::Plan small = sm::plan(rows, c.K, c.N, c.act != ESC_ACT_NONE, false, abi::sm_count());   // its blocks, as many with fp32 gradients, leave a part each
+    const int fused = c.dtype == ESC_BF16 && small.stages > 0 ? small.grid : 0;
     int splits = fused;
     for (int kind = 0; kind < 4; ++kind) splits = std::max(splits, cut(lin::kGradW, c.N, c.K, rows, c.es(), kind & 1, kind & 2).splits);   // whatever the call takes
     size_t part = (size_t)splits * c.N * c.K;
@@ -314,8 +315,8 @@ template <typename T> int linear_forward_t(const Call& c, const lin::Layer<T>& l
 constexpr int kNotThis = -1;
 int backward_small(const Call& c, const lin::Layer<bf16>& l, void* gw, void* gb, int grad_dtype, const LinearWs& w, cudaStream_t st) {
     const bool act = c.act != ESC_ACT_NONE;
-    const sm::Plan d = sm::plan(c.rows, c.K, c.N, act, abi::sm_count());
-    if (d.stages == 0 || (!l.gx && !gw) || (gw && grad_dtype == ESC_F32)) return kNotThis;   // its sums run over all of a block's rows (see kRun)
+    const sm::Plan d = sm::plan(c.rows, c.K, c.N, act, gw && grad_dtype == ESC_F32, abi::sm_count());
+    if (d.stages == 0 || (!l.gx && !gw)) return kNotThis;
     if (!whole_pieces(l.go, c.N, 2) || !whole_pieces(c.x, c.x_stride, 2) || !whole_pieces(c.w, c.K, 2) || (act && !whole_pieces(l.kept, c.N, 2)) ||
         (l.gx && !whole_pieces(l.gx, c.K, 2))) return kNotThis;
     CUtensorMap go{}, z{}, x{}, wm{}, gx{}, part{};
@@ -323,8 +324,9 @@ int backward_small(const Call& c, const lin::Layer<bf16>& l, void* gw, void* gb,
         (act && !map_of<bf16>(&z, l.kept, 0, c.rows, c.N, c.N, sm::kRows)) || (l.gx && !map_of<bf16>(&gx, l.gx, 1, c.rows, c.K, c.K, 32)) ||
         (gw && !map_of<float>(&part, w.part, d.grid, c.N, c.K, c.K, 32))) return kNotThis;
     const sm::Args p{(int)c.rows, c.N, c.K, d.tiles, c.act, d.stages, d.nb, d.kb, d.gx_buffers, l.gx != nullptr, gw != nullptr, gb != nullptr, w.bias};
-    ESC_ABI_CUDA(cudaFuncSetAttribute(sm::backward, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)um::kMostSmem));   // the same for every call
-    sm::backward<<<(unsigned)d.grid, sm::kThreads, d.smem, st>>>(go, z, x, wm, gx, part, p);
+    const auto kernel = d.runs ? sm::backward<true> : sm::backward<false>;
+    ESC_ABI_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)um::kMostSmem));   // the same for every call
+    kernel<<<(unsigned)d.grid, sm::kThreads, d.smem, st>>>(go, z, x, wm, gx, part, p);
     ESC_TRY(launched());
     return sum_to({w.part, d.grid, gw ? (long long)c.N * c.K : 0}, {w.bias, d.grid, gb ? c.N : 0}, gw, gb, grad_dtype, st);
 }

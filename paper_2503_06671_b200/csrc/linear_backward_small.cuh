@@ -8,7 +8,7 @@
 // as contraction (K-major) for gx, with the columns as rows of the result and 128 rows as contraction (MN-major) for gw.  w stays in shared
 // memory and the sums of gw in tensor memory for the life of the block (N / 128 x K columns beside one or two tiles of gx); each block leaves
 // one partial sum of gw and gb.  64 x 64x64 rows, 64 to 128 channels, GELU: 51 us (3.9 TB/s), where three
-// kernels that wrote and read g took 96.  What bounds it: the act' of 33 million values on eight warps, and latency of three boxes a tile.
+// kernels that wrote and read g took 96, and as long with fp32 gradients (87 in three kernels).  What bounds it: the act' of 33 million values on eight warps, and latency of three boxes a tile.
 #pragma once
 #include "linear_umma.cuh"
 
@@ -20,6 +20,7 @@ using bf16 = __nv_bfloat16;
 constexpr int kRows = 128, kBox = kRows * 128, kActWarps = 8, kOutWarps = 4, kFirstAct = 4, kFirstOut = kFirstAct + kActWarps, kThreads = 32 * (kFirstOut + kOutWarps);
 constexpr int kMostBoxes = 4;                                      // of go: N up to 256
 constexpr int kMostStages = 4;
+constexpr int kRunTiles = kRun * kBlockC / kRows;                  // tiles after which a sum of gw ends, where gw is fp32
 
 struct Args {
     int rows, N, K, tiles, act, stages;
@@ -33,7 +34,8 @@ __device__ __forceinline__ unsigned long long desc(uint32_t addr, uint32_t lbo) 
     return (unsigned long long)((addr >> 4) & 0x3FFFu) | ((unsigned long long)(lbo >> 4) << 16) | ((unsigned long long)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
-__global__ void __launch_bounds__(kThreads, 1)
+// RUNS: gw is fp32 and a block has more than kRunTiles tiles: their sum is added to a running one beside it in tensor memory (see kRun).
+template <bool RUNS> __global__ void __launch_bounds__(kThreads, 1)
 backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUtensorMap map_z, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
          const __grid_constant__ CUtensorMap map_gx, const __grid_constant__ CUtensorMap map_part, const __grid_constant__ Args p)
 {
@@ -45,14 +47,15 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
     const uint32_t x_at = p.nb * kBox, z_at = x_at + p.kb * kBox, stage_bytes = z_at + (has_act ? p.nb * kBox : 0);
     const uint32_t w_at = base + p.stages * stage_bytes, w_block = p.kb * 64 * 128, staging = w_at + p.nb * w_block;
     const uint32_t full = staging + kOutWarps * kSlotBytes, ready = full + 8 * kMostStages, empty = ready + 8 * kMostStages, gx_full = empty + 8 * kMostStages,
-                   gx_empty = gx_full + 16, w_full = gx_empty + 16, gw_done = w_full + 8, gb_done = gw_done + 8, slot = gb_done + 8,
-                   strip = slot + 24;                              // [kActWarps][256] floats: columns of g
+                   gx_empty = gx_full + 16, w_full = gx_empty + 16, gw_done = w_full + 8, gb_done = gw_done + 8, gw_taken = gb_done + 8, slot = gw_taken + 8,
+                   strip = slot + 16;                              // [kActWarps][256] floats: columns of g
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(ready + 8 * s, kActWarps); mbar_init(empty + 8 * s, 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(gx_full + 8 * s, 1); mbar_init(gx_empty + 8 * s, kOutWarps); }
         mbar_init(w_full, 1);
         mbar_init(gw_done, 1);
         mbar_init(gb_done, kActWarps);
+        mbar_init(gw_taken, kOutWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) {
@@ -110,15 +113,22 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
                 }
                 commit(gx_full + 8 * buf);
             }
+            const int in_run = RUNS ? n % kRunTiles : n;
             if (p.gw) {
+                if (RUNS && n > 0 && in_run == 0) {                // the sum of the run before has been read
+                    alive = wait_warp(gw_taken, (unsigned)(n / kRunTiles - 1) & 1, 0xB1000000u | (unsigned)n);
+                    if (!alive) break;
+                    fence_after();
+                }
 #pragma unroll 1
                 for (int m = 0; m < p.nb; m += 2) {
                     const unsigned long long a = desc(at + m * kBox, kBox), b = desc(at + x_at, kBox);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) mma(gw_at + m / 2 * columns, a + k * 128, b + k * 128, idesc_w, n > 0 || k > 0);
+                    for (int k = 0; k < 8; ++k) mma(gw_at + m / 2 * columns, a + k * 128, b + k * 128, idesc_w, in_run > 0 || k > 0);
                 }
             }
             commit(empty + 8 * r.s);
+            if (RUNS && in_run == kRunTiles - 1 && t + gridDim.x < p.tiles) commit(gw_done);
         }
         commit(gw_done);
     } else if (warp >= kFirstAct && warp < kFirstOut) {
@@ -182,9 +192,11 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
         // ---- gx of each tile, gw at the end: 128 bytes of 32 rows at a time ---------------------------------------------------
         const int e = warp - kFirstOut, quarter = warp & 3, member = e / 4;
         const uint32_t mine = staging + e * kSlotBytes, lane_at = lane * 128 + ((lane & 7) << 4), lanes = (uint32_t)(quarter * 32) << 16;
-        if (p.gx) {
-            int turn = 0;
-            for (int t = blockIdx.x; t < p.tiles && alive; t += gridDim.x, ++n) {
+        const int across = (int)(columns / 32), units = (p.nb + 1) / 2 * across;
+        const uint32_t run_at = gw_at + (p.nb + 1) / 2 * columns;  // the running sum
+        int turn = 0, runs = 0;
+        for (int t = blockIdx.x; t < p.tiles && alive; t += gridDim.x, ++n) {
+            if (p.gx) {
                 const int buf = p.gx_buffers == 2 ? n & 1 : 0, use = p.gx_buffers == 2 ? n >> 1 : n;
                 alive = wait_warp(gx_full + 8 * buf, use & 1, 0x61000000u | (unsigned)n);
                 if (!alive) break;
@@ -210,11 +222,20 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
                 fence_before();
                 if (lane == 0) mbar_arrive(gx_empty + 8 * buf);
             }
+            if (RUNS && p.gw && n % kRunTiles == kRunTiles - 1 && t + gridDim.x < p.tiles) {
+                alive = wait_warp(gw_done, (unsigned)runs & 1, 0x82000000u | (unsigned)runs);
+                if (!alive) break;
+                fence_after();
+                for (int v = member; v < units; v += kOutWarps / 4) add_run<1, 16>(gw_at + lanes + v * 32, run_at + lanes + v * 32, runs > 0);
+                ++runs;
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(gw_taken);
+            }
         }
-        if (p.gw && alive) alive = wait_warp(gw_done, 0, 0x81000000u);
+        if (p.gw && alive) alive = wait_warp(gw_done, (unsigned)runs & 1, 0x81000000u);
         if (p.gw && alive) {
             fence_after();
-            const int across = (int)(columns / 32), units = (p.nb + 1) / 2 * across;
             for (int v = member; v < units; v += kOutWarps / 4) {
                 const int m = v / across, c = v - m * across, n0 = m * 128 + quarter * 32;
                 if (n0 >= p.N || c * 32 >= p.K) continue;
@@ -223,8 +244,7 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
 #pragma unroll 1
                 for (int q = 0; q < 8; q += 2) {
                     float f[8];
-                    tmem_ld(gw_at + lanes + m * columns + c * 32 + q * 4, f);
-                    tmem_wait_ld();
+                    sums<1>(f, gw_at + lanes + v * 32 + q * 4, run_at + lanes + v * 32 + q * 4, RUNS && runs > 0);
                     st_shared(mine + (lane_at ^ (uint32_t)(q << 4)), pack16<float>(f));
                     st_shared(mine + (lane_at ^ (uint32_t)((q + 1) << 4)), pack16<float>(f + 4));
                 }
@@ -245,17 +265,18 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
     }
 }
 
-// Sizes: whether a layer is one of these, and how its block is laid out (stages 0: it is not).
-struct Plan { int stages, gx_buffers, nb, kb, tiles, grid; size_t smem; };
-inline Plan plan(long long rows, int K, int N, bool act, int sms) {
+// Sizes: whether a layer is one of these, and how its block is laid out (stages 0: it is not).  wide: gw is fp32.
+struct Plan { int stages, gx_buffers, nb, kb, tiles, grid; bool runs; size_t smem; };
+inline Plan plan(long long rows, int K, int N, bool act, bool wide, int sms) {
     Plan d{};
     if (N > 64 * kMostBoxes || K > 256 || rows < 1 || rows > 0x7fffffffLL - kRows) return d;
     d.nb = (N + 63) / 64; d.kb = (K + 63) / 64;
-    const int gw_columns = (d.nb + 1) / 2 * d.kb * 64;
-    d.gx_buffers = gw_columns + 2 * d.kb * 64 <= 512 ? 2 : 1;
-    if (gw_columns + d.kb * 64 > 512) return d;
     d.tiles = (int)((rows + kRows - 1) / kRows);
     d.grid = d.tiles < sms ? d.tiles : sms;
+    d.runs = wide && (d.tiles + d.grid - 1) / d.grid > kRunTiles;
+    const int gw_columns = (d.nb + 1) / 2 * d.kb * 64 * (d.runs ? 2 : 1);
+    d.gx_buffers = gw_columns + 2 * d.kb * 64 <= 512 ? 2 : 1;
+    if (gw_columns + d.kb * 64 > 512) return d;
     const size_t stage = (size_t)(d.nb * (act ? 2 : 1) + d.kb) * kBox, fixed = (size_t)d.nb * d.kb * 64 * 128 + kOutWarps * kSlotBytes + 1024 + kActWarps * 1024;
     if (fixed + stage > kMostSmem) return d;
     size_t stages = (kMostSmem - fixed) / stage;
