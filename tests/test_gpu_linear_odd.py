@@ -1,0 +1,36 @@
+"""Linear layers whose rows start anywhere and lie between values that are not numbers, against their formulas in 64 bits."""
+import pytest
+import torch
+
+from tests.test_gpu_linear import backward, forward, make, pkg   # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def among_nans(t, shift, pad=0):
+    """The same values `shift` behind a 16-byte border, rows `pad` values further apart, NaN all around."""
+    rows, width = t.shape if t.dim() == 2 else (1, t.numel())
+    flat = torch.full((shift + rows * (width + pad) + 16,), float("nan"), dtype=t.dtype, device="cuda")
+    new = flat[shift:shift + rows * (width + pad)].view(rows, width + pad)[:, :width]
+    new.copy_(t.view(rows, width))
+    return new if t.dim() == 2 else new.view(-1)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("shift", range(8))
+@pytest.mark.parametrize("rows,K,N,pad", [(20, 1, 3, 0), (40, 7, 9, 2), (130, 9, 63, 1), (33, 61, 65, 3), (200, 64, 64, 5), (150, 65, 129, 0), (70, 250, 777, 6), (300, 131, 8, 7)])
+def test_rows_anywhere(pkg, dtype, shift, rows, K, N, pad):   # noqa: F811
+    s = make(rows, K, N, dtype)
+    s = {k: among_nans(t, shift, pad if k == "x" else 0) for k, t in s.items()}
+    forward(pkg, s, "gelu")
+    backward(pkg, s, "relu")
+    backward(pkg, s, "none", torch.float32)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("which", ["x", "w", "go", "z", "residual", "b"])
+def test_one_tensor_is_not_aligned(pkg, dtype, which):   # noqa: F811
+    s = make(400, 72, 136, dtype)
+    s[which] = among_nans(s[which], 3)
+    forward(pkg, s, "relu")
+    backward(pkg, s, "gelu")
