@@ -133,6 +133,7 @@ template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long lon
     if (c.bn == 0) return ESC_ERR_UNSUPPORTED;                     // more tiles than a launch can count
     p.tiles_i = c.tiles_i; p.tiles_j = c.tiles_j; p.bn = c.bn; p.splits = c.splits; p.stages = c.stages; p.resident = c.resident;
     p.blocks = (int)((depth + um::kBlockC - 1) / um::kBlockC);
+    p.per_split = p.blocks / c.splits; p.longer = p.blocks % c.splits;
     p.units = (unsigned)((long long)c.tiles_i * c.tiles_j * c.splits);
     if (splits) *splits = c.splits;
     const void* out = p.out;

@@ -188,7 +188,8 @@ template <typename T> struct Source {
 
 template <typename T> struct Args {
     long long I;
-    int J, tiles_i, tiles_j, bn, blocks, splits, stages;   // blocks: of c
+    int J, tiles_i, tiles_j, bn, blocks, stages;           // blocks: of c
+    int splits, per_split, longer;      // a split has per_split blocks, the first `longer` of them one more
     bool resident;                      // B stays in shared memory; a block keeps its tile of j
     unsigned units;
     Source<T> a, b;
@@ -219,10 +220,10 @@ template <typename T> __device__ __forceinline__ void place(Walk& w, const Args<
     if (p.resident) { w.i = (int)w.t; return; }
     const unsigned r = p.tiles_j == 1 ? w.t : w.t / (unsigned)p.tiles_j;
     w.j = (int)(w.t - r * (unsigned)p.tiles_j);
-    w.split = (int)(r / (unsigned)p.tiles_i);
+    w.split = p.splits == 1 ? 0 : (int)(r / (unsigned)p.tiles_i);
     w.i = (int)(r - (unsigned)w.split * (unsigned)p.tiles_i);
-    w.c0 = (int)((long long)p.blocks * w.split / p.splits);
-    w.c1 = (int)((long long)p.blocks * (w.split + 1) / p.splits);
+    w.c0 = w.split * p.per_split + min(w.split, p.longer);
+    w.c1 = w.c0 + p.per_split + (w.split < p.longer);
 }
 template <typename T> __device__ __forceinline__ Walk walk(const Args<T>& p) {
     Walk w{blockIdx.x, gridDim.x, 0, 0, 0, 0, p.blocks, false};
