@@ -61,13 +61,12 @@ struct Cut {
     bool resident;
     size_t smem;
 };
-constexpr size_t kBarBytes = 1024 + um::kMostEpi * 256;        // barriers and strips
 constexpr double kLoadRate = 35, kStoreRate = 20;   // bytes per cycle of one SM: from L2 into its ring, to memory
 Cut cut(lin::Role role, long long I, int J, long long depth, size_t es, bool tma, bool runs) {
-    const int sms = abi::sm_count(), step = role == lin::kForward ? 16 : 64, most = es == 4 ? um::most_columns<float> : runs ? um::kMostRunColumns : um::most_columns<bf16>;
+    const int sms = abi::sm_count(), step = role == lin::kForward ? 16 : 64, most = es == 4 ? um::most_columns<float> : um::most_columns<bf16>, most_run = es == 4 ? um::most_run_columns<float> : um::most_run_columns<bf16>;
     const int parts = es == 4 ? 3 : 1, products = es == 4 ? 6 : 1;
     const long long blocks = (depth + um::kBlockC - 1) / um::kBlockC, tiles_i = (I + um::kBlockI - 1) / um::kBlockI;
-    const size_t out_es = role == lin::kGradW ? 4 : es, slot_bytes = (size_t)(tma ? um::epi_warps<true> : um::epi_warps<false>) * um::kSlotBytes;
+    const size_t out_es = role == lin::kGradW ? 4 : es, epi = tma ? um::epi_warps<true> : um::epi_warps<false>;
     const int unit = (int)(128 / out_es);                          // columns that leave together
     Cut best{};
     double least = 1e300;
@@ -75,7 +74,7 @@ Cut cut(lin::Role role, long long I, int J, long long depth, size_t es, bool tma
         const long long tiles_j = ((long long)J + bn - 1) / bn;
         if (tiles_j > 1 && bn > unit && bn % unit != 0) continue;
         // w stays where it leaves room for a ring of rows and a block has several tiles
-        const size_t b_bytes = (size_t)bn * 128 * parts, a_bytes = (size_t)um::kABytes * parts, fixed = slot_bytes + kBarBytes;
+        const size_t b_bytes = (size_t)bn * 128 * parts, a_bytes = (size_t)um::kABytes * parts, fixed = epi * (um::kSlotBytes + 256) + 1024;   // with a strip of an epilogue warp, and the barriers
         const bool resident = role != lin::kGradW && blocks * b_bytes + fixed + 3 * a_bytes <= um::kMostSmem && tiles_j <= sms && tiles_i * tiles_j >= 2LL * sms;
         const size_t kept = resident ? blocks * b_bytes : 0, stage = a_bytes + (resident ? 0 : b_bytes);
         const int stages = (int)std::min<long long>(um::kMaxStages, ((long long)um::kMostSmem - (long long)(fixed + kept)) / (long long)stage);
@@ -87,6 +86,7 @@ Cut cut(lin::Role role, long long I, int J, long long depth, size_t es, bool tma
             const long long splits = fill == 0 ? 1 : std::min<long long>(blocks, (long long)fill * sms / (tiles_i * tiles_j));
             const long long units = tiles_i * tiles_j * splits, waves = (units + sms - 1) / sms;
             if (splits < 1 || units > 0x7fffffffLL) continue;
+            if (runs && bn > most_run && (blocks + splits - 1) / splits > um::kRun) continue;
             const double body = (double)((blocks + splits - 1) / splits) * std::max(mma, load);
             double cost = (double)waves * (std::max(body, store) + 200) + std::min(body, store) + 1500;
             if (role == lin::kGradW) cost += 2.0 * splits * I * J * 4 / (kStoreRate * sms);

@@ -206,8 +206,8 @@ template <typename T> constexpr int parts_of = sizeof(T) == 4 ? 3 : 1;
 // result is fp32 a sum therefore ends after kRun blocks of c and is added, rounded to nearest, to a running sum beside it in tensor memory
 // (4096 values: 4.4e-6 -> below 1e-6 of the result's norm; 16 x 8000: 9.1e-6 -> 3e-7).  That takes columns, so tiles are narrower.
 constexpr int kRun = 8;
-template <typename T> constexpr int most_columns = sizeof(T) == 4 ? 96 : 256;
-constexpr int kMostRunColumns = 128;                               // of bf16 with such runs
+template <typename T> constexpr int most_columns = sizeof(T) == 4 ? 128 : 256;
+template <typename T> constexpr int most_run_columns = sizeof(T) == 4 ? 96 : 128;
 
 // A block's tiles, in the order of its loops.  32-bit arithmetic: a warp that does little else spends a tile's time on divisions.
 struct Walk {
@@ -245,9 +245,10 @@ __device__ __forceinline__ void st_shared(uint32_t at, uint4 v) { asm volatile("
 // The three bf16 parts of two values; the differences are exact.
 __device__ __forceinline__ void split(float a, float b, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
     hi = pack(a, b);
-    a -= __uint_as_float(hi << 16); b -= __uint_as_float(hi & 0xffff0000u);
+    const F2 minus = f2(-1.f, -1.f);
+    un2(fma2(f2(__uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u)), minus, f2(a, b)), a, b);
     mid = pack(a, b);
-    a -= __uint_as_float(mid << 16); b -= __uint_as_float(mid & 0xffff0000u);
+    un2(fma2(f2(__uint_as_float(mid << 16), __uint_as_float(mid & 0xffff0000u)), minus, f2(a, b)), a, b);
     lo = pack(a, b);
 }
 
@@ -715,7 +716,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 const bool ours = turn == member && c * UC < wide && rows > 0;
                 turn = turn + 1 == TEAM ? 0 : turn + 1;
                 if (!ours) continue;
-                const uint32_t sum_at = tmem + ((uint32_t)(quarter * 32) << 16) + (PARTS == 3 ? most_columns<T> + c * (kTmemBuffer / 2) : kMostRunColumns + c * UC);
+                const uint32_t sum_at = tmem + ((uint32_t)(quarter * 32) << 16) + most_run_columns<T> + c * (PARTS == 3 ? kTmemBuffer / 2 : UC);
                 if (RUNS && !last) {                              // the same warp has this unit in every run
                     add_run<PARTS, 2 * V>(d + c * UC, sum_at, begun);
                     continue;
