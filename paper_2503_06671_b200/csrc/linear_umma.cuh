@@ -684,7 +684,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         unsigned units = 0;                                        // of this warp so far
         // the residual of this warp's next unit, from unit c of tile u on, into its slot; `turn` is whose c is
         auto fetch = [&](Walk u, int c, int turn) {
-            for (; u.live; next(u, p), c = 0) {
+            for (; u.live; next(u, p), c = 0, turn = RUNS ? 0 : turn) {
                 const int i0 = u.i * kBlockI + quarter * 32, j0 = u.j * p.bn, wide = min(p.J - j0, p.bn);
                 for (; c < per_tile; ++c) {
                     const bool ours = turn == member && c * UC < wide && i0 < p.I;
@@ -711,7 +711,6 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             done = last ? 0 : done + kRun;
             const int i0 = u.i * kBlockI + quarter * 32, j0 = u.j * p.bn, wide = min(p.J - j0, p.bn), rows = (int)min(p.I - i0, 32LL);
             const uint32_t d = tmem + buf * kTmemBuffer + ((uint32_t)(quarter * 32) << 16);
-            const int tile_turn = turn;
             for (int c = 0; c < per_tile; ++c) {
                 const bool ours = turn == member && c * UC < wide && rows > 0;
                 turn = turn + 1 == TEAM ? 0 : turn + 1;
@@ -797,7 +796,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             __syncwarp();
             if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
             if (last) next(u, p);
-            else turn = tile_turn;
+            if (RUNS) turn = 0;                                    // a unit's running sum belongs to one warp, in every tile
         }
         if (lane == 0) bulk_wait_read<0>();                        // shared memory outlives what is read from it
     }
