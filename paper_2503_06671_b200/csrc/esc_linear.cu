@@ -58,7 +58,7 @@ template <typename T> lin::Layer<T> layer_of(const Call& c) {
 // What a product is cut into (`runs`: its result is fp32).  Times in cycles of an SM, from the rates below; the cheapest width of a tile and number of runs of rows.
 struct Cut {
     int tiles_i, tiles_j, bn, splits, stages, grid;
-    bool resident;
+    bool resident, single;
     size_t smem;
 };
 constexpr double kLoadRate = 35, kStoreRate = 20;   // bytes per cycle of one SM: from L2 into its ring, to memory
@@ -86,13 +86,16 @@ Cut cut(lin::Role role, long long I, int J, long long depth, size_t es, bool tma
             const long long splits = fill == 0 ? 1 : std::min<long long>(blocks, (long long)fill * sms / (tiles_i * tiles_j));
             const long long units = tiles_i * tiles_j * splits, waves = (units + sms - 1) / sms;
             if (splits < 1 || units > 0x7fffffffLL) continue;
-            if (runs && bn > most_run && (blocks + splits - 1) / splits > um::kRun) continue;
-            const double body = (double)((blocks + splits - 1) / splits) * std::max(mma, load);
+            // runs of c: a narrow tile, or fp32 with one buffer for sums, which waits while they are added (about 1500 cycles)
+            const long long each = (blocks + splits - 1) / splits;
+            const bool single = runs && bn > most_run && each > um::kRun;
+            if (single && es == 2) continue;
+            const double body = (double)each * std::max(mma, load) + (single ? 1500.0 * (each / um::kRun) : 0.0);
             double cost = (double)waves * (std::max(body, store) + 200) + std::min(body, store) + 1500;
             if (role == lin::kGradW) cost += 2.0 * splits * I * J * 4 / (kStoreRate * sms);
             if (cost < least * 0.995) {
                 least = cost;
-                best = Cut{(int)tiles_i, (int)tiles_j, bn, (int)splits, stages, resident ? (int)(sms / tiles_j * tiles_j) : (int)std::min<long long>(units, sms), resident,
+                best = Cut{(int)tiles_i, (int)tiles_j, bn, (int)splits, stages, resident ? (int)(sms / tiles_j * tiles_j) : (int)std::min<long long>(units, sms), resident, single,
                            stages * stage + kept + fixed};
             }
         }
@@ -131,7 +134,7 @@ template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long lon
     }
     const bool tma = p.a_tma && p.b_tma;
     if (c.bn == 0) return ESC_ERR_UNSUPPORTED;                     // more tiles than a launch can count
-    p.tiles_i = c.tiles_i; p.tiles_j = c.tiles_j; p.bn = c.bn; p.splits = c.splits; p.stages = c.stages; p.resident = c.resident;
+    p.tiles_i = c.tiles_i; p.tiles_j = c.tiles_j; p.bn = c.bn; p.splits = c.splits; p.stages = c.stages; p.resident = c.resident; p.single = c.single;
     p.blocks = (int)((depth + um::kBlockC - 1) / um::kBlockC);
     p.per_split = p.blocks / c.splits; p.longer = p.blocks % c.splits;
     p.units = (unsigned)((long long)c.tiles_i * c.tiles_j * c.splits);

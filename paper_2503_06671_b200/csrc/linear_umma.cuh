@@ -190,6 +190,7 @@ template <typename T> struct Args {
     long long I;
     int J, tiles_i, tiles_j, bn, blocks, stages;           // blocks: of c
     int splits, per_split, longer;      // a split has per_split blocks, the first `longer` of them one more
+    bool single;                        // RUNS of fp32: a run's sums have one buffer
     bool resident;                      // B stays in shared memory; a block keeps its tile of j
     unsigned units;
     Source<T> a, b;
@@ -204,7 +205,8 @@ template <typename T> struct Args {
 template <typename T> constexpr int parts_of = sizeof(T) == 4 ? 3 : 1;
 // The tensor cores add to a sum by truncation: about a quarter of a step of fp32 is lost per 16 values of c, always towards zero.  Where the
 // result is fp32 a sum therefore ends after kRun blocks of c and is added, rounded to nearest, to a running sum beside it in tensor memory
-// (4096 values: 4.4e-6 -> below 1e-6 of the result's norm; 16 x 8000: 9.1e-6 -> 3e-7).  That takes columns, so tiles are narrower.
+// (4096 values: 4.4e-6 -> below 1e-6 of the result's norm; 16 x 8000: 9.1e-6 -> 3e-7).  That takes columns: tiles are narrower or, in fp32, which
+// waits for its operands and not for the tensor cores, have one buffer for a run's sums instead of two (`single`).
 constexpr int kRun = 8;
 template <typename T> constexpr int most_columns = sizeof(T) == 4 ? 128 : 256;
 template <typename T> constexpr int most_run_columns = sizeof(T) == 4 ? 96 : 128;
@@ -516,6 +518,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
     tmem = __shfl_sync(0xffffffffu, tmem, 0);                      // known to be uniform, as an instruction's operands have to be
 
+    const bool single = RUNS && PARTS == 3 && p.single;
     bool alive = true;
     int n = 0;                                                     // tiles so far
     if (TMA && warp == 0) {
@@ -642,8 +645,8 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         if (p.resident) alive = wait_warp(b_full, 0, 0x40000000u);
         for (Walk u = walk(p); u.live && alive; next(u, p))
             for (int c = u.c0; c < u.c1 && alive; ++n) {           // n: runs so far
-                const int first = c, end = RUNS ? min(c + kRun, u.c1) : u.c1, buf = n & 1;
-                if (n >= 2) alive = wait_warp(acc_empty + 8 * buf, (unsigned)((n >> 1) - 1) & 1, 0x30000000u | (unsigned)n);
+                const int first = c, end = RUNS ? min(c + kRun, u.c1) : u.c1, buf = single ? 0 : n & 1, use = single ? n : n >> 1;
+                if (use > 0) alive = wait_warp(acc_empty + 8 * buf, (unsigned)(use - 1) & 1, 0x30000000u | (unsigned)n);
                 if (!alive) break;
                 fence_after();
                 const uint32_t d = tmem + buf * kTmemBuffer;
@@ -703,8 +706,8 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         int turn = 0;                                              // which member of the team has the next unit
         int done = 0;                                              // blocks of c of this tile that are summed; n: runs so far
         for (; u.live && alive; ++n) {
-            const int buf = n & 1;
-            alive = wait_warp(acc_full + 8 * buf, (unsigned)(n >> 1) & 1, 0x60000000u | (unsigned)n);
+            const int buf = single ? 0 : n & 1;
+            alive = wait_warp(acc_full + 8 * buf, (unsigned)(single ? n : n >> 1) & 1, 0x60000000u | (unsigned)n);
             if (!alive) break;
             fence_after();
             const bool begun = RUNS && done > 0, last = !RUNS || done + kRun >= u.c1 - u.c0;
@@ -715,7 +718,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 const bool ours = turn == member && c * UC < wide && rows > 0;
                 turn = turn + 1 == TEAM ? 0 : turn + 1;
                 if (!ours) continue;
-                const uint32_t sum_at = tmem + ((uint32_t)(quarter * 32) << 16) + most_run_columns<T> + c * (PARTS == 3 ? kTmemBuffer / 2 : UC);
+                const uint32_t sum_at = tmem + ((uint32_t)(quarter * 32) << 16) + (single ? kTmemBuffer + c * UC : most_run_columns<T> + c * (PARTS == 3 ? kTmemBuffer / 2 : UC));
                 if (RUNS && !last) {                              // the same warp has this unit in every run
                     add_run<PARTS, 2 * V>(d + c * UC, sum_at, begun);
                     continue;

@@ -34,3 +34,15 @@ def test_one_tensor_is_not_aligned(pkg, dtype, which):   # noqa: F811
     s[which] = among_nans(s[which], 3)
     forward(pkg, s, "relu")
     backward(pkg, s, "gelu")
+
+
+@pytest.mark.parametrize("rows,K,N", [(700, 2050, 96), (300, 1024, 260), (5000, 130, 140), (20000, 64, 200), (129, 4100, 33)])
+def test_long_sums(pkg, rows, K, N):   # noqa: F811
+    """fp32 sums of more than 512 values, in each of the three products, in tiles of one and several units and with a residual between them."""
+    s = make(rows, K, N, "fp32")
+    for residual in (False, True):
+        forward(pkg, s, "none", residual=residual, keep=residual)
+    backward(pkg, s, "gelu")
+    s = make(rows, N, K, "fp32")
+    forward(pkg, s, "relu", keep=False)
+    backward(pkg, s, "none")
