@@ -173,9 +173,11 @@ BiasCut bias_cut(const Call& c, int vec) {
     const int across = blocks == 1 ? all : std::min(32, (int)abi::round_up((all + blocks - 1) / blocks, line));
     return {blocks, across, (int)std::max(1LL, std::min(((long long)lin::kSumBlocks * abi::sm_count() + blocks - 1) / blocks, (c.rows + 31) / 32))};
 }
-// A copy of ragged bf16 rows to rows of whole pieces costs two passes over them and a launch; a product that takes them as they are runs at a
-// third of the speed: 70640 x 906 x 441 backward 595 us as they are.  Below a million values the launch costs more.
+// A copy of ragged bf16 rows to rows of whole pieces costs two passes over them and a launch, and pays where a product reads them several times:
+// 70640 x 906 to 441 backward 505 us, 654 without, 4000 x 777 to 1999 93 and 165.  Below a million values the launch costs more; x is read once for
+// every 128 outputs (100000 x 61 to 64: 45 us with a copy of it, 39 without).
 bool copied(long long rows, int K) { return rows * K >= 1 << 20; }
+bool x_copied(const Call& c) { return copied(c.rows, c.K) && c.N > um::kBlockI; }
 long long piece_stride(int K) { return (long long)abi::round_up(K, 8); }
 // g lies in rows of whole 16-byte pieces, whatever N is.
 long long g_stride(const Call& c) { return (long long)abi::round_up(c.N, 16 / c.es()); }
@@ -203,7 +205,7 @@ LinearWs carve(void* ws, const Call& c) {
     w.g = take(c.act != ESC_ACT_NONE ? (size_t)c.rows * g_stride(c) * c.es() : 0);
     // bf16 with K that is no multiple of eight: x and the weights as rows of whole 16-byte pieces, where copying them pays
     const bool ragged = c.dtype == ESC_BF16 && c.K % 8 != 0;
-    w.x = reinterpret_cast<bf16*>(take(ragged && copied(c.rows, c.K) ? (size_t)c.rows * piece_stride(c.K) * 2 : 0));
+    w.x = reinterpret_cast<bf16*>(take(ragged && x_copied(c) ? (size_t)c.rows * piece_stride(c.K) * 2 : 0));
     w.w = reinterpret_cast<bf16*>(take(ragged && copied(c.N, c.K) ? (size_t)c.N * piece_stride(c.K) * 2 : 0));
     w.bytes = off;
     return w;
@@ -369,7 +371,7 @@ template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& 
     if constexpr (sizeof(T) == 2) {
         if (c.K % 8 != 0) {
             const long long ld = piece_stride(c.K);
-            if (gw && copied(c.rows, c.K)) {
+            if (gw && x_copied(c)) {
                 ESC_TRY(launch_copy(x, w.x, ld, st));
                 x = source<T>(w.x, c.rows, c.K, ld);
             }

@@ -7,8 +7,8 @@
 // turn go into g in place and add up its columns; then the same boxes of g are the operand of both products: with 128 rows and the columns
 // as contraction (K-major) for gx, with the columns as rows of the result and 128 rows as contraction (MN-major) for gw.  w stays in shared
 // memory and the sums of gw in tensor memory for the life of the block (N / 128 x K columns beside one or two tiles of gx); each block leaves
-// one partial sum of gw and gb.  64 x 64x64 rows, 64 to 128 channels, GELU: 51 us (3.9 TB/s), where three
-// kernels that wrote and read g took 96, and as long with fp32 gradients (87 in three kernels).  What bounds it: the act' of 33 million values on eight warps, and latency of three boxes a tile.
+// one partial sum of gw and gb.  64 x 64x64 rows, 64 to 128 channels, GELU: 52 us (3.9 TB/s), with gradients of the weights in bf16 or fp32, where
+// three kernels that wrote and read g took 96 and 87.  What bounds it: the act' of 33 million values on eight warps of an SM, and latency.
 #pragma once
 #include "linear_umma.cuh"
 

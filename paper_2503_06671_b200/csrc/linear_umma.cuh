@@ -20,7 +20,8 @@
 // adds the residual, rounds once and puts them, exchanged as the 128-byte swizzle has it, into the warp's 4 KB of shared memory; TMA brings the
 // residual there and takes the results from there.  Rows that TMA cannot take leave through the same 4 KB by plain stores of whole warps.
 //
-// Large products run at the tensor cores' rate under the power limit: 16384 x 4096 x 4096 in bf16 410 us, 1.33 PFLOP/s.
+// Large products run at the tensor cores' rate under the power limit: 16384 x 4096 x 4096 in bf16 410 us, 1.33 PFLOP/s.  fp32 is bound by the warps
+// that split: 57600 x 192 to 384 78 us, 8192 x 512 to 512 44 us, with the tensor cores busy a quarter to a third of the time.
 // Small layers (K and N of a few hundred, many rows) are bound by memory: w then stays in shared memory for the whole life of a block
 // (`resident`), and the ring holds rows alone.
 #pragma once
@@ -264,7 +265,7 @@ __device__ __forceinline__ uint32_t staged(int r, uint32_t b) { return r * 128 +
 template <typename T> struct Chunk;
 
 // bf16: 16 bytes of a line to a lane, out of the two aligned pieces in which they lie, whatever the rows' alignment.  (Two loads of one value
-// each for two values: 10007 x 250 to 777 40 us, 17467 x 605 to 3664 467 us.)
+// each for two values: 38391 x 96 to 1580 backward 218 us, 194 so; 17467 x 605 to 3664 468 and 395.)
 template <> struct Chunk<__nv_bfloat16> {
     static constexpr int kStep = kGroupWarps * 4, kTurns = kBlockC / kStep;
     static_assert(kGroupWarps == 8, "the pieces of a lane's lines are exchanged alike");

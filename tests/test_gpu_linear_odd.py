@@ -46,3 +46,11 @@ def test_long_sums(pkg, rows, K, N):   # noqa: F811
     s = make(rows, N, K, "fp32")
     forward(pkg, s, "relu", keep=False)
     backward(pkg, s, "none")
+
+
+@pytest.mark.parametrize("rows,K,N", [(20000, 61, 64), (20000, 61, 128), (20000, 61, 129), (1100, 1001, 1100)])
+def test_with_and_without_a_copy(pkg, rows, K, N):   # noqa: F811
+    """Ragged bf16 rows that the backward pass takes as they are, and copies."""
+    s = make(rows, K, N, "bf16", 3)
+    backward(pkg, s, "gelu")
+    backward(pkg, s, "none", torch.float32)
