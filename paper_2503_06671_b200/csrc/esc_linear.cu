@@ -115,8 +115,8 @@ template <typename T> bool map_of(CUtensorMap* m, const void* base, long long ba
 }
 bool whole_pieces(const void* p, long long ld, size_t es) { return abi::aligned(p, 16) && (size_t)ld * es % 16 == 0; }
 
-// The result lies in memory as O [splits, I, J].  Returns the number of splits through `splits`.  `beside`: the kernel before it in the stream is
-// the other product of the same g, and need not have ended.
+// The result lies in memory as O [splits, I, J].  Returns the number of splits through `splits`.  `beside`: the kernel before it in the stream
+// (the other product of the same g, or grad_out's column sums) need not have ended.
 template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long long depth, bool runs, cudaStream_t st, int* splits = nullptr, bool beside = false) {
     using O = typename um::Result<T, ROLE>::type;
     constexpr bool a_mn = ROLE == lin::kGradW, b_mn = ROLE != lin::kForward;
@@ -347,6 +347,7 @@ template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& 
     um::Source<T> g = source<T>(l.go, c.rows, c.N, c.N);
     lin::Parts pw{w.part, 0, 0}, pb{w.bias, 0, 0};
     const bool acts = c.act != ESC_ACT_NONE && (l.gx || gw);
+    bool beside = gb && !acts;                                     // the next product needs nothing of the kernel before it
     if (acts || gb) {
         T* to = acts ? static_cast<T*>(w.g) : nullptr;
         const long long ld = g_stride(c);
@@ -373,10 +374,12 @@ template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& 
             const long long ld = piece_stride(c.K);
             if (gw && x_copied(c)) {
                 ESC_TRY(launch_copy(x, w.x, ld, st));
+                beside = false;
                 x = source<T>(w.x, c.rows, c.K, ld);
             }
             if (l.gx && copied(c.N, c.K)) {
                 ESC_TRY(launch_copy(weight, w.w, ld, st));
+                beside = false;
                 weight = source<T>(w.w, c.N, c.K, ld);
             }
         }
@@ -385,13 +388,14 @@ template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& 
         um::Args<T> p{};
         p.I = c.rows; p.J = c.K;
         p.a = g; p.b = weight; p.out = l.gx;
-        ESC_TRY((launch_product<T, lin::kGradX>(p, c.N, sizeof(T) == 4, st)));
+        ESC_TRY((launch_product<T, lin::kGradX>(p, c.N, sizeof(T) == 4, st, nullptr, beside)));
+        beside = true;
     }
     if (gw) {
         um::Args<T> p{};
         p.I = c.N; p.J = c.K;
         p.a = g; p.b = x; p.part = w.part;
-        ESC_TRY((launch_product<T, lin::kGradW>(p, c.rows, sizeof(T) == 4 || grad_dtype == ESC_F32, st, &pw.parts, l.gx != nullptr)));
+        ESC_TRY((launch_product<T, lin::kGradW>(p, c.rows, sizeof(T) == 4 || grad_dtype == ESC_F32, st, &pw.parts, beside)));
         pw.count = (long long)c.N * c.K;
     }
     return sum_to(pw, pb, gw, gb, grad_dtype, st);

@@ -149,6 +149,7 @@ template <typename T, int V> __device__ __forceinline__ void store_values(T* p, 
 template <typename T, int V> __global__ void __launch_bounds__(256, kSumBlocks) grad_z_sums(const Layer<T> p, T* g, long long g_ld, float* part, int across)
 {
     __shared__ float acc[256 * V];
+    pdl_launch_dependents();                                       // products of a g that is not written here need not wait
     const int all = p.N / V, down = 256 / across;
     const int col = threadIdx.x % across, v = blockIdx.x * across + col, r = threadIdx.x / across;
     float sum[V] = {};
@@ -175,7 +176,6 @@ template <typename T, int V> __global__ void __launch_bounds__(256, kSumBlocks) 
             }
         }
     }
-    pdl_launch_dependents();
     if (!part) return;
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e * 256 + threadIdx.x] = sum[e];

@@ -805,7 +805,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         if (lane == 0) bulk_wait_read<0>();                        // shared memory outlives what is read from it
     }
     pdl_launch_dependents();
-    if (ROLE == kGradW) pdl_wait_primary();                        // it may have started beside the other product: what comes next waits for both
+    if (ROLE != kForward) pdl_wait_primary();                      // it may have started beside the kernel before it: what comes next waits for both
     fence_before();
     __syncthreads();
     if (warp == kIssue) {
