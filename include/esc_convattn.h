@@ -536,7 +536,8 @@ int esc_linear_forward(const void* x, long long x_stride, const void* weight, co
 
 /*
  * Its gradients, with g = grad_out act'(z):  grad_x = g weight,  grad_weight = g^T x,  grad_bias = sum over rows of g.
- *   z          what the forward pass wrote; not read, and may be NULL, with ESC_ACT_NONE.  act'(0) of ESC_ACT_RELU is 0.
+ *   z          what the forward pass wrote; not read, and may be NULL, with ESC_ACT_NONE.  act'(0) of ESC_ACT_RELU is 0;
+ *              where it is 0 nothing of grad_out passes, an infinity or a NaN neither.
  *   grad_out   [rows, N] dense (also the residual's gradient, as it is)
  *   grad_x     [rows, K] dense;  grad_weight [N, K] and grad_bias [N] of grad_dtype; each may be NULL.  No rows: zeros.
  *   workspace  esc_linear_backward_workspace_bytes(...) bytes, 256-byte aligned, no preparation needed

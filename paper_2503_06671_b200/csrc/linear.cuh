@@ -93,7 +93,7 @@ template <int V> __device__ __forceinline__ void times_slope(int act, const Gaus
         }
     } else if (act == kActRelu) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) f[e] *= z[e] > 0.f ? 1.f : 0.f;
+        for (int e = 0; e < V; ++e) f[e] = z[e] > 0.f ? f[e] : 0.f;   // nothing passes where the slope is zero, an infinity neither
     }
 }
 
