@@ -47,7 +47,7 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
     const uint32_t x_at = p.nb * kBox, z_at = x_at + p.kb * kBox, stage_bytes = z_at + (has_act ? p.nb * kBox : 0);
     const uint32_t w_at = base + p.stages * stage_bytes, w_block = p.kb * 64 * 128, staging = w_at + p.nb * w_block;
     const uint32_t full = staging + kOutWarps * kSlotBytes, ready = full + 8 * kMostStages, empty = ready + 8 * kMostStages, gx_full = empty + 8 * kMostStages,
-                   gx_empty = gx_full + 16, w_full = gx_empty + 16, gw_done = w_full + 8, gb_done = gw_done + 8, gw_taken = gb_done + 8, slot = gw_taken + 8,
+                   gx_empty = gx_full + 16, w_full = gx_empty + 16, gw_done = w_full + 8, gb_done = gw_done + 8, gw_taken = gb_done + 8, finished = gw_taken + 8, slot = finished + 8,
                    strip = slot + 16;                              // [kActWarps][256] floats: columns of g
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8 * s, 1); mbar_init(ready + 8 * s, kActWarps); mbar_init(empty + 8 * s, 1); }
@@ -56,6 +56,7 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
         mbar_init(gw_done, 1);
         mbar_init(gb_done, kActWarps);
         mbar_init(gw_taken, kOutWarps);
+        mbar_init(finished, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) {
@@ -89,9 +90,8 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
                 }
                 for (int c = 0; c < p.kb; ++c) tma_load_2d(at + x_at + c * kBox, &map_x, bar, c * 64, t * kRows);
             }
-            if (!alive)                                            // what is still on its way here lands before the block goes
-                for (unsigned s = 0; s < (unsigned)p.stages; ++s)
-                    if (r.round > 0 || s < r.s) wait_lane(full + 8 * s, (s < r.s ? r.round : r.round - 1) & 1, 0x71000000u | s);
+            wait_lane(w_full, 0, 0x7B000000u);
+            landed(full, p.stages, r);
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -131,6 +131,7 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
             if (RUNS && in_run == kRunTiles - 1 && t + gridDim.x < p.tiles) commit(gw_done);
         }
         commit(gw_done);
+        finish(finished);
     } else if (warp >= kFirstAct && warp < kFirstOut) {
         // ---- g in place, and its columns' sums ------------------------------------------------------------------------------
         // A lane has the eight columns of one piece in every box, a warp four rows at a time.

@@ -79,6 +79,12 @@ struct Ring {
     unsigned s, round;
     __device__ __forceinline__ void next(int stages) { if (++s == (unsigned)stages) { s = 0; ++round; } }
 };
+// Loads into the ring up to place r have landed, by the lane that asked for them: also where the block gave up, shared memory outlives what is written to it.
+__device__ __forceinline__ void landed(uint32_t full, int stages, Ring r) {
+#pragma unroll 1
+    for (unsigned s = 0; s < (unsigned)stages; ++s)
+        if (r.round > 0 || s < r.s) wait_lane(full + 8 * s, (s < r.s ? r.round : r.round - 1) & 1, 0x70000000u | s);
+}
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                  ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
@@ -111,6 +117,11 @@ __device__ __forceinline__ void mma(uint32_t d, unsigned long long a, unsigned l
 __device__ __forceinline__ void commit(uint32_t bar) {
     asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
                  "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
+}
+// All products issued so far have been done, likewise.
+__device__ __forceinline__ void finish(uint32_t bar) {
+    commit(bar);
+    wait_warp(bar, 0, 0xC0000000u);
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -497,11 +508,12 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     const uint32_t staging = resident + (p.resident ? (uint32_t)p.blocks * b_bytes : 0);
     const uint32_t strips = staging + EPI * kSlotBytes;    // of an epilogue warp: the bias of its columns
     const uint32_t full = strips + EPI * 256, empty = full + 8 * kMaxStages, acc_full = empty + 8 * kMaxStages, acc_empty = acc_full + 16,
-                   b_full = acc_empty + 16, res_full = b_full + 8, slot = res_full + 8 * kMostEpi;
+                   b_full = acc_empty + 16, res_full = b_full + 8, finished = res_full + 8 * kMostEpi, slot = finished + 8;
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) { mbar_init(full + 8 * s, TMA ? 1 : kGroupWarps); mbar_init(empty + 8 * s, 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(acc_full + 8 * s, 1); mbar_init(acc_empty + 8 * s, EPI); }
         mbar_init(b_full, TMA ? 1 : kFillWarps);
+        mbar_init(finished, 1);
         for (int s = 0; s < EPI; ++s) mbar_init(res_full + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -551,9 +563,8 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     }
                 }
             }
-            if (!alive)                                            // what is still on its way here lands before the block goes
-                for (unsigned s = 0; s < (unsigned)p.stages; ++s)
-                    if (r.round > 0 || s < r.s) wait_lane(full + 8 * s, (s < r.s ? r.round : r.round - 1) & 1, 0x70000000u | s);
+            if (p.resident) wait_lane(b_full, 0, 0x7B000000u);
+            landed(full, p.stages, r);
         }
         __syncwarp();
     } else if (!TMA && warp >= kFirstFill) {
@@ -639,6 +650,11 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             if (lane == 0) mbar_arrive(bar);
             here = after;
         }
+        if ((ta || tb) && w == 0 && lane == 0) {
+            if (tb && p.resident) wait_lane(b_full, 0, 0x7B000000u);
+            landed(full, p.stages, here.r);
+        }
+        __syncwarp();
     } else if (warp == kIssue) {
         // ---- issue --------------------------------------------------------------------------------------------------------------
         const uint32_t idesc = instr_desc<A_MN, B_MN>(p.bn);
@@ -676,6 +692,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 }
                 commit(acc_full + 8 * buf);
             }
+        finish(finished);
     } else if (warp >= kFirstEpi && warp < kFirstFill) {
         // ---- write out ------------------------------------------------------------------------------------------------------
         // A unit: 128 bytes of 32 rows.  The warps of a quarter of the lanes take units in turn, over the tiles.
@@ -802,7 +819,9 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             if (last) next(u, p);
             if (RUNS) turn = 0;                                    // a unit's running sum belongs to one warp, in every tile
         }
+        if (OUT && has_res && !alive && lane == 0) wait_lane(res_bar, units & 1, 0x7E000000u);   // a residual on its way, as in `landed`
         if (lane == 0) bulk_wait_read<0>();                        // shared memory outlives what is read from it
+        __syncwarp();
     }
     pdl_launch_dependents();
     if (ROLE != kForward) pdl_wait_primary();                      // it may have started beside the kernel before it: what comes next waits for both
