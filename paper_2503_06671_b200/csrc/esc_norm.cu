@@ -74,8 +74,15 @@ template <typename T, bool BACK> int launch_norm_any(const Spread& s, const ln::
 
 // Blocks of the backward pass at most: each leaves a partial sum of every column.
 int norm_parts(long long rows, int per_sm = 4) { return (int)std::max(1LL, std::min<long long>(rows, (long long)per_sm * abi::sm_count())); }
-bool long_row(int C) { return C > ln::kThreads * 8; }   // may need the wide kernels: C odd
-size_t norm_stats_offset(long long rows, int C) { return abi::round_up((size_t)norm_parts(rows) * 2 * C * sizeof(float), 256); }
+// Of the wide kernels: the blocks that share a column's rows, one where there are more columns than SMs could have blocks for.
+int wide_across(int C) { return (C + ln::kThreads - 1) / ln::kThreads; }
+int wide_parts(long long rows, int C) { return std::max(1, norm_parts(rows) / wide_across(C)); }
+bool long_row(int C) { return C > ln::kThreads * 8; }       // may need the wide kernels: C odd
+bool longest_row(int C) { return C > ln::kThreads * 4 * esc::Elem<bf16>::kVec; }   // always does, whatever its type and alignment
+size_t norm_stats_offset(long long rows, int C) {
+    const size_t parts = longest_row(C) ? wide_parts(rows, C) : norm_parts(rows);
+    return abi::round_up(parts * 2 * C * sizeof(float), 256);
+}
 size_t norm_ws_bytes(long long rows, int C) { return norm_stats_offset(rows, C) + (long_row(C) ? abi::round_up((size_t)rows * 2 * sizeof(float), 256) : 0); }
 
 template <typename T> bool all_aligned(const ln::Rows<T>& p, size_t bytes) {
@@ -111,10 +118,9 @@ template <typename T> int norm_backward_t(ln::Rows<T> p, bool columns, int grad_
         float2* stats = reinterpret_cast<float2*>(ws + norm_stats_offset(p.rows, p.C));
         ln::backward_wide<T><<<most, ln::kThreads, 0, st>>>(p, stats);
         ESC_TRY(launched());
-        const int across = (p.C + ln::kThreads - 1) / ln::kThreads;
-        parts = std::max(1, most / across);
+        parts = wide_parts(p.rows, p.C);
         if (columns) {
-            ln::columns_wide<T><<<dim3(across, parts), ln::kThreads, 0, st>>>(p, stats);
+            ln::columns_wide<T><<<dim3(wide_across(p.C), parts), ln::kThreads, 0, st>>>(p, stats);
             ESC_TRY(launched());
         }
     } else {
