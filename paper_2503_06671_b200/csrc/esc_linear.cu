@@ -55,7 +55,7 @@ template <typename T> lin::Layer<T> layer_of(const Call& c) {
 
 // ---- tensor-core products ----------------------------------------------------------------------------------------------------
 
-// What a product is cut into (`runs`: its result is fp32).  Times in cycles of an SM, from the rates below; the cheapest width of a tile and number of runs of rows.
+// What a product is cut into (`runs`: its sums end, after run_of blocks; otherwise its runs of rows have kLongRun blocks at most).  Times in cycles of an SM, from the rates below; the cheapest width of a tile and number of runs of rows.
 struct Cut {
     int tiles_i, tiles_j, bn, splits, stages, grid;
     bool resident, single;
@@ -67,7 +67,8 @@ Cut cut(lin::Role role, long long I, int J, long long depth, size_t es, bool tma
     const int parts = es == 4 ? 3 : 1, products = es == 4 ? 6 : 1;
     const long long blocks = (depth + um::kBlockC - 1) / um::kBlockC, tiles_i = (I + um::kBlockI - 1) / um::kBlockI;
     const size_t out_es = role == lin::kGradW ? 4 : es, epi = tma ? um::epi_warps<true> : um::epi_warps<false>;
-    const int unit = (int)(128 / out_es);                          // columns that leave together
+    const int unit = (int)(128 / out_es), run = um::run_of(role, es);   // unit: columns that leave together
+    const long long least_splits = runs ? 1 : (blocks + um::kLongRun - 1) / um::kLongRun;
     Cut best{};
     double least = 1e300;
     for (int bn = std::min(most / step, (J + step - 1) / step) * step; bn >= step; bn -= step) {
@@ -83,14 +84,14 @@ Cut cut(lin::Role role, long long I, int J, long long depth, size_t es, bool tma
         const double mma = 4.0 * products * std::max(40.0, bn / 2.0), load = (rows + b_rows) * um::kBlockC * es / kLoadRate, store = rows * bn * out_es / kStoreRate;
         // runs of rows: one, or as many as fill the SMs one to four times
         for (int fill = 0; fill <= (role == lin::kGradW ? 4 : 0); ++fill) {
-            const long long splits = fill == 0 ? 1 : std::min<long long>(blocks, (long long)fill * sms / (tiles_i * tiles_j));
+            const long long splits = fill == 0 ? least_splits : std::min<long long>(blocks, (long long)fill * sms / (tiles_i * tiles_j));
             const long long units = tiles_i * tiles_j * splits, waves = (units + sms - 1) / sms;
-            if (splits < 1 || units > 0x7fffffffLL) continue;
+            if (splits < least_splits || units > 0x7fffffffLL) continue;
             // runs of c: a narrow tile, or fp32 with one buffer for sums, which waits while they are added (about 1500 cycles)
             const long long each = (blocks + splits - 1) / splits;
-            const bool single = runs && bn > most_run && each > um::kRun;
+            const bool single = runs && bn > most_run && each > run;
             if (single && es == 2) continue;
-            const double body = (double)each * std::max(mma, load) + (single ? 1500.0 * (each / um::kRun) : 0.0);
+            const double body = (double)each * std::max(mma, load) + (single ? 1500.0 * (each / run) : 0.0);
             double cost = (double)waves * (std::max(body, store) + 200) + std::min(body, store) + 1500;
             if (role == lin::kGradW) cost += 2.0 * splits * I * J * 4 / (kStoreRate * sms);
             if (cost < least * 0.995) {
@@ -154,8 +155,7 @@ template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long lon
     };
     auto pick = [&](auto in, auto out_by) {
         constexpr bool TMA = decltype(in)::value, OUT = decltype(out_by)::value;
-        if constexpr (sizeof(T) == 4 || ROLE == lin::kGradW)
-            if (runs && (p.blocks + c.splits - 1) / c.splits > um::kRun) return launch(um::product_umma<T, ROLE, TMA, true, OUT>, um::all_warps<TMA>);
+        if (runs && (p.blocks + c.splits - 1) / c.splits > um::run_of(ROLE, sizeof(T))) return launch(um::product_umma<T, ROLE, TMA, true, OUT>, um::all_warps<TMA>);
         return launch(um::product_umma<T, ROLE, TMA, false, OUT>, um::all_warps<TMA>);
     };
     using yes = std::true_type;
@@ -314,7 +314,7 @@ template <typename T> int linear_forward_t(const Call& c, const lin::Layer<T>& l
     p.I = c.rows; p.J = c.N; p.act = c.act;
     p.a = source<T>(c.x, c.rows, c.K, c.x_stride); p.b = source<T>(c.w, c.N, c.K, c.K);
     p.bias = l.b; p.residual = l.residual; p.out = l.out; p.z = l.z;
-    return launch_product<T, lin::kForward>(p, c.K, sizeof(T) == 4, st);
+    return launch_product<T, lin::kForward>(p, c.K, true, st);
 }
 
 // A small bf16 layer in one pass; kNotThis: it is not one, or its tensors are not rows of whole 16-byte pieces.
@@ -388,7 +388,7 @@ template <typename T> int linear_backward_t(const Call& c, const lin::Layer<T>& 
         um::Args<T> p{};
         p.I = c.rows; p.J = c.K;
         p.a = g; p.b = weight; p.out = l.gx;
-        ESC_TRY((launch_product<T, lin::kGradX>(p, c.N, sizeof(T) == 4, st, nullptr, beside)));
+        ESC_TRY((launch_product<T, lin::kGradX>(p, c.N, true, st, nullptr, beside)));
         beside = true;
     }
     if (gw) {

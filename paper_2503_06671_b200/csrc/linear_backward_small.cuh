@@ -20,7 +20,7 @@ using bf16 = __nv_bfloat16;
 constexpr int kRows = 128, kBox = kRows * 128, kActWarps = 8, kOutWarps = 4, kFirstAct = 4, kFirstOut = kFirstAct + kActWarps, kThreads = 32 * (kFirstOut + kOutWarps);
 constexpr int kMostBoxes = 4;                                      // of go: N up to 256
 constexpr int kMostStages = 4;
-constexpr int kRunTiles = kRun * kBlockC / kRows;                  // tiles after which a sum of gw ends, where gw is fp32
+constexpr int kRunTiles = kRun * kBlockC / kRows, kLongTiles = kLongRun * kBlockC / kRows;   // tiles after which a sum of gw has to end, where gw is fp32, and bf16
 
 struct Args {
     int rows, N, K, tiles, act, stages;
@@ -34,7 +34,7 @@ __device__ __forceinline__ unsigned long long desc(uint32_t addr, uint32_t lbo) 
     return (unsigned long long)((addr >> 4) & 0x3FFFu) | ((unsigned long long)(lbo >> 4) << 16) | ((unsigned long long)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
-// RUNS: gw is fp32 and a block has more than kRunTiles tiles: their sum is added to a running one beside it in tensor memory (see kRun).
+// RUNS: a block has more tiles than a sum of gw may: that of kRunTiles is added to a running one beside it in tensor memory (see kRun).
 template <bool RUNS> __global__ void __launch_bounds__(kThreads, 1)
 backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUtensorMap map_z, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
          const __grid_constant__ CUtensorMap map_gx, const __grid_constant__ CUtensorMap map_part, const __grid_constant__ Args p)
@@ -227,7 +227,7 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
                 alive = wait_warp(gw_done, (unsigned)runs & 1, 0x82000000u | (unsigned)runs);
                 if (!alive) break;
                 fence_after();
-                for (int v = member; v < units; v += kOutWarps / 4) add_run<1, 16>(gw_at + lanes + v * 32, run_at + lanes + v * 32, runs > 0);
+                for (int v = member; v < units; v += kOutWarps / 4) add_run<1, 16, 32>(gw_at + lanes + v * 32, run_at + lanes + v * 32, runs > 0);
                 ++runs;
                 fence_before();
                 __syncwarp();
@@ -274,7 +274,7 @@ inline Plan plan(long long rows, int K, int N, bool act, bool wide, int sms) {
     d.nb = (N + 63) / 64; d.kb = (K + 63) / 64;
     d.tiles = (int)((rows + kRows - 1) / kRows);
     d.grid = d.tiles < sms ? d.tiles : sms;
-    d.runs = wide && (d.tiles + d.grid - 1) / d.grid > kRunTiles;
+    d.runs = (d.tiles + d.grid - 1) / d.grid > (wide ? kRunTiles : kLongTiles);
     const int gw_columns = (d.nb + 1) / 2 * d.kb * 64 * (d.runs ? 2 : 1);
     d.gx_buffers = gw_columns + 2 * d.kb * 64 <= 512 ? 2 : 1;
     if (gw_columns + d.kb * 64 > 512) return d;

@@ -215,11 +215,15 @@ template <typename T> struct Args {
 };
 
 template <typename T> constexpr int parts_of = sizeof(T) == 4 ? 3 : 1;
-// The tensor cores add to a sum by truncation: about a quarter of a step of fp32 is lost per 16 values of c, always towards zero.  Where the
-// result is fp32 a sum therefore ends after kRun blocks of c and is added, rounded to nearest, to a running sum beside it in tensor memory
-// (4096 values: 4.4e-6 -> below 1e-6 of the result's norm; 16 x 8000: 9.1e-6 -> 3e-7).  That takes columns: tiles are narrower or, in fp32, which
-// waits for its operands and not for the tensor cores, have one buffer for a run's sums instead of two (`single`).
-constexpr int kRun = 8;
+// The tensor cores add to a sum by truncation, always towards zero, of the sum and of the products: where all have one sign 512 values lose 2.4e-7 of
+// their sum, and from some 16384 on, when the sum has left the products' low bits behind, every 16 values lose 1e-7 (65536 values 3.7e-4, 2^20
+// 6.6e-3).  A sum therefore ends after a number of blocks of c and is added, rounded to nearest, to a running sum beside it in tensor memory:
+// after kRun where the result is fp32 (4096 values: 4.4e-6 -> below 1e-6 of the result's norm; 16 x 8000: 9.1e-6 -> 3e-7), after kLongRun where it
+// is bf16, when 2^-12 are lost at most (65536: 3.7e-4 -> 1.7e-4, 2^20: 6.6e-3 -> 1.9e-4).  That takes columns: tiles are narrower or, in fp32,
+// which waits for its operands and not for the tensor cores, have one buffer for a run's sums instead of two (`single`).  Gradients of weights
+// in bf16 are cut into runs of rows, which are added in fp32 anyway, of kLongRun blocks at most.
+constexpr int kRun = 8, kLongRun = 512;
+__host__ __device__ constexpr int run_of(Role role, size_t es) { return role == kGradW || es == 4 ? kRun : kLongRun; }
 template <typename T> constexpr int most_columns = sizeof(T) == 4 ? 128 : 256;
 template <typename T> constexpr int most_run_columns = sizeof(T) == 4 ? 96 : 128;
 
@@ -476,10 +480,10 @@ template <int PARTS, int N> __device__ __forceinline__ void sums(float (&f)[N], 
         for (int v = 0; v < N; ++v) f[v] += more[v];
     }
 }
-// A unit's 32 columns of a run that is not its tile's last, onto the running sum.  Out of the way of the code that every tile runs.
-template <int PARTS, int N> __device__ __noinline__ void add_run(uint32_t d, uint32_t sum_at, bool begun) {
+// A unit's columns of a run that is not its tile's last, onto the running sum.  Out of the way of the code that every tile runs.
+template <int PARTS, int N, int COLUMNS> __device__ __noinline__ void add_run(uint32_t d, uint32_t sum_at, bool begun) {
 #pragma unroll 1
-    for (int c = 0; c < 32; c += N) {
+    for (int c = 0; c < COLUMNS; c += N) {
         float f[N];
         sums<PARTS>(f, d + c, sum_at + c, begun);
         tmem_st(sum_at + c, f);
@@ -489,7 +493,7 @@ template <int PARTS, int N> __device__ __noinline__ void add_run(uint32_t d, uin
 
 // ---- the kernel ---------------------------------------------------------------------------------------------------------------
 
-// RUNS: the contraction is longer than kRun blocks, and the result fp32.  Of its own: the code of the running sum, though it did not run,
+// RUNS: the contraction is longer than a run (run_of).  Of its own: the code of the running sum, though it did not run,
 // cost 427x240, 64 to 64 channels in fp32 six of 33 us.
 // OUT: results leave and residuals come by TMA: rows of whole aligned 16-byte pieces.
 template <typename T, Role ROLE, bool TMA, bool RUNS, bool OUT>
@@ -498,7 +502,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
              const __grid_constant__ CUtensorMap map_res, const __grid_constant__ CUtensorMap map_z, const __grid_constant__ Args<T> p)
 {
     constexpr bool A_MN = ROLE == kGradW, B_MN = ROLE != kForward;
-    constexpr int PARTS = parts_of<T>, EPI = epi_warps<TMA>, kIssue = 1, kFirstFill = kFirstEpi + EPI;
+    constexpr int PARTS = parts_of<T>, EPI = epi_warps<TMA>, kIssue = 1, kFirstFill = kFirstEpi + EPI, run = run_of(ROLE, sizeof(T));
     static_assert(!TMA || PARTS == 1, "TMA brings bf16 as it is");
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t base = smem_u32(smem);
@@ -662,7 +666,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         if (p.resident) alive = wait_warp(b_full, 0, 0x40000000u);
         for (Walk u = walk(p); u.live && alive; next(u, p))
             for (int c = u.c0; c < u.c1 && alive; ++n) {           // n: runs so far
-                const int first = c, end = RUNS ? min(c + kRun, u.c1) : u.c1, buf = single ? 0 : n & 1, use = single ? n : n >> 1;
+                const int first = c, end = RUNS ? min(c + run, u.c1) : u.c1, buf = single ? 0 : n & 1, use = single ? n : n >> 1;
                 if (use > 0) alive = wait_warp(acc_empty + 8 * buf, (unsigned)(use - 1) & 1, 0x30000000u | (unsigned)n);
                 if (!alive) break;
                 fence_after();
@@ -717,7 +721,6 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 }
             }
         };
-        static_assert(!RUNS || sizeof(O) == 4, "see kRun");
         Walk u = walk(p);
         if (OUT && has_res && !has_z && lane == 0) fetch(u, 0, 0);
         __syncwarp();
@@ -728,8 +731,8 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             alive = wait_warp(acc_full + 8 * buf, (unsigned)(single ? n : n >> 1) & 1, 0x60000000u | (unsigned)n);
             if (!alive) break;
             fence_after();
-            const bool begun = RUNS && done > 0, last = !RUNS || done + kRun >= u.c1 - u.c0;
-            done = last ? 0 : done + kRun;
+            const bool begun = RUNS && done > 0, last = !RUNS || done + run >= u.c1 - u.c0;
+            done = last ? 0 : done + run;
             const int i0 = u.i * kBlockI + quarter * 32, j0 = u.j * p.bn, wide = min(p.J - j0, p.bn), rows = (int)min(p.I - i0, 32LL);
             const uint32_t d = tmem + buf * kTmemBuffer + ((uint32_t)(quarter * 32) << 16);
             for (int c = 0; c < per_tile; ++c) {
@@ -738,7 +741,7 @@ product_umma(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 if (!ours) continue;
                 const uint32_t sum_at = tmem + ((uint32_t)(quarter * 32) << 16) + (single ? kTmemBuffer + c * UC : most_run_columns<T> + c * (PARTS == 3 ? kTmemBuffer / 2 : UC));
                 if (RUNS && !last) {                              // the same warp has this unit in every run
-                    add_run<PARTS, 2 * V>(d + c * UC, sum_at, begun);
+                    add_run<PARTS, 2 * V, UC>(d + c * UC, sum_at, begun);
                     continue;
                 }
                 const int col = j0 + c * UC, cols = min(wide - c * UC, UC);
