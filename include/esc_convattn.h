@@ -526,7 +526,8 @@ int esc_layer_norm_backward(const void* x, long long x_stride, const void* weigh
  * 2^31 tiles of 128 x 16).  Fastest where pointers are 16-byte aligned and K, N and x_stride multiples of 16 bytes.
  * Arithmetic: the products run on the tensor cores.  bf16 values are multiplied exactly and added in fp32, cut off rather than rounded; sums end after
  * 32768 values and are added, rounded: terms of one sign lose 2^-12 of their sum at most, which is a sixteenth of a rounding to bf16.  fp32 values are
- * three bf16 parts each (24 bits), of whose products those above 2^-26 are taken, and sums end after 512 values: about as far from
+ * three bf16 parts each (24 bits; of values below 2^-110 fewer, as bf16 ends at 2^-133: each is off by 2^-134 at most), six of whose nine products
+ * are taken (the others come to 2^-24 of a product at most, 2^-27 on average), and sums end after 512 values: about as far from
  * the exact result as fp32 multiply-adds.  An fp32 value that is not finite (or 3.39e38 or more) makes its row, in a gradient of the weights
  * its column, NaN; with bf16 it gives what the sums give.  Up to 16 rows may be multiplied and added in fp32 instead.  Each output is
  * rounded once.

@@ -12,7 +12,8 @@
 //
 // bf16 with rows of whole 16-byte pieces: TMA fills the ring.  Otherwise two groups of eight warps load values as they lie and store them
 // swizzled, a group every other block: any stride and alignment, and fp32, where every value is split into three bf16 parts (24 bits: hi + mid
-// + lo exactly) and six of the nine products are taken; what is left out is below 2^-26 of a product.  The largest of them has an accumulator
+// + lo exactly, down to 2^-110; smaller values lose what lies below bf16's last bit, 2^-133) and six of the nine products are taken; the parts are 2^-8
+// of one another at most, so what is left out is two products of 2^-25 (rms of all: 2^-27).  The largest of them has an accumulator
 // of its own (the tensor cores add as fp32, and small terms would be rounded at the large sum's step).  An infinity has no such parts: a row
 // or column with one comes out as NaN.
 //
@@ -260,7 +261,7 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
 __device__ __forceinline__ void st_shared(uint32_t at, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
 __device__ __forceinline__ void st_shared(uint32_t at, uint32_t v, uint32_t w) { asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(v), "r"(w) : "memory"); }
 __device__ __forceinline__ void st_shared(uint32_t at, uint4 v) { asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); }
-// The three bf16 parts of two values; the differences are exact.
+// The three bf16 parts of two values; the differences are exact, and lo is too where the value is not below 2^-110.
 __device__ __forceinline__ void split(float a, float b, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
     hi = pack(a, b);
     const F2 minus = f2(-1.f, -1.f);
