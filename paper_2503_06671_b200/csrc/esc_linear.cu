@@ -143,7 +143,7 @@ template <typename T, lin::Role ROLE> int launch_product(um::Args<T> p, long lon
     const void* out = p.out;
     if constexpr (ROLE == lin::kGradW) out = p.part;
     const bool out_tma = (c.tiles_j == 1 || c.bn % (int)(128 / sizeof(O)) == 0) && whole_pieces(out, p.J, sizeof(O)) && map_of<O>(&mo, out, c.splits, p.I, p.J, p.J, 32) &&
-               abi::aligned(p.bias, 16) && (!p.residual || (whole_pieces(p.residual, p.J, sizeof(T)) && map_of<T>(&mr, p.residual, 1, p.I, p.J, p.J, 32))) &&
+               (!p.residual || (whole_pieces(p.residual, p.J, sizeof(T)) && map_of<T>(&mr, p.residual, 1, p.I, p.J, p.J, 32))) &&
                (!p.z || (whole_pieces(p.z, p.J, sizeof(T)) && map_of<T>(&mz, p.z, 1, p.I, p.J, p.J, 32)));
     p.a.pieces = a_pieces && p.a.width % V == 0;
     p.b.pieces = b_pieces && p.b.width % V == 0;
