@@ -230,7 +230,7 @@ int launch_copy(const um::Source<bf16>& s, bf16* out, long long ld, cudaStream_t
 
 // The partial sums of the weights' and the bias' gradients, in one launch.
 template <typename G> int launch_sums(const lin::Parts& w, const lin::Parts& b, void* gw, void* gb, cudaStream_t st) {
-    return launch_behind(lin::sum_parts<G>, (unsigned)(lin::sum_blocks(w) + lin::sum_blocks(b)), lin::kSumThreads, st, 0, w, b, static_cast<G*>(gw), static_cast<G*>(gb));
+    return launch_behind(lin::sum_parts<G>, (unsigned)(lin::sum_blocks(w) + lin::sum_blocks(b)), esc::kSumThreads, st, 0, w, b, static_cast<G*>(gw), static_cast<G*>(gb));
 }
 int sum_to(const lin::Parts& w, const lin::Parts& b, void* gw, void* gb, int grad_dtype, cudaStream_t st) {
     if (w.count + b.count == 0) return ESC_OK;

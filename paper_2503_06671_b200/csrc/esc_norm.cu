@@ -105,8 +105,8 @@ template <typename T> int norm_forward_t(const ln::Rows<T>& p, cudaStream_t st) 
 
 int launch_sum_columns(const float* part, int parts, int C, int grad_dtype, void* gw, void* gb, cudaStream_t st) {
     const unsigned blocks = (unsigned)((2LL * C + 31) / 32);
-    if (grad_dtype == ESC_F32) return launch_behind(ln::sum_columns<float>, blocks, ln::kSumThreads, st, 0, part, parts, C, static_cast<float*>(gw), static_cast<float*>(gb));
-    return launch_behind(ln::sum_columns<bf16>, blocks, ln::kSumThreads, st, 0, part, parts, C, static_cast<bf16*>(gw), static_cast<bf16*>(gb));
+    if (grad_dtype == ESC_F32) return launch_behind(ln::sum_columns<float>, blocks, esc::kSumThreads, st, 0, part, parts, C, static_cast<float*>(gw), static_cast<float*>(gb));
+    return launch_behind(ln::sum_columns<bf16>, blocks, esc::kSumThreads, st, 0, part, parts, C, static_cast<bf16*>(gw), static_cast<bf16*>(gb));
 }
 
 template <typename T> int norm_backward_t(ln::Rows<T> p, bool columns, int grad_dtype, void* gw, void* gb, char* ws, cudaStream_t st) {

@@ -17,7 +17,7 @@
 // shared memory, the blocks by `sum_columns`, all in a fixed order.
 // 640x360 rows of 64 in bf16: 16.4 us (3.6 TB/s; a copy of these bytes takes 16); backward of 64 x 64x64 with skip 33 + 1.5 us (4 TB/s).
 #pragma once
-#include "common.cuh"
+#include "sum_rows.cuh"
 
 namespace esc { namespace norm {
 
@@ -390,23 +390,13 @@ template <typename T> __global__ void __launch_bounds__(kThreads) columns_wide(c
     p.part[(size_t)blockIdx.y * 2 * p.C + p.C + c] = gb;
 }
 
-// Column sums of `parts` partial sums [parts][2][C]: 32 columns to a block, a warp takes every 32nd part, the warps are added in order.
-constexpr int kSumThreads = 1024;
+// Column sums of `parts` partial sums [parts][2][C]: 32 columns to a block.
 template <typename G> __global__ void __launch_bounds__(kSumThreads) sum_columns(const float* part, int parts, int C, G* gw, G* gb)
 {
-    __shared__ float acc[kSumThreads / 32][32];
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, c = blockIdx.x * 32 + lane;
+    const int c = blockIdx.x * 32 + threadIdx.x % 32;
     pdl_wait_primary();
-    float s = 0.f;
-    if (c < 2 * C) {
-#pragma unroll 8
-        for (int i = warp; i < parts; i += kSumThreads / 32) s += __ldcg(part + (size_t)i * 2 * C + c);
-    }
-    acc[warp][lane] = s;
-    __syncthreads();
-    if (warp != 0 || c >= 2 * C) return;
-#pragma unroll
-    for (int v = 1; v < kSumThreads / 32; ++v) s += acc[v][lane];
+    const float s = sum_rows(part + c, c < 2 * C, parts, (size_t)2 * C);
+    if (threadIdx.x >= 32 || c >= 2 * C) return;
     G* out = c < C ? gw : gb;
     if (out) out[c < C ? c : c - C] = Elem<G>::from_f32(s);
 }

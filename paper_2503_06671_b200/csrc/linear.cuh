@@ -1,7 +1,7 @@
 // Linear layers of rows: z = x w^T + b, out = act(z) + residual, and their gradients g = grad_out act'(z), gx = g w, gw = g^T x,
-// gb = sum of g.  Here: the activations, the sums over rows, and products on the FP32 pipe for operands of any alignment.
+// gb = sum of g.  Here: the activations, g and its columns' sums, copies of ragged rows, and the sums of partial results.
 #pragma once
-#include "common.cuh"
+#include "sum_rows.cuh"
 
 namespace esc { namespace linear {
 
@@ -214,12 +214,11 @@ template <typename U> __global__ void __launch_bounds__(256) copy_rows(const U* 
 // Partial sums [parts][count], to be added up: the weights' and the bias' gradients in one launch, either may be empty.
 struct Parts { const float* p; int parts; long long count; };
 
-// Many parts: 32 sums to a block, a warp takes every 32nd part, the warps are added in order.  Up to kFewParts: a thread has four sums.
-constexpr int kFewParts = 8, kSumThreads = 1024;
+// Many parts: 32 sums to a block.  Up to kFewParts: a thread has four sums.
+constexpr int kFewParts = 8;
 inline __host__ __device__ long long sum_blocks(const Parts& t) { return t.parts <= kFewParts ? (t.count + 4 * kSumThreads - 1) / (4 * kSumThreads) : (t.count + 31) / 32; }
 template <typename G> __global__ void __launch_bounds__(kSumThreads) sum_parts(const Parts w, const Parts b, G* gw, G* gb)
 {
-    __shared__ float acc[kSumThreads / 32][32];
     pdl_wait_primary();
     const long long ours = sum_blocks(w);
     const bool of_b = blockIdx.x >= ours;
@@ -241,18 +240,9 @@ template <typename G> __global__ void __launch_bounds__(kSumThreads) sum_parts(c
         for (int u = 0; u < 4 && e + u < t.count; ++u) out[e + u] = Elem<G>::from_f32(s[u]);
         return;
     }
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const long long e = block * 32 + lane;
-    float s = 0.f;
-    if (e < t.count) {
-#pragma unroll 8
-        for (int i = warp; i < t.parts; i += kSumThreads / 32) s += __ldcg(t.p + (size_t)i * t.count + e);
-    }
-    acc[warp][lane] = s;
-    __syncthreads();
-    if (warp != 0 || e >= t.count) return;
-#pragma unroll
-    for (int v = 1; v < kSumThreads / 32; ++v) s += acc[v][lane];
+    const long long e = block * 32 + threadIdx.x % 32;
+    const float s = sum_rows(t.p + e, e < t.count, t.parts, (size_t)t.count);
+    if (threadIdx.x >= 32 || e >= t.count) return;
     out[e] = Elem<G>::from_f32(s);
 }
 

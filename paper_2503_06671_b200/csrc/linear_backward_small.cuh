@@ -191,11 +191,12 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
         }
     } else if (warp >= kFirstOut) {
         // ---- gx of each tile, gw at the end: 128 bytes of 32 rows at a time ---------------------------------------------------
-        const int e = warp - kFirstOut, quarter = warp & 3, member = e / 4;
-        const uint32_t mine = staging + e * kSlotBytes, lane_at = lane * 128 + ((lane & 7) << 4), lanes = (uint32_t)(quarter * 32) << 16;
+        static_assert(kOutWarps == 4, "a warp to each quarter of the lanes");
+        const int quarter = warp & 3;
+        const uint32_t mine = staging + (warp - kFirstOut) * kSlotBytes, lane_at = lane * 128 + ((lane & 7) << 4), lanes = (uint32_t)(quarter * 32) << 16;
         const int across = (int)(columns / 32), units = (p.nb + 1) / 2 * across;
         const uint32_t run_at = gw_at + (p.nb + 1) / 2 * columns;  // the running sum
-        int turn = 0, runs = 0;
+        int runs = 0;
         for (int t = blockIdx.x; t < p.tiles && alive; t += gridDim.x, ++n) {
             if (p.gx) {
                 const int buf = p.gx_buffers == 2 ? n & 1 : 0, use = p.gx_buffers == 2 ? n >> 1 : n;
@@ -203,8 +204,8 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
                 if (!alive) break;
                 fence_after();
                 const int i0 = t * kRows + quarter * 32;
-                for (int c = 0; c < p.kb; ++c, turn = turn + 1 == kOutWarps / 4 ? 0 : turn + 1) {
-                    if (turn != member || i0 >= p.rows) continue;
+                for (int c = 0; c < p.kb; ++c) {
+                    if (i0 >= p.rows) break;
                     if (lane == 0) bulk_wait_read<0>();
                     __syncwarp();
 #pragma unroll 1
@@ -227,7 +228,7 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
                 alive = wait_warp(gw_done, (unsigned)runs & 1, 0x82000000u | (unsigned)runs);
                 if (!alive) break;
                 fence_after();
-                for (int v = member; v < units; v += kOutWarps / 4) add_run<1, 16, 32>(gw_at + lanes + v * 32, run_at + lanes + v * 32, runs > 0);
+                for (int v = 0; v < units; ++v) add_run<1, 16, 32>(gw_at + lanes + v * 32, run_at + lanes + v * 32, runs > 0);
                 ++runs;
                 fence_before();
                 __syncwarp();
@@ -237,7 +238,7 @@ backward(const __grid_constant__ CUtensorMap map_go, const __grid_constant__ CUt
         if (p.gw && alive) alive = wait_warp(gw_done, (unsigned)runs & 1, 0x81000000u);
         if (p.gw && alive) {
             fence_after();
-            for (int v = member; v < units; v += kOutWarps / 4) {
+            for (int v = 0; v < units; ++v) {
                 const int m = v / across, c = v - m * across, n0 = m * 128 + quarter * 32;
                 if (n0 >= p.N || c * 32 >= p.K) continue;
                 if (lane == 0) bulk_wait_read<0>();
