@@ -111,9 +111,13 @@ enum Role { kForward, kGradX, kGradW };
 
 constexpr int kSumBlocks = 4;                                      // of grad_z_sums, of an SM
 
-// g = go act'(z) and its column sums, as far as they are asked for: g [rows, g_ld] of the type (rounded: the operand that two products
-// read), part [gridDim.y][N] fp32 sums of the unrounded g.  A thread has V neighbouring columns and every so many rows; a block has
-// `across` such pieces of a row; they divide the rows and their alignment.
+// g = go act'(z) and its column sums, as far as they are asked for: g [rows, g_ld] of the type, part [gridDim.y][N] fp32 sums of the unrounded g.  A
+// thread has V neighbouring columns and every so many rows; a block has `across` such pieces of a row; they divide the rows and their alignment.
+//
+// g of bf16 tensors is rounded to bf16: the operand of two products on the tensor cores, which take both operands in one type.  With GELU (ReLU's g needs
+// no rounding) gradients are 2.3e-3 from exact in norm, 1.7e-3 with an unrounded g, which their own rounding leaves.  g in two bf16 parts would
+// double both products (16384 x 1024 to 4096: 127 and 149 us) and the bytes of g; in the one-pass kernel (linear_backward_small.cuh), which has
+// room for a second part where z was, it measured 51 -> 56 us (262144 x 64 to 128).
 template <typename T, int V> __device__ __forceinline__ void load_values(const T* p, float* f) {
     constexpr int words = V * sizeof(T) / 4;
     if constexpr (words == 0) {
