@@ -555,8 +555,9 @@ int esc_linear_backward(const void* x, long long x_stride, const void* weight, c
 /*
  * The linear layers' kernels wait, with a limit of about a second, for their own loads and products.  Should a wait run out, the call's
  * results are not valid; esc_linear_device_status(), which synchronises `stream`, then returns ESC_DEV_TIMEOUT once (for all streams of the
- * current device) and clears that.  Not while `stream` is being captured (ESC_ERR_UNSUPPORTED).  The self-test launches one warp that
- * waits in vain.
+ * current device, of which `stream` has to be) and clears that.  It is a status of its own: esc_convattn_device_status() reads that of the
+ * workspace it is given, which these calls do not have.  Not while `stream` is being captured (ESC_ERR_UNSUPPORTED).  The self-test launches
+ * one warp that waits in vain.
  */
 int esc_linear_device_status(void* stream);
 int esc_linear_selftest_bounded_wait(void* stream);

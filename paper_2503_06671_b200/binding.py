@@ -950,10 +950,21 @@ def esc_linear_backward(x, weight, z, activation, grad_out, grad_x=None, grad_we
     return grad_x, grad_weight, grad_bias
 
 
+def _on_device_of(stream):
+    """The device of a torch stream, made current for the call that follows; without one the current device stays."""
+    import torch
+
+    device = getattr(stream, "device", None)
+    return _HERE if device is None or device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
 def esc_linear_device_status(stream=None) -> int:
-    """0, or ESC_DEV_TIMEOUT once if a wait of a linear layer's kernel ran out on this device; synchronises."""
-    return lib().esc_linear_device_status(_stream(stream))
+    """0, or ESC_DEV_TIMEOUT once if a wait of a linear layer's kernel ran out on the stream's device, on any of its streams; synchronises `stream`.
+    A status of its own: esc_convattn_device_status reads that of the workspace it is given."""
+    with _on_device_of(stream):
+        return lib().esc_linear_device_status(_stream(stream))
 
 
 def esc_linear_selftest_bounded_wait(stream=None) -> None:
-    _check(lib().esc_linear_selftest_bounded_wait(_stream(stream)), "esc_linear_selftest_bounded_wait")
+    with _on_device_of(stream):
+        _check(lib().esc_linear_selftest_bounded_wait(_stream(stream)), "esc_linear_selftest_bounded_wait")
