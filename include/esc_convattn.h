@@ -492,7 +492,8 @@ int esc_adamw_scalars(long long step, double lr, double beta1, double beta2, dou
  *   weight, bias   [C] of x's type; NULL: ones, zeros
  *   eps      finite, not negative.  With eps = 0 a row of equal values gives NaN.
  *   y        [rows, C], rows `y_stride` values apart; what lies between them is left as it is
- * rows may be 0, C is at most 2^20.  Arithmetic in fp32, one rounding.  Fastest where pointers and strides are multiples of 16 bytes.
+ * rows may be 0, C is at most 2^20.  Arithmetic in fp32, one rounding; rows of equal values give the bias exactly, rows far from zero lose nothing.
+ * Values 1.8e19 and more apart overflow when squared.  Fastest where pointers and strides are multiples of 16 bytes.
  */
 int esc_layer_norm_forward(const void* x, long long x_stride, const void* weight, const void* bias, float eps, void* y,
                            long long y_stride, long long rows, int C, int dtype, void* stream);
