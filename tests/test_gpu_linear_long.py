@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from tests import layers_close as close
+from tests import layers_ref as ref
 from tests.test_gpu_linear import backward, forward, make, pkg   # noqa: F401
 from tests.test_gpu_linear_close import positive
 
@@ -61,3 +62,19 @@ def test_long_bf16_sums_beside_the_epilogue(pkg, rows, K, N, pad):   # noqa: F81
     t = make(rows, N, K, "bf16")                                          # the gradient of x sums over so many outputs
     backward(pkg, t, "gelu")
     backward(pkg, t, "none", torch.float32)
+
+
+@pytest.mark.parametrize("rows,K,N,act", [(40000, 1536, 1536, 0), (200000, 320, 72, 2), (148 * 128 * 260, 64, 64, 0)])
+def test_nothing_behind_the_workspace(pkg, rows, K, N, act):   # noqa: F811
+    """bf16 gradients over so many rows that they are cut into runs; the same bits with scratch of the call's own."""
+    x, w, go, z = (torch.randn(*s, device="cuda").bfloat16() for s in ((rows, K), (N, K), (rows, N), (rows, N)))
+    n = pkg.esc_linear_backward_workspace_bytes(rows, K, N, act, torch.bfloat16)
+    ws = torch.full((n + 4096,), 123, dtype=torch.uint8, device="cuda")
+    results = []
+    for scratch in (ws[:n], None):
+        got = [torch.empty_like(x), torch.empty_like(w), torch.empty(N, dtype=torch.bfloat16, device="cuda")]
+        pkg.esc_linear_backward(x, w, z if act else None, act, go, *got, scratch)
+        results.append(got)
+    assert (ws[n:] == 123).all()
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    assert close.rel(results[0][1], ref.linear_grad(x, w, z, ["none", "relu", "gelu"][act], go, True)[0]["gw"]) <= 2 * close.H8
