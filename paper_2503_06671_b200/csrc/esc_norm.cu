@@ -83,7 +83,7 @@ size_t norm_stats_offset(long long rows, int C) {
     const size_t parts = longest_row(C) ? wide_parts(rows, C) : norm_parts(rows);
     return abi::round_up(parts * 2 * C * sizeof(float), 256);
 }
-size_t norm_ws_bytes(long long rows, int C) { return norm_stats_offset(rows, C) + (long_row(C) ? abi::round_up((size_t)rows * 2 * sizeof(float), 256) : 0); }
+size_t norm_ws_bytes(long long rows, int C) { return norm_stats_offset(rows, C) + (long_row(C) ? abi::round_up((size_t)rows * (sizeof(float2) + sizeof(float)), 256) : 0); }
 
 template <typename T> bool all_aligned(const ln::Rows<T>& p, size_t bytes) {
     const void* pointers[] = {p.x, p.weight, p.bias, p.y, p.gy, p.skip, p.gx};
@@ -116,11 +116,12 @@ template <typename T> int norm_backward_t(ln::Rows<T> p, bool columns, int grad_
     int parts;
     if (s.nv == 0) {
         float2* stats = reinterpret_cast<float2*>(ws + norm_stats_offset(p.rows, p.C));
-        ln::backward_wide<T><<<most, ln::kThreads, 0, st>>>(p, stats);
+        float* from = reinterpret_cast<float*>(stats + p.rows);
+        ln::backward_wide<T><<<most, ln::kThreads, 0, st>>>(p, stats, from);
         ESC_TRY(launched());
         parts = wide_parts(p.rows, p.C);
         if (columns) {
-            ln::columns_wide<T><<<dim3(wide_across(p.C), parts), ln::kThreads, 0, st>>>(p, stats);
+            ln::columns_wide<T><<<dim3(wide_across(p.C), parts), ln::kThreads, 0, st>>>(p, stats, from);
             ESC_TRY(launched());
         }
     } else {

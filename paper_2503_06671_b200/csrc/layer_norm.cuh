@@ -1,15 +1,16 @@
 // Layer norm of rows of C channels, forward and backward.
 //
-//   mu = x0 + sum (x - x0) / C,  r = 1 / sqrt(sum (x - mu)^2 / C + eps),  xh = (x - mu) r
+//   mu = p + sum (x - p) / C,  r = 1 / sqrt(sum (x - mu)^2 / C + eps),  xh = (x - mu) r
 //   y  = xh w + b
 //   a  = gy w;  gx = r (a - sum a / C - xh sum (a xh) / C) + skip;  gw = sum over rows of gy xh;  gb = of gy
 //
 // Bound by memory: a row is read once into registers, by G threads that hold NV vectors of VEC values each, and everything is worked
-// out there.  The mean comes first and the squares are those of the differences, and all of a row is taken from x0, its first value: near x0
+// out there.  The mean comes first and the squares are those of the differences, and all of a row is taken from p, one of its values: near p
 // differences are exact, so a row far from zero loses nothing, and one of equal values has differences of zero.  (With the mean of x itself,
-// a step of x off, such a row came out as large as that step by 1 / sqrt(eps): 61 values of 1000 gave 0.06.)  Where x0 lies far from the others
-// the row is as wide as that, and rounding at x0's size is below it.  The backward pass works mean and r out anew from x, which it reads anyway:
-// nothing is kept from the forward pass.
+// a step of x off, such a row came out as large as that step by 1 / sqrt(eps): 61 values of 1000 gave 0.06.)  p is the middle one of three, as a
+// channel may be far larger than the others: differences would be rounded at its size, and all of a row be off by some sqrt(C) steps.  (To look at
+// mean and variance and take such a row again cost 57600 x 192 in fp32 18.7 -> 20.8 us, long rows a quarter.)  The backward pass works mean and r out
+// anew from x, which it reads anyway: nothing is kept from the forward pass.
 // G <= 32: 32 / G rows to a warp, so narrow rows (64 channels of bf16: eight threads, 16 bytes each) keep every lane loading and a
 // sum over a row is log2 G shuffles; G = 256: a row to a block.  What no block holds in registers goes through `wide` kernels that read
 // x again (from L2).
@@ -73,7 +74,8 @@ template <typename T> struct Rows {
     float* part;                        // [gridDim.x][2][C] or null
 };
 
-// Sums over the G threads of a row, to all of them.  G > 32: over the block, in the order of its warps.
+// Sums over the G threads of a row, to all of them.  G > 32: over the block, in the order of its warps; another call, or whatever else the block meets
+// at, comes before these words of `scratch` are written again.
 template <int G, int N> __device__ __forceinline__ void sum_row(float (&v)[N], float* scratch) {
 #pragma unroll
     for (int o = (G < 32 ? G : 32) / 2; o > 0; o >>= 1)
@@ -93,24 +95,37 @@ template <int G, int N> __device__ __forceinline__ void sum_row(float (&v)[N], f
             for (int w = 0; w < warps; ++w) s += scratch[i * warps + w];
             v[i] = s;
         }
-        __syncthreads();
     }
 }
 
-// The values of a row, f, become what they are above the row's mean.  x0: the row's first value, which a row's first thread has in f[0].  Threads without
-// a value, and rows without one, hold zeros.
-template <int G, int NV, int VEC> __device__ __forceinline__ void center(float (&f)[NV * VEC], float x0, const bool (&real)[NV], float inv_c, float* scratch) {
-    if (G <= 32) x0 = __shfl_sync(0xffffffffu, f[0], 0, G <= 32 ? G : 32);
+__device__ __forceinline__ float middle(float a, float b, float c) { return fmaxf(fminf(a, b), fminf(fmaxf(a, b), c)); }
+// The values of a row, f, become what they are above the row's mean.  p is the middle one of three threads' first values, or of one thread's where it
+// has all or half of the row.  Threads without a value, and rows without one, hold zeros.
+// A row to a block: three meetings a row, here twice and once for the sums behind it, each over words of its own: who writes some has met the others
+// twice since these were read.
+constexpr int kScratch = 3 + kThreads / 32;                        // words of `scratch` that this takes; the others are its callers'
+template <int G, int NV, int VEC> __device__ __forceinline__ void center(float (&f)[NV * VEC], const bool (&real)[NV], int C, float inv_c, float* scratch) {
+    float p;
+    if constexpr (G > 32) {
+        if (threadIdx.x < 3) scratch[threadIdx.x] = f[0];
+        __syncthreads();
+        p = middle(scratch[0], scratch[1], scratch[2]);
+    } else if constexpr (G < 4) {
+        p = __shfl_sync(0xffffffffu, middle(f[0], f[VEC / 2], f[VEC - 1]), 0, G);
+    } else {
+        const int last = VEC > 2 ? 2 : C / VEC - 1;                // thread with a first value; of 16-byte pieces a row has three or more here
+        p = middle(__shfl_sync(0xffffffffu, f[0], 0, G), __shfl_sync(0xffffffffu, f[0], min(1, last), G), __shfl_sync(0xffffffffu, f[0], min(2, last), G));
+    }
     float s[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < NV; ++i)
         if (real[i])
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                f[i * VEC + j] -= x0;
+                f[i * VEC + j] -= p;
                 s[0] += f[i * VEC + j];
             }
-    sum_row<G>(s, scratch);
+    sum_row<G>(s, scratch + 3);
     const float mean = s[0] * inv_c;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -123,7 +138,7 @@ template <typename T, int VEC, int NV, int G>
 __global__ void __launch_bounds__(kThreads) forward(const Rows<T> p)
 {
     constexpr int per_block = kThreads / G, F = VEC * NV;
-    __shared__ float scratch[G > 32 ? kThreads / 32 : 1];
+    __shared__ float scratch[G > 32 ? kScratch + kThreads / 32 : 1];
     const int in_row = threadIdx.x % G;
     const float inv_c = 1.f / (float)p.C;
     Vec<T, VEC> w[NV], b[NV];
@@ -139,18 +154,16 @@ __global__ void __launch_bounds__(kThreads) forward(const Rows<T> p)
     const long long step = (long long)gridDim.x * per_block;
     long long row = (long long)blockIdx.x * per_block + threadIdx.x / G;
     Vec<T, VEC> x[NV], ahead[NV];
-    Vec<T, 1> x0, ahead0;                                          // where a row is a block's
-    auto load = [&](Vec<T, VEC> (&v)[NV], Vec<T, 1>& v0, long long r) {
-        if (G > 32 && r < p.rows) v0.load(p.x + r * p.x_stride);
+    auto load = [&](Vec<T, VEC> (&v)[NV], long long r) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (r < p.rows && real[i]) v[i].load(p.x + r * p.x_stride + (i * G + in_row) * VEC);
     };
-    load(x, x0, row);
+    load(x, row);
     for (; row - threadIdx.x / G < p.rows; row += step) {
-        load(ahead, ahead0, row + step);
+        load(ahead, row + step);
         const bool live = row < p.rows;
-        float f[F], first[1] = {0.f};
+        float f[F];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (live && real[i]) x[i].get(f + i * VEC);
@@ -158,12 +171,11 @@ __global__ void __launch_bounds__(kThreads) forward(const Rows<T> p)
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) f[i * VEC + j] = 0.f;
         }
-        if (G > 32 && live) x0.get(first);
-        center<G, NV, VEC>(f, first[0], real, inv_c, scratch);
+        center<G, NV, VEC>(f, real, p.C, inv_c, scratch);
         float s[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < F; ++i) s[0] += f[i] * f[i];
-        sum_row<G>(s, scratch);
+        sum_row<G>(s, scratch + kScratch);
         const float r = rsqrtf(s[0] * inv_c + p.eps);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -181,7 +193,6 @@ __global__ void __launch_bounds__(kThreads) forward(const Rows<T> p)
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) x[i] = ahead[i];
-        x0 = ahead0;
     }
 }
 
@@ -189,7 +200,7 @@ template <typename T, int VEC, int NV, int G>
 __global__ void __launch_bounds__(kThreads, back_blocks(VEC * NV)) backward(const Rows<T> p)
 {
     constexpr int per_block = kThreads / G, F = VEC * NV;
-    __shared__ float scratch[G > 32 ? 3 * (kThreads / 32) : 1];
+    __shared__ float scratch[G > 32 ? kScratch + 3 * (kThreads / 32) : 1];
     const int in_row = threadIdx.x % G;
     const float inv_c = 1.f / (float)p.C;
     Vec<T, VEC> w[NV];
@@ -207,9 +218,8 @@ __global__ void __launch_bounds__(kThreads, back_blocks(VEC * NV)) backward(cons
     constexpr bool kAhead = F <= 8;
     const long long step = (long long)gridDim.x * per_block;
     long long row = (long long)blockIdx.x * per_block + threadIdx.x / G;
-    struct Values { Vec<T, VEC> x[NV], g[NV], k[NV]; Vec<T, 1> x0; } at, ahead;   // x0: where a row is a block's
+    struct Values { Vec<T, VEC> x[NV], g[NV], k[NV]; } at, ahead;
     auto load = [&](Values& v, long long r) {
-        if (G > 32 && r < p.rows) v.x0.load(p.x + r * p.x_stride);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (r < p.rows && real[i]) {
@@ -224,7 +234,7 @@ __global__ void __launch_bounds__(kThreads, back_blocks(VEC * NV)) backward(cons
         if (kAhead) load(ahead, row + step);
         else load(at, row);
         const bool live = row < p.rows;
-        float f[F], first[1] = {0.f};
+        float f[F];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (live && real[i]) at.x[i].get(f + i * VEC);
@@ -232,8 +242,7 @@ __global__ void __launch_bounds__(kThreads, back_blocks(VEC * NV)) backward(cons
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) f[i * VEC + j] = 0.f;
         }
-        if (G > 32 && live) at.x0.get(first);
-        center<G, NV, VEC>(f, first[0], real, inv_c, scratch);
+        center<G, NV, VEC>(f, real, p.C, inv_c, scratch);
         float t[3] = {0.f, 0.f, 0.f};                              // sums of d^2, a and a d with d = x - mu
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -247,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, back_blocks(VEC * NV)) backward(cons
                 t[0] += d * d; t[1] += a; t[2] += a * d;
             }
         }
-        sum_row<G>(t, scratch);
+        sum_row<G>(t, scratch + kScratch);
         const float r = rsqrtf(t[0] * inv_c + p.eps), mean_a = t[1] * inv_c, along = t[2] * inv_c * r;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -310,13 +319,17 @@ __global__ void __launch_bounds__(kThreads, back_blocks(VEC * NV)) backward(cons
 }
 
 // Rows that no block holds in registers, three times over (backward five), eight values of a thread under way: 4096 rows of 5001 in bf16 42 us, 2048
-// of 20000 in fp32 131; backward 120 and 340.
-template <int N> __device__ __forceinline__ void sum_block(float (&v)[N], float* scratch) { sum_row<kThreads, N>(v, scratch); }
+// of 20000 in fp32 131; backward 126 and 368.
+template <int N> __device__ __forceinline__ void sum_block(float (&v)[N], float* scratch) {
+    sum_row<kThreads, N>(v, scratch);
+    __syncthreads();
+}
 
-struct Stats { float x0, mean, r; };                               // mean: of x - x0
-template <typename T> __device__ __forceinline__ float above(const Stats& st, T x) { return Elem<T>::to_f32(x) - st.x0 - st.mean; }
+struct Stats { float p, mean, r; };                                // mean: of x - p
+template <typename T> __device__ __forceinline__ float above(const Stats& st, T x) { return Elem<T>::to_f32(x) - st.p - st.mean; }
 template <typename T> __device__ __forceinline__ Stats wide_stats(const T* x, int C, float eps, float* scratch) {
-    Stats st{Elem<T>::to_f32(x[0]), 0.f, 0.f};
+    // values of the lines that come first anyway; elsewhere in the row 20000 values in fp32 131 -> 144 us
+    Stats st{middle(Elem<T>::to_f32(x[0]), Elem<T>::to_f32(x[kThreads]), Elem<T>::to_f32(x[2 * kThreads])), 0.f, 0.f};
     float s[1] = {0.f};
 #pragma unroll 8
     for (int c = threadIdx.x; c < C; c += kThreads) s[0] += above(st, x[c]);
@@ -349,13 +362,13 @@ template <typename T> __global__ void __launch_bounds__(kThreads) forward_wide(c
     }
 }
 
-template <typename T> __global__ void __launch_bounds__(kThreads) backward_wide(const Rows<T> p, float2* stats)
+template <typename T> __global__ void __launch_bounds__(kThreads) backward_wide(const Rows<T> p, float2* stats, float* from)
 {
     __shared__ float scratch[2 * (kThreads / 32)];
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
         const T *x = p.x + row * p.x_stride, *gy = p.gy + row * p.C;
         const Stats st = wide_stats(x, p.C, p.eps, scratch);
-        if (threadIdx.x == 0) stats[row] = make_float2(st.mean, st.r);
+        if (threadIdx.x == 0) { stats[row] = make_float2(st.mean, st.r); from[row] = st.p; }
         float t[2] = {0.f, 0.f};
         for (int c = threadIdx.x; c < p.C; c += kThreads) {
             const float a = Elem<T>::to_f32(gy[c]) * (p.weight ? Elem<T>::to_f32(p.weight[c]) : 1.f);
@@ -374,14 +387,14 @@ template <typename T> __global__ void __launch_bounds__(kThreads) backward_wide(
 }
 
 // Their columns: block (x, y) has kThreads columns and the rows y, y + gridDim.y, ...
-template <typename T> __global__ void __launch_bounds__(kThreads) columns_wide(const Rows<T> p, const float2* stats)
+template <typename T> __global__ void __launch_bounds__(kThreads) columns_wide(const Rows<T> p, const float2* stats, const float* from)
 {
     const int c = blockIdx.x * kThreads + threadIdx.x;
     if (c >= p.C) return;
     float gw = 0.f, gb = 0.f;
     for (long long row = blockIdx.y; row < p.rows; row += gridDim.y) {
         const T* x = p.x + row * p.x_stride;
-        const Stats st{Elem<T>::to_f32(x[0]), stats[row].x, stats[row].y};
+        const Stats st{from[row], stats[row].x, stats[row].y};
         const float g = Elem<T>::to_f32(p.gy[row * p.C + c]);
         gw += g * (above(st, x[c]) * st.r);
         gb += g;

@@ -1,10 +1,10 @@
 """Layer norm of rows of equal values, and of rows far from zero: a mean that is off by a step of its own is large beside differences that are none.
 
-Rows of one value: all differences from the row's first value are 0, their mean is 0, y is the bias (rounded), and the weights' gradients
+Rows of one value: all differences from one of the row's values are 0, their mean is 0, y is the bias (rounded), and the weights' gradients
 get nothing from such a row.
-Rows far from zero: differences from the first value x0 are exact, and from there on their size counts, not x's.  The bounds of the row
-x - base hold, twice: x0 lies 16 steps below base and the others 9.5 on average, so mean|x - x0| is 20 steps at most for five values (x0's own
-is 0) and 25 for many; a sum of five values rounds four times, its mean once more and the difference once, 6 u 20 steps against 2 (5 + 2) u 9.5, and
+Rows far from zero: differences from one of the values, x0, are exact, and from there on their size counts, not x's.  The bounds of the row
+x - base hold, twice: x0 lies 18 steps from base at most and the others 9.5 on average, so mean|x - x0| is 22 steps at most for five values (x0's own
+is 0) and 28 for many; a sum of five values rounds four times, its mean once more and the difference once, 6 u 22 steps against 2 (5 + 2) u 9.5, and
 for more values the sums' depth (at most n / 256 + 13 threads and shuffles) falls behind n + 2.
 """
 import pytest
@@ -76,3 +76,27 @@ def test_rows_far_from_zero(pkg, dtype, C):
     for val, far, got in ((*ref.norm(near, w, b, eps), {"y": y}), (*ref.norm(near, w, None, eps, gy, skip), {"gx": gx, "gw": gw, "gb": gb})):
         for name, t in got.items():
             ref.check(name, t, val, {name: 2 * far[name]})
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("C", WIDTHS)
+def test_first_values_unlike_the_others(pkg, dtype, C):
+    """The first value, or another one, is far from the rest, tiny beside it, or not finite: that row has the bounds of its own size, or is NaN, and
+    its neighbours know nothing of it."""
+    w, b, rand = weights(C, dtype, 3)
+    x, gy, skip = rand(40, C), rand(40, C), rand(40, C)
+    x[3] += 100
+    x[3, 0], x[4, 0], x[5, 0], x[6, 0], x[7, C // 2], x[8, C - 1] = 0.0, 1e4, -3e9, 1e-30, 3e9, -1e4
+    for bad in (None, float("inf"), float("-inf"), float("nan")):
+        rows = list(range(40))
+        if bad is not None:
+            x[9, 0] = bad
+            rows.remove(9)
+        y, gx = torch.empty_like(x), torch.empty_like(x)
+        pkg.esc_layer_norm_forward(x, w, b, 1e-5, y)
+        pkg.esc_layer_norm_backward(x, w, 1e-5, gy, gx, None, None, skip)
+        assert bad is None or (y[9].isnan().all() and gx[9].isnan().all())
+        val, far = ref.norm(x[rows], w, b, 1e-5)
+        ref.check("y", y[rows], val, far)
+        val, far = ref.norm(x[rows], w, None, 1e-5, gy[rows], skip[rows])
+        ref.check("gx", gx[rows], val, far)

@@ -13,6 +13,6 @@ def L():
 @pytest.mark.parametrize("rows", [1, 592, 100000])
 @pytest.mark.parametrize("C", [8193, 20000, 1 << 17, 1 << 20])
 def test_long_rows_ask_for_what_they_use(L, rows, C):
-    """256 columns to a block and four blocks an SM at most: no more than 592 x 256 columns of partial sums, or one of each, and two values a row."""
+    """256 columns to a block and four blocks an SM at most: no more than 592 x 256 columns of partial sums, or one of each, and three values a row."""
     sums = max(min(rows, 592) * 256 + C, C) * 2 * 4
-    assert 0 < L.esc_layer_norm_backward_workspace_bytes(rows, C) <= sums + rows * 8 + 1024
+    assert 0 < L.esc_layer_norm_backward_workspace_bytes(rows, C) <= sums + rows * 12 + 1024
