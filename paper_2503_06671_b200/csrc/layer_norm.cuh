@@ -16,7 +16,7 @@
 // x again (from L2).
 // gw and gb: a thread meets the same columns in all its rows and adds them up in registers, the threads of a block are added through
 // shared memory, the blocks by `sum_columns`, all in a fixed order.
-// 640x360 rows of 64 in bf16: 16.4 us (3.6 TB/s; a copy of these bytes takes 16); backward of 64 x 64x64 with skip 32.8 us (4.1 TB/s).
+// 640x360 rows of 64 in bf16: 16.4 us (3.6 TB/s; a copy of these bytes takes 16); backward of 64 x 64x64 with skip 34.9 us (3.8 TB/s).
 #pragma once
 #include "sum_rows.cuh"
 
